@@ -12,6 +12,9 @@ CSRC = os.path.join(HERE, "csrc")
 HOST_UNIT = "ffsim.hip"
 KERNEL_UNITS = ["ffsim_k_loop.hip", "ffsim_k_batch.hip", "ffsim_k_chain.hip", "ffsim_k_try.hip", "ffsim_k_nodes.hip"]   # each compiled per (EXT, GPN)
 VARIANTS = [(0, 4), (0, 0), (1, 4), (1, 0), (2, 4), (2, 0)]
+# the training operators: kernels and host side of each in one file, compiled once
+OPERATOR_UNITS = ["ffops_layernorm.hip", "ffops_attention_fwd.hip", "ffops_attention_bwd.hip", "ffops_vocab.hip"]
+OPERATOR_HEADERS = ["ffops_device.h", "ffops_tiles.h", "ffops_attention.h"]
 UNITS = [HOST_UNIT] + KERNEL_UNITS
 HEADERS = ["ffsim_select.h", "ffsim_loop_chain.h", "ffsim_loop_kernels.h", "ffsim_loop.h", "ffsim_kept.h", "ffsim_sweep.h", "ffsim_ahead.h", "ffsim_kernels.h", "ffsim_chain.h", "ffsim_events.h", "ffsim_strategy.h",
            "ffsim_device.h"]
@@ -21,7 +24,8 @@ LIB = os.path.join(HERE, "libffsim.so")
 # record then holds clock ticks per section instead of its counters; `bench.py --sections` reads it)
 SECTIONS_OBJ_DIR = os.path.join(HERE, "_build_sections")
 SECTIONS_LIB = os.path.join(HERE, "libffsim_sections.so")
-DEPS = [os.path.join(CSRC, f) for f in UNITS + HEADERS] + [os.path.join(os.path.dirname(HERE), "include", "ff_sim.h")]
+DEPS = [os.path.join(CSRC, f) for f in UNITS + HEADERS + OPERATOR_UNITS + OPERATOR_HEADERS] + \
+    [os.path.join(os.path.dirname(HERE), "include", f) for f in ("ff_sim.h", "ff_ops.h")]
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
                # keep the compiler from forming packed-fp32 instructions
@@ -52,7 +56,7 @@ def build_library(force: bool = True, sections: bool = False) -> str:
         return lib_path
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(obj_dir, exist_ok=True)
-    jobs = [(HOST_UNIT, extra, "ffsim.o")]
+    jobs = [(HOST_UNIT, extra, "ffsim.o")] + [(u, [], os.path.splitext(u)[0] + ".o") for u in OPERATOR_UNITS]
     for ext, gpn in VARIANTS:
         for u in KERNEL_UNITS:
             jobs.append((u, [f"-DFFSIM_EXT={ext}", f"-DFFSIM_GPN={gpn}", *extra], f"{os.path.splitext(u)[0]}_e{ext}_g{gpn}.o"))

@@ -1,0 +1,239 @@
+// Attention, forward.
+#include "ffops_attention.h"
+
+namespace ffops {
+namespace {
+
+// A wave owns 32 rows and keeps its q in registers; the block's waves share tiles of KEYS keys
+// and values in LDS, loaded one tile ahead.  Scores are made transposed, s^T = k q^T: a lane then holds 16 of 32 keys
+// of one row, the softmax of a row needs one exchange with lane ^ 32, its statistics are one register each, and the
+// probabilities are the second operand of o^T += v^T p^T as they lie.  The running maximum moves only when it grows by more than
+// 2^8: sums then stay within 2^8 of their scale, which costs 32-bit sums nothing and saves most rescalings.
+constexpr int KEYS = 64;
+
+template <class T, int D, int WAVES>
+__device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const char* kn, const char* vn, int64_t ks,
+                                          int64_t vs, int rows_next, int chunks, const typename T::vec8* qf, f32x16* o, float& m, float& l,
+                                          float c, int key0, int seen, int seen_least, int seen_most)
+{
+    constexpr int DB = D / 32;
+    const int half = (threadIdx.x % 64) / 32;
+    if (more) {
+        stage<KEYS, D, WAVES>(next, kn, ks, rows_next, chunks);
+        stage<KEYS, D, WAVES>(next + KEYS * D * 2, vn, vs, rows_next, chunks);
+    }
+    if (key0 >= seen_most) return;
+    const lds_char *kt = cur, *vt = cur + KEYS * D * 2;
+    f32x16 s[KEYS / 32];
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b) {
+        s[b] = f32x16{};
+#pragma unroll
+        for (int st = 0; st < D / 16; ++st) s[b] = T::mma(along<T, D>(kt, b * 32, st), qf[st], s[b]);
+    }
+    if (key0 + KEYS > seen_least) {
+#pragma unroll
+        for (int b = 0; b < KEYS / 32; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (key0 + b * 32 + c_row(r, half) >= seen) s[b][r] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+    top = fmaxf(top, other_half(top)) * c;
+    if (__any(top > m + 8.0f)) {        // m starts at -inf; a row that sees nothing keeps it
+        const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.0f : exp2_(m - mn);
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[d][r] *= f;
+        m = mn;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0;
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[b][r] = exp2_(fmaf(s[b][r], c, -base));
+            sum += s[b][r];
+        }
+    l += sum;
+#pragma unroll
+    for (int b = 0; b < KEYS / 32; ++b)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = s[b][st * 8 + e];
+            const typename T::vec8 p = round8<T>(f);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d] = T::mma(across<T, D>(vt, b * 32 + st * 16, d * 32), p, o[d]);
+        }
+}
+
+template <class T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_attention_fwd(AttnArgs a)
+{
+    constexpr int DB = D / 32, TILE = KEYS * D * 2;
+    __shared__ __attribute__((aligned(256))) char lds_[4 * TILE];
+    lds_char* lds = (lds_char*)lds_;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const uint32_t bk = blockIdx.x, b = bk / a.kv_heads, kh = bk % a.kv_heads;
+    const Rows w = rows_of_wave<WAVES>(a, b, kh, wave, lane);
+    const uint32_t i = w.i, h = w.h;
+    const int nk = w.nk;
+    int t0 = 0, t1 = (w.keys + KEYS - 1) / KEYS;
+    if (a.splits > 1) {
+        const int per = (t1 + (int)a.splits - 1) / (int)a.splits;
+        t0 = min(t1, per * (int)blockIdx.z);
+        t1 = min(t1, t0 + per);
+    }
+    const int chunks = a.dim / 8;
+    const char* kp = a.k.p + b * a.k.batch + kh * a.k.head;
+    const char* vp = a.v.p + b * a.v.batch + kh * a.v.head;
+    typename T::vec8 qf[D / 16];
+    row_operand<T, D>(qf, w.in && (int)i < w.nq ? a.q.p + b * a.q.batch + h * a.q.head + i * a.q.pos : nullptr, a.dim, half);
+    f32x16 o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = f32x16{};
+    float m = -INFINITY, l = 0;
+    if (t0 < t1) {
+        stage<KEYS, D, WAVES>(lds, kp + (int64_t)t0 * KEYS * a.k.pos, a.k.pos, nk - t0 * KEYS, chunks);
+        stage<KEYS, D, WAVES>(lds + TILE, vp + (int64_t)t0 * KEYS * a.v.pos, a.v.pos, nk - t0 * KEYS, chunks);
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int now = ((t - t0) & 1) * 2 * TILE, k1 = (t + 1) * KEYS;
+        tile_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), t + 1 < t1, kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, a.k.pos, a.v.pos,
+                               nk - k1, chunks, qf, o, m, l, a.scale_log2, t * KEYS, w.seen, w.seen_least, w.seen_most);
+        __syncthreads();
+    }
+    l += other_half(l);
+    if (!w.in) return;
+    const float inv = l > 0 ? 1.0f / l : l == l ? 0.0f : l;         // a NaN stays one
+    const uint64_t at = ((uint64_t)b * a.heads + h) * a.q_len + i;
+    if (a.splits > 1) {
+        float* p = a.part + ((uint64_t)blockIdx.z * a.batch * a.heads * a.q_len + at) * a.dim;
+        if (half == 0) a.part_lse[(uint64_t)blockIdx.z * a.batch * a.heads * a.q_len + at] = m + log2_(l);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int x = d * 32 + c_row(r, half);
+                if (x < (int)a.dim) *(f32x4*)(p + x) = f32x4{o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv};
+            }
+        return;
+    }
+    if (half == 0) a.lse[at] = (m + log2_(l)) * LN2;
+    char* p = a.o.p + b * a.o.batch + h * a.o.head + i * a.o.pos;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int x = d * 32 + c_row(r, half);
+            if (x < (int)a.dim) store4<T>(p + x * 2, o[d][r] * inv, o[d][r + 1] * inv, o[d][r + 2] * inv, o[d][r + 3] * inv);
+        }
+}
+
+// joins the parts of a row: o = sum_s 2^(lse_s - lse) o_s.  16 lanes per row, 8 elements each.
+template <class T>
+__global__ __launch_bounds__(256) void k_attention_join(AttnArgs a)
+{
+    const uint64_t n = (uint64_t)a.batch * a.heads * a.q_len, at = (uint64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    if (at >= n) return;
+    const int x = (threadIdx.x % 16) * 8;
+    float m = -INFINITY;
+    for (uint32_t s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * n + at]);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float sum = 0, o[8] = {};
+    for (uint32_t s = 0; s < a.splits; ++s) {
+        const float w = exp2_(a.part_lse[s * n + at] - base);
+        sum += w;
+        if (x < (int)a.dim) {
+            const float* p = a.part + (s * n + at) * a.dim + x;
+            const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += w * u[e], o[4 + e] += w * v[e];
+        }
+    }
+    const float inv = sum > 0 ? 1.0f / sum : sum == sum ? 0.0f : sum;
+    if (threadIdx.x % 16 == 0) a.lse[at] = (base + log2_(sum)) * LN2;
+    if (x >= (int)a.dim) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] *= inv;
+    const uint64_t i = at % a.q_len, bh = at / a.q_len;
+    *(typename T::vec8*)(a.o.p + bh / a.heads * a.o.batch + bh % a.heads * a.o.head + i * a.o.pos + x * 2) = round8<T>(o);
+}
+
+uint32_t waves_of(const AttnArgs& a)
+{
+    const uint64_t rows = (uint64_t)a.q_len * a.group;
+    return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+}
+
+// Keys are split over blocks where the rows alone do not fill the device's 512 places (two blocks on each of 256 compute units), by
+// no more than leaves a split four tiles.
+uint32_t splits_of(const AttnArgs& a)
+{
+    const uint64_t blocks = (uint64_t)a.batch * a.kv_heads * ceil_div((uint64_t)a.q_len * a.group, waves_of(a) * 32), tiles = ceil_div(a.kv_len, KEYS);
+    if (blocks == 0 || blocks >= 256) return 1;
+    const uint64_t s = std::min<uint64_t>(512 / blocks, tiles / 4);
+    return (uint32_t)std::max<uint64_t>(1, s);
+}
+
+template <class T, int D>
+void launch(const AttnArgs& a, hipStream_t st)
+{
+    const uint32_t w = waves_of(a);
+    const dim3 grid(a.batch * a.kv_heads, (uint32_t)ceil_div((uint64_t)a.q_len * a.group, w * 32), a.splits);
+    if (w == 1) k_attention_fwd<T, D, 1><<<grid, 64, 0, st>>>(a);
+    else if (w == 2) k_attention_fwd<T, D, 2><<<grid, 128, 0, st>>>(a);
+    else k_attention_fwd<T, D, 4><<<grid, 256, 0, st>>>(a);
+}
+
+template <class T>
+int run(const AttnArgs& a, hipStream_t st)
+{
+    if (a.dim <= 64) launch<T, 64>(a, st);
+    else launch<T, 128>(a, st);
+    if (a.splits > 1) k_attention_join<T><<<(uint32_t)ceil_div((uint64_t)a.batch * a.heads * a.q_len, 16), 256, 0, st>>>(a);
+    return launched();
+}
+
+uint64_t part_floats(const AttnArgs& a) { return (uint64_t)a.splits * a.batch * a.heads * a.q_len; }
+
+}  // namespace
+}  // namespace ffops
+
+using namespace ffops;
+
+extern "C" size_t ff_op_attention_fwd_workspace_bytes(const ff_attention_fwd_t* p)
+{
+    if (!p || check_attention(p) != FF_OK) return 0;
+    AttnArgs a = args_of(p);
+    a.splits = splits_of(a);
+    return a.splits > 1 ? part_floats(a) * (a.dim + 1) * sizeof(float) : 0;
+}
+
+extern "C" int ff_op_attention_fwd(const ff_attention_fwd_t* p, void* stream)
+{
+    if (!p) return FF_EINVAL;
+    if (const int rc = check_attention(p)) return rc;
+    if (p->batch == 0 || p->q_len == 0) return FF_OK;
+    if (!heads_ok(p->q) || !heads_ok(p->o) || !p->lse || (p->kv_len && (!heads_ok(p->k) || !heads_ok(p->v)))) return FF_EINVAL;
+    AttnArgs a = args_of(p);
+    a.lse = p->lse;
+    a.splits = splits_of(a);
+    const size_t need = ff_op_attention_fwd_workspace_bytes(p);
+    if (need) {
+        if (!p->workspace || p->workspace_bytes < need || !aligned(p->workspace, 256)) return FF_EWORKSPACE;
+        a.part = (float*)p->workspace;
+        a.part_lse = a.part + part_floats(a) * a.dim;
+    }
+    return p->dtype == FF_F16 ? run<F16>(a, (hipStream_t)stream) : run<BF16>(a, (hipStream_t)stream);
+}

@@ -1,0 +1,348 @@
+// Layer norm, forward and backward.
+#include "ffops_device.h"
+
+namespace ffops {
+namespace {
+
+struct FwdArgs {
+    uint64_t rows;
+    uint32_t cols;
+    float eps;
+    const void *x, *res;
+    void *h, *y;
+    int64_t xs, rs, hs, ys;
+    const void *w, *b;
+    float *mean, *rstd;
+};
+
+struct BwdArgs {
+    uint64_t rows;
+    uint32_t cols, groups;          // groups: partial sums of the weight's gradient
+    const void *dy, *h, *dh;
+    void* dx;
+    int64_t dys, hs, dhs, dxs;
+    const void* w;
+    const float *mean, *rstd;
+    float* part;                    // [2][groups][cols]
+};
+
+// V elements at p[i] as floats; V * sizeof(elem) is 16 bytes, or V = 1
+template <class T, int V>
+__device__ __forceinline__ void load(const void* p, int64_t i, float* f)
+{
+    typedef typename T::elem vec __attribute__((ext_vector_type(V)));
+    if constexpr (V == 1) f[0] = (float)((const typename T::elem*)p)[i];
+    else {
+        const vec v = *(const vec*)((const typename T::elem*)p + i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = (float)v[e];
+    }
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store(void* p, int64_t i, const float* f)
+{
+    typedef typename T::elem vec __attribute__((ext_vector_type(V)));
+    if constexpr (V == 1) ((typename T::elem*)p)[i] = (typename T::elem)f[0];
+    else {
+        vec v;
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = (typename T::elem)f[e];
+        *(vec*)((typename T::elem*)p + i) = v;
+    }
+}
+
+// sums of N values over the THREADS lanes that share a row; every lane gets them.  `red` holds N floats per wave.
+template <int THREADS, int N>
+__device__ __forceinline__ void row_sum(float* s, float* red)
+{
+#pragma unroll
+    for (int n = 0; n < N; ++n) s[n] = wave_sum(s[n]);
+    if constexpr (THREADS > 64) {
+        const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+        __syncthreads();        // the previous sums have been read
+        if (lane == 0)
+            for (int n = 0; n < N; ++n) red[wave * N + n] = s[n];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            s[n] = 0;
+            for (int w = 0; w < THREADS / 64; ++w) s[n] += red[w * N + n];
+        }
+    }
+}
+
+// A row is held in registers by THREADS lanes, E elements each, in accesses of V; rows of a wave of their own go four to a
+// block.  One read of x (and res), one write of h and y: the kernel is bound by memory.
+template <class T, int V, int THREADS, int E>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_fwd(FwdArgs a)
+{
+    constexpr int RPB = THREADS == 64 ? 4 : 1, N = E / V;
+    __shared__ float red[THREADS / 64];
+    const int t = threadIdx.x % THREADS;
+    const uint64_t row = (uint64_t)blockIdx.x * RPB + threadIdx.x / THREADS;
+    if (row >= a.rows) return;      // whole waves, and no barrier where a row is a wave's
+    const int64_t r = (int64_t)row;
+    float f[E];
+    float s = 0;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t c = (n * THREADS + t) * V;
+        float* v = f + n * V;
+        if (c < a.cols) {
+            load<T, V>(a.x, r * a.xs + c, v);
+            if (a.res) {
+                float u[V];
+                load<T, V>(a.res, r * a.rs + c, u);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = (float)(typename T::elem)(v[e] + u[e]);     // the sum is an output, and what is normed
+                store<T, V>(a.h, r * a.hs + c, v);
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) s += v[e];
+        } else
+            for (int e = 0; e < V; ++e) v[e] = 0;
+    }
+    row_sum<THREADS, 1>(&s, red);
+    const float mean = s / (float)a.cols;
+    float q = 0;                    // of the differences, from registers: no cancellation
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+        if ((uint32_t)(n * THREADS + t) * V < a.cols)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = f[n * V + e] - mean;
+                q += d * d;
+            }
+    row_sum<THREADS, 1>(&q, red);
+    const float rstd = 1.0f / sqrtf(q / (float)a.cols + a.eps);
+    if (t == 0) {
+        if (a.mean) a.mean[r] = mean;
+        if (a.rstd) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t c = (n * THREADS + t) * V;
+        if (c < a.cols) {
+            float w[V], b[V], y[V];
+            load<T, V>(a.w, c, w);
+            if (a.b) load<T, V>(a.b, c, b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = (f[n * V + e] - mean) * rstd * w[e] + (a.b ? b[e] : 0.0f);
+            store<T, V>(a.y, r * a.ys + c, y);
+        }
+    }
+}
+
+// Rows are dealt to the groups in turn (block b takes rows b, b + groups, ...; a wave of its own the rows of its place in
+// the block too), so that a lane keeps its columns and sums the weight's and the bias's gradient in registers.  One read
+// of dy, h (and dh), one write of dx; the partial sums are groups * cols * 8 bytes more, each way.
+template <class T, int V, int THREADS, int E>
+__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_bwd(BwdArgs a)
+{
+    constexpr int RPB = THREADS == 64 ? 4 : 1, N = E / V;
+    __shared__ float red[2 * THREADS / 64];
+    __shared__ float both[THREADS == 64 ? 2 * 64 * E : 1];
+    const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
+    float w[E], dw[E], db[E];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t c = (n * THREADS + t) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[n * V + e] = dw[n * V + e] = db[n * V + e] = 0;
+        if (c < a.cols) load<T, V>(a.w, c, w + n * V);
+    }
+    for (uint64_t row = (uint64_t)blockIdx.x * RPB + sub; row < a.rows; row += (uint64_t)a.groups * RPB) {
+        const int64_t r = (int64_t)row;
+        const float mean = a.mean[r], rstd = a.rstd[r];
+        float g[E], xh[E], s[2] = {0, 0};
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t c = (n * THREADS + t) * V;
+            float *gn = g + n * V, *xn = xh + n * V;
+            if (c < a.cols) {
+                load<T, V>(a.dy, r * a.dys + c, gn);
+                load<T, V>(a.h, r * a.hs + c, xn);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float dy = gn[e];
+                    xn[e] = (xn[e] - mean) * rstd;
+                    gn[e] = dy * w[n * V + e];
+                    dw[n * V + e] += dy * xn[e];
+                    db[n * V + e] += dy;
+                    s[0] += gn[e];
+                    s[1] += gn[e] * xn[e];
+                }
+            }
+        }
+        row_sum<THREADS, 2>(s, red);
+        const float mg = s[0] / (float)a.cols, mx = s[1] / (float)a.cols;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const uint32_t c = (n * THREADS + t) * V;
+            if (c < a.cols) {
+                float d[V], u[V];
+                if (a.dh) load<T, V>(a.dh, r * a.dhs + c, u);
+#pragma unroll
+                for (int e = 0; e < V; ++e) d[e] = rstd * (g[n * V + e] - mg - xh[n * V + e] * mx) + (a.dh ? u[e] : 0.0f);
+                store<T, V>(a.dx, r * a.dxs + c, d);
+            }
+        }
+    }
+    if (!a.part) return;
+    if constexpr (THREADS == 64) {          // the four waves of a block into one, in turn
+        for (int k = 0; k < RPB; ++k) {
+            if (sub == k)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    if (k) dw[e] += both[e * 64 + t], db[e] += both[(E + e) * 64 + t];
+                    both[e * 64 + t] = dw[e], both[(E + e) * 64 + t] = db[e];
+                }
+            __syncthreads();
+        }
+        if (sub != RPB - 1) return;
+    }
+    float *pw = a.part + (uint64_t)blockIdx.x * a.cols, *pb = pw + (uint64_t)a.groups * a.cols;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t c = (n * THREADS + t) * V;
+        if (c < a.cols) {
+            store<F32, V == 1 ? 1 : 4>(pw, c, dw + n * V);
+            store<F32, V == 1 ? 1 : 4>(pb, c, db + n * V);
+            if constexpr (V == 8) {
+                store<F32, 4>(pw, c + 4, dw + n * V + 4);
+                store<F32, 4>(pb, c + 4, db + n * V + 4);
+            }
+        }
+    }
+}
+
+// sums of the partial sums: 64 columns per block, 16 waves each a sixteenth of the groups
+template <class T>
+__global__ __launch_bounds__(1024) void k_layernorm_join(const float* part, uint32_t groups, uint32_t cols, void* dw, void* db)
+{
+    __shared__ float red[16][64];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    void* out = blockIdx.y ? db : dw;
+    if (!out) return;
+    const float* p = part + (uint64_t)blockIdx.y * groups * cols;
+    float s = 0;
+    if (c < cols) {
+#pragma unroll 8
+        for (uint32_t g = wave; g < groups; g += 16) s += p[(uint64_t)g * cols + c];
+    }
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+        for (int k = 1; k < 16; ++k) s += red[k][lane];
+        ((typename T::elem*)out)[c] = (typename T::elem)s;
+    }
+}
+
+// lanes that share a row and elements of a lane: a wave for rows of up to 2048 elements, 256 lanes up to 8192, 1024 beyond
+int threads_of(uint32_t cols) { return cols <= 2048 ? 64 : cols <= 8192 ? 256 : 1024; }
+
+template <class F>
+int by_size(uint32_t cols, F f)
+{
+    if (cols <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
+    if (cols <= 1024) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+    if (cols <= 2048) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 32>());
+    if (cols <= 4096) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 16>());
+    if (cols <= 8192) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 32>());
+    if (cols <= 16384) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
+    if (cols <= 32768) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 32>());
+    return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 64>());
+}
+
+template <class T>
+int fwd(const FwdArgs& a, bool vec, hipStream_t st)
+{
+    return by_size(a.cols, [&](auto threads, auto e) {
+        constexpr int TH = decltype(threads)::value, E = decltype(e)::value;
+        const dim3 grid((uint32_t)ceil_div(a.rows, TH == 64 ? 4 : 1)), block(TH == 64 ? 256 : TH);
+        if (vec) k_layernorm_fwd<T, T::VEC, TH, E><<<grid, block, 0, st>>>(a);
+        else k_layernorm_fwd<T, 1, TH, E><<<grid, block, 0, st>>>(a);
+        return launched();
+    });
+}
+
+template <class T>
+int bwd(const BwdArgs& a, bool vec, void* dw, void* db, hipStream_t st)
+{
+    if (a.groups) {
+        const int rc = by_size(a.cols, [&](auto threads, auto e) {
+            constexpr int TH = decltype(threads)::value, E = decltype(e)::value;
+            const dim3 grid(a.groups), block(TH == 64 ? 256 : TH);
+            if (vec) k_layernorm_bwd<T, T::VEC, TH, E><<<grid, block, 0, st>>>(a);
+            else k_layernorm_bwd<T, 1, TH, E><<<grid, block, 0, st>>>(a);
+            return launched();
+        });
+        if (rc != FF_OK) return rc;
+    }
+    if (!dw && !db) return FF_OK;
+    k_layernorm_join<T><<<dim3((uint32_t)ceil_div(a.cols, 64), 2), 1024, 0, st>>>(a.part, a.groups, a.cols, dw, db);
+    return launched();
+}
+
+size_t elem_bytes(uint32_t dtype) { return dtype == FF_F32 ? 4 : 2; }
+bool vec_rows(const ff_rows_t& m, size_t e) { return aligned(m.p, 16) && (uint64_t)m.stride * e % 16 == 0; }
+
+int check_size(uint32_t dtype, uint64_t rows, uint32_t cols)
+{
+    if (dtype > FF_BF16 || cols == 0) return FF_EINVAL;
+    if (cols > FF_OP_MAX_COLS || rows > FF_OP_MAX_ROWS) return FF_ERANGE;
+    return FF_OK;
+}
+
+// partial sums of the weight's gradient: as many blocks as fill the device, each with four rows at least where there are that many
+uint32_t groups_of(uint64_t rows, uint32_t cols)
+{
+    const uint32_t th = threads_of(cols);
+    const uint64_t per_block = th == 64 ? 4 : 1, most = th == 1024 ? 512 : 1024;
+    const uint64_t blocks = ceil_div(rows, per_block);
+    return (uint32_t)(blocks < most ? blocks : most);
+}
+
+}  // namespace
+}  // namespace ffops
+
+using namespace ffops;
+
+extern "C" int ff_op_layernorm_fwd(const ff_layernorm_fwd_t* p, void* stream)
+{
+    if (!p) return FF_EINVAL;
+    if (const int rc = check_size(p->dtype, p->rows, p->cols)) return rc;
+    if (!(p->eps >= 0) || !std::isfinite(p->eps)) return FF_EINVAL;
+    if (p->rows == 0) return FF_OK;
+    if (!p->x.p || !p->y.p || !p->weight || (p->res.p && !p->h.p)) return FF_EINVAL;
+    const size_t e = elem_bytes(p->dtype);
+    const bool vec = p->cols * e % 16 == 0 && vec_rows(p->x, e) && vec_rows(p->y, e) && (!p->res.p || (vec_rows(p->res, e) && vec_rows(p->h, e))) &&
+                     aligned(p->weight, 16) && aligned(p->bias, 16);
+    const FwdArgs a = {p->rows, p->cols, p->eps, p->x.p, p->res.p, p->h.p, p->y.p, p->x.stride, p->res.stride, p->h.stride, p->y.stride,
+                       p->weight, p->bias, p->mean, p->rstd};
+    const hipStream_t st = (hipStream_t)stream;
+    return p->dtype == FF_F32 ? fwd<F32>(a, vec, st) : p->dtype == FF_F16 ? fwd<F16>(a, vec, st) : fwd<BF16>(a, vec, st);
+}
+
+extern "C" size_t ff_op_layernorm_bwd_workspace_bytes(const ff_layernorm_bwd_t* p)
+{
+    if (!p || check_size(p->dtype, p->rows, p->cols) != FF_OK || (!p->dweight && !p->dbias)) return 0;
+    return (size_t)2 * groups_of(p->rows, p->cols) * p->cols * sizeof(float);
+}
+
+extern "C" int ff_op_layernorm_bwd(const ff_layernorm_bwd_t* p, void* stream)
+{
+    if (!p) return FF_EINVAL;
+    if (const int rc = check_size(p->dtype, p->rows, p->cols)) return rc;
+    if (p->rows && (!p->dy.p || !p->h.p || !p->dx.p || !p->weight || !p->mean || !p->rstd)) return FF_EINVAL;
+    const size_t need = ff_op_layernorm_bwd_workspace_bytes(p);
+    if (need && (!p->workspace || p->workspace_bytes < need || !aligned(p->workspace, 256))) return FF_EWORKSPACE;
+    const size_t e = elem_bytes(p->dtype);
+    const bool vec = p->cols * e % 16 == 0 && vec_rows(p->dy, e) && vec_rows(p->h, e) && vec_rows(p->dx, e) && (!p->dh.p || vec_rows(p->dh, e)) && aligned(p->weight, 16);
+    const BwdArgs a = {p->rows, p->cols, groups_of(p->rows, p->cols), p->dy.p, p->h.p, p->dh.p, p->dx.p, p->dy.stride, p->h.stride, p->dh.stride, p->dx.stride,
+                       p->weight, p->mean, p->rstd, need ? (float*)p->workspace : nullptr};
+    const hipStream_t st = (hipStream_t)stream;
+    return p->dtype == FF_F32 ? bwd<F32>(a, vec, p->dweight, p->dbias, st) : p->dtype == FF_F16 ? bwd<F16>(a, vec, p->dweight, p->dbias, st)
+                                                                                               : bwd<BF16>(a, vec, p->dweight, p->dbias, st);
+}

@@ -1,0 +1,545 @@
+// Softmax cross entropy over a vocabulary, forward and backward, from the vectors and the vocabulary's matrix.
+#include "ffops_tiles.h"
+
+namespace ffops {
+namespace {
+
+struct Mat {
+    const char* p;
+    int64_t stride;         // bytes from row to row
+};
+
+// One side of a product over k, as a block sees it.  Along: p is the tile's first row, rows of k elements; across: p is the
+// tile's first column, rows of the tile's elements, one per k.  `count`: rows (columns) of the tile that exist; `ks`: values of k
+// that exist, along in multiples of 8 (with zeros where the other side has none).
+struct Side {
+    Mat m;
+    int count;
+    int64_t ks;
+};
+
+constexpr int KT = 64;      // k of a tile in LDS
+
+template <int SIZE, bool ACROSS, int WAVES>
+__device__ __forceinline__ void stage_side(lds_char* dst, const Side& s, int64_t k)
+{
+    const int left = (int)min(s.ks - k, (int64_t)KT);
+    if constexpr (ACROSS) stage<KT, SIZE, WAVES>(dst, s.m.p + k * s.m.stride, s.m.stride, left, (s.count + 7) / 8);
+    else stage<SIZE, KT, WAVES>(dst, s.m.p + k * 2, s.m.stride, s.count, left / 8);
+}
+
+template <class T, int SIZE, bool ACROSS>
+__device__ __forceinline__ typename T::vec8 operand(const lds_char* tile, int at, int step)
+{
+    if constexpr (ACROSS) return across<T, SIZE, true>(tile, step * 16, at);
+    else return along<T, KT>(tile, at, step);
+}
+
+// The product of a block: c[m][n] += sum_k a[m][k] b[n][k] over k0 .. k1, M x N of it in WM x WN waves of 32 x 32 tiles, the
+// tiles of both sides loaded straight into LDS one tile of k ahead.  Along sides have k in multiples of 8.
+template <class T, int M, int N, int WM, int WN, bool A_ACROSS, bool B_ACROSS>
+struct Product {
+    static constexpr int WAVES = WM * WN, TM = M / WM / 32, TN = N / WN / 32, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
+
+    static __device__ __forceinline__ void step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const Side& a, const Side& b, int64_t k,
+                                                f32x16 (&c)[TM][TN], int wm, int wn)
+    {
+        if (more) {
+            stage_side<M, A_ACROSS, WAVES>(next, a, k + KT);
+            stage_side<N, B_ACROSS, WAVES>(next + A_BYTES, b, k + KT);
+        }
+#pragma unroll
+        for (int st = 0; st < KT / 16; ++st) {
+            typename T::vec8 fa[TM], fb[TN];
+#pragma unroll
+            for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, B_ACROSS>(cur + A_BYTES, wn + n * 32, st);
+#pragma unroll
+            for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, A_ACROSS>(cur, wm + m * 32, st);
+#pragma unroll
+            for (int m = 0; m < TM; ++m)
+#pragma unroll
+                for (int n = 0; n < TN; ++n) c[m][n] = T::mma(fa[m], fb[n], c[m][n]);
+        }
+    }
+
+    static __device__ __forceinline__ void run(lds_char* lds, const Side& a, const Side& b, int64_t k0, int64_t k1, f32x16 (&c)[TM][TN], int wm, int wn)
+    {
+        if (k0 < k1) {
+            stage_side<M, A_ACROSS, WAVES>(lds, a, k0);
+            stage_side<N, B_ACROSS, WAVES>(lds + A_BYTES, b, k0);
+        }
+        __syncthreads();
+        int now = 0;
+        for (int64_t k = k0; k < k1; k += KT) {
+            step(lds + now, lds + (BYTES - now), k + KT < k1, a, b, k, c, wm, wn);
+            now = BYTES - now;
+            __syncthreads();
+        }
+    }
+};
+
+// Blocks go to the 8 dies in turn, each with a cache of its own: a die takes a run of tiles, in groups of 8 along m, so that what
+// runs at one time on a die shares its rows of both sides.
+__device__ __forceinline__ void tile_of_block(uint32_t id, uint32_t ms, uint32_t ns, uint32_t& m, uint32_t& n)
+{
+    const uint32_t total = ms * ns, die = id % 8, each = total / 8, rest = total % 8;
+    const uint32_t at = die * each + min(die, rest) + id / 8;
+    const uint32_t group = at / (8 * ns), first = group * 8, size = min(8u, ms - first), in = at - group * 8 * ns;
+    m = first + in % size;
+    n = in / size;
+}
+
+struct VocabArgs {
+    uint32_t rows, dim, words, word0;       // words of this piece, the first of them in the matrix
+    uint32_t m_tiles, n_tiles;
+    int32_t ignore, first_word;
+    Mat x, w;
+    const int32_t* targets;
+    const float *dloss, *lse_in;
+    const uint32_t* top;
+    float2* part;                           // [m_tiles][rows]: maximum and sum of a tile's words
+    float* target_logit;
+    char* g;                                // [rows][g_stride]: gradient of the logits of a piece
+    uint32_t g_stride;
+    float* sum;                             // [splits][rows][dim]: dx, over pieces and splits
+    uint32_t splits, first, whole;          // dx: the first piece; one piece and no splits, so that dx is written at once
+    char* out;
+    int64_t out_stride;                     // bytes
+    uint32_t out_vec;                       // rows of the output take 8-byte stores
+};
+
+// four neighbouring elements of a row of an output, those below `n`
+template <class T>
+__device__ __forceinline__ void store_out(char* row, uint32_t x, uint32_t n, bool vec, float a, float b, float c, float d)
+{
+    if (vec && x + 4 <= n) store4<T>(row + x * 2, a, b, c, d);
+    else {
+        typename T::elem* p = (typename T::elem*)row;
+        if (x < n) p[x] = (typename T::elem)a;
+        if (x + 1 < n) p[x + 1] = (typename T::elem)b;
+        if (x + 2 < n) p[x + 2] = (typename T::elem)c;
+        if (x + 3 < n) p[x + 3] = (typename T::elem)d;
+    }
+}
+
+// z^T = w x^T: words down, tokens across, so that a lane holds words of one token.  GRAD false: maximum and sum of exp per
+// token and tile of words, and the target's logit; GRAD true: the gradient of the logits, rounded, into g.
+// g is kept relative to the largest |dloss| and times a power of two.  Where all rows weigh the same, a row's entry for its target is then
+// p - 1, which for a small p rounds to nearly itself; and a 16-bit float's exponents do not hold a probability of 1 / vocabulary times a loss' weight.
+// 2^12 keeps them, and 1 stays below its largest number.  With bfloat 2^40 keeps probabilities that a float's exponents do not hold.
+template <class T>
+constexpr float G_SHIFT = std::is_same<T, F16>::value ? 12.0f : 40.0f;
+
+__device__ __forceinline__ float unit_of(const uint32_t* top)
+{
+    const float m = __uint_as_float(*top);
+    return m > 0 && m < INFINITY ? m : 1.0f;
+}
+
+// maximum (a power of two's exponent) and sum of two sets; an empty one has -inf and 0
+__device__ __forceinline__ float2 join(float2 s, float2 o)
+{
+    const float top = fmaxf(s.x, o.x), base = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, s.y * exp2_(s.x - base) + o.y * exp2_(o.x - base));
+}
+
+template <class T, int M, int N, int WM, int WN, bool GRAD>
+__global__ __launch_bounds__(WM * WN * 64) void k_vocab_logits(VocabArgs a)
+{
+    typedef Product<T, M, N, WM, WN, false, false> P;
+    __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
+    lds_char* lds = (lds_char*)lds_;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
+    uint32_t tm, tn;
+    tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
+    const uint32_t m0 = tm * M, n0 = tn * N;
+    const Side sw = {{a.w.p + (int64_t)(a.word0 + m0) * a.w.stride, a.w.stride}, (int)min(a.words - m0, (uint32_t)M), a.dim};
+    const Side sx = {{a.x.p + (int64_t)n0 * a.x.stride, a.x.stride}, (int)min(a.rows - n0, (uint32_t)N), a.dim};
+    f32x16 c[P::TM][P::TN];
+#pragma unroll
+    for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x16{};
+    P::run(lds, sw, sx, 0, a.dim, c, wm, wn);
+    float2* stat = (float2*)lds_;           // [WM][N], the tiles have been read
+#pragma unroll
+    for (int n = 0; n < P::TN; ++n) {
+        const uint32_t token = n0 + wn + n * 32 + lane % 32;
+        const bool in = token < a.rows;
+        const int32_t target = in ? a.targets[token] : a.ignore;
+        const bool live = target != a.ignore;
+        // the target's place among the piece's words
+        const int64_t want = live ? (int64_t)target - a.first_word - a.word0 : -1;
+        if constexpr (GRAD) {
+            const float unit = unit_of(a.top);
+            const float ls = in ? a.lse_in[token] * LOG2E - G_SHIFT<T> : 0, f = live && in ? a.dloss[token] / unit : 0;
+            char* row = a.g + (uint64_t)token * a.g_stride * 2;
+#pragma unroll
+            for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const uint32_t v = m0 + wm + m * 32 + c_row(r, half);
+                    float g[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        g[e] = (exp2_(fmaf(c[m][n][r + e], LOG2E, -ls)) - (v + e == want ? exp2f(G_SHIFT<T>) : 0.0f)) * f;
+                        if (!live || v + e >= a.words) g[e] = 0;
+                    }
+                    if (in && v < a.g_stride) store4<T>(row + v * 2, g[0], g[1], g[2], g[3]);
+                }
+        } else {
+            float top = -INFINITY, sum = 0;
+#pragma unroll
+            for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const uint32_t v = m0 + wm + m * 32 + c_row(r, half);
+                    if (in && v == want && v < a.words) a.target_logit[token] = c[m][n][r];
+                    if (v >= a.words) c[m][n][r] = -INFINITY;
+                    top = fmaxf(top, c[m][n][r]);
+                }
+            top = fmaxf(top, other_half(top));
+            const float base = top == -INFINITY ? 0.0f : top * LOG2E;
+#pragma unroll
+            for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum += exp2_(fmaf(c[m][n][r], LOG2E, -base));
+            sum += other_half(sum);
+            if (half == 0) stat[wave / WN * N + wn + n * 32 + lane] = make_float2(top * LOG2E, sum);
+        }
+    }
+    if constexpr (!GRAD) {
+        __syncthreads();
+        for (int n = threadIdx.x; n < N; n += WM * WN * 64) {
+            if (n0 + n >= a.rows) break;
+            float2 s = stat[n];
+#pragma unroll
+            for (int k = 1; k < WM; ++k) s = join(s, stat[k * N + n]);
+            a.part[(uint64_t)tm * a.rows + n0 + n] = s;
+        }
+    }
+}
+
+// joins the statistics of the tiles of words: 64 tokens per block, 16 waves each a sixteenth of the tiles
+__global__ __launch_bounds__(1024) void k_vocab_join(VocabArgs a, float* loss, float* lse, float* target_logit)
+{
+    __shared__ float2 red[16][64];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint64_t token = (uint64_t)blockIdx.x * 64 + lane;
+    float2 s = make_float2(-INFINITY, 0);
+    if (token < a.rows)
+        for (uint32_t t = wave; t < a.m_tiles; t += 16) s = join(s, a.part[(uint64_t)t * a.rows + token]);
+    red[wave][lane] = s;
+    __syncthreads();
+    if (wave || token >= a.rows) return;
+    for (int k = 1; k < 16; ++k) s = join(s, red[k][lane]);
+    const float l = (s.x + log2_(s.y)) * LN2;
+    const int32_t target = a.targets[token];
+    const int64_t at = (int64_t)target - a.first_word;
+    const bool here = target != a.ignore && at >= 0 && at < a.words;
+    const float z = here ? a.target_logit[token] : 0.0f;
+    lse[token] = l;
+    if (target_logit) target_logit[token] = z;
+    if (loss) loss[token] = target == a.ignore ? 0.0f : here ? l - z : NAN;
+}
+
+// dx^T = w^T g^T over the words of a piece: elements down, tokens across
+template <class T, int M, int N, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void k_vocab_dx(VocabArgs a)
+{
+    typedef Product<T, M, N, WM, WN, true, false> P;
+    __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
+    uint32_t tm, tn;
+    tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
+    const uint32_t m0 = tm * M, n0 = tn * N;
+    const Side sw = {{a.w.p + (int64_t)a.word0 * a.w.stride + m0 * 2, a.w.stride}, (int)min(a.dim - m0, (uint32_t)M), a.words};
+    // g has zeros beyond the last word, up to a multiple of 8
+    const int64_t ks = ((int64_t)a.words + 7) / 8 * 8;
+    const Side sg = {{a.g + (uint64_t)n0 * a.g_stride * 2, (int64_t)a.g_stride * 2}, (int)min(a.rows - n0, (uint32_t)N), ks};
+    const int64_t run = ((ks + a.splits - 1) / a.splits + KT - 1) / KT * KT;
+    const int64_t k0 = min(ks, run * blockIdx.y), k1 = min(ks, k0 + run);
+    f32x16 c[P::TM][P::TN];
+    const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
+    float* sum = a.sum + (uint64_t)blockIdx.y * a.rows * a.dim;
+#pragma unroll
+    for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x16{};
+    P::run((lds_char*)lds_, sw, sg, k0, k1, c, wm, wn);
+#pragma unroll
+    for (int n = 0; n < P::TN; ++n) {
+        const uint32_t token = n0 + wn + n * 32 + lane % 32;
+        if (token >= a.rows) continue;
+#pragma unroll
+        for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const uint32_t x = m0 + wm + m * 32 + c_row(r, half);
+                if (x >= a.dim) continue;
+                const f32x16& q = c[m][n];
+                if (a.whole) store_out<T>(a.out + (int64_t)token * a.out_stride, x, a.dim, a.out_vec, q[r] * f, q[r + 1] * f, q[r + 2] * f, q[r + 3] * f);
+                else {          // dim is a multiple of 8
+                    f32x4* p = (f32x4*)(sum + (uint64_t)token * a.dim + x);
+                    const f32x4 v = {q[r], q[r + 1], q[r + 2], q[r + 3]};
+                    *p = a.first ? v : *p + v;
+                }
+            }
+    }
+}
+
+// dx from the sums of its splits
+template <class T>
+__global__ __launch_bounds__(256) void k_vocab_dx_out(VocabArgs a, uint32_t dim)
+{
+    const uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (uint64_t)a.rows * a.dim;
+    if (at >= n) return;
+    f32x4 s = {};
+    for (uint32_t k = 0; k < a.splits; ++k) s += *(const f32x4*)(a.sum + k * n + at);
+    const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
+    store_out<T>(a.out + (int64_t)(at / a.dim) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_vec, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+}
+
+// dw of a piece = g^T x, made transposed over the tokens: elements down, words across
+template <class T, int M, int N, int WM, int WN>
+__global__ __launch_bounds__(WM * WN * 64) void k_vocab_dw(VocabArgs a, uint32_t dim)
+{
+    typedef Product<T, M, N, WM, WN, true, true> P;
+    __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
+    uint32_t tm, tn;
+    tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
+    const uint32_t m0 = tm * M, n0 = tn * N;
+    const Side sx = {{a.x.p + m0 * 2, a.x.stride}, (int)min(a.dim - m0, (uint32_t)M), a.rows};
+    const Side sg = {{a.g + n0 * 2, (int64_t)a.g_stride * 2}, (int)min(a.words - n0, (uint32_t)N), a.rows};
+    f32x16 c[P::TM][P::TN];
+#pragma unroll
+    for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x16{};
+    P::run((lds_char*)lds_, sx, sg, 0, a.rows, c, wm, wn);
+    const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
+#pragma unroll
+    for (int n = 0; n < P::TN; ++n) {
+        const uint32_t word = n0 + wn + n * 32 + lane % 32;
+        if (word >= a.words) continue;
+        char* row = a.out + (int64_t)(a.word0 + word) * a.out_stride;
+#pragma unroll
+        for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const f32x16& q = c[m][n];
+                store_out<T>(row, m0 + wm + m * 32 + c_row(r, half), dim, a.out_vec, q[r] * f, q[r + 1] * f, q[r + 2] * f, q[r + 3] * f);
+            }
+    }
+}
+
+// rows whose length or place does not suit 16-byte accesses, laid out anew: `dim` elements, zeros up to `to`, a multiple of 8
+template <class E>
+__global__ __launch_bounds__(256) void k_vocab_lay_out(const E* p, int64_t stride, uint64_t rows, uint32_t dim, uint32_t to, E* out)
+{
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / (to / 2);
+    const uint32_t x = (uint32_t)(at % (to / 2)) * 2;
+    if (row >= rows) return;
+    const E* s = p + (int64_t)row * stride;
+    out[row * to + x] = x < dim ? s[x] : (E)0;
+    out[row * to + x + 1] = x + 1 < dim ? s[x + 1] : (E)0;
+}
+
+__global__ void k_vocab_clear(uint32_t* top) { *top = 0; }
+
+__global__ __launch_bounds__(256) void k_vocab_top(const float* dloss, uint32_t rows, uint32_t* top)
+{
+    float m = 0;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < rows; i += (uint64_t)gridDim.x * 256) m = fmaxf(m, fabsf(dloss[i]));
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if (threadIdx.x % 64 == 0) atomicMax(top, __float_as_uint(m));         // the largest of a set does not depend on the order
+}
+
+// ---- host ------------------------------------------------------------------------------
+
+constexpr uint64_t PIECE_BYTES = 256ull << 20;      // gradient of the logits of a piece: what the last-level cache holds
+
+struct Plan {
+    uint32_t dim;               // a multiple of 8
+    bool copy_x, copy_w, big;
+    uint32_t tile, m_tiles, n_tiles, piece, splits;
+    uint64_t x, w, part, logit, top, g, sum, bytes;
+};
+
+bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0; }
+
+template <class A>
+Plan plan_of(const A* p, bool back)
+{
+    Plan q = {};
+    q.dim = (uint32_t)round_up(p->dim, 8);
+    q.copy_x = !suits(p->x, p->dim), q.copy_w = !suits(p->w, p->dim);
+    uint64_t at = 0;
+    const auto take = [&](uint64_t bytes) {
+        const uint64_t o = at;
+        at += round_up(bytes, 256);
+        return o;
+    };
+    q.x = take(q.copy_x ? (uint64_t)p->rows * q.dim * 2 : 0);
+    q.w = take(q.copy_w ? (uint64_t)p->vocab * q.dim * 2 : 0);
+    // 256 x 256 tiles where they give every compute unit one; below that 64 x 64, more of them at a time on each
+    q.big = ceil_div(p->vocab, 256) * ceil_div(p->rows, 256) >= 256;
+    q.tile = q.big ? 256 : 64;
+    q.m_tiles = (uint32_t)ceil_div(p->vocab, q.tile), q.n_tiles = (uint32_t)ceil_div(p->rows, q.tile);
+    if (!back) {
+        q.part = take((uint64_t)q.m_tiles * p->rows * sizeof(float2));
+        q.logit = take((uint64_t)p->rows * sizeof(float));
+    } else {
+        q.top = take(sizeof(uint32_t));
+        const uint64_t fit = PIECE_BYTES / 2 / std::max(1u, p->rows) / 256 * 256;
+        q.piece = (uint32_t)std::min<uint64_t>(round_up(p->vocab, 256), std::max<uint64_t>(fit, 256));
+        q.g = take((uint64_t)p->rows * q.piece * 2);
+        const uint64_t tiles = ceil_div(q.dim, q.tile) * q.n_tiles, ks = std::min(p->vocab, q.piece) / KT;
+        const uint64_t want = q.big ? 256 : 1024;
+        q.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({tiles ? want / tiles : 1, ks / 8, 16}));
+        q.sum = take(q.splits > 1 || q.piece < p->vocab ? (uint64_t)q.splits * p->rows * q.dim * sizeof(float) : 0);
+    }
+    q.bytes = at;
+    return q;
+}
+
+template <class A>
+int check_vocab(const A* p)
+{
+    if (p->dtype != FF_F16 && p->dtype != FF_BF16) return FF_EINVAL;
+    if (p->vocab == 0 || p->dim == 0) return FF_EINVAL;
+    if (p->rows > FF_OP_MAX_ROWS || p->vocab > FF_OP_MAX_ROWS || p->dim > FF_OP_MAX_DIM) return FF_ERANGE;
+    // tiles of a launch, which 32 bits count
+    if (ceil_div(p->vocab, 64) * ceil_div(p->rows, 64) >= (1ull << 31) || ceil_div(p->vocab, 64) * ceil_div(p->dim, 64) >= (1ull << 31)) return FF_ERANGE;
+    return FF_OK;
+}
+
+template <class T>
+int lay_out(const ff_rows_t& m, uint64_t rows, uint32_t dim, uint32_t to, bool copy, char* ws, Mat& out, hipStream_t st)
+{
+    if (!copy) {
+        out = {(const char*)m.p, m.stride * 2};
+        return FF_OK;
+    }
+    out = {ws, (int64_t)to * 2};
+    if (rows * (to / 2) > (1ull << 38)) return FF_ERANGE;
+    k_vocab_lay_out<typename T::elem><<<(uint32_t)ceil_div(rows * (to / 2), 256), 256, 0, st>>>((const typename T::elem*)m.p, m.stride, rows, dim, to, (typename T::elem*)ws);
+    return launched();
+}
+
+template <class A>
+VocabArgs args_of(const A* p, const Plan& q)
+{
+    VocabArgs a = {};
+    a.rows = p->rows, a.dim = q.dim, a.words = p->vocab, a.ignore = p->ignore_index, a.first_word = p->first_word;
+    a.m_tiles = q.m_tiles, a.n_tiles = q.n_tiles, a.targets = p->targets, a.splits = 1;
+    return a;
+}
+
+template <class T>
+int fwd(const ff_vocab_loss_fwd_t* p, const Plan& q, hipStream_t st)
+{
+    char* ws = (char*)p->workspace;
+    VocabArgs a = args_of(p, q);
+    if (const int rc = lay_out<T>(p->x, p->rows, p->dim, q.dim, q.copy_x, ws + q.x, a.x, st)) return rc;
+    if (const int rc = lay_out<T>(p->w, p->vocab, p->dim, q.dim, q.copy_w, ws + q.w, a.w, st)) return rc;
+    a.part = (float2*)(ws + q.part);
+    a.target_logit = (float*)(ws + q.logit);
+    const uint32_t tiles = a.m_tiles * a.n_tiles;
+    if (q.big) k_vocab_logits<T, 256, 256, 2, 4, false><<<tiles, 512, 0, st>>>(a);
+    else k_vocab_logits<T, 64, 64, 2, 2, false><<<tiles, 256, 0, st>>>(a);
+    k_vocab_join<<<(uint32_t)ceil_div(p->rows, 64), 1024, 0, st>>>(a, p->loss, p->lse, p->target_logit);
+    return launched();
+}
+
+template <class T>
+int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
+{
+    char* ws = (char*)p->workspace;
+    VocabArgs a = args_of(p, q);
+    if (const int rc = lay_out<T>(p->x, p->rows, p->dim, q.dim, q.copy_x, ws + q.x, a.x, st)) return rc;
+    if (const int rc = lay_out<T>(p->w, p->vocab, p->dim, q.dim, q.copy_w, ws + q.w, a.w, st)) return rc;
+    a.dloss = p->dloss, a.lse_in = p->lse, a.top = (uint32_t*)(ws + q.top);
+    a.g = ws + q.g, a.g_stride = q.piece, a.sum = (float*)(ws + q.sum);
+    k_vocab_clear<<<1, 1, 0, st>>>((uint32_t*)a.top);
+    if (p->rows) k_vocab_top<<<(uint32_t)std::min<uint64_t>(ceil_div(p->rows, 256), 256), 256, 0, st>>>(p->dloss, p->rows, (uint32_t*)a.top);
+    const uint32_t d_tiles = (uint32_t)ceil_div(q.dim, q.tile);
+    const bool whole = q.splits == 1 && q.piece >= p->vocab;
+    for (uint64_t word0 = 0; word0 < p->vocab; word0 += q.piece) {
+        a.word0 = (uint32_t)word0;
+        a.words = (uint32_t)std::min<uint64_t>(q.piece, p->vocab - word0);
+        a.m_tiles = (uint32_t)ceil_div(a.words, q.tile), a.n_tiles = q.n_tiles;
+        const uint32_t v_tiles = a.m_tiles;
+        if (p->rows) {
+            if (q.big) k_vocab_logits<T, 256, 256, 2, 4, true><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a);
+            else k_vocab_logits<T, 64, 64, 2, 2, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
+        }
+        if (p->dx.p && p->rows) {
+            a.m_tiles = d_tiles, a.n_tiles = q.n_tiles, a.splits = q.splits, a.first = word0 == 0, a.whole = whole;
+            a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
+            a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
+            a.dim = whole ? p->dim : q.dim;         // as many as are stored; the tiles of w have zeros beyond
+            const dim3 grid(a.m_tiles * a.n_tiles, q.splits);
+            if (q.big) k_vocab_dx<T, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
+            else k_vocab_dx<T, 64, 64, 2, 2><<<grid, 256, 0, st>>>(a);
+            a.dim = q.dim;
+        }
+        if (p->dw.p) {
+            a.m_tiles = d_tiles, a.n_tiles = v_tiles;
+            a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
+            a.out_vec = aligned(p->dw.p, 8) && p->dw.stride % 4 == 0;
+            if (q.big) k_vocab_dw<T, 256, 256, 2, 4><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a, p->dim);
+            else k_vocab_dw<T, 64, 64, 2, 2><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
+        }
+    }
+    if (p->dx.p && p->rows && !whole) {
+        a.splits = q.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
+        a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
+        k_vocab_dx_out<T><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->dim);
+    }
+    return launched();
+}
+
+}  // namespace
+}  // namespace ffops
+
+using namespace ffops;
+
+extern "C" size_t ff_op_vocab_loss_fwd_workspace_bytes(const ff_vocab_loss_fwd_t* p)
+{
+    if (!p || check_vocab(p) != FF_OK || p->rows == 0) return 0;
+    return plan_of(p, false).bytes;
+}
+
+extern "C" int ff_op_vocab_loss_fwd(const ff_vocab_loss_fwd_t* p, void* stream)
+{
+    if (!p) return FF_EINVAL;
+    if (const int rc = check_vocab(p)) return rc;
+    if (p->rows == 0) return FF_OK;
+    if (!p->x.p || !p->w.p || !p->targets || !p->lse) return FF_EINVAL;
+    const Plan q = plan_of(p, false);
+    if (!p->workspace || p->workspace_bytes < q.bytes || !aligned(p->workspace, 256)) return FF_EWORKSPACE;
+    return p->dtype == FF_F16 ? fwd<F16>(p, q, (hipStream_t)stream) : fwd<BF16>(p, q, (hipStream_t)stream);
+}
+
+extern "C" size_t ff_op_vocab_loss_bwd_workspace_bytes(const ff_vocab_loss_bwd_t* p)
+{
+    if (!p || check_vocab(p) != FF_OK) return 0;
+    return plan_of(p, true).bytes;
+}
+
+extern "C" int ff_op_vocab_loss_bwd(const ff_vocab_loss_bwd_t* p, void* stream)
+{
+    if (!p) return FF_EINVAL;
+    if (const int rc = check_vocab(p)) return rc;
+    if (!p->w.p || (p->rows && (!p->x.p || !p->targets || !p->dloss || !p->lse))) return FF_EINVAL;
+    if (!p->dx.p && !p->dw.p) return FF_OK;
+    const Plan q = plan_of(p, true);
+    if (!p->workspace || p->workspace_bytes < q.bytes || !aligned(p->workspace, 256)) return FF_EWORKSPACE;
+    return p->dtype == FF_F16 ? bwd<F16>(p, q, (hipStream_t)stream) : bwd<BF16>(p, q, (hipStream_t)stream);
+}
