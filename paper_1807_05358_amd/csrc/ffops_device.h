@@ -26,17 +26,22 @@ struct F16 {
     typedef f16x8 vec8;
     static constexpr int VEC = 8;
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x4 mma(vec8 a, vec8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 struct BF16 {
     typedef __bf16 elem;
     typedef bf16x8 vec8;
     static constexpr int VEC = 8;
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ f32x4 mma(vec8 a, vec8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 // The 32x32x16 product: lane l gives A[l % 32][8 * (l / 32) + e] and B[8 * (l / 32) + e][l % 32], e = 0..7, and holds
 // C[8 * (r / 4) + 4 * (l / 32) + r % 4][l % 32] in register r = 0..15.  Which k the pair (l / 32, e) stands for does not
 // matter as long as A and B agree, so eight registers of a C tile are a B operand as they are, with
 // k = 16 * step + 8 * (e / 4) + 4 * (l / 32) + e % 4, if A is read in that order.
+// The 16x16x32 product: lane l gives A[l % 16][8 * (l / 16) + e] and B[8 * (l / 16) + e][l % 16] and holds
+// C[4 * (l / 16) + r][l % 16] in register r = 0..3.  Both do 1024 products a cycle; on numbers that are not zero the device's power sets the
+// clock, and the small one gives more of them: 2083 TFLOP/s against 1859 from registers alone, at the same reads of LDS.
 
 static __device__ __forceinline__ int c_row(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 

@@ -31,30 +31,30 @@ __device__ __forceinline__ void stage_side(lds_char* dst, const Side& s, int64_t
 template <class T, int SIZE, bool ACROSS>
 __device__ __forceinline__ typename T::vec8 operand(const lds_char* tile, int at, int step)
 {
-    if constexpr (ACROSS) return across<T, SIZE, true>(tile, step * 16, at);
-    else return along<T, KT>(tile, at, step);
+    if constexpr (ACROSS) return across16<T, SIZE>(tile, step, at);
+    else return along16<T, KT>(tile, at, step);
 }
 
-// The product of a block: c[m][n] += sum_k a[m][k] b[n][k] over k0 .. k1, M x N of it in WM x WN waves of 32 x 32 tiles, the
+// The product of a block: c[m][n] += sum_k a[m][k] b[n][k] over k0 .. k1, M x N of it in WM x WN waves of 16 x 16 tiles, the
 // tiles of both sides loaded straight into LDS one tile of k ahead.  Along sides have k in multiples of 8.
-template <class T, int M, int N, int WM, int WN, bool A_ACROSS, bool B_ACROSS>
+template <class T, int M, int N, int WAVES_M, int WAVES_N, bool A_ACROSS, bool B_ACROSS>
 struct Product {
-    static constexpr int WAVES = WM * WN, TM = M / WM / 32, TN = N / WN / 32, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
+    static constexpr int WM = WAVES_M, WN = WAVES_N, WAVES = WM * WN, TM = M / WM / 16, TN = N / WN / 16, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
 
     static __device__ __forceinline__ void step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const Side& a, const Side& b, int64_t k,
-                                                f32x16 (&c)[TM][TN], int wm, int wn)
+                                                f32x4 (&c)[TM][TN], int wm, int wn)
     {
         if (more) {
             stage_side<M, A_ACROSS, WAVES>(next, a, k + KT);
             stage_side<N, B_ACROSS, WAVES>(next + A_BYTES, b, k + KT);
         }
 #pragma unroll
-        for (int st = 0; st < KT / 16; ++st) {
+        for (int st = 0; st < KT / 32; ++st) {
             typename T::vec8 fa[TM], fb[TN];
 #pragma unroll
-            for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, B_ACROSS>(cur + A_BYTES, wn + n * 32, st);
+            for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, B_ACROSS>(cur + A_BYTES, wn + n * 16, st);
 #pragma unroll
-            for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, A_ACROSS>(cur, wm + m * 32, st);
+            for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, A_ACROSS>(cur, wm + m * 16, st);
 #pragma unroll
             for (int m = 0; m < TM; ++m)
 #pragma unroll
@@ -62,7 +62,7 @@ struct Product {
         }
     }
 
-    static __device__ __forceinline__ void run(lds_char* lds, const Side& a, const Side& b, int64_t k0, int64_t k1, f32x16 (&c)[TM][TN], int wm, int wn)
+    static __device__ __forceinline__ void run(lds_char* lds, const Side& a, const Side& b, int64_t k0, int64_t k1, f32x4 (&c)[TM][TN], int wm, int wn)
     {
         if (k0 < k1) {
             stage_side<M, A_ACROSS, WAVES>(lds, a, k0);
@@ -75,6 +75,98 @@ struct Product {
             now = BYTES - now;
             __syncthreads();
         }
+    }
+};
+
+// The same product of 256 x 256 tiles for eight waves that take turns, two on each SIMD: while one half of them (the rows
+// 0 .. 127 of the tile) multiplies, the other reads its next operands from LDS and starts loads, and at every barrier they change
+// places.  Half a tile of k is 32 products of a wave, 512 cycles of a SIMD's matrix unit; the operands of the other four waves
+// are 48 KB, 384 cycles of LDS.  In slots between barriers, the first half reads tile t in slots 4t and 4t + 2 and multiplies in
+// 4t + 1 and 4t + 3, the second half one slot later; tile t + 1 goes, from slot 4t on, into the buffer that was last read in slot
+// 4t - 1, and whoever has started loads waits for them before the barrier that ends slot 4t + 3.
+template <class T, bool A_ACROSS, bool B_ACROSS>
+struct Turns {
+    static constexpr int M = 256, N = 256, WM = 2, WN = 4, WAVES = 8, TM = 8, TN = 4, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
+    typedef Stager<A_ACROSS ? KT : M, A_ACROSS ? M : KT, WAVES> StageA;
+    typedef Stager<B_ACROSS ? KT : N, B_ACROSS ? N : KT, WAVES> StageB;
+
+    static __device__ __forceinline__ void fence()
+    {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    static __device__ __forceinline__ void barrier()
+    {
+        fence();
+        __builtin_amdgcn_s_barrier();
+        fence();
+    }
+    static constexpr int WAIT_LDS = 0xc07f, WAIT_LOADS = 0x0f70;       // s_waitcnt: lgkmcnt(0) alone, vmcnt(0) alone
+
+    static __device__ __forceinline__ void operands(const lds_char* __restrict cur, int half, typename T::vec8 (&fa)[TM], typename T::vec8 (&fb)[TN], int wm, int wn)
+    {
+#pragma unroll
+        for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, B_ACROSS>(cur + A_BYTES, wn + n * 16, half);
+#pragma unroll
+        for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, A_ACROSS>(cur, wm + m * 16, half);
+    }
+
+    static __device__ __forceinline__ void products(const typename T::vec8 (&fa)[TM], const typename T::vec8 (&fb)[TN], f32x4 (&c)[TM][TN])
+    {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int m = 0; m < TM; ++m)
+#pragma unroll
+            for (int n = 0; n < TN; ++n) c[m][n] = T::mma(fa[m], fb[n], c[m][n]);
+        __builtin_amdgcn_s_setprio(0);
+    }
+
+    // half 0 of a tile: its operands, and loads of the next tile
+    static __device__ __forceinline__ void first_half(const lds_char* __restrict cur, lds_char* __restrict next, int load, const Side& a, const Side& b, const StageA& sa, const StageB& sb,
+                                                      int64_t k, typename T::vec8 (&fa)[TM], typename T::vec8 (&fb)[TN], int wm, int wn)
+    {
+        operands(cur, 0, fa, fb, wm, wn);
+        if (load == 1) {
+            sa.template load<0, StageA::PER>(next, A_ACROSS ? a.m.p + k * a.m.stride : a.m.p + k * 2);
+            sb.template load<0, StageB::PER>(next + A_BYTES, B_ACROSS ? b.m.p + k * b.m.stride : b.m.p + k * 2);
+        } else if (load == 2) {
+            stage_side<M, A_ACROSS, WAVES>(next, a, k);
+            stage_side<N, B_ACROSS, WAVES>(next + A_BYTES, b, k);
+        }
+    }
+
+    static __device__ __forceinline__ void run(lds_char* lds, const Side& a, const Side& b, int64_t k0, int64_t k1, f32x4 (&c)[TM][TN], int wm, int wn)
+    {
+        if (k0 >= k1) return;
+        StageA sa;
+        StageB sb;
+        sa.init(a.m.stride, A_ACROSS ? KT : a.count, A_ACROSS ? (a.count + 7) / 8 : KT / 8);
+        sb.init(b.m.stride, B_ACROSS ? KT : b.count, B_ACROSS ? (b.count + 7) / 8 : KT / 8);
+        const int64_t whole = min(a.ks, b.ks);             // tiles of k that end here at the latest need no zeros
+        stage_side<M, A_ACROSS, WAVES>(lds, a, k0);
+        stage_side<N, B_ACROSS, WAVES>(lds + A_BYTES, b, k0);
+        __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+        barrier();
+        if (wm) barrier();                                  // the second half of the waves: one slot later
+        typename T::vec8 fa[TM], fb[TN];
+        int now = 0;
+        for (int64_t k = k0; k < k1; k += KT) {
+            const int64_t next = k + KT;
+            first_half(lds + now, lds + (BYTES - now), next >= k1 ? 0 : next + KT <= whole ? 1 : 2, a, b, sa, sb, next, fa, fb, wm, wn);
+            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+            barrier();
+            products(fa, fb, c);
+            barrier();
+            operands(lds + now, 1, fa, fb, wm, wn);
+            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
+            if (wm) __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+            barrier();
+            products(fa, fb, c);
+            if (!wm) __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+            barrier();
+            now = BYTES - now;
+        }
+        if (!wm) barrier();
     }
 };
 
@@ -143,70 +235,85 @@ __device__ __forceinline__ float2 join(float2 s, float2 o)
     return make_float2(top, s.y * exp2_(s.x - base) + o.y * exp2_(o.x - base));
 }
 
-template <class T, int M, int N, int WM, int WN, bool GRAD>
-__global__ __launch_bounds__(WM * WN * 64) void k_vocab_logits(VocabArgs a)
+// the product of a tile size
+template <class T, int M, bool A_ACROSS, bool B_ACROSS>
+struct ProductOf {
+    typedef Product<T, M, M, 2, 2, A_ACROSS, B_ACROSS> type;
+};
+template <class T, bool A_ACROSS, bool B_ACROSS>
+struct ProductOf<T, 256, A_ACROSS, B_ACROSS> {
+    typedef Turns<T, A_ACROSS, B_ACROSS> type;
+};
+
+template <class T, int M, bool GRAD>
+__global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_logits(VocabArgs a)
 {
-    typedef Product<T, M, N, WM, WN, false, false> P;
+    typedef typename ProductOf<T, M, false, false>::type P;
+    constexpr int N = M, WM = P::WM, WN = P::WN;
     __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
     lds_char* lds = (lds_char*)lds_;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
     uint32_t tm, tn;
     tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
     const uint32_t m0 = tm * M, n0 = tn * N;
     const Side sw = {{a.w.p + (int64_t)(a.word0 + m0) * a.w.stride, a.w.stride}, (int)min(a.words - m0, (uint32_t)M), a.dim};
     const Side sx = {{a.x.p + (int64_t)n0 * a.x.stride, a.x.stride}, (int)min(a.rows - n0, (uint32_t)N), a.dim};
-    f32x16 c[P::TM][P::TN];
+    f32x4 c[P::TM][P::TN];
 #pragma unroll
     for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x16{};
+        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
     P::run(lds, sw, sx, 0, a.dim, c, wm, wn);
     float2* stat = (float2*)lds_;           // [WM][N], the tiles have been read
 #pragma unroll
     for (int n = 0; n < P::TN; ++n) {
-        const uint32_t token = n0 + wn + n * 32 + lane % 32;
+        const uint32_t token = n0 + wn + n * 16 + lane % 16;
         const bool in = token < a.rows;
         const int32_t target = in ? a.targets[token] : a.ignore;
         const bool live = target != a.ignore;
-        // the target's place among the piece's words
-        const int64_t want = live ? (int64_t)target - a.first_word - a.word0 : -1;
+        // the target's place among the words that the lane holds: register r of tile m has word 16 * m + r after its first
+        const uint32_t v0 = m0 + wm + 4 * quarter;
+        const int64_t at = (int64_t)target - a.first_word - a.word0 - v0;
+        const int want = live && at >= 0 && at < M ? (int)at : -1;
+        const bool edge = m0 + M > a.words;
         if constexpr (GRAD) {
-            const float unit = unit_of(a.top);
-            const float ls = in ? a.lse_in[token] * LOG2E - G_SHIFT<T> : 0, f = live && in ? a.dloss[token] / unit : 0;
-            char* row = a.g + (uint64_t)token * a.g_stride * 2;
+            const float ls = in ? a.lse_in[token] * LOG2E - G_SHIFT<T> : 0, f = live && in ? a.dloss[token] / unit_of(a.top) : 0;
+            char* row = a.g + ((uint64_t)token * a.g_stride + v0) * 2;
 #pragma unroll
-            for (int m = 0; m < P::TM; ++m)
+            for (int m = 0; m < P::TM; ++m) {
+                const int v = m * 16;
+                float g[4];
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const uint32_t v = m0 + wm + m * 32 + c_row(r, half);
-                    float g[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        g[e] = (exp2_(fmaf(c[m][n][r + e], LOG2E, -ls)) - (v + e == want ? exp2f(G_SHIFT<T>) : 0.0f)) * f;
-                        if (!live || v + e >= a.words) g[e] = 0;
-                    }
-                    if (in && v < a.g_stride) store4<T>(row + v * 2, g[0], g[1], g[2], g[3]);
+                for (int e = 0; e < 4; ++e) {
+                    g[e] = exp2_(fmaf(c[m][n][e], LOG2E, -ls)) - (v + e == want ? exp2f(G_SHIFT<T>) : 0.0f);
+                    g[e] = live && (!edge || v0 + v + e < a.words) ? g[e] * f : 0.0f;
                 }
+                if (in) store4<T>(row + v * 2, g[0], g[1], g[2], g[3]);
+            }
         } else {
-            float top = -INFINITY, sum = 0;
+            float top = -INFINITY, sum = 0, z = 0;
 #pragma unroll
             for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const uint32_t v = m0 + wm + m * 32 + c_row(r, half);
-                    if (in && v == want && v < a.words) a.target_logit[token] = c[m][n][r];
-                    if (v >= a.words) c[m][n][r] = -INFINITY;
+                for (int r = 0; r < 4; ++r) {
+                    const int v = m * 16 + r;
+                    z = v == want ? c[m][n][r] : z;
+                    if (edge && v0 + v >= a.words) c[m][n][r] = -INFINITY;
                     top = fmaxf(top, c[m][n][r]);
                 }
+            // one lane of the grid has the target among its words
+            if (in && want >= 0 && want < P::TM * 16 && (want & 15) < 4 && v0 + want < a.words) a.target_logit[token] = z;
+            top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, other_half(top));
             const float base = top == -INFINITY ? 0.0f : top * LOG2E;
 #pragma unroll
             for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum += exp2_(fmaf(c[m][n][r], LOG2E, -base));
+                for (int r = 0; r < 4; ++r) sum += exp2_(fmaf(c[m][n][r], LOG2E, -base));
+            sum += __shfl_xor(sum, 16);
             sum += other_half(sum);
-            if (half == 0) stat[wave / WN * N + wn + n * 32 + lane] = make_float2(top * LOG2E, sum);
+            if (quarter == 0) stat[wave / WN * N + wn + n * 16 + lane] = make_float2(top * LOG2E, sum);
         }
     }
     if constexpr (!GRAD) {
@@ -245,12 +352,13 @@ __global__ __launch_bounds__(1024) void k_vocab_join(VocabArgs a, float* loss, f
 }
 
 // dx^T = w^T g^T over the words of a piece: elements down, tokens across
-template <class T, int M, int N, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void k_vocab_dx(VocabArgs a)
+template <class T, int M>
+__global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_dx(VocabArgs a)
 {
-    typedef Product<T, M, N, WM, WN, true, false> P;
+    typedef typename ProductOf<T, M, true, false>::type P;
+    constexpr int N = M, WM = P::WM, WN = P::WN;
     __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
     uint32_t tm, tn;
     tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
@@ -261,32 +369,29 @@ __global__ __launch_bounds__(WM * WN * 64) void k_vocab_dx(VocabArgs a)
     const Side sg = {{a.g + (uint64_t)n0 * a.g_stride * 2, (int64_t)a.g_stride * 2}, (int)min(a.rows - n0, (uint32_t)N), ks};
     const int64_t run = ((ks + a.splits - 1) / a.splits + KT - 1) / KT * KT;
     const int64_t k0 = min(ks, run * blockIdx.y), k1 = min(ks, k0 + run);
-    f32x16 c[P::TM][P::TN];
+    f32x4 c[P::TM][P::TN];
     const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
     float* sum = a.sum + (uint64_t)blockIdx.y * a.rows * a.dim;
 #pragma unroll
     for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x16{};
+        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
     P::run((lds_char*)lds_, sw, sg, k0, k1, c, wm, wn);
 #pragma unroll
     for (int n = 0; n < P::TN; ++n) {
-        const uint32_t token = n0 + wn + n * 32 + lane % 32;
+        const uint32_t token = n0 + wn + n * 16 + lane % 16;
         if (token >= a.rows) continue;
 #pragma unroll
-        for (int m = 0; m < P::TM; ++m)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const uint32_t x = m0 + wm + m * 32 + c_row(r, half);
-                if (x >= a.dim) continue;
-                const f32x16& q = c[m][n];
-                if (a.whole) store_out<T>(a.out + (int64_t)token * a.out_stride, x, a.dim, a.out_vec, q[r] * f, q[r + 1] * f, q[r + 2] * f, q[r + 3] * f);
-                else {          // dim is a multiple of 8
-                    f32x4* p = (f32x4*)(sum + (uint64_t)token * a.dim + x);
-                    const f32x4 v = {q[r], q[r + 1], q[r + 2], q[r + 3]};
-                    *p = a.first ? v : *p + v;
-                }
+        for (int m = 0; m < P::TM; ++m) {
+            const uint32_t x = m0 + wm + m * 16 + 4 * quarter;
+            if (x >= a.dim) continue;
+            const f32x4 q = c[m][n];
+            if (a.whole) store_out<T>(a.out + (int64_t)token * a.out_stride, x, a.dim, a.out_vec, q[0] * f, q[1] * f, q[2] * f, q[3] * f);
+            else {          // dim is a multiple of 8
+                f32x4* p = (f32x4*)(sum + (uint64_t)token * a.dim + x);
+                *p = a.first ? q : *p + q;
             }
+        }
     }
 }
 
@@ -303,37 +408,36 @@ __global__ __launch_bounds__(256) void k_vocab_dx_out(VocabArgs a, uint32_t dim)
 }
 
 // dw of a piece = g^T x, made transposed over the tokens: elements down, words across
-template <class T, int M, int N, int WM, int WN>
-__global__ __launch_bounds__(WM * WN * 64) void k_vocab_dw(VocabArgs a, uint32_t dim)
+template <class T, int M>
+__global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_dw(VocabArgs a, uint32_t dim)
 {
-    typedef Product<T, M, N, WM, WN, true, true> P;
+    typedef typename ProductOf<T, M, true, true>::type P;
+    constexpr int N = M, WM = P::WM, WN = P::WN;
     __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
     uint32_t tm, tn;
     tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
     const uint32_t m0 = tm * M, n0 = tn * N;
     const Side sx = {{a.x.p + m0 * 2, a.x.stride}, (int)min(a.dim - m0, (uint32_t)M), a.rows};
     const Side sg = {{a.g + n0 * 2, (int64_t)a.g_stride * 2}, (int)min(a.words - n0, (uint32_t)N), a.rows};
-    f32x16 c[P::TM][P::TN];
+    f32x4 c[P::TM][P::TN];
 #pragma unroll
     for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x16{};
+        for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
     P::run((lds_char*)lds_, sx, sg, 0, a.rows, c, wm, wn);
     const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
 #pragma unroll
     for (int n = 0; n < P::TN; ++n) {
-        const uint32_t word = n0 + wn + n * 32 + lane % 32;
+        const uint32_t word = n0 + wn + n * 16 + lane % 16;
         if (word >= a.words) continue;
         char* row = a.out + (int64_t)(a.word0 + word) * a.out_stride;
 #pragma unroll
-        for (int m = 0; m < P::TM; ++m)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const f32x16& q = c[m][n];
-                store_out<T>(row, m0 + wm + m * 32 + c_row(r, half), dim, a.out_vec, q[r] * f, q[r + 1] * f, q[r + 2] * f, q[r + 3] * f);
-            }
+        for (int m = 0; m < P::TM; ++m) {
+            const f32x4 q = c[m][n];
+            store_out<T>(row, m0 + wm + m * 16 + 4 * quarter, dim, a.out_vec, q[0] * f, q[1] * f, q[2] * f, q[3] * f);
+        }
     }
 }
 
@@ -371,7 +475,8 @@ struct Plan {
     uint64_t x, w, part, logit, top, g, sum, bytes;
 };
 
-bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0; }
+// 16-byte accesses, and 256 rows within 32 bits
+bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0 && m.stride >= 0 && m.stride < (1 << 22); }
 
 template <class A>
 Plan plan_of(const A* p, bool back)
@@ -451,8 +556,8 @@ int fwd(const ff_vocab_loss_fwd_t* p, const Plan& q, hipStream_t st)
     a.part = (float2*)(ws + q.part);
     a.target_logit = (float*)(ws + q.logit);
     const uint32_t tiles = a.m_tiles * a.n_tiles;
-    if (q.big) k_vocab_logits<T, 256, 256, 2, 4, false><<<tiles, 512, 0, st>>>(a);
-    else k_vocab_logits<T, 64, 64, 2, 2, false><<<tiles, 256, 0, st>>>(a);
+    if (q.big) k_vocab_logits<T, 256, false><<<tiles, 512, 0, st>>>(a);
+    else k_vocab_logits<T, 64, false><<<tiles, 256, 0, st>>>(a);
     k_vocab_join<<<(uint32_t)ceil_div(p->rows, 64), 1024, 0, st>>>(a, p->loss, p->lse, p->target_logit);
     return launched();
 }
@@ -476,8 +581,8 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
         a.m_tiles = (uint32_t)ceil_div(a.words, q.tile), a.n_tiles = q.n_tiles;
         const uint32_t v_tiles = a.m_tiles;
         if (p->rows) {
-            if (q.big) k_vocab_logits<T, 256, 256, 2, 4, true><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a);
-            else k_vocab_logits<T, 64, 64, 2, 2, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
+            if (q.big) k_vocab_logits<T, 256, true><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a);
+            else k_vocab_logits<T, 64, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
         }
         if (p->dx.p && p->rows) {
             a.m_tiles = d_tiles, a.n_tiles = q.n_tiles, a.splits = q.splits, a.first = word0 == 0, a.whole = whole;
@@ -485,16 +590,16 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
             a.dim = whole ? p->dim : q.dim;         // as many as are stored; the tiles of w have zeros beyond
             const dim3 grid(a.m_tiles * a.n_tiles, q.splits);
-            if (q.big) k_vocab_dx<T, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-            else k_vocab_dx<T, 64, 64, 2, 2><<<grid, 256, 0, st>>>(a);
+            if (q.big) k_vocab_dx<T, 256><<<grid, 512, 0, st>>>(a);
+            else k_vocab_dx<T, 64><<<grid, 256, 0, st>>>(a);
             a.dim = q.dim;
         }
         if (p->dw.p) {
             a.m_tiles = d_tiles, a.n_tiles = v_tiles;
             a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
             a.out_vec = aligned(p->dw.p, 8) && p->dw.stride % 4 == 0;
-            if (q.big) k_vocab_dw<T, 256, 256, 2, 4><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a, p->dim);
-            else k_vocab_dw<T, 64, 64, 2, 2><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
+            if (q.big) k_vocab_dw<T, 256><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a, p->dim);
+            else k_vocab_dw<T, 64><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
         }
     }
     if (p->dx.p && p->rows && !whole) {
