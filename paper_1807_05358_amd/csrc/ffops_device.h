@@ -27,6 +27,7 @@ struct F16 {
     static constexpr int VEC = 8;
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4 mma(vec8 a, vec8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void mma_acc(vec8 a, vec8 b, f32x4& c) { asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 struct BF16 {
     typedef __bf16 elem;
@@ -34,6 +35,7 @@ struct BF16 {
     static constexpr int VEC = 8;
     static __device__ __forceinline__ f32x16 mma(vec8 a, vec8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ f32x4 mma(vec8 a, vec8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void mma_acc(vec8 a, vec8 b, f32x4& c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 // The 32x32x16 product: lane l gives A[l % 32][8 * (l / 32) + e] and B[8 * (l / 32) + e][l % 32], e = 0..7, and holds
 // C[8 * (r / 4) + 4 * (l / 32) + r % 4][l % 32] in register r = 0..15.  Which k the pair (l / 32, e) stands for does not
@@ -52,6 +54,13 @@ static __device__ const uint4 zero16 = {0, 0, 0, 0};
 static __device__ __forceinline__ void load_lds16(const char* src, lds_char* dst)
 {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
+// the same from base + off, base uniform: the address takes one register of a lane and no arithmetic
+static __device__ __forceinline__ void load_lds16(const char* base, uint32_t off, lds_char* dst)
+{
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
 }
 
 // eight elements at p as an operand

@@ -7,12 +7,15 @@ namespace ffops {
 // A tile of rows of D elements, read along the rows (16 bytes per lane, 32 rows) or transposed (4 x 16 blocks).  The 16-byte
 // chunk c of row r lies at chunk c ^ spread(r) of its row, which puts 16 rows' chunk c, and four rows' four neighbouring
 // chunks, into different banks (a bank line of 256 bytes holds one row of 128 elements or two of 64).  Rows of 256 elements are only read transposed,
-// rows r .. r + 3 and r + 8 .. r + 11 and two chunks of each at a time.
+// rows r .. r + 3 and r + 8 .. r + 11 and two chunks of each at a time.  A 16-byte read serves lanes 0-3, 12-15, 20-23 and 24-27 together, then
+// the other sixteen of a half wave; where lanes 16-31 ask for the neighbouring chunk (16x16x32 products), rows 0-3 and 12-15 have to lie in
+// pairs of chunks that rows 4-11 leave free: hence the order 0, 2, 3, 1 of row fours in rows of 64 elements.
 template <int D>
 static __device__ __forceinline__ int spread(int r)
 {
-    static_assert(D == 64 || D == 128 || D == 256, "row lengths in use");
-    if constexpr (D == 64) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    static_assert(D == 32 || D == 64 || D == 128 || D == 256, "row lengths in use");
+    if constexpr (D == 32) return (((r >> 2) & 1) << 1) ^ (((r >> 3) & 1) * 3);
+    else if constexpr (D == 64) return (((r >> 1) & 1) << 2) | ((((r >> 2) & 1) << 1) ^ (((r >> 3) & 1) * 3));
     else if constexpr (D == 128) return ((r & 3) << 2) | ((r >> 2) & 3);
     else return ((r & 3) << 2) | (((r >> 3) & 1) << 1);
 }
@@ -51,13 +54,16 @@ struct Stager {
         }
     }
 
-    // loads FROM .. TO-1 of PER; base is uniform
-    template <int FROM, int TO>
-    __device__ __forceinline__ void load(lds_char* dst, const char* base) const
+    // base is uniform; load n of PER
+    __device__ __forceinline__ void load_one(lds_char* dst, const char* base, int n) const
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        load_lds16(base, off[n], dst + (n * WAVES + wave) * 1024);
+    }
+    __device__ __forceinline__ void load(lds_char* dst, const char* base) const
+    {
 #pragma unroll
-        for (int n = FROM; n < TO; ++n) load_lds16(base + (size_t)off[n], dst + (n * WAVES + wave) * 1024);
+        for (int n = 0; n < PER; ++n) load_one(dst, base, n);
     }
 };
 

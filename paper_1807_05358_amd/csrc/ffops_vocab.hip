@@ -18,9 +18,7 @@ struct Side {
     int64_t ks;
 };
 
-constexpr int KT = 64;      // k of a tile in LDS
-
-template <int SIZE, bool ACROSS, int WAVES>
+template <int SIZE, int KT, bool ACROSS, int WAVES>
 __device__ __forceinline__ void stage_side(lds_char* dst, const Side& s, int64_t k)
 {
     const int left = (int)min(s.ks - k, (int64_t)KT);
@@ -28,7 +26,7 @@ __device__ __forceinline__ void stage_side(lds_char* dst, const Side& s, int64_t
     else stage<SIZE, KT, WAVES>(dst, s.m.p + k * 2, s.m.stride, s.count, left / 8);
 }
 
-template <class T, int SIZE, bool ACROSS>
+template <class T, int SIZE, int KT, bool ACROSS>
 __device__ __forceinline__ typename T::vec8 operand(const lds_char* tile, int at, int step)
 {
     if constexpr (ACROSS) return across16<T, SIZE>(tile, step, at);
@@ -39,22 +37,23 @@ __device__ __forceinline__ typename T::vec8 operand(const lds_char* tile, int at
 // tiles of both sides loaded straight into LDS one tile of k ahead.  Along sides have k in multiples of 8.
 template <class T, int M, int N, int WAVES_M, int WAVES_N, bool A_ACROSS, bool B_ACROSS>
 struct Product {
-    static constexpr int WM = WAVES_M, WN = WAVES_N, WAVES = WM * WN, TM = M / WM / 16, TN = N / WN / 16, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
+    static constexpr int KT = 64;       // k of a tile in LDS
+    static constexpr int WM = WAVES_M, WN = WAVES_N, WAVES = WM * WN, TM = M / WM / 16, TN = N / WN / 16, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2, LDS = 2 * BYTES;
 
     static __device__ __forceinline__ void step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const Side& a, const Side& b, int64_t k,
                                                 f32x4 (&c)[TM][TN], int wm, int wn)
     {
         if (more) {
-            stage_side<M, A_ACROSS, WAVES>(next, a, k + KT);
-            stage_side<N, B_ACROSS, WAVES>(next + A_BYTES, b, k + KT);
+            stage_side<M, KT, A_ACROSS, WAVES>(next, a, k + KT);
+            stage_side<N, KT, B_ACROSS, WAVES>(next + A_BYTES, b, k + KT);
         }
 #pragma unroll
         for (int st = 0; st < KT / 32; ++st) {
             typename T::vec8 fa[TM], fb[TN];
 #pragma unroll
-            for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, B_ACROSS>(cur + A_BYTES, wn + n * 16, st);
+            for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, KT, B_ACROSS>(cur + A_BYTES, wn + n * 16, st);
 #pragma unroll
-            for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, A_ACROSS>(cur, wm + m * 16, st);
+            for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, KT, A_ACROSS>(cur, wm + m * 16, st);
 #pragma unroll
             for (int m = 0; m < TM; ++m)
 #pragma unroll
@@ -65,8 +64,8 @@ struct Product {
     static __device__ __forceinline__ void run(lds_char* lds, const Side& a, const Side& b, int64_t k0, int64_t k1, f32x4 (&c)[TM][TN], int wm, int wn)
     {
         if (k0 < k1) {
-            stage_side<M, A_ACROSS, WAVES>(lds, a, k0);
-            stage_side<N, B_ACROSS, WAVES>(lds + A_BYTES, b, k0);
+            stage_side<M, KT, A_ACROSS, WAVES>(lds, a, k0);
+            stage_side<N, KT, B_ACROSS, WAVES>(lds + A_BYTES, b, k0);
         }
         __syncthreads();
         int now = 0;
@@ -78,60 +77,54 @@ struct Product {
     }
 };
 
-// The same product of 256 x 256 tiles for eight waves that take turns, two on each SIMD: while one half of them (the rows
-// 0 .. 127 of the tile) multiplies, the other reads its next operands from LDS and starts loads, and at every barrier they change
-// places.  Half a tile of k is 32 products of a wave, 512 cycles of a SIMD's matrix unit; the operands of the other four waves
-// are 48 KB, 384 cycles of LDS.  In slots between barriers, the first half reads tile t in slots 4t and 4t + 2 and multiplies in
-// 4t + 1 and 4t + 3, the second half one slot later; tile t + 1 goes, from slot 4t on, into the buffer that was last read in slot
-// 4t - 1, and whoever has started loads waits for them before the barrier that ends slot 4t + 3.
+// The same product of 256 x 256 tiles by four waves, one on each SIMD, 128 x 128 each: 16 products of 32 in k need four operands
+// of 16 rows and four of 16 columns, a third less from LDS than waves of 128 x 64 would read, and LDS is what two waves a SIMD wait for (its
+// reads and the loads' writes share it).  Half a tile of k is 64 products of a wave, 1024 cycles of its SIMD's matrix unit, in eight rows of eight.
+// Between the products the wave reads, two rows ahead, the row's operand of a, one of the next half's of b, and starts one load.
+// LDS holds three tiles of a and two of b, all of its 160 KB.  Half 0 of tile s starts the loads of a's tile s + 2, half 1 those of b's, whose buffer has been
+// read by then; half 1 reads the first operands of tile s + 1, which have had a half at least to arrive.
 template <class T, bool A_ACROSS, bool B_ACROSS>
-struct Turns {
-    static constexpr int M = 256, N = 256, WM = 2, WN = 4, WAVES = 8, TM = 8, TN = 4, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
+struct Wide {
+    static constexpr int KT = 64;               // rows of 128 bytes: caches are asked for whole lines
+    static constexpr int M = 256, N = 256, WM = 2, WN = 2, WAVES = 4, TM = 8, TN = 8, TILE = 256 * KT * 2, LDS = 5 * TILE;
     typedef Stager<A_ACROSS ? KT : M, A_ACROSS ? M : KT, WAVES> StageA;
     typedef Stager<B_ACROSS ? KT : N, B_ACROSS ? N : KT, WAVES> StageB;
+    typedef typename T::vec8 vec8;
+    static constexpr int LOADS = StageA::PER;   // of a wave, for a tile of either side
+    static_assert(StageA::PER == 8 && StageB::PER == 8, "one load for every row of products");
 
-    static __device__ __forceinline__ void fence()
+    // what this wave has asked of LDS, and of memory but for the latest `newer` loads, is there, and so is what all others have
+    template <int NEWER>
+    static __device__ __forceinline__ void meet()
     {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-    }
-    static __device__ __forceinline__ void barrier()
-    {
-        fence();
+        __builtin_amdgcn_s_waitcnt(0x0070 | NEWER);     // vmcnt, lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
-        fence();
-    }
-    static constexpr int WAIT_LDS = 0xc07f, WAIT_LOADS = 0x0f70;       // s_waitcnt: lgkmcnt(0) alone, vmcnt(0) alone
-
-    static __device__ __forceinline__ void operands(const lds_char* __restrict cur, int half, typename T::vec8 (&fa)[TM], typename T::vec8 (&fb)[TN], int wm, int wn)
-    {
-#pragma unroll
-        for (int n = 0; n < TN; ++n) fb[n] = operand<T, N, B_ACROSS>(cur + A_BYTES, wn + n * 16, half);
-#pragma unroll
-        for (int m = 0; m < TM; ++m) fa[m] = operand<T, M, A_ACROSS>(cur, wm + m * 16, half);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
     }
 
-    static __device__ __forceinline__ void products(const typename T::vec8 (&fa)[TM], const typename T::vec8 (&fb)[TN], f32x4 (&c)[TM][TN])
-    {
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int m = 0; m < TM; ++m)
-#pragma unroll
-            for (int n = 0; n < TN; ++n) c[m][n] = T::mma(fa[m], fb[n], c[m][n]);
-        __builtin_amdgcn_s_setprio(0);
-    }
+    static __device__ __forceinline__ const char* at(const Side& s, bool across, int64_t k) { return across ? s.m.p + k * s.m.stride : s.m.p + k * 2; }
+    static __device__ __forceinline__ vec8 of_a(const lds_char* tile, int half, int m, int wm) { return operand<T, M, KT, A_ACROSS>(tile, wm + m * 16, half); }
+    static __device__ __forceinline__ vec8 of_b(const lds_char* tile, int half, int n, int wn) { return operand<T, N, KT, B_ACROSS>(tile, wn + n * 16, half); }
 
-    // half 0 of a tile: its operands, and loads of the next tile
-    static __device__ __forceinline__ void first_half(const lds_char* __restrict cur, lds_char* __restrict next, int load, const Side& a, const Side& b, const StageA& sa, const StageB& sb,
-                                                      int64_t k, typename T::vec8 (&fa)[TM], typename T::vec8 (&fb)[TN], int wm, int wn)
+    // the products of half HALF of a tile whose a is at `a`; the next half's operands are in `an` and `bn`.  fa: the row's operand and the next two.
+    template <int HALF, int LOAD, class S>
+    static __device__ __forceinline__ void half(const lds_char* __restrict a, const lds_char* __restrict an, const lds_char* __restrict bn, lds_char* __restrict into, const char* from, const S& stage,
+                                                vec8 (&fa)[4], const vec8 (&fb)[TN], vec8 (&gb)[TN], f32x4 (&c)[TM][TN], int wm, int wn)
     {
-        operands(cur, 0, fa, fb, wm, wn);
-        if (load == 1) {
-            sa.template load<0, StageA::PER>(next, A_ACROSS ? a.m.p + k * a.m.stride : a.m.p + k * 2);
-            sb.template load<0, StageB::PER>(next + A_BYTES, B_ACROSS ? b.m.p + k * b.m.stride : b.m.p + k * 2);
-        } else if (load == 2) {
-            stage_side<M, A_ACROSS, WAVES>(next, a, k);
-            stage_side<N, B_ACROSS, WAVES>(next + A_BYTES, b, k);
+#pragma unroll
+        for (int m = 0; m < TM; ++m) {
+            gb[m] = of_b(bn, 1 - HALF, m, wn);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) T::mma_acc(fa[m % 4], fb[n], c[m][n]);
+            fa[(m + 2) % 4] = m + 2 < TM ? of_a(a, HALF, m + 2, wm) : of_a(an, 1 - HALF, m + 2 - TM, wm);
+#pragma unroll
+            for (int n = 3; n < 6; ++n) T::mma_acc(fa[m % 4], fb[n], c[m][n]);
+            if (LOAD) stage.load_one(into, from, m);
+#pragma unroll
+            for (int n = 6; n < TN; ++n) T::mma_acc(fa[m % 4], fb[n], c[m][n]);
         }
     }
 
@@ -142,31 +135,49 @@ struct Turns {
         StageB sb;
         sa.init(a.m.stride, A_ACROSS ? KT : a.count, A_ACROSS ? (a.count + 7) / 8 : KT / 8);
         sb.init(b.m.stride, B_ACROSS ? KT : b.count, B_ACROSS ? (b.count + 7) / 8 : KT / 8);
-        const int64_t whole = min(a.ks, b.ks);             // tiles of k that end here at the latest need no zeros
-        stage_side<M, A_ACROSS, WAVES>(lds, a, k0);
-        stage_side<N, B_ACROSS, WAVES>(lds + A_BYTES, b, k0);
-        __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
-        barrier();
-        if (wm) barrier();                                  // the second half of the waves: one slot later
-        typename T::vec8 fa[TM], fb[TN];
-        int now = 0;
-        for (int64_t k = k0; k < k1; k += KT) {
-            const int64_t next = k + KT;
-            first_half(lds + now, lds + (BYTES - now), next >= k1 ? 0 : next + KT <= whole ? 1 : 2, a, b, sa, sb, next, fa, fb, wm, wn);
-            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
-            barrier();
-            products(fa, fb, c);
-            barrier();
-            operands(lds + now, 1, fa, fb, wm, wn);
-            __builtin_amdgcn_s_waitcnt(WAIT_LDS);
-            if (wm) __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
-            barrier();
-            products(fa, fb, c);
-            if (!wm) __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
-            barrier();
-            now = BYTES - now;
+        // the order of k is free: what is no whole tile comes first, so that the loop has whole ones
+        const int64_t wholes = (min(k1, min(a.ks, b.ks)) - k0) / KT, rest = k0 + wholes * KT;
+        const int odd = rest < k1;
+        int left = (int)wholes + odd;
+        lds_char* lb = lds + 3 * TILE;
+        for (int j = 0; j < 2 && j < left; ++j) {
+            if (j < odd) {
+                stage_side<M, KT, A_ACROSS, WAVES>(lds, a, rest);
+                stage_side<N, KT, B_ACROSS, WAVES>(lb, b, rest);
+            } else {
+                sa.load(lds + j * TILE, at(a, A_ACROSS, k0 + (j - odd) * KT));
+                sb.load(lb + j * TILE, at(b, B_ACROSS, k0 + (j - odd) * KT));
+            }
         }
-        if (!wm) barrier();
+        const int64_t as = A_ACROSS ? KT * a.m.stride : KT * 2, bs = B_ACROSS ? KT * b.m.stride : KT * 2;
+        const char *pa = at(a, A_ACROSS, k0 + (2 - odd) * KT), *pb = at(b, B_ACROSS, k0 + (2 - odd) * KT);
+        vec8 fa[4], fb[TN], gb[TN];
+        meet<0>();
+        fa[0] = of_a(lds, 0, 0, wm), fa[1] = of_a(lds, 0, 1, wm);
+#pragma unroll
+        for (int n = 0; n < TN; ++n) fb[n] = of_b(lb, 0, n, wn);
+        int ia = 0, ib = 0;
+        for (; left > 2; --left) {
+            const int next = ia == 2 * TILE ? 0 : ia + TILE, free = next == 2 * TILE ? 0 : next + TILE;
+            half<0, 1>(lds + ia, lds + ia, lb + ib, lds + free, pa, sa, fa, fb, gb, c, wm, wn);
+            meet<LOADS>();
+            half<1, 1>(lds + ia, lds + next, lb + (TILE - ib), lb + ib, pb, sb, fa, gb, fb, c, wm, wn);
+            meet<15>();                          // for the reads alone
+            pa += as, pb += bs;
+            ia = next, ib = TILE - ib;
+        }
+        for (; left > 0; --left) {              // the last operands read are of what is there, and not used
+            const int next = ia == 2 * TILE ? 0 : ia + TILE;
+            half<0, 0>(lds + ia, lds + ia, lb + ib, lds, pa, sa, fa, fb, gb, c, wm, wn);
+            meet<0>();
+            half<1, 0>(lds + ia, lds + next, lb + (TILE - ib), lb, pb, sb, fa, gb, fb, c, wm, wn);
+            meet<0>();
+            ia = next, ib = TILE - ib;
+        }
+        // the last products write their registers some cycles after they were issued, of which the compiler knows nothing
+        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+        for (int m = 0; m < TM; ++m) asm volatile("" : "+a"(c[m][0]), "+a"(c[m][1]), "+a"(c[m][2]), "+a"(c[m][3]), "+a"(c[m][4]), "+a"(c[m][5]), "+a"(c[m][6]), "+a"(c[m][7]));
     }
 };
 
@@ -242,15 +253,15 @@ struct ProductOf {
 };
 template <class T, bool A_ACROSS, bool B_ACROSS>
 struct ProductOf<T, 256, A_ACROSS, B_ACROSS> {
-    typedef Turns<T, A_ACROSS, B_ACROSS> type;
+    typedef Wide<T, A_ACROSS, B_ACROSS> type;
 };
 
 template <class T, int M, bool GRAD>
-__global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_logits(VocabArgs a)
+__global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
 {
     typedef typename ProductOf<T, M, false, false>::type P;
     constexpr int N = M, WM = P::WM, WN = P::WN;
-    __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
+    __shared__ __attribute__((aligned(256))) char lds_[P::LDS];
     lds_char* lds = (lds_char*)lds_;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
@@ -353,11 +364,11 @@ __global__ __launch_bounds__(1024) void k_vocab_join(VocabArgs a, float* loss, f
 
 // dx^T = w^T g^T over the words of a piece: elements down, tokens across
 template <class T, int M>
-__global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_dx(VocabArgs a)
+__global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
 {
     typedef typename ProductOf<T, M, true, false>::type P;
     constexpr int N = M, WM = P::WM, WN = P::WN;
-    __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
+    __shared__ __attribute__((aligned(256))) char lds_[P::LDS];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
     uint32_t tm, tn;
@@ -367,7 +378,7 @@ __global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_dx(VocabArgs a)
     // g has zeros beyond the last word, up to a multiple of 8
     const int64_t ks = ((int64_t)a.words + 7) / 8 * 8;
     const Side sg = {{a.g + (uint64_t)n0 * a.g_stride * 2, (int64_t)a.g_stride * 2}, (int)min(a.rows - n0, (uint32_t)N), ks};
-    const int64_t run = ((ks + a.splits - 1) / a.splits + KT - 1) / KT * KT;
+    const int64_t run = ((ks + a.splits - 1) / a.splits + 63) / 64 * 64;
     const int64_t k0 = min(ks, run * blockIdx.y), k1 = min(ks, k0 + run);
     f32x4 c[P::TM][P::TN];
     const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
@@ -409,11 +420,11 @@ __global__ __launch_bounds__(256) void k_vocab_dx_out(VocabArgs a, uint32_t dim)
 
 // dw of a piece = g^T x, made transposed over the tokens: elements down, words across
 template <class T, int M>
-__global__ __launch_bounds__(M == 256 ? 512 : 256) void k_vocab_dw(VocabArgs a, uint32_t dim)
+__global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
 {
     typedef typename ProductOf<T, M, true, true>::type P;
     constexpr int N = M, WM = P::WM, WN = P::WN;
-    __shared__ __attribute__((aligned(256))) char lds_[2 * P::BYTES];
+    __shared__ __attribute__((aligned(256))) char lds_[P::LDS];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
     uint32_t tm, tn;
@@ -504,7 +515,7 @@ Plan plan_of(const A* p, bool back)
         const uint64_t fit = PIECE_BYTES / 2 / std::max(1u, p->rows) / 256 * 256;
         q.piece = (uint32_t)std::min<uint64_t>(round_up(p->vocab, 256), std::max<uint64_t>(fit, 256));
         q.g = take((uint64_t)p->rows * q.piece * 2);
-        const uint64_t tiles = ceil_div(q.dim, q.tile) * q.n_tiles, ks = std::min(p->vocab, q.piece) / KT;
+        const uint64_t tiles = ceil_div(q.dim, q.tile) * q.n_tiles, ks = std::min(p->vocab, q.piece) / 64;
         const uint64_t want = q.big ? 256 : 1024;
         q.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({tiles ? want / tiles : 1, ks / 8, 16}));
         q.sum = take(q.splits > 1 || q.piece < p->vocab ? (uint64_t)q.splits * p->rows * q.dim * sizeof(float) : 0);
@@ -556,7 +567,7 @@ int fwd(const ff_vocab_loss_fwd_t* p, const Plan& q, hipStream_t st)
     a.part = (float2*)(ws + q.part);
     a.target_logit = (float*)(ws + q.logit);
     const uint32_t tiles = a.m_tiles * a.n_tiles;
-    if (q.big) k_vocab_logits<T, 256, false><<<tiles, 512, 0, st>>>(a);
+    if (q.big) k_vocab_logits<T, 256, false><<<tiles, 256, 0, st>>>(a);
     else k_vocab_logits<T, 64, false><<<tiles, 256, 0, st>>>(a);
     k_vocab_join<<<(uint32_t)ceil_div(p->rows, 64), 1024, 0, st>>>(a, p->loss, p->lse, p->target_logit);
     return launched();
@@ -581,7 +592,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
         a.m_tiles = (uint32_t)ceil_div(a.words, q.tile), a.n_tiles = q.n_tiles;
         const uint32_t v_tiles = a.m_tiles;
         if (p->rows) {
-            if (q.big) k_vocab_logits<T, 256, true><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a);
+            if (q.big) k_vocab_logits<T, 256, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
             else k_vocab_logits<T, 64, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
         }
         if (p->dx.p && p->rows) {
@@ -590,7 +601,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
             a.dim = whole ? p->dim : q.dim;         // as many as are stored; the tiles of w have zeros beyond
             const dim3 grid(a.m_tiles * a.n_tiles, q.splits);
-            if (q.big) k_vocab_dx<T, 256><<<grid, 512, 0, st>>>(a);
+            if (q.big) k_vocab_dx<T, 256><<<grid, 256, 0, st>>>(a);
             else k_vocab_dx<T, 64><<<grid, 256, 0, st>>>(a);
             a.dim = q.dim;
         }
@@ -598,7 +609,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             a.m_tiles = d_tiles, a.n_tiles = v_tiles;
             a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
             a.out_vec = aligned(p->dw.p, 8) && p->dw.stride % 4 == 0;
-            if (q.big) k_vocab_dw<T, 256><<<a.m_tiles * a.n_tiles, 512, 0, st>>>(a, p->dim);
+            if (q.big) k_vocab_dw<T, 256><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
             else k_vocab_dw<T, 64><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
         }
     }
