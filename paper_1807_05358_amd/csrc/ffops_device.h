@@ -96,6 +96,13 @@ static __device__ __forceinline__ void store4(void* p, float a, float b, float c
     *(v4*)p = v4{(typename T::elem)a, (typename T::elem)b, (typename T::elem)c, (typename T::elem)d};
 }
 
+template <class T>
+static __device__ __forceinline__ uint2 pack4(f32x4 c)
+{
+    typedef typename T::elem v4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint2, v4{(typename T::elem)c[0], (typename T::elem)c[1], (typename T::elem)c[2], (typename T::elem)c[3]});
+}
+
 static __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 static __device__ __forceinline__ float log2_(float x) { return __builtin_amdgcn_logf(x); }
 

@@ -288,40 +288,58 @@ __global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
         const int64_t at = (int64_t)target - a.first_word - a.word0 - v0;
         const int want = live && at >= 0 && at < M ? (int)at : -1;
         const bool edge = m0 + M > a.words;
+        // almost no tile has a lane's target or the last word
         if constexpr (GRAD) {
-            const float ls = in ? a.lse_in[token] * LOG2E - G_SHIFT<T> : 0, f = live && in ? a.dloss[token] / unit_of(a.top) : 0;
-            char* row = a.g + ((uint64_t)token * a.g_stride + v0) * 2;
+            // a row that takes no part has exp(-inf)
+            const float ls = live ? a.lse_in[token] * LOG2E - G_SHIFT<T> : INFINITY, f = live ? a.dloss[token] / unit_of(a.top) : 0;
+            char* row = a.g + ((uint64_t)token * a.g_stride + v0 + (quarter & 1) * 12) * 2;
 #pragma unroll
-            for (int m = 0; m < P::TM; ++m) {
-                const int v = m * 16;
-                float g[4];
+            for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    g[e] = exp2_(fmaf(c[m][n][e], LOG2E, -ls)) - (v + e == want ? exp2f(G_SHIFT<T>) : 0.0f);
-                    g[e] = live && (!edge || v0 + v + e < a.words) ? g[e] * f : 0.0f;
-                }
-                if (in) store4<T>(row + v * 2, g[0], g[1], g[2], g[3]);
+                for (int e = 0; e < 4; ++e) c[m][n][e] = exp2_(fmaf(c[m][n][e], LOG2E, -ls)) * f;
+            if (edge || __any(want >= 0))
+#pragma unroll
+                for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int v = m * 16 + e;
+                        if (v == want) c[m][n][e] -= exp2f(G_SHIFT<T>) * f;
+                        if (!live || v0 + v >= a.words) c[m][n][e] = 0;
+                    }
+            // of two tiles, even quarters take their own and their odd neighbour's words of the first, odd ones of the second: 16 bytes a lane
+#pragma unroll
+            for (int m = 0; m < P::TM; m += 2) {
+                const uint2 x = pack4<T>(c[m][n]), y = pack4<T>(c[m + 1][n]);
+                const auto s = __builtin_amdgcn_permlane16_swap(x.x, y.x, false, false), t = __builtin_amdgcn_permlane16_swap(x.y, y.y, false, false);
+                if (in) *(uint4*)(row + m * 32) = make_uint4(s[0], t[0], s[1], t[1]);
             }
         } else {
-            float top = -INFINITY, sum = 0, z = 0;
+            if (__any(want >= 0)) {
+                float z = 0;
 #pragma unroll
-            for (int m = 0; m < P::TM; ++m)
+                for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int v = m * 16 + r;
-                    z = v == want ? c[m][n][r] : z;
-                    if (edge && v0 + v >= a.words) c[m][n][r] = -INFINITY;
-                    top = fmaxf(top, c[m][n][r]);
-                }
-            // one lane of the grid has the target among its words
-            if (in && want >= 0 && want < P::TM * 16 && (want & 15) < 4 && v0 + want < a.words) a.target_logit[token] = z;
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, other_half(top));
-            const float base = top == -INFINITY ? 0.0f : top * LOG2E;
+                    for (int r = 0; r < 4; ++r) z = m * 16 + r == want ? c[m][n][r] : z;
+                // one lane of the grid has the target among its words
+                if (in && want >= 0 && want < P::TM * 16 && (want & 15) < 4 && v0 + want < a.words) a.target_logit[token] = z;
+            }
+            float top = -INFINITY, sum = 0, base;
+            const auto sums = [&](auto last) {
+                const auto z = [&](int m, int r) { return last && v0 + m * 16 + r >= a.words ? -INFINITY : c[m][n][r]; };
 #pragma unroll
-            for (int m = 0; m < P::TM; ++m)
+                for (int m = 0; m < P::TM; ++m)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) sum += exp2_(fmaf(c[m][n][r], LOG2E, -base));
+                    for (int r = 0; r < 4; ++r) top = fmaxf(top, z(m, r));
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, other_half(top));
+                base = top == -INFINITY ? 0.0f : top * LOG2E;
+#pragma unroll
+                for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) sum += exp2_(fmaf(z(m, r), LOG2E, -base));
+            };
+            if (edge) sums(std::true_type());
+            else sums(std::false_type());
             sum += __shfl_xor(sum, 16);
             sum += other_half(sum);
             if (quarter == 0) stat[wave / WN * N + wn + n * 16 + lane] = make_float2(top * LOG2E, sum);
