@@ -204,7 +204,7 @@ struct VocabArgs {
     float* target_logit;
     char* g;                                // [rows][g_stride]: gradient of the logits of a piece
     uint32_t g_stride;
-    float* sum;                             // [splits][rows][dim]: dx, over pieces and splits
+    float* sum;                             // [splits][rows or words][dim]: dx, over pieces and splits; dw, over splits
     uint32_t splits, first, whole;          // dx: the first piece; one piece and no splits, so that dx is written at once
     char* out;
     int64_t out_stride;                     // bytes
@@ -424,11 +424,11 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
     }
 }
 
-// dx from the sums of its splits
+// rows of an output from the sums of their splits
 template <class T>
-__global__ __launch_bounds__(256) void k_vocab_dx_out(VocabArgs a, uint32_t dim)
+__global__ __launch_bounds__(256) void k_vocab_add(VocabArgs a, uint32_t rows, uint32_t dim)
 {
-    const uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (uint64_t)a.rows * a.dim;
+    const uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (uint64_t)rows * a.dim;
     if (at >= n) return;
     f32x4 s = {};
     for (uint32_t k = 0; k < a.splits; ++k) s += *(const f32x4*)(a.sum + k * n + at);
@@ -455,8 +455,11 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
     for (int m = 0; m < P::TM; ++m)
 #pragma unroll
         for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
-    P::run((lds_char*)lds_, sx, sg, 0, a.rows, c, wm, wn);
+    const int64_t run = (((int64_t)a.rows + a.splits - 1) / a.splits + 63) / 64 * 64;
+    const int64_t k0 = min((int64_t)a.rows, run * blockIdx.y), k1 = min((int64_t)a.rows, k0 + run);
+    P::run((lds_char*)lds_, sx, sg, k0, k1, c, wm, wn);
     const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
+    float* sum = a.sum + (uint64_t)blockIdx.y * a.words * a.dim;
 #pragma unroll
     for (int n = 0; n < P::TN; ++n) {
         const uint32_t word = n0 + wn + n * 16 + lane % 16;
@@ -464,8 +467,11 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
         char* row = a.out + (int64_t)(a.word0 + word) * a.out_stride;
 #pragma unroll
         for (int m = 0; m < P::TM; ++m) {
+            const uint32_t x = m0 + wm + m * 16 + 4 * quarter;
+            if (x >= a.dim) continue;
             const f32x4 q = c[m][n];
-            store_out<T>(row, m0 + wm + m * 16 + 4 * quarter, dim, a.out_vec, q[0] * f, q[1] * f, q[2] * f, q[3] * f);
+            if (a.splits == 1) store_out<T>(row, x, dim, a.out_vec, q[0] * f, q[1] * f, q[2] * f, q[3] * f);
+            else *(f32x4*)(sum + (uint64_t)word * a.dim + x) = q;
         }
     }
 }
@@ -501,8 +507,15 @@ struct Plan {
     uint32_t dim;               // a multiple of 8
     bool copy_x, copy_w, big;
     uint32_t tile, m_tiles, n_tiles, piece, splits;
-    uint64_t x, w, part, logit, top, g, sum, bytes;
+    uint64_t x, w, part, logit, top, g, sum, dw, bytes;
 };
+
+// A product of fewer tiles than the device has places is split over k, into no less than 512 of it, its sums added up afterwards.
+uint32_t splits_of(uint64_t tiles, uint64_t k, bool big)
+{
+    if (tiles == 0) return 1;
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({(big ? 256 : 1024) / tiles, k / 512, 16}));
+}
 
 // 16-byte accesses, and 256 rows within 32 bits
 bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0 && m.stride >= 0 && m.stride < (1 << 22); }
@@ -533,10 +546,16 @@ Plan plan_of(const A* p, bool back)
         const uint64_t fit = PIECE_BYTES / 2 / std::max(1u, p->rows) / 256 * 256;
         q.piece = (uint32_t)std::min<uint64_t>(round_up(p->vocab, 256), std::max<uint64_t>(fit, 256));
         q.g = take((uint64_t)p->rows * q.piece * 2);
-        const uint64_t tiles = ceil_div(q.dim, q.tile) * q.n_tiles, ks = std::min(p->vocab, q.piece) / 64;
-        const uint64_t want = q.big ? 256 : 1024;
-        q.splits = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({tiles ? want / tiles : 1, ks / 8, 16}));
+        const uint64_t d_tiles = ceil_div(q.dim, q.tile);
+        q.splits = splits_of(d_tiles * q.n_tiles, std::min(p->vocab, q.piece), q.big);
         q.sum = take(q.splits > 1 || q.piece < p->vocab ? (uint64_t)q.splits * p->rows * q.dim * sizeof(float) : 0);
+        // the last piece may be smaller than the others, and the only one whose dw is split
+        uint64_t dw = 0;
+        for (const uint64_t words : {(uint64_t)std::min(p->vocab, q.piece), (uint64_t)(p->vocab - 1) % q.piece + 1}) {
+            const uint32_t n = splits_of(d_tiles * ceil_div(words, q.tile), p->rows, q.big);
+            if (n > 1) dw = std::max<uint64_t>(dw, n * words * q.dim * sizeof(float));
+        }
+        q.dw = take(dw);
     }
     q.bytes = at;
     return q;
@@ -627,14 +646,22 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             a.m_tiles = d_tiles, a.n_tiles = v_tiles;
             a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
             a.out_vec = aligned(p->dw.p, 8) && p->dw.stride % 4 == 0;
-            if (q.big) k_vocab_dw<T, 256><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
-            else k_vocab_dw<T, 64><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a, p->dim);
+            a.splits = splits_of((uint64_t)d_tiles * v_tiles, p->rows, q.big), a.sum = (float*)(ws + q.dw);
+            const dim3 grid(a.m_tiles * a.n_tiles, a.splits);
+            if (q.big) k_vocab_dw<T, 256><<<grid, 256, 0, st>>>(a, p->dim);
+            else k_vocab_dw<T, 64><<<grid, 256, 0, st>>>(a, p->dim);
+            if (a.splits > 1) {
+                VocabArgs o = a;
+                o.out += (int64_t)word0 * a.out_stride;
+                k_vocab_add<T><<<(uint32_t)ceil_div((uint64_t)a.words * q.dim / 4, 256), 256, 0, st>>>(o, a.words, p->dim);
+            }
+            a.sum = (float*)(ws + q.sum);
         }
     }
     if (p->dx.p && p->rows && !whole) {
         a.splits = q.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
         a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
-        k_vocab_dx_out<T><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->dim);
+        k_vocab_add<T><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->rows, p->dim);
     }
     return launched();
 }
