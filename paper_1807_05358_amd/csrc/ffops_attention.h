@@ -37,6 +37,31 @@ static __device__ __forceinline__ int seen_by(const AttnArgs& a, int i, int nq, 
     return n < 0 ? 0 : n > nk ? nk : n;
 }
 
+// Loads of tiles of ROWS positions: whole ones from places worked out once (those of a tile have to fit 32 bits), others with zeros for what is missing.  Elements
+// beyond a head's are zeros in the operands in registers, so what a whole tile holds in their place does not matter.
+template <int ROWS, int D, int WAVES>
+struct TileLoads {
+    Stager<ROWS, D, WAVES> whole;
+    int64_t stride;
+    int chunks;
+    bool near;
+
+    __device__ __forceinline__ void init(int64_t pos, int n)
+    {
+        stride = pos, chunks = n;
+        near = pos >= 0 && pos < (1 << 25);
+        whole.init(pos, ROWS, n);
+    }
+    __device__ __forceinline__ void load(lds_char* dst, const char* p, int rows) const
+    {
+        if (near && rows >= ROWS) whole.load(dst, p);
+        else stage<ROWS, D, WAVES>(dst, p, stride, rows, chunks);
+    }
+};
+
+// keeps what follows it in its branch: without it the compiler takes comparisons for every tile that only the last ones need
+static __device__ __forceinline__ void stay_here() { asm volatile(""); }
+
 // operands in registers: a row of D elements at p (null: zeros), element 16 * step + 8 * half + e
 template <class T, int D>
 static __device__ __forceinline__ void row_operand(typename T::vec8* f, const char* p, int dim, int half)

@@ -72,23 +72,22 @@ __device__ __forceinline__ void store_row(char* p, const f32x16& c, int x, int d
         if (x + c_row(r, half) < dim) store4<T>(p + (x + c_row(r, half)) * 2, c[r] * f, c[r + 1] * f, c[r + 2] * f, c[r + 3] * f);
 }
 
-struct Next {           // what is staged while a tile is worked on
+struct Next {           // what is loaded while a tile is worked on
     const char *a, *b;
-    int64_t as, bs;
     int rows;
     bool more;
 };
 
 template <class T, int D, int WAVES>
-__device__ __forceinline__ void dkv_step(const lds_char* __restrict cur, lds_char* __restrict next, const float* stat, const Next& n, int chunks,
+__device__ __forceinline__ void dkv_step(const lds_char* __restrict cur, lds_char* __restrict next, const float* stat, const Next& n, const TileLoads<STEP, D, WAVES>& la, const TileLoads<STEP, D, WAVES>& lb,
                                          const typename T::vec8* kf, const typename T::vec8* vf, f32x16* dk, f32x16* dv, float c, float per, int key0, int nk,
                                          int i0, int shift, bool causal)
 {
     constexpr int DB = D / 32;
     const int lane = threadIdx.x % 64, half = lane / 32, key = key0 + lane % 32;
     if (n.more) {
-        stage<STEP, D, WAVES>(next, n.a, n.as, n.rows, chunks);
-        stage<STEP, D, WAVES>(next + STEP * D * 2, n.b, n.bs, n.rows, chunks);
+        la.load(next, n.a, n.rows);
+        lb.load(next + STEP * D * 2, n.b, n.rows);
     }
     if (key0 >= nk) return;
     const lds_char *qt = cur, *dt = cur + STEP * D * 2;
@@ -98,9 +97,11 @@ __device__ __forceinline__ void dkv_step(const lds_char* __restrict cur, lds_cha
         if (causal && key0 > ib + 31 + shift) continue;
         f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st) s = T::mma(along<T, D>(qt, b * 32, st), kf[st], s);
-#pragma unroll
-        for (int st = 0; st < D / 16; ++st) dp = T::mma(along<T, D>(dt, b * 32, st), vf[st], dp);
+        for (int st = 0; st < D / 16; ++st) {
+            s = T::mma(along<T, D>(qt, b * 32, st), kf[st], s);
+            dp = T::mma(along<T, D>(dt, b * 32, st), vf[st], dp);
+        }
+        interleave<D / 8, 1, 4, 0>();
         const bool edge = key0 + 32 > nk || (causal && key0 + 31 > ib + shift);
         float p[16], ds[16];
 #pragma unroll
@@ -112,10 +113,12 @@ __device__ __forceinline__ void dkv_step(const lds_char* __restrict cur, lds_cha
                 ds[r + e] = p[r + e] * fmaf(dp[r + e], per, -de[e]);
             }
         }
-        if (edge)
+        if (edge) {
+            stay_here();
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (key >= nk || (causal && key > ib + c_row(r, half) + shift)) p[r] = ds[r] = 0;
+        }
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const typename T::vec8 pf = round8<T>(p + st * 8), df = round8<T>(ds + st * 8);
@@ -125,6 +128,7 @@ __device__ __forceinline__ void dkv_step(const lds_char* __restrict cur, lds_cha
                 dk[d] = T::mma(across<T, D>(qt, b * 32 + st * 16, d * 32), df, dk[d]);
             }
         }
+        interleave<4 * DB, 2, 3, 2>();
     }
 }
 
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
     const auto tile_of = [&](int g, int t, bool more) {
         const uint32_t h = kh * a.group + g;
         const int64_t i = (int64_t)t * STEP;
-        return Next{a.q.p + b * a.q.batch + h * a.q.head + i * a.q.pos, a.dout.p + b * a.dout.batch + h * a.dout.head + i * a.dout.pos, a.q.pos, a.dout.pos, nq - t * STEP, more};
+        return Next{a.q.p + b * a.q.batch + h * a.q.head + i * a.q.pos, a.dout.p + b * a.dout.batch + h * a.dout.head + i * a.dout.pos, nq - t * STEP, more};
     };
     // the statistics of a tile's rows, for lane r of the first wave those of row r: a row that sees nothing has no probabilities
     const auto stat_of = [&](int g, int t, float& ls, float& de) {
@@ -181,10 +185,13 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
         de = a.delta[at] * per;
         if (x != -INFINITY) ls = x * LOG2E - P_SHIFT<T>;
     };
+    TileLoads<STEP, D, WAVES> ql, dl;
+    ql.init(a.q.pos, chunks);
+    dl.init(a.dout.pos, chunks);
     if (u0 < u1) {
         const Next n = tile_of(g, t, true);
-        stage<STEP, D, WAVES>(lds, n.a, n.as, n.rows, chunks);
-        stage<STEP, D, WAVES>(lds + TILE, n.b, n.bs, n.rows, chunks);
+        ql.load(lds, n.a, n.rows);
+        dl.load(lds + TILE, n.b, n.rows);
         if (wave == 0) stat_of(g, t, stat[0][lane], stat[0][STEP + lane]);
     }
     __syncthreads();
@@ -195,7 +202,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
         const bool more = u + 1 < u1;
         float ls = 0, de = 0;
         if (more && wave == 0) stat_of(gn, tn, ls, de);
-        dkv_step<T, D, WAVES>(lds + now * 2 * TILE, lds + (1 - now) * 2 * TILE, stat[now], tile_of(more ? gn : g, more ? tn : t, more), chunks, kf, vf, dk, dv,
+        dkv_step<T, D, WAVES>(lds + now * 2 * TILE, lds + (1 - now) * 2 * TILE, stat[now], tile_of(more ? gn : g, more ? tn : t, more), ql, dl, kf, vf, dk, dv,
                               a.scale_log2, per, key0, nk, t * STEP, shift, causal);
         if (more && wave == 0) stat[1 - now][lane] = ls, stat[1 - now][STEP + lane] = de;
         __syncthreads();
@@ -222,14 +229,14 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
 }
 
 template <class T, int D, int WAVES>
-__device__ __forceinline__ void dq_step(const lds_char* __restrict cur, lds_char* __restrict next, const Next& n, int chunks, const typename T::vec8* qf,
+__device__ __forceinline__ void dq_step(const lds_char* __restrict cur, lds_char* __restrict next, const Next& n, const TileLoads<STEP, D, WAVES>& la, const TileLoads<STEP, D, WAVES>& lb, const typename T::vec8* qf,
                                         const typename T::vec8* df, f32x16* dq, float c, float ls, float de, float per, int key0, int seen, int seen_least, int seen_most)
 {
     constexpr int DB = D / 32;
     const int half = (threadIdx.x % 64) / 32;
     if (n.more) {
-        stage<STEP, D, WAVES>(next, n.a, n.as, n.rows, chunks);
-        stage<STEP, D, WAVES>(next + STEP * D * 2, n.b, n.bs, n.rows, chunks);
+        la.load(next, n.a, n.rows);
+        lb.load(next + STEP * D * 2, n.b, n.rows);
     }
     const lds_char *kt = cur, *vt = cur + STEP * D * 2;
 #pragma unroll 1
@@ -238,22 +245,27 @@ __device__ __forceinline__ void dq_step(const lds_char* __restrict cur, lds_char
         if (kb >= seen_most) break;
         f32x16 s = {}, dp = {};
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st) s = T::mma(along<T, D>(kt, b * 32, st), qf[st], s);
-#pragma unroll
-        for (int st = 0; st < D / 16; ++st) dp = T::mma(along<T, D>(vt, b * 32, st), df[st], dp);
+        for (int st = 0; st < D / 16; ++st) {
+            s = T::mma(along<T, D>(kt, b * 32, st), qf[st], s);
+            dp = T::mma(along<T, D>(vt, b * 32, st), df[st], dp);
+        }
+        interleave<D / 8, 1, 4, 0>();
         float ds[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = exp2_(fmaf(s[r], c, -ls)) * fmaf(dp[r], per, -de);
-        if (kb + 32 > seen_least)
+        if (kb + 32 > seen_least) {
+            stay_here();
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (kb + c_row(r, half) >= seen) ds[r] = 0;
+        }
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const typename T::vec8 dsf = round8<T>(ds + st * 8);
 #pragma unroll
             for (int d = 0; d < DB; ++d) dq[d] = T::mma(across<T, D>(kt, b * 32 + st * 16, d * 32), dsf, dq[d]);
         }
+        interleave<2 * DB, 2, 3, 2>();
     }
 }
 
@@ -290,15 +302,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     f32x16 dq[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dq[d] = f32x16{};
+    TileLoads<STEP, D, WAVES> kl, vl;
+    kl.init(a.k.pos, chunks);
+    vl.init(a.v.pos, chunks);
     if (t0 < t1) {
-        stage<STEP, D, WAVES>(lds, kp + (int64_t)t0 * STEP * a.k.pos, a.k.pos, nk - t0 * STEP, chunks);
-        stage<STEP, D, WAVES>(lds + TILE, vp + (int64_t)t0 * STEP * a.v.pos, a.v.pos, nk - t0 * STEP, chunks);
+        kl.load(lds, kp + (int64_t)t0 * STEP * a.k.pos, nk - t0 * STEP);
+        vl.load(lds + TILE, vp + (int64_t)t0 * STEP * a.v.pos, nk - t0 * STEP);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int now = ((t - t0) & 1) * 2 * TILE, k1 = (t + 1) * STEP;
-        const Next n = {kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, a.k.pos, a.v.pos, nk - k1, t + 1 < t1};
-        dq_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), n, chunks, qf, df, dq, a.scale_log2, ls, de, 1.0f / unit, t * STEP, w.seen, w.seen_least, w.seen_most);
+        const Next n = {kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, nk - k1, t + 1 < t1};
+        dq_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), n, kl, vl, qf, df, dq, a.scale_log2, ls, de, 1.0f / unit, t * STEP, w.seen, w.seen_least, w.seen_most);
         __syncthreads();
     }
     if (!w.in) return;

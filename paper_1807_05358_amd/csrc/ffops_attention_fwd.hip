@@ -12,26 +12,28 @@ namespace {
 constexpr int KEYS = 64;
 
 template <class T, int D, int WAVES>
-__device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const char* kn, const char* vn, int64_t ks,
-                                          int64_t vs, int rows_next, int chunks, const typename T::vec8* qf, f32x16* o, float& m, float& l,
+__device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const char* kn, const char* vn, int rows_next,
+                                          const TileLoads<KEYS, D, WAVES>& kl, const TileLoads<KEYS, D, WAVES>& vl, const typename T::vec8* qf, f32x16* o, float& m, float& l,
                                           float c, int key0, int seen, int seen_least, int seen_most)
 {
     constexpr int DB = D / 32;
     const int half = (threadIdx.x % 64) / 32;
     if (more) {
-        stage<KEYS, D, WAVES>(next, kn, ks, rows_next, chunks);
-        stage<KEYS, D, WAVES>(next + KEYS * D * 2, vn, vs, rows_next, chunks);
+        kl.load(next, kn, rows_next);
+        vl.load(next + KEYS * D * 2, vn, rows_next);
     }
     if (key0 >= seen_most) return;
     const lds_char *kt = cur, *vt = cur + KEYS * D * 2;
     f32x16 s[KEYS / 32];
 #pragma unroll
-    for (int b = 0; b < KEYS / 32; ++b) {
-        s[b] = f32x16{};
+    for (int b = 0; b < KEYS / 32; ++b) s[b] = f32x16{};
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st) s[b] = T::mma(along<T, D>(kt, b * 32, st), qf[st], s[b]);
-    }
+    for (int st = 0; st < D / 16; ++st)
+#pragma unroll
+        for (int b = 0; b < KEYS / 32; ++b) s[b] = T::mma(along<T, D>(kt, b * 32, st), qf[st], s[b]);
+    interleave<D / 16 * (KEYS / 32), 1, 4, 0>();
     if (key0 + KEYS > seen_least) {
+        stay_here();
 #pragma unroll
         for (int b = 0; b < KEYS / 32; ++b)
 #pragma unroll
@@ -74,6 +76,7 @@ __device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_ch
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] = T::mma(across<T, D>(vt, b * 32 + st * 16, d * 32), p, o[d]);
         }
+    interleave<KEYS / 16 * DB, 2, 3, 32 / DB>();
 }
 
 template <class T, int D, int WAVES>
@@ -102,15 +105,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_fwd(AttnArgs a)
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = f32x16{};
     float m = -INFINITY, l = 0;
+    TileLoads<KEYS, D, WAVES> kl, vl;
+    kl.init(a.k.pos, chunks);
+    vl.init(a.v.pos, chunks);
     if (t0 < t1) {
-        stage<KEYS, D, WAVES>(lds, kp + (int64_t)t0 * KEYS * a.k.pos, a.k.pos, nk - t0 * KEYS, chunks);
-        stage<KEYS, D, WAVES>(lds + TILE, vp + (int64_t)t0 * KEYS * a.v.pos, a.v.pos, nk - t0 * KEYS, chunks);
+        kl.load(lds, kp + (int64_t)t0 * KEYS * a.k.pos, nk - t0 * KEYS);
+        vl.load(lds + TILE, vp + (int64_t)t0 * KEYS * a.v.pos, nk - t0 * KEYS);
     }
     __syncthreads();
     for (int t = t0; t < t1; ++t) {
         const int now = ((t - t0) & 1) * 2 * TILE, k1 = (t + 1) * KEYS;
-        tile_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), t + 1 < t1, kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, a.k.pos, a.v.pos,
-                               nk - k1, chunks, qf, o, m, l, a.scale_log2, t * KEYS, w.seen, w.seen_least, w.seen_most);
+        tile_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), t + 1 < t1, kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, nk - k1, kl, vl, qf, o, m, l, a.scale_log2, t * KEYS, w.seen, w.seen_least, w.seen_most);
         __syncthreads();
     }
     l += other_half(l);

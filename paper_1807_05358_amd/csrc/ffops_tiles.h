@@ -103,4 +103,18 @@ static __device__ __forceinline__ typename T::vec8 across16(const lds_char* tile
     return read8_tr<T>(lo, hi);
 }
 
+// The order of what stands before it in its block: N products of which every one needs READS reads of LDS, read AHEAD products before they are
+// used, and OTHER other instructions after each product
+template <int N, int READS, int AHEAD, int OTHER>
+static __device__ __forceinline__ void interleave()
+{
+    __builtin_amdgcn_sched_group_barrier(0x100, READS * AHEAD, 0);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (n + AHEAD < N) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+        if (OTHER) __builtin_amdgcn_sched_group_barrier(0x002, OTHER, 0);
+    }
+}
+
 }  // namespace ffops
