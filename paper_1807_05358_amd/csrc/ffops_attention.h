@@ -15,6 +15,7 @@ struct AttnArgs {
     Heads q, k, v, o, dout, dq, dk, dv;
     float* lse;                     // [batch][heads][q_len]
     float* delta;                   // the same shape: <do_i, o_i>
+    float* lse2;                    // the same shape: lse in powers of two, infinite where a query sees nothing
     uint32_t* top;                  // [batch][heads]: bits of the largest |do|, 16-bit floats only
     const int32_t *q_lengths, *kv_lengths;
     float* part;                    // splits > 1: partial sums

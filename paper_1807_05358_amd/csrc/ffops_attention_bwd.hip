@@ -6,19 +6,18 @@ namespace {
 
 // Two kernels, one per side of the score matrix, each of which makes the probabilities for itself: seven products instead of
 // five, but every sum has one owner -- no atomic additions, the same bits every time -- and nothing of the size of the score matrix moves.
+//   k_attention_dq   owns 32 rows a wave: s^T = k q^T, dp^T = v do^T, dq^T += k^T ds^T; and delta_i = <do_i, o_i>, which it leaves to
 //   k_attention_dkv  owns 32 keys a wave: s = q k^T, dp = do v^T, dv^T += do^T p, dk^T += q^T ds
-//   k_attention_dq   owns 32 rows a wave: s^T = k q^T, dp^T = v do^T, dq^T += k^T ds^T
 // In both, what the wave owns is the column of every product, so that p and ds are second operands as they lie in the registers.
 constexpr int STEP = 64;            // rows (keys) of a tile in LDS
 
 // A 16-bit float has too few exponents for probabilities and gradients of small losses: p is kept times 2^10 (it is at most 1),
-// ds relative to the power of two below the largest |do| of its heads.  bfloat has a float's exponents and needs neither.
+// ds relative to the power of two below the largest |do| of its row (dq) or of its heads (dkv).  bfloat has a float's exponents and needs neither.
 template <class T>
 constexpr float P_SHIFT = std::is_same<T, F16>::value ? 10.0f : 0.0f;
 
-__device__ __forceinline__ float unit_below(uint32_t bits)
+__device__ __forceinline__ float unit_below(float m)
 {
-    const float m = __uint_as_float(bits);
     return m > 0 && m < INFINITY ? ldexpf(1.0f, ilogbf(m)) : 1.0f;
 }
 
@@ -26,35 +25,6 @@ __global__ void k_attention_clear(uint32_t* top, uint32_t n)
 {
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     if (i < n) top[i] = 0;
-}
-
-// delta_i = <do_i, o_i>, and the largest |do| per head where the type needs it.  16 lanes per row, 8 elements each.
-template <class T>
-__global__ __launch_bounds__(256) void k_attention_delta(AttnArgs a)
-{
-    const uint64_t n = (uint64_t)a.batch * a.heads * a.q_len, at = (uint64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const uint32_t i = at % a.q_len, bh = (uint32_t)(at / a.q_len), b = bh / a.heads, h = bh % a.heads;
-    const int x = (threadIdx.x % 16) * 8;
-    float s = 0, top = 0;
-    if (at < n && (int)i < seq_len(a.q_lengths, a.q_len, b) && x < (int)a.dim) {
-        const typename T::vec8 u = *(const typename T::vec8*)(a.dout.p + b * a.dout.batch + h * a.dout.head + i * a.dout.pos + x * 2);
-        const typename T::vec8 v = *(const typename T::vec8*)(a.o.p + b * a.o.batch + h * a.o.head + i * a.o.pos + x * 2);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s += (float)u[e] * (float)v[e];
-            top = fmaxf(top, fabsf((float)u[e]));
-        }
-    }
-#pragma unroll
-    for (int d = 8; d; d >>= 1) s += __shfl_xor(s, d);
-    if (at < n && threadIdx.x % 16 == 0) a.delta[at] = s;
-    if constexpr (std::is_same<T, F16>::value) {
-#pragma unroll
-        for (int d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        // the largest of a set does not depend on the order; most rows find it there already
-        if (at < n && threadIdx.x % 16 == 0 && __float_as_uint(top) > __hip_atomic_load(a.top + bh, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT))
-            atomicMax(a.top + bh, __float_as_uint(top));
-    }
 }
 
 __device__ __forceinline__ void store_part(float* p, const f32x16& c, int x, int dim, int half, float f)
@@ -72,77 +42,139 @@ __device__ __forceinline__ void store_row(char* p, const f32x16& c, int x, int d
         if (x + c_row(r, half) < dim) store4<T>(p + (x + c_row(r, half)) * 2, c[r] * f, c[r + 1] * f, c[r + 2] * f, c[r + 3] * f);
 }
 
-struct Next {           // what is loaded while a tile is worked on
-    const char *a, *b;
-    int rows;
-    bool more;
+static __device__ const float infinity = INFINITY, zero = 0;
+
+// Tiles of queries and their gradients, with the rows' statistics: four of them in LDS (three where one wave starts all loads, whose counter ends at 63), all but one on their way, because a tile lasts
+// less long than memory takes to answer and nothing else runs on the wave's SIMD meanwhile.
+template <class T, int D, int WAVES>
+struct Queries {
+    static constexpr int STEP = 64, TILE = STEP * D * 2, STAGE = 2 * TILE + 2 * STEP * 4, STAGES = WAVES == 1 ? 3 : 4;
+    static constexpr int LOADS = 2 * TILE / 1024 / WAVES;       // of a wave, for a tile, statistics aside
+    TileLoads<STEP, D, WAVES> ql, dl;
+
+    // a tile of `rows` queries, none for rows <= 0; as many loads in any case, since they are counted
+    __device__ __forceinline__ void load(lds_char* dst, const char* q, const char* d, const float* lse2, const float* delta, int rows) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+        ql.load(dst, q, rows);
+        dl.load(dst + TILE, d, rows);
+        if (wave == 0) load_lds4(lane < rows ? lse2 + lane : &infinity, dst + 2 * TILE);
+        if (wave == WAVES - 1) load_lds4(lane < rows ? delta + lane : &zero, dst + 2 * TILE + STEP * 4);
+    }
 };
 
+// What a wave of k_attention_dkv holds.  It has its SIMD to itself, so its own products have to hide its exponentials: while it makes p and ds of one block
+// of 32 queries, it multiplies for the scores of the next and for the sums of the one before, neither of which waits for them.
 template <class T, int D, int WAVES>
-__device__ __forceinline__ void dkv_step(const lds_char* __restrict cur, lds_char* __restrict next, const float* stat, const Next& n, const TileLoads<STEP, D, WAVES>& la, const TileLoads<STEP, D, WAVES>& lb,
-                                         const typename T::vec8* kf, const typename T::vec8* vf, f32x16* dk, f32x16* dv, float c, float per, int key0, int nk,
-                                         int i0, int shift, bool causal)
-{
-    constexpr int DB = D / 32;
-    const int lane = threadIdx.x % 64, half = lane / 32, key = key0 + lane % 32;
-    if (n.more) {
-        la.load(next, n.a, n.rows);
-        lb.load(next + STEP * D * 2, n.b, n.rows);
+struct Keys32 {
+    typedef Queries<T, D, WAVES> Q;
+    typedef typename T::vec8 vec8;
+    static constexpr int DB = D / 32;
+
+    vec8 k[D / 16], v[D / 16];
+    f32x16 dk[DB], dv[DB];
+
+    static constexpr int SCORES = D / 8, SUMS = 4 * DB;        // products
+
+    // the first operand of product i of the scores of the queries from row r of a tile, and of the sums over them
+    static __device__ __forceinline__ vec8 for_scores(const lds_char* tile, int r, int i) { return along<T, D>(i % 2 ? tile + Q::TILE : tile, r, i / 2); }
+    static __device__ __forceinline__ vec8 for_sums(const lds_char* tile, int r, int i) { return across<T, D>(i % 2 ? tile : tile + Q::TILE, r + i / (2 * DB) * 16, i / 2 % DB * 32); }
+
+    __device__ __forceinline__ void scores(const lds_char* tile, int r, f32x16& s, f32x16& dp) const
+    {
+        s = dp = f32x16{};
+#pragma unroll
+        for (int i = 0; i < SCORES; ++i) {
+            if (i % 2) dp = T::mma(for_scores(tile, r, i), v[i / 2], dp);
+            else s = T::mma(for_scores(tile, r, i), k[i / 2], s);
+        }
     }
-    if (key0 >= nk) return;
-    const lds_char *qt = cur, *dt = cur + STEP * D * 2;
-#pragma unroll 1
-    for (int b = 0; b < STEP / 32; ++b) {
-        const int ib = i0 + b * 32;
-        if (causal && key0 > ib + 31 + shift) continue;
-        f32x16 s = {}, dp = {};
+
+    __device__ __forceinline__ void sums(const lds_char* tile, int r, const vec8 (&p)[2], const vec8 (&ds)[2])
+    {
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st) {
-            s = T::mma(along<T, D>(qt, b * 32, st), kf[st], s);
-            dp = T::mma(along<T, D>(dt, b * 32, st), vf[st], dp);
-        }
-        interleave<D / 8, 1, 4, 0>();
-        const bool edge = key0 + 32 > nk || (causal && key0 + 31 > ib + shift);
-        float p[16], ds[16];
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const f32x4 ls = *(const f32x4*)(stat + b * 32 + c_row(r, half)), de = *(const f32x4*)(stat + STEP + b * 32 + c_row(r, half));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                p[r + e] = exp2_(fmaf(s[r + e], c, -ls[e]));
-                ds[r + e] = p[r + e] * fmaf(dp[r + e], per, -de[e]);
-            }
-        }
-        if (edge) {
-            stay_here();
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key >= nk || (causal && key > ib + c_row(r, half) + shift)) p[r] = ds[r] = 0;
-        }
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            const typename T::vec8 pf = round8<T>(p + st * 8), df = round8<T>(ds + st * 8);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                dv[d] = T::mma(across<T, D>(dt, b * 32 + st * 16, d * 32), pf, dv[d]);
-                dk[d] = T::mma(across<T, D>(qt, b * 32 + st * 16, d * 32), df, dk[d]);
-            }
-        }
-        interleave<4 * DB, 2, 3, 2>();
+        for (int i = 0; i < SUMS; ++i) sum(i, for_sums(tile, r, i), p, ds);
     }
-}
+    __device__ __forceinline__ void sum(int i, vec8 f, const vec8 (&p)[2], const vec8 (&ds)[2])
+    {
+        const int st = i / (2 * DB), d = i / 2 % DB;
+        if (i % 2) dk[d] = T::mma(f, ds[st], dk[d]);
+        else dv[d] = T::mma(f, p[st], dv[d]);
+    }
+
+    // scores of no key, and of queries that do not see it, are -inf
+    __device__ __forceinline__ void mask(f32x16& s, int key0, int nk, int i0, int shift, bool causal) const
+    {
+        if (key0 + 32 <= nk && !(causal && key0 + 31 > i0 + shift)) return;
+        stay_here();
+        const int lane = threadIdx.x % 64, key = key0 + lane % 32;
+        // the first of the 32 queries that sees the key, less what c_row adds for this half of the wave
+        const int first = (key >= nk ? 32 : causal ? key - i0 - shift : 0) - 4 * (lane / 32);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = c_row(r, 0) >= first ? s[r] : -INFINITY;
+    }
+
+    // p and ds of the queries from row R of tile `cur` from their scores; meanwhile sn and dpn of the next 32, from row 32 - R of tile `ahead`, and the sums over the
+    // 32 before, from row 32 - R of tile `behind`; LOAD: and the loads of a tile into `into`
+    template <int R, bool LOAD>
+    __device__ __forceinline__ void body(const lds_char* __restrict cur, const lds_char* __restrict ahead, const lds_char* __restrict behind, lds_char* __restrict into, const Q& queries, const char* qn, const char* dn,
+                                         const float* ln, const float* en, int rows, const f32x16& s, const f32x16& dp, f32x16& sn, f32x16& dpn, const vec8 (&pl)[2], const vec8 (&dsl)[2], vec8 (&p)[2], vec8 (&ds)[2],
+                                         float c, float per)
+    {
+        typedef __attribute__((address_space(3))) const f32x4 lds_f32x4;
+        const int half = (threadIdx.x % 64) / 32;
+        if (LOAD) queries.load(into, qn, dn, ln, en, rows);
+        // One product, the reads of LDS for the one READ later, and a share of the arithmetic; the compiler keeps to that order.
+        constexpr int N = SCORES + SUMS, READ = 5;
+        const lds_char* stat = cur + (2 * Q::TILE + (R + 4 * half) * 4);
+        const auto first_operand = [&](int i) { return i < SCORES ? for_scores(ahead, 32 - R, i) : for_sums(behind, 32 - R, i - SCORES); };
+        vec8 f[N];
+        f32x4 ls[5], de[5];
+        float fp[16];
+#pragma unroll
+        for (int i = 0; i < READ; ++i) f[i] = first_operand(i);
+        ls[0] = *(lds_f32x4*)stat, de[0] = *(lds_f32x4*)(stat + Q::STEP * 4);
+        sn = dpn = f32x16{};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i + READ < N) f[i + READ] = first_operand(i + READ);
+            const int e0 = i * 32 / N, e1 = (i + 1) * 32 / N;      // halves of the work on an element
+#pragma unroll
+            for (int h = e0; h < e1; ++h) {
+                const int e = h / 2, g = e / 4;
+                if (h % 8 == 0 && g < 3) ls[g + 1] = *(lds_f32x4*)(stat + 32 * (g + 1)), de[g + 1] = *(lds_f32x4*)(stat + 32 * (g + 1) + Q::STEP * 4);
+            }
+            if (i >= SCORES) sum(i - SCORES, f[i], pl, dsl);
+            else if (i % 2) dpn = T::mma(f[i], v[i / 2], dpn);
+            else sn = T::mma(f[i], k[i / 2], sn);
+#pragma unroll
+            for (int h = e0; h < e1; ++h) {
+                const int e = h / 2, g = e / 4;
+                if (h % 2 == 0) fp[e] = exp2_(fmaf(s[e], c, -ls[g][e % 4]));
+                else {
+                    p[e / 8][e % 8] = (typename T::elem)fp[e];
+                    ds[e / 8][e % 8] = (typename T::elem)(fp[e] * ((dp[e] - de[g][e % 4]) * per));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // here, and not in the branches that follow
+        asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(ds[0]), "+v"(ds[1]));
+    }
+};
 
 template <class T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
 {
-    constexpr int DB = D / 32, TILE = STEP * D * 2;
-    __shared__ __attribute__((aligned(256))) char lds_[4 * TILE];
-    __shared__ __attribute__((aligned(16))) float stat[2][2 * STEP];
+    typedef Queries<T, D, WAVES> Q;
+    constexpr int DB = D / 32, STEP = Q::STEP;
+    __shared__ __attribute__((aligned(256))) char lds_[Q::STAGES * Q::STAGE];
     lds_char* lds = (lds_char*)lds_;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
     const uint32_t bk = blockIdx.x, b = bk / a.kv_heads, kh = bk % a.kv_heads;
     const int nq = seq_len(a.q_lengths, a.q_len, b), nk = seq_len(a.kv_lengths, a.kv_len, b), shift = nk - nq;
-    const int block0 = blockIdx.y * (WAVES * 32), key0 = block0 + wave * 32, key = key0 + lane % 32;
+    const int block0 = blockIdx.y * (WAVES * 32), key0 = block0 + wave * 32, key = key0 + lane % 32;       // causal: the keys that most queries see first
     const bool own = key < nk;
     const int chunks = a.dim / 8;
     const bool causal = a.causal;
@@ -150,16 +182,15 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
     if constexpr (std::is_same<T, F16>::value) {
         uint32_t top = 0;
         for (uint32_t g = 0; g < a.group; ++g) top = max(top, a.top[b * a.heads + kh * a.group + g]);
-        unit = unit_below(top);
+        unit = unit_below(__uint_as_float(top));
     }
     // p is 2^P_SHIFT too large in ds, too
     const float per = exp2_(-P_SHIFT<T>) / unit;
-    typename T::vec8 kf[D / 16], vf[D / 16];
-    row_operand<T, D>(kf, own ? a.k.p + b * a.k.batch + kh * a.k.head + key * a.k.pos : nullptr, a.dim, half);
-    row_operand<T, D>(vf, own ? a.v.p + b * a.v.batch + kh * a.v.head + key * a.v.pos : nullptr, a.dim, half);
-    f32x16 dk[DB], dv[DB];
+    Keys32<T, D, WAVES> x;
+    row_operand<T, D>(x.k, own ? a.k.p + b * a.k.batch + kh * a.k.head + key * a.k.pos : nullptr, a.dim, half);
+    row_operand<T, D>(x.v, own ? a.v.p + b * a.v.batch + kh * a.v.head + key * a.v.pos : nullptr, a.dim, half);
 #pragma unroll
-    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = f32x16{};
+    for (int d = 0; d < DB; ++d) x.dk[d] = x.dv[d] = f32x16{};
     // tiles of queries that see a key of the block, for each head of the group; a split takes a run of them
     const int first = causal && block0 - shift > 0 ? (block0 - shift) / STEP : 0;
     const int per_head = block0 < nk ? max(0, (nq + STEP - 1) / STEP - first) : 0;
@@ -169,44 +200,55 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
         u0 = min(u1, run * (int)blockIdx.z);
         u1 = min(u1, u0 + run);
     }
-    int g = per_head ? u0 / per_head : 0, t = per_head ? first + u0 % per_head : 0;
-    const auto tile_of = [&](int g, int t, bool more) {
-        const uint32_t h = kh * a.group + g;
-        const int64_t i = (int64_t)t * STEP;
-        return Next{a.q.p + b * a.q.batch + h * a.q.head + i * a.q.pos, a.dout.p + b * a.dout.batch + h * a.dout.head + i * a.dout.pos, nq - t * STEP, more};
-    };
-    // the statistics of a tile's rows, for lane r of the first wave those of row r: a row that sees nothing has no probabilities
-    const auto stat_of = [&](int g, int t, float& ls, float& de) {
-        const int i = t * STEP + lane;
-        ls = INFINITY, de = 0;
-        if (i >= nq) return;
-        const uint64_t at = ((uint64_t)b * a.heads + kh * a.group + g) * a.q_len + i;
-        const float x = a.lse[at];
-        de = a.delta[at] * per;
-        if (x != -INFINITY) ls = x * LOG2E - P_SHIFT<T>;
-    };
-    TileLoads<STEP, D, WAVES> ql, dl;
-    ql.init(a.q.pos, chunks);
-    dl.init(a.dout.pos, chunks);
     if (u0 < u1) {
-        const Next n = tile_of(g, t, true);
-        ql.load(lds, n.a, n.rows);
-        dl.load(lds + TILE, n.b, n.rows);
-        if (wave == 0) stat_of(g, t, stat[0][lane], stat[0][STEP + lane]);
-    }
-    __syncthreads();
-    for (int u = u0; u < u1; ++u) {
-        const int now = (u - u0) & 1;
-        int gn = g, tn = t + 1;
-        if (tn == first + per_head) ++gn, tn = first;
-        const bool more = u + 1 < u1;
-        float ls = 0, de = 0;
-        if (more && wave == 0) stat_of(gn, tn, ls, de);
-        dkv_step<T, D, WAVES>(lds + now * 2 * TILE, lds + (1 - now) * 2 * TILE, stat[now], tile_of(more ? gn : g, more ? tn : t, more), ql, dl, kf, vf, dk, dv,
-                              a.scale_log2, per, key0, nk, t * STEP, shift, causal);
-        if (more && wave == 0) stat[1 - now][lane] = ls, stat[1 - now][STEP + lane] = de;
-        __syncthreads();
-        g = gn, t = tn;
+        Q queries;
+        queries.ql.init(a.q.pos, chunks);
+        queries.dl.init(a.dout.pos, chunks);
+        // the tile that is loaded next
+        int g = u0 / per_head, t = first + u0 % per_head, ahead = u0;
+        const char *qp, *dp;
+        const float *lp, *ep;
+        int rows;
+        const auto aim = [&] {
+            const uint32_t h = kh * a.group + min(g, (int)a.group - 1);
+            const int64_t i = (int64_t)t * STEP;
+            const uint64_t at = ((uint64_t)b * a.heads + h) * a.q_len + i;
+            qp = a.q.p + b * a.q.batch + h * a.q.head + i * a.q.pos;
+            dp = a.dout.p + b * a.dout.batch + h * a.dout.head + i * a.dout.pos;
+            lp = a.lse2 + at, ep = a.delta + at;
+            rows = ahead < u1 ? nq - t * STEP : 0;
+        };
+        const auto advance = [&] {
+            ++ahead;
+            if (++t == first + per_head) ++g, t = first;
+        };
+        for (int n = 0; n < Q::STAGES - 1; ++n) {
+            aim();
+            queries.load(lds + n * Q::STAGE, qp, dp, lp, ep, rows);
+            advance();
+        }
+        queries.load(lds + (Q::STAGES - 1) * Q::STAGE, qp, dp, lp, ep, 0);      // zeros, for the queries before the first
+        meet<0>();
+        typedef typename T::vec8 vec8;
+        const float c = a.scale_log2;
+        f32x16 s0, s1, d0, d1;
+        vec8 p0[2], p1[2] = {}, e0[2], e1[2] = {};
+        int i0 = (first + u0 % per_head) * STEP, now = 0;
+        x.scores(lds, 0, s0, d0);
+        x.mask(s0, key0, nk, i0, shift, causal);
+        for (int u = u0; u < u1; ++u) {
+            const int before = now == 0 ? (Q::STAGES - 1) * Q::STAGE : now - Q::STAGE, next = now == (Q::STAGES - 1) * Q::STAGE ? 0 : now + Q::STAGE;
+            x.template body<0, false>(lds + now, lds + now, lds + before, lds, queries, qp, dp, lp, ep, 0, s0, d0, s1, d1, p1, e1, p0, e0, c, per);
+            x.mask(s1, key0, nk, i0 + 32, shift, causal);
+            i0 = i0 + STEP == (first + per_head) * STEP ? first * STEP : i0 + STEP;
+            meet<(Q::STAGES - 3) * Q::LOADS>();        // the next tile has arrived, and the one before has been read by all
+            aim();
+            x.template body<32, true>(lds + now, lds + next, lds + now, lds + before, queries, qp, dp, lp, ep, rows, s1, d1, s0, d0, p0, e0, p1, e1, c, per);
+            advance();
+            x.mask(s0, key0, nk, i0, shift, causal);
+            now = next;
+        }
+        x.sums(lds + (now == 0 ? (Q::STAGES - 1) * Q::STAGE : now - Q::STAGE), 32, p1, e1);
     }
     if (key >= (int)a.kv_len) return;
     const float fk = a.scale * unit, fv = exp2_(-P_SHIFT<T>);
@@ -215,18 +257,24 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
         float *pk = a.part + (2 * (uint64_t)blockIdx.z * n + at) * a.dim, *pv = pk + n * a.dim;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-            store_part(pk, dk[d], d * 32, a.dim, half, fk);
-            store_part(pv, dv[d], d * 32, a.dim, half, fv);
+            store_part(pk, x.dk[d], d * 32, a.dim, half, fk);
+            store_part(pv, x.dv[d], d * 32, a.dim, half, fv);
         }
         return;
     }
     char *pk = a.dk.p + b * a.dk.batch + kh * a.dk.head + key * a.dk.pos, *pv = a.dv.p + b * a.dv.batch + kh * a.dv.head + key * a.dv.pos;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-        store_row<T>(pk, dk[d], d * 32, a.dim, half, fk);
-        store_row<T>(pv, dv[d], d * 32, a.dim, half, fv);
+        store_row<T>(pk, x.dk[d], d * 32, a.dim, half, fk);
+        store_row<T>(pv, x.dv[d], d * 32, a.dim, half, fv);
     }
 }
+
+struct Next {           // what is loaded while a tile is worked on
+    const char *a, *b;
+    int rows;
+    bool more;
+};
 
 template <class T, int D, int WAVES>
 __device__ __forceinline__ void dq_step(const lds_char* __restrict cur, lds_char* __restrict next, const Next& n, const TileLoads<STEP, D, WAVES>& la, const TileLoads<STEP, D, WAVES>& lb, const typename T::vec8* qf,
@@ -292,13 +340,32 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     row_operand<T, D>(qf, query ? a.q.p + b * a.q.batch + w.h * a.q.head + w.i * a.q.pos : nullptr, a.dim, half);
     row_operand<T, D>(df, query ? a.dout.p + b * a.dout.batch + w.h * a.dout.head + w.i * a.dout.pos : nullptr, a.dim, half);
     const uint64_t at = ((uint64_t)b * a.heads + w.h) * a.q_len + w.i;
-    float ls = INFINITY, de = 0, unit = 1.0f;
+    float ls = INFINITY, de = 0, unit = 1.0f, top = 0;
+    {
+        typename T::vec8 of[D / 16];
+        row_operand<T, D>(of, query ? a.o.p + b * a.o.batch + w.h * a.o.head + w.i * a.o.pos : nullptr, a.dim, half);
+#pragma unroll
+        for (int st = 0; st < D / 16; ++st)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                de += (float)df[st][e] * (float)of[st][e];
+                top = fmaxf(top, fabsf((float)df[st][e]));
+            }
+        de += other_half(de);
+    }
+    if constexpr (std::is_same<T, F16>::value) {
+        top = fmaxf(top, other_half(top));
+        unit = unit_below(top);
+        // the largest of a set does not depend on the order; most rows find it there already
+        uint32_t* head = a.top + b * a.heads + w.h;
+        if (query && half == 0 && blockIdx.z == 0 && __float_as_uint(top) > __hip_atomic_load(head, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(head, __float_as_uint(top));
+    }
     if (query) {
         const float x = a.lse[at];
-        if constexpr (std::is_same<T, F16>::value) unit = unit_below(a.top[b * a.heads + w.h]);
         if (x != -INFINITY) ls = x * LOG2E;
-        de = a.delta[at] / unit;
     }
+    if (w.in && half == 0 && blockIdx.z == 0) a.delta[at] = de, a.lse2[at] = ls - P_SHIFT<T>;
+    de /= unit;
     f32x16 dq[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dq[d] = f32x16{};
@@ -360,7 +427,7 @@ uint32_t splits_of(uint64_t blocks, uint64_t tiles)
 
 struct Plan {
     uint32_t kv_waves, kv_splits, q_waves, q_splits;
-    uint64_t delta, top, part, bytes;       // offsets in the workspace
+    uint64_t lse2, top, part, bytes;        // offsets in the workspace, delta first
 };
 
 Plan plan_of(const AttnArgs& a)
@@ -370,7 +437,8 @@ Plan plan_of(const AttnArgs& a)
     p.kv_waves = waves_of(a.kv_len), p.q_waves = waves_of(rows);
     p.kv_splits = splits_of(bk * ceil_div(a.kv_len, p.kv_waves * 32), a.group * ceil_div(a.q_len, STEP));
     p.q_splits = splits_of(bk * ceil_div(rows, p.q_waves * 32), ceil_div(a.kv_len, STEP));
-    p.top = round_up((uint64_t)a.batch * a.heads * a.q_len * sizeof(float), 256);
+    p.lse2 = round_up((uint64_t)a.batch * a.heads * a.q_len * sizeof(float), 256);
+    p.top = 2 * p.lse2;
     p.part = p.top + round_up((uint64_t)a.batch * a.heads * sizeof(uint32_t), 256);
     // one area for the partial sums of both: the kernels run one after another
     const uint64_t kv = p.kv_splits > 1 ? 2ull * p.kv_splits * bk * a.kv_len * a.dim : 0, q = p.q_splits > 1 ? (uint64_t)p.q_splits * bk * rows * a.dim : 0;
@@ -399,9 +467,13 @@ void launch_dq(const AttnArgs& a, uint32_t w, hipStream_t st)
 template <class T>
 int run(AttnArgs a, const Plan& p, hipStream_t st)
 {
-    if (a.q_len) {
+    if (a.q_len) {          // first: delta and the largest |do| are what the keys' side needs of it
         if (std::is_same<T, F16>::value) k_attention_clear<<<(uint32_t)ceil_div((uint64_t)a.batch * a.heads, 256), 256, 0, st>>>(a.top, a.batch * a.heads);
-        k_attention_delta<T><<<(uint32_t)ceil_div((uint64_t)a.batch * a.heads * a.q_len, 16), 256, 0, st>>>(a);
+        a.splits = p.q_splits;
+        if (a.dim <= 64) launch_dq<T, 64>(a, p.q_waves, st);
+        else launch_dq<T, 128>(a, p.q_waves, st);
+        if (a.splits > 1)
+            k_attention_add<T><<<dim3((uint32_t)ceil_div((uint64_t)a.batch * a.heads * a.q_len, 16), 1), 256, 0, st>>>(a.part, a.splits, 1, a.dq, a.dq, a.batch, a.heads, a.q_len, a.dim);
     }
     if (a.kv_len) {
         a.splits = p.kv_splits;
@@ -409,13 +481,6 @@ int run(AttnArgs a, const Plan& p, hipStream_t st)
         else launch_dkv<T, 128>(a, p.kv_waves, st);
         if (a.splits > 1)
             k_attention_add<T><<<dim3((uint32_t)ceil_div((uint64_t)a.batch * a.kv_heads * a.kv_len, 16), 2), 256, 0, st>>>(a.part, a.splits, 2, a.dk, a.dv, a.batch, a.kv_heads, a.kv_len, a.dim);
-    }
-    if (a.q_len) {
-        a.splits = p.q_splits;
-        if (a.dim <= 64) launch_dq<T, 64>(a, p.q_waves, st);
-        else launch_dq<T, 128>(a, p.q_waves, st);
-        if (a.splits > 1)
-            k_attention_add<T><<<dim3((uint32_t)ceil_div((uint64_t)a.batch * a.heads * a.q_len, 16), 1), 256, 0, st>>>(a.part, a.splits, 1, a.dq, a.dq, a.batch, a.heads, a.q_len, a.dim);
     }
     return launched();
 }
@@ -445,6 +510,7 @@ extern "C" int ff_op_attention_bwd(const ff_attention_bwd_t* p, void* stream)
     a.lse = const_cast<float*>(p->lse);
     char* ws = (char*)p->workspace;
     a.delta = (float*)ws;
+    a.lse2 = (float*)(ws + plan.lse2);
     a.top = (uint32_t*)(ws + plan.top);
     a.part = (float*)(ws + plan.part);
     return p->dtype == FF_F16 ? run<F16>(a, plan, (hipStream_t)stream) : run<BF16>(a, plan, (hipStream_t)stream);

@@ -45,6 +45,20 @@ struct BF16 {
 // C[4 * (l / 16) + r][l % 16] in register r = 0..3.  Both do 1024 products a cycle; on numbers that are not zero the device's power sets the
 // clock, and the small one gives more of them: 2083 TFLOP/s against 1859 from registers alone, at the same reads of LDS.
 
+// Waits until what this wave has asked of LDS, and of memory but for the latest NEWER loads, is there, and then for all other waves of the block.
+// Unlike __syncthreads it lets loads into LDS pass.
+template <int NEWER>
+static __device__ __forceinline__ void meet()
+{
+    static_assert(NEWER < 64, "what the counter of loads holds");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x0070 | (NEWER & 15) | (NEWER >> 4 << 14));     // vmcnt, lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 static __device__ __forceinline__ int c_row(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
 
 // 16 bytes that rows and columns beyond a matrix are read from
@@ -56,7 +70,13 @@ static __device__ __forceinline__ void load_lds16(const char* src, lds_char* dst
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// the same from base + off, base uniform: the address takes one register of a lane and no arithmetic
+// 4 bytes per lane, at dst + 4 * lane
+static __device__ __forceinline__ void load_lds4(const float* src, lds_char* dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 4, 0, 0);
+}
+
+// the same as load_lds16 from base + off, base uniform: the address takes one register of a lane and no arithmetic
 static __device__ __forceinline__ void load_lds16(const char* base, uint32_t off, lds_char* dst)
 {
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0xffffffffu, 0x00027000);

@@ -93,18 +93,6 @@ struct Wide {
     static constexpr int LOADS = StageA::PER;   // of a wave, for a tile of either side
     static_assert(StageA::PER == 8 && StageB::PER == 8, "one load for every row of products");
 
-    // what this wave has asked of LDS, and of memory but for the latest `newer` loads, is there, and so is what all others have
-    template <int NEWER>
-    static __device__ __forceinline__ void meet()
-    {
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0070 | NEWER);     // vmcnt, lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
-    }
-
     static __device__ __forceinline__ const char* at(const Side& s, bool across, int64_t k) { return across ? s.m.p + k * s.m.stride : s.m.p + k * 2; }
     static __device__ __forceinline__ vec8 of_a(const lds_char* tile, int half, int m, int wm) { return operand<T, M, KT, A_ACROSS>(tile, wm + m * 16, half); }
     static __device__ __forceinline__ vec8 of_b(const lds_char* tile, int half, int n, int wn) { return operand<T, N, KT, B_ACROSS>(tile, wn + n * 16, half); }
@@ -162,7 +150,7 @@ struct Wide {
             half<0, 1>(lds + ia, lds + ia, lb + ib, lds + free, pa, sa, fa, fb, gb, c, wm, wn);
             meet<LOADS>();
             half<1, 1>(lds + ia, lds + next, lb + (TILE - ib), lb + ib, pb, sb, fa, gb, fb, c, wm, wn);
-            meet<15>();                          // for the reads alone
+            meet<2 * LOADS>();                   // for the reads alone
             pa += as, pb += bs;
             ia = next, ib = TILE - ib;
         }
