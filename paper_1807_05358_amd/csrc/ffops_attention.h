@@ -16,7 +16,8 @@ struct AttnArgs {
     float* lse;                     // [batch][heads][q_len]
     float* delta;                   // the same shape: <do_i, o_i>
     float* lse2;                    // the same shape: lse in powers of two, infinite where a query sees nothing
-    uint32_t* top;                  // [batch][heads]: bits of the largest |do|, 16-bit floats only
+    float* top;                     // [batch][kv_heads][tops]: the largest |do| of 32 rows, 16-bit floats only
+    uint32_t tops;
     const int32_t *q_lengths, *kv_lengths;
     float* part;                    // splits > 1: partial sums
     float* part_lse;                // splits > 1, forward: their statistics
@@ -60,8 +61,8 @@ struct TileLoads {
     }
 };
 
-// keeps what follows it in its branch: without it the compiler takes comparisons for every tile that only the last ones need
-static __device__ __forceinline__ void stay_here() { asm volatile(""); }
+// keeps what is made of x in its branch: without it the compiler takes comparisons for every tile that only the last ones need
+static __device__ __forceinline__ void stay_here(int& x) { asm volatile("" : "+v"(x)); }
 
 // operands in registers: a row of D elements at p (null: zeros), element 16 * step + 8 * half + e
 template <class T, int D>

@@ -21,12 +21,6 @@ __device__ __forceinline__ float unit_below(float m)
     return m > 0 && m < INFINITY ? ldexpf(1.0f, ilogbf(m)) : 1.0f;
 }
 
-__global__ void k_attention_clear(uint32_t* top, uint32_t n)
-{
-    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n) top[i] = 0;
-}
-
 __device__ __forceinline__ void store_part(float* p, const f32x16& c, int x, int dim, int half, float f)
 {
 #pragma unroll
@@ -48,7 +42,7 @@ static __device__ const float infinity = INFINITY, zero = 0;
 // less long than memory takes to answer and nothing else runs on the wave's SIMD meanwhile.
 template <class T, int D, int WAVES>
 struct Queries {
-    static constexpr int STEP = 64, TILE = STEP * D * 2, STAGE = 2 * TILE + 2 * STEP * 4, STAGES = WAVES == 1 ? 3 : 4;
+    static constexpr int STEP = 64, TILE = STEP * D * 2, STAGE = 2 * TILE + 2 * STEP * 4, STAGES = WAVES == 1 || D == 64 ? 3 : 4;
     static constexpr int LOADS = 2 * TILE / 1024 / WAVES;       // of a wave, for a tile, statistics aside
     TileLoads<STEP, D, WAVES> ql, dl;
 
@@ -106,10 +100,10 @@ struct Keys32 {
     __device__ __forceinline__ void mask(f32x16& s, int key0, int nk, int i0, int shift, bool causal) const
     {
         if (key0 + 32 <= nk && !(causal && key0 + 31 > i0 + shift)) return;
-        stay_here();
         const int lane = threadIdx.x % 64, key = key0 + lane % 32;
         // the first of the 32 queries that sees the key, less what c_row adds for this half of the wave
-        const int first = (key >= nk ? 32 : causal ? key - i0 - shift : 0) - 4 * (lane / 32);
+        int first = (key >= nk ? 32 : causal ? key - i0 - shift : 0) - 4 * (lane / 32);
+        stay_here(first);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = c_row(r, 0) >= first ? s[r] : -INFINITY;
     }
@@ -180,9 +174,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
     const bool causal = a.causal;
     float unit = 1.0f;
     if constexpr (std::is_same<T, F16>::value) {
-        uint32_t top = 0;
-        for (uint32_t g = 0; g < a.group; ++g) top = max(top, a.top[b * a.heads + kh * a.group + g]);
-        unit = unit_below(__uint_as_float(top));
+        float top = 0;
+        for (uint32_t i = lane; i < a.tops; i += 64) top = fmaxf(top, a.top[(uint64_t)bk * a.tops + i]);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        unit = unit_below(top);
     }
     // p is 2^P_SHIFT too large in ds, too
     const float per = exp2_(-P_SHIFT<T>) / unit;
@@ -302,10 +298,10 @@ __device__ __forceinline__ void dq_step(const lds_char* __restrict cur, lds_char
 #pragma unroll
         for (int r = 0; r < 16; ++r) ds[r] = exp2_(fmaf(s[r], c, -ls)) * fmaf(dp[r], per, -de);
         if (kb + 32 > seen_least) {
-            stay_here();
+            int first = seen - kb - 4 * half;       // key that the row does not see
+            stay_here(first);
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (kb + c_row(r, half) >= seen) ds[r] = 0;
+            for (int r = 0; r < 16; ++r) ds[r] = c_row(r, 0) >= first ? 0.0f : ds[r];
         }
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
@@ -356,9 +352,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     if constexpr (std::is_same<T, F16>::value) {
         top = fmaxf(top, other_half(top));
         unit = unit_below(top);
-        // the largest of a set does not depend on the order; most rows find it there already
-        uint32_t* head = a.top + b * a.heads + w.h;
-        if (query && half == 0 && blockIdx.z == 0 && __float_as_uint(top) > __hip_atomic_load(head, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(head, __float_as_uint(top));
+        // and of the wave's rows, for the keys' side
+        float most = top;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+        if (lane == 0 && blockIdx.z == 0) a.top[(uint64_t)bk * a.tops + (gridDim.y - 1 - blockIdx.y) * WAVES + wave] = most;
     }
     if (query) {
         const float x = a.lse[at];
@@ -426,7 +424,7 @@ uint32_t splits_of(uint64_t blocks, uint64_t tiles)
 }
 
 struct Plan {
-    uint32_t kv_waves, kv_splits, q_waves, q_splits;
+    uint32_t kv_waves, kv_splits, q_waves, q_splits, tops;
     uint64_t lse2, top, part, bytes;        // offsets in the workspace, delta first
 };
 
@@ -439,7 +437,8 @@ Plan plan_of(const AttnArgs& a)
     p.q_splits = splits_of(bk * ceil_div(rows, p.q_waves * 32), ceil_div(a.kv_len, STEP));
     p.lse2 = round_up((uint64_t)a.batch * a.heads * a.q_len * sizeof(float), 256);
     p.top = 2 * p.lse2;
-    p.part = p.top + round_up((uint64_t)a.batch * a.heads * sizeof(uint32_t), 256);
+    p.tops = (uint32_t)ceil_div(rows, p.q_waves * 32) * p.q_waves;
+    p.part = p.top + round_up(bk * p.tops * sizeof(float), 256);
     // one area for the partial sums of both: the kernels run one after another
     const uint64_t kv = p.kv_splits > 1 ? 2ull * p.kv_splits * bk * a.kv_len * a.dim : 0, q = p.q_splits > 1 ? (uint64_t)p.q_splits * bk * rows * a.dim : 0;
     p.bytes = p.part + std::max(kv, q) * sizeof(float);
@@ -468,7 +467,6 @@ template <class T>
 int run(AttnArgs a, const Plan& p, hipStream_t st)
 {
     if (a.q_len) {          // first: delta and the largest |do| are what the keys' side needs of it
-        if (std::is_same<T, F16>::value) k_attention_clear<<<(uint32_t)ceil_div((uint64_t)a.batch * a.heads, 256), 256, 0, st>>>(a.top, a.batch * a.heads);
         a.splits = p.q_splits;
         if (a.dim <= 64) launch_dq<T, 64>(a, p.q_waves, st);
         else launch_dq<T, 128>(a, p.q_waves, st);
@@ -505,13 +503,13 @@ extern "C" int ff_op_attention_bwd(const ff_attention_bwd_t* p, void* stream)
     if (p->kv_len && (!heads_ok(p->k) || !heads_ok(p->v) || !heads_ok(p->dk) || !heads_ok(p->dv))) return FF_EINVAL;
     AttnArgs a = args_of(p);
     const Plan plan = plan_of(a);
-    if (!p->workspace || p->workspace_bytes < plan.bytes || !aligned(p->workspace, 256)) return FF_EWORKSPACE;
+    if (plan.bytes && (!p->workspace || p->workspace_bytes < plan.bytes || !aligned(p->workspace, 256))) return FF_EWORKSPACE;
     a.dout = in_bytes(p->dout), a.dq = in_bytes(p->dq), a.dk = in_bytes(p->dk), a.dv = in_bytes(p->dv);
     a.lse = const_cast<float*>(p->lse);
     char* ws = (char*)p->workspace;
     a.delta = (float*)ws;
     a.lse2 = (float*)(ws + plan.lse2);
-    a.top = (uint32_t*)(ws + plan.top);
+    a.top = (float*)(ws + plan.top), a.tops = plan.tops;
     a.part = (float*)(ws + plan.part);
     return p->dtype == FF_F16 ? run<F16>(a, plan, (hipStream_t)stream) : run<BF16>(a, plan, (hipStream_t)stream);
 }

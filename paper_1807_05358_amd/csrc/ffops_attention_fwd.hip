@@ -33,12 +33,12 @@ __device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_ch
         for (int b = 0; b < KEYS / 32; ++b) s[b] = T::mma(along<T, D>(kt, b * 32, st), qf[st], s[b]);
     interleave<D / 16 * (KEYS / 32), 1, 4, 0>();
     if (key0 + KEYS > seen_least) {
-        stay_here();
+        int first = seen - key0 - 4 * half;         // key of the tile that the row does not see
+        stay_here(first);
 #pragma unroll
         for (int b = 0; b < KEYS / 32; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key0 + b * 32 + c_row(r, half) >= seen) s[b][r] = -INFINITY;
+            for (int r = 0; r < 16; ++r) s[b][r] = b * 32 + c_row(r, 0) >= first ? -INFINITY : s[b][r];
     }
     float top = s[0][0];
 #pragma unroll
@@ -145,30 +145,38 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_fwd(AttnArgs a)
         }
 }
 
-// joins the parts of a row: o = sum_s 2^(lse_s - lse) o_s.  16 lanes per row, 8 elements each.
+// joins the parts of a row: o = sum_s 2^(lse_s - lse) o_s.  A wave per row: 16 lanes cover its elements, 8 each, and four of them the splits in turn.
 template <class T>
 __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a)
 {
-    const uint64_t n = (uint64_t)a.batch * a.heads * a.q_len, at = (uint64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const uint64_t n = (uint64_t)a.batch * a.heads * a.q_len, at = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
     if (at >= n) return;
-    const int x = (threadIdx.x % 16) * 8;
+    const uint32_t lane = threadIdx.x % 64, x = lane % 16 * 8;
     float m = -INFINITY;
-    for (uint32_t s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_lse[s * n + at]);
+    for (uint32_t s = lane; s < a.splits; s += 64) m = fmaxf(m, a.part_lse[s * n + at]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     const float base = m == -INFINITY ? 0.0f : m;
     float sum = 0, o[8] = {};
-    for (uint32_t s = 0; s < a.splits; ++s) {
+#pragma unroll 4
+    for (uint32_t s = lane / 16; s < a.splits; s += 4) {
         const float w = exp2_(a.part_lse[s * n + at] - base);
         sum += w;
-        if (x < (int)a.dim) {
-            const float* p = a.part + (s * n + at) * a.dim + x;
-            const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
+        const float* p = a.part + (s * n + at) * a.dim + (x < a.dim ? x : 0);
+        const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += w * u[e], o[4 + e] += w * v[e];
-        }
+        for (int e = 0; e < 4; ++e) o[e] += w * u[e], o[4 + e] += w * v[e];
     }
+#pragma unroll
+    for (int d = 16; d < 64; d *= 2) {
+        sum += __shfl_xor(sum, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] += __shfl_xor(o[e], d);
+    }
+    if (lane >= 16) return;
     const float inv = sum > 0 ? 1.0f / sum : sum == sum ? 0.0f : sum;
-    if (threadIdx.x % 16 == 0) a.lse[at] = (base + log2_(sum)) * LN2;
-    if (x >= (int)a.dim) return;
+    if (lane == 0) a.lse[at] = (base + log2_(sum)) * LN2;
+    if (x >= a.dim) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] *= inv;
     const uint64_t i = at % a.q_len, bh = at / a.q_len;
@@ -206,7 +214,7 @@ int run(const AttnArgs& a, hipStream_t st)
 {
     if (a.dim <= 64) launch<T, 64>(a, st);
     else launch<T, 128>(a, st);
-    if (a.splits > 1) k_attention_join<T><<<(uint32_t)ceil_div((uint64_t)a.batch * a.heads * a.q_len, 16), 256, 0, st>>>(a);
+    if (a.splits > 1) k_attention_join<T><<<(uint32_t)ceil_div((uint64_t)a.batch * a.heads * a.q_len, 4), 256, 0, st>>>(a);
     return launched();
 }
 

@@ -188,7 +188,7 @@ struct VocabArgs {
     const int32_t* targets;
     const float *dloss, *lse_in;
     const uint32_t* top;
-    float2* part;                           // [m_tiles][rows]: maximum and sum of a tile's words
+    float2* part;                           // [rows][m_tiles]: maximum and sum of a tile's words
     float* target_logit;
     char* g;                                // [rows][g_stride]: gradient of the logits of a piece
     uint32_t g_stride;
@@ -340,24 +340,23 @@ __global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
             float2 s = stat[n];
 #pragma unroll
             for (int k = 1; k < WM; ++k) s = join(s, stat[k * N + n]);
-            a.part[(uint64_t)tm * a.rows + n0 + n] = s;
+            a.part[(uint64_t)(n0 + n) * a.m_tiles + tm] = s;
         }
     }
 }
 
-// joins the statistics of the tiles of words: 64 tokens per block, 16 waves each a sixteenth of the tiles
-__global__ __launch_bounds__(1024) void k_vocab_join(VocabArgs a, float* loss, float* lse, float* target_logit)
+// joins the statistics of the tiles of words: a wave per token
+__global__ __launch_bounds__(256) void k_vocab_join(VocabArgs a, float* loss, float* lse, float* target_logit)
 {
-    __shared__ float2 red[16][64];
-    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint64_t token = (uint64_t)blockIdx.x * 64 + lane;
+    const uint32_t lane = threadIdx.x % 64;
+    const uint64_t token = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (token >= a.rows) return;
     float2 s = make_float2(-INFINITY, 0);
-    if (token < a.rows)
-        for (uint32_t t = wave; t < a.m_tiles; t += 16) s = join(s, a.part[(uint64_t)t * a.rows + token]);
-    red[wave][lane] = s;
-    __syncthreads();
-    if (wave || token >= a.rows) return;
-    for (int k = 1; k < 16; ++k) s = join(s, red[k][lane]);
+#pragma unroll 4
+    for (uint32_t t = lane; t < a.m_tiles; t += 64) s = join(s, a.part[token * a.m_tiles + t]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s = join(s, make_float2(__shfl_xor(s.x, d), __shfl_xor(s.y, d)));
+    if (lane) return;
     const float l = (s.x + log2_(s.y)) * LN2;
     const int32_t target = a.targets[token];
     const int64_t at = (int64_t)target - a.first_word;
@@ -594,7 +593,7 @@ int fwd(const ff_vocab_loss_fwd_t* p, const Plan& q, hipStream_t st)
     const uint32_t tiles = a.m_tiles * a.n_tiles;
     if (q.big) k_vocab_logits<T, 256, false><<<tiles, 256, 0, st>>>(a);
     else k_vocab_logits<T, 64, false><<<tiles, 256, 0, st>>>(a);
-    k_vocab_join<<<(uint32_t)ceil_div(p->rows, 64), 1024, 0, st>>>(a, p->loss, p->lse, p->target_logit);
+    k_vocab_join<<<(uint32_t)ceil_div(p->rows, 4), 256, 0, st>>>(a, p->loss, p->lse, p->target_logit);
     return launched();
 }
 

@@ -10,7 +10,9 @@ memory.  What a call refuses on the library's side raises binding.FFSimError.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
+import struct
 
 from . import binding
 
@@ -72,17 +74,16 @@ _declared = None
 
 
 def lib():
-    """the library with the operators' calls declared"""
+    """the library with the operators' calls declared: a record by its address, or as the bytes that it consists of"""
     global _declared
     L = binding.lib()
     if _declared is not L:
         for name in EXPORTS:
             f = getattr(L, name)
-            record = C.POINTER(_RECORDS[name.replace("_workspace_bytes", "")])
             if name.endswith("_workspace_bytes"):
-                f.restype, f.argtypes = C.c_size_t, [record]
+                f.restype, f.argtypes = C.c_size_t, [_vp]
             else:
-                f.restype, f.argtypes = C.c_int, [record, _vp]
+                f.restype, f.argtypes = C.c_int, [_vp, _vp]
         _declared = L
     return L
 
@@ -98,62 +99,104 @@ def workspace_bytes(name, record):
     return getattr(lib(), name + "_workspace_bytes")(C.byref(record))
 
 
+_CODES = {C.c_uint32: "I", C.c_int32: "i", C.c_uint64: "Q", C.c_int64: "q", C.c_float: "f", C.c_void_p: "P", C.c_size_t: "N"}
+
+
+def _format(record):
+    """the record as a format of struct.pack: its fields in order, records in it field by field"""
+    fmt, at = "", 0
+    for name, kind in record._fields_:
+        place = getattr(record, name).offset
+        fmt += "%dx" % (place - at) if place > at else ""
+        fmt += _format(kind)[1:] if issubclass(kind, C.Structure) else _CODES[kind]
+        at = place + C.sizeof(kind)
+    return "@" + fmt + ("%dx" % (C.sizeof(record) - at) if C.sizeof(record) > at else "")
+
+
+@functools.lru_cache(maxsize=None)
+def _call_of(name, L):
+    """(pack, function, workspace function or None) of a call; packing a record's values takes a tenth of the time that filling a Structure does"""
+    packer = struct.Struct(_format(_RECORDS[name]))
+    if packer.size != C.sizeof(_RECORDS[name]):
+        raise RuntimeError(f"{name}: the packed record has {packer.size} bytes")
+    more = name + "_workspace_bytes"
+    return packer.pack, getattr(L, name), getattr(L, more) if more in EXPORTS else None
+
+
 # ---- torch tensors ---------------------------------------------------------------------
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
-def _dtype(t, what, allowed=("float16", "bfloat16")):
-    torch = _torch()
-    for name, code in (("float32", FF_F32), ("float16", FF_F16), ("bfloat16", FF_BF16)):
-        if t.dtype == getattr(torch, name) and name in allowed:
-            return code
-    raise ValueError(f"{what} is {t.dtype}; one of {', '.join(allowed)} is wanted")
+_DTYPES = {}
+
+
+def _dtype(t, what, f32=False):
+    if not _DTYPES:
+        torch = _torch()
+        _DTYPES.update({torch.float32: FF_F32, torch.float16: FF_F16, torch.bfloat16: FF_BF16})
+    code = _DTYPES.get(t.dtype, -1)
+    if code < (0 if f32 else 1):
+        raise ValueError(f"{what} is {t.dtype}; float16, bfloat16{' or float32' if f32 else ''} is wanted")
+    if not t.is_cuda:
+        raise ValueError(f"{what} is on {t.device}: the operators have no CPU path")
+    return code
 
 
 def _check(t, what, shape, dtype, device):
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, {tuple(shape)} is wanted")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{what} is {t.dtype}, {dtype} is wanted")
     if t.device != device:
         raise ValueError(f"{what} is on {t.device}, {device} is wanted")
 
 
-def _on_gpu(t, what):
-    if t.device.type != "cuda":
-        raise ValueError(f"{what} is on {t.device}: the operators have no CPU path")
-
-
-def _rows(t):
-    """a matrix whose rows' elements lie side by side, as a record; `t` must outlive the launch"""
-    return ff_rows_t(t.data_ptr(), t.stride(0))
-
-
 def _dense_rows(t):
+    """the matrix itself where its rows' elements lie side by side, else a copy"""
     return t if t is None or t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
 
 
 def _vector(t):
-    return None if t is None else t.contiguous()
+    return t if t is None or t.is_contiguous() else t.contiguous()
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
-def _launch(name, record, device):
+def _launch(name, device, *values):
+    """packs the record, with a workspace if there is to be one, and calls `name` on the device's current stream"""
     torch = _torch()
-    with torch.cuda.device(device):
-        ws = None
-        if name + "_workspace_bytes" in EXPORTS:
-            n = workspace_bytes(name, record)
-            if n:
-                ws = torch.empty(n, dtype=torch.uint8, device=device)
-                record.workspace, record.workspace_bytes = ws.data_ptr(), n
-        call(name, record, torch.cuda.current_stream(device).cuda_stream)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _launch(name, device, *values)
+    pack, function, workspace = _call_of(name, lib())
+    if workspace is None:
+        record = pack(*values)
+    else:
+        record = pack(*values, 0, 0)
+        n = workspace(record)
+        if n:
+            ws = torch.empty(n, dtype=torch.uint8, device=device)      # its memory is reused in the order of the stream
+            record = pack(*values, ws.data_ptr(), n)
+    code = function(record, _stream(torch, device))
+    if code != binding.FF_OK:
+        raise binding.FFSimError(code, name)
+
+
+def _stream(torch, device):
+    """the device's current stream; the object that torch.cuda.current_stream makes of it takes longer than all else here"""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
 def layernorm_fwd(x, weight, bias=None, *, residual=None, eps=1e-5):
@@ -162,22 +205,19 @@ def layernorm_fwd(x, weight, bias=None, *, residual=None, eps=1e-5):
     torch = _torch()
     if x.dim() != 2:
         raise ValueError("x is a matrix [rows, cols]")
-    dtype = _dtype(x, "x", ("float32", "float16", "bfloat16"))
-    _on_gpu(x, "x")
+    dtype, device = _dtype(x, "x", True), x.device
     R, Cn = x.shape
-    _check(weight, "weight", (Cn,), x.dtype, x.device)
+    _check(weight, "weight", (Cn,), x.dtype, device)
     if bias is not None:
-        _check(bias, "bias", (Cn,), x.dtype, x.device)
+        _check(bias, "bias", (Cn,), x.dtype, device)
     if residual is not None:
-        _check(residual, "residual", (R, Cn), x.dtype, x.device)
+        _check(residual, "residual", (R, Cn), x.dtype, device)
     xs, res, weight, bias = _dense_rows(x), _dense_rows(residual), _vector(weight), _vector(bias)
-    y = torch.empty(R, Cn, dtype=x.dtype, device=x.device)
+    y = torch.empty((R, Cn), dtype=x.dtype, device=device)
     h = x if residual is None else torch.empty_like(y)
-    mean, rstd = (torch.empty(R, dtype=torch.float32, device=x.device) for _ in range(2))
-    none = ff_rows_t(None, 0)
-    rec = ff_layernorm_fwd_t(dtype, Cn, R, eps, _rows(xs), none if res is None else _rows(res), none if res is None else _rows(h), _rows(y),
-                             _ptr(weight), _ptr(bias), _ptr(mean), _ptr(rstd))
-    _launch("ff_op_layernorm_fwd", rec, x.device)
+    mean, rstd = torch.empty((2, R), dtype=torch.float32, device=device).unbind()
+    _launch("ff_op_layernorm_fwd", device, dtype, Cn, R, eps, xs.data_ptr(), xs.stride(0), _ptr(res), 0 if res is None else res.stride(0),
+            0 if res is None else h.data_ptr(), Cn, y.data_ptr(), Cn, weight.data_ptr(), _ptr(bias), mean.data_ptr(), rstd.data_ptr())
     return y, h, mean, rstd
 
 
@@ -187,31 +227,31 @@ def layernorm_bwd(dy, h, weight, mean, rstd, *, dh=None):
     torch = _torch()
     if h.dim() != 2:
         raise ValueError("h is a matrix [rows, cols]")
-    dtype = _dtype(h, "h", ("float32", "float16", "bfloat16"))
-    _on_gpu(h, "h")
+    dtype, device = _dtype(h, "h", True), h.device
     R, Cn = h.shape
-    _check(dy, "dy", (R, Cn), h.dtype, h.device)
-    _check(weight, "weight", (Cn,), h.dtype, h.device)
-    _check(mean, "mean", (R,), torch.float32, h.device)
-    _check(rstd, "rstd", (R,), torch.float32, h.device)
+    _check(dy, "dy", (R, Cn), h.dtype, device)
+    _check(weight, "weight", (Cn,), h.dtype, device)
+    _check(mean, "mean", (R,), torch.float32, device)
+    _check(rstd, "rstd", (R,), torch.float32, device)
     if dh is not None:
-        _check(dh, "dh", (R, Cn), h.dtype, h.device)
+        _check(dh, "dh", (R, Cn), h.dtype, device)
     dy, hs, dh, weight, mean, rstd = _dense_rows(dy), _dense_rows(h), _dense_rows(dh), _vector(weight), _vector(mean), _vector(rstd)
-    dx = torch.empty(R, Cn, dtype=h.dtype, device=h.device)
-    dw, db = (torch.empty(Cn, dtype=h.dtype, device=h.device) for _ in range(2))
-    rec = ff_layernorm_bwd_t(dtype, Cn, R, _rows(dy), _rows(hs), ff_rows_t(None, 0) if dh is None else _rows(dh), _rows(dx),
-                             _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dw), _ptr(db))
-    _launch("ff_op_layernorm_bwd", rec, h.device)
+    dx = torch.empty((R, Cn), dtype=h.dtype, device=device)
+    dw, db = torch.empty((2, Cn), dtype=h.dtype, device=device).unbind()
+    _launch("ff_op_layernorm_bwd", device, dtype, Cn, R, dy.data_ptr(), dy.stride(0), hs.data_ptr(), hs.stride(0), _ptr(dh), 0 if dh is None else dh.stride(0),
+            dx.data_ptr(), Cn, weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dw.data_ptr(), db.data_ptr())
     return dx, dw, db
 
 
-def _heads(t):
-    return ff_heads_t(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+def _heads(*ts):
+    """addresses and strides of batch, head and position, one tensor after another"""
+    return [x for t in ts for x in (t.data_ptr(), *t.stride()[:3])]
 
 
 def _dense_heads(t):
     """the tensor itself where the kernels can read it (elements of a head side by side, 16-byte steps), else a copy"""
-    fits = t.stride(3) == 1 and all(s % 8 == 0 for s in t.stride()[:3]) and t.data_ptr() % 16 == 0
+    b, h, p, e = t.stride()
+    fits = e == 1 and not (b | h | p) & 7 and t.data_ptr() % 16 == 0
     return t if fits or t.numel() == 0 else t.clone(memory_format=_torch().contiguous_format)
 
 
@@ -220,7 +260,6 @@ def _attention_args(q, k, v, causal, q_lengths, kv_lengths, scale):
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k are [batch, heads, positions, elements]")
     dtype = _dtype(q, "q")
-    _on_gpu(q, "q")
     B, H, Sq, D = q.shape
     K, Sk = k.shape[1], k.shape[2]
     _check(k, "k", (B, K, Sk, D), q.dtype, q.device)
@@ -258,8 +297,7 @@ def attention_fwd(q, k, v, *, causal=False, q_lengths=None, kv_lengths=None, sca
     o = _like_heads(q)
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
     q, k, v = _dense_heads(q), _dense_heads(k), _dense_heads(v)
-    rec = ff_attention_fwd_t(*sizes, _heads(q), _heads(k), _heads(v), _heads(o), _ptr(lse), _ptr(q_lengths), _ptr(kv_lengths))
-    _launch("ff_op_attention_fwd", rec, q.device)
+    _launch("ff_op_attention_fwd", q.device, *sizes, *_heads(q, k, v, o), lse.data_ptr(), _ptr(q_lengths), _ptr(kv_lengths))
     return o, lse
 
 
@@ -272,8 +310,7 @@ def attention_bwd(dout, q, k, v, o, lse, *, causal=False, q_lengths=None, kv_len
     _check(lse, "lse", q.shape[:3], torch.float32, q.device)
     dq, dk, dv = _like_heads(q), _like_heads(k), _like_heads(v)
     dout, q, k, v, o, lse = _dense_heads(dout), _dense_heads(q), _dense_heads(k), _dense_heads(v), _dense_heads(o), lse.contiguous()
-    rec = ff_attention_bwd_t(*sizes, *(_heads(t) for t in (dout, q, k, v, o, dq, dk, dv)), _ptr(lse), _ptr(q_lengths), _ptr(kv_lengths))
-    _launch("ff_op_attention_bwd", rec, q.device)
+    _launch("ff_op_attention_bwd", q.device, *sizes, *_heads(dout, q, k, v, o, dq, dk, dv), lse.data_ptr(), _ptr(q_lengths), _ptr(kv_lengths))
     return dq, dk, dv
 
 
@@ -282,7 +319,6 @@ def _vocab_args(x, weight, targets, ignore_index, first_word):
     if x.dim() != 2 or weight.dim() != 2:
         raise ValueError("x is a matrix [rows, dim], weight [vocab, dim]")
     dtype = _dtype(x, "x")
-    _on_gpu(x, "x")
     N, D = x.shape
     _check(weight, "weight", (weight.shape[0], D), x.dtype, x.device)
     _check(targets, "targets", (N,), torch.int32, x.device)
@@ -304,10 +340,10 @@ def vocab_loss_fwd(x, weight, targets, *, ignore_index=-100, first_word=None):
     their target_logit, make the loss, and vocab_loss_bwd of a shard takes the joined lse."""
     torch = _torch()
     sizes, x, weight, targets = _vocab_args(x, weight, targets, ignore_index, first_word or 0)
-    loss = torch.empty(x.shape[0], dtype=torch.float32, device=x.device) if first_word is None else None
-    lse, logit = (torch.empty(x.shape[0], dtype=torch.float32, device=x.device) for _ in range(2))
-    rec = ff_vocab_loss_fwd_t(*sizes, _rows(x), _rows(weight), _ptr(targets), _ptr(loss), _ptr(lse), _ptr(logit))
-    _launch("ff_op_vocab_loss_fwd", rec, x.device)
+    loss, lse, logit = torch.empty((3, x.shape[0]), dtype=torch.float32, device=x.device).unbind()
+    if first_word is not None:
+        loss = None
+    _launch("ff_op_vocab_loss_fwd", x.device, *sizes, x.data_ptr(), x.stride(0), weight.data_ptr(), weight.stride(0), targets.data_ptr(), _ptr(loss), lse.data_ptr(), logit.data_ptr())
     return loss, lse, logit
 
 
@@ -317,9 +353,10 @@ def vocab_loss_bwd(dloss, x, weight, targets, lse, *, ignore_index=-100, first_w
     sizes, xs, ws, targets = _vocab_args(x, weight, targets, ignore_index, first_word or 0)
     _check(dloss, "dloss", targets.shape, torch.float32, x.device)
     _check(lse, "lse", targets.shape, torch.float32, x.device)
-    dloss, lse = dloss.contiguous(), lse.contiguous()
+    dloss, lse = _vector(dloss), _vector(lse)
+    D = x.shape[1]
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     dw = torch.empty(weight.shape, dtype=x.dtype, device=x.device)
-    rec = ff_vocab_loss_bwd_t(*sizes, _rows(xs), _rows(ws), _rows(dx), _rows(dw), _ptr(targets), _ptr(dloss), _ptr(lse))
-    _launch("ff_op_vocab_loss_bwd", rec, x.device)
+    _launch("ff_op_vocab_loss_bwd", x.device, *sizes, xs.data_ptr(), xs.stride(0), ws.data_ptr(), ws.stride(0), dx.data_ptr(), D, dw.data_ptr(), D,
+            targets.data_ptr(), dloss.data_ptr(), lse.data_ptr())
     return dx, dw
