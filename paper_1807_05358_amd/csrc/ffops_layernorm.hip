@@ -239,27 +239,46 @@ __global__ __launch_bounds__(1024) void k_layernorm_join(const float* part, uint
     }
 }
 
-// lanes that share a row and elements of a lane: a wave for rows of up to 2048 elements, 256 lanes up to 8192, 1024 beyond
-int threads_of(uint32_t cols) { return cols <= 2048 ? 64 : cols <= 8192 ? 256 : 1024; }
+template <int THREADS, int E>
+struct Row {        // lanes that share a row, and elements of a lane
+    static constexpr int threads = THREADS, elems = E;
+};
 
+// Forward: a wave for rows of up to 2048 elements; its lanes hold little, so wide rows take few lanes and many elements (256 x 16 reads 16384 x 4096 elements
+// in 41 us, 512 x 8 in 51).
 template <class F>
-int by_size(uint32_t cols, F f)
+int by_size_fwd(uint32_t cols, F f)
 {
-    if (cols <= 512) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
-    if (cols <= 1024) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
-    if (cols <= 2048) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 32>());
-    if (cols <= 4096) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 16>());
-    if (cols <= 8192) return f(std::integral_constant<int, 256>(), std::integral_constant<int, 32>());
-    if (cols <= 16384) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
-    if (cols <= 32768) return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 32>());
-    return f(std::integral_constant<int, 1024>(), std::integral_constant<int, 64>());
+    if (cols <= 512) return f(Row<64, 8>());
+    if (cols <= 1024) return f(Row<64, 16>());
+    if (cols <= 2048) return f(Row<64, 32>());
+    if (cols <= 4096) return f(Row<256, 16>());
+    if (cols <= 8192) return f(Row<512, 16>());
+    if (cols <= 16384) return f(Row<1024, 16>());
+    if (cols <= 32768) return f(Row<1024, 32>());
+    return f(Row<1024, 64>());
+}
+
+// Backward: five values an element, so few elements a lane (8192 x 8192 elements: 1024 x 8 takes 101 us, 512 x 16 117; 16384 x 2048: 256 x 8 41 us, 64 x 32
+// 49), but for rows of a wave's own, whose sums need no barrier.  Beyond 16384 elements a lane's values no longer fit its registers.
+template <class F>
+int by_size_bwd(uint32_t cols, F f)
+{
+    if (cols <= 512) return f(Row<64, 8>());
+    if (cols <= 1024) return f(Row<64, 16>());
+    if (cols <= 2048) return f(Row<256, 8>());
+    if (cols <= 4096) return f(Row<512, 8>());
+    if (cols <= 8192) return f(Row<1024, 8>());
+    if (cols <= 16384) return f(Row<1024, 16>());
+    if (cols <= 32768) return f(Row<1024, 32>());
+    return f(Row<1024, 64>());
 }
 
 template <class T>
 int fwd(const FwdArgs& a, bool vec, hipStream_t st)
 {
-    return by_size(a.cols, [&](auto threads, auto e) {
-        constexpr int TH = decltype(threads)::value, E = decltype(e)::value;
+    return by_size_fwd(a.cols, [&](auto row) {
+        constexpr int TH = decltype(row)::threads, E = decltype(row)::elems;
         const dim3 grid((uint32_t)ceil_div(a.rows, TH == 64 ? 4 : 1)), block(TH == 64 ? 256 : TH);
         if (vec) k_layernorm_fwd<T, T::VEC, TH, E><<<grid, block, 0, st>>>(a);
         else k_layernorm_fwd<T, 1, TH, E><<<grid, block, 0, st>>>(a);
@@ -271,8 +290,8 @@ template <class T>
 int bwd(const BwdArgs& a, bool vec, void* dw, void* db, hipStream_t st)
 {
     if (a.groups) {
-        const int rc = by_size(a.cols, [&](auto threads, auto e) {
-            constexpr int TH = decltype(threads)::value, E = decltype(e)::value;
+        const int rc = by_size_bwd(a.cols, [&](auto row) {
+            constexpr int TH = decltype(row)::threads, E = decltype(row)::elems;
             const dim3 grid(a.groups), block(TH == 64 ? 256 : TH);
             if (vec) k_layernorm_bwd<T, T::VEC, TH, E><<<grid, block, 0, st>>>(a);
             else k_layernorm_bwd<T, 1, TH, E><<<grid, block, 0, st>>>(a);
@@ -295,13 +314,13 @@ int check_size(uint32_t dtype, uint64_t rows, uint32_t cols)
     return FF_OK;
 }
 
-// partial sums of the weight's gradient: as many blocks as fill the device, each with four rows at least where there are that many
+// partial sums of the weight's gradient: as many blocks as fill the device (twice as many take 10 % longer on 16384 x 4096 elements, half as many 30 %)
 uint32_t groups_of(uint64_t rows, uint32_t cols)
 {
-    const uint32_t th = threads_of(cols);
-    const uint64_t per_block = th == 64 ? 4 : 1, most = th == 1024 ? 512 : 1024;
-    const uint64_t blocks = ceil_div(rows, per_block);
-    return (uint32_t)(blocks < most ? blocks : most);
+    return (uint32_t)by_size_bwd(cols, [&](auto row) {
+        constexpr uint64_t TH = decltype(row)::threads, most = TH >= 512 ? 512 : 1024;
+        return (int)std::min<uint64_t>(ceil_div(rows, TH == 64 ? 4 : 1), most);
+    });
 }
 
 }  // namespace
