@@ -302,7 +302,8 @@ def attention_fwd(q, k, v, *, causal=False, q_lengths=None, kv_lengths=None, sca
 
 
 def attention_bwd(dout, q, k, v, o, lse, *, causal=False, q_lengths=None, kv_lengths=None, scale=None):
-    """(dq, dk, dv) from the gradient of o and what attention_fwd returned for the same arguments"""
+    """(dq, dk, dv) from the gradient of o and what attention_fwd returned for the same arguments.  Where k and v are a piece of the
+    keys, o and lse those of all pieces: this piece's dk and dv, and its part of dq."""
     torch = _torch()
     sizes, q_lengths, kv_lengths = _attention_args(q, k, v, causal, q_lengths, kv_lengths, scale)
     _check(dout, "dout", q.shape, q.dtype, q.device)

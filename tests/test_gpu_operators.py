@@ -240,6 +240,56 @@ def test_attention_gradients_against_differences(ops):
         assert abs(slope - (grad.double() * d).sum()) < spread + 1e-5 * d.norm(), (n, slope.item())
 
 
+def of_exact_delta(want, dout, q, k, v, causal):
+    """the bounds without the rounding of o: what is left if the row sums of p dp stand for <do, o>"""
+    t = q.dtype
+    qd, kd, vd, do = (x.double() for x in (q, k, v, dout))
+    z = q.shape[3] ** -0.5 * qd @ kd.transpose(2, 3)
+    if causal:
+        z = z.masked_fill(~R.sees(1, q.shape[2], k.shape[2], True, None, None, q.device), -math.inf)
+    p = torch.softmax(z, 3)
+    extra = 1.01 * q.shape[3] ** -0.5 * p * R.half(t) * (do * (p @ vd)).abs().sum(3, keepdim=True)
+    return {"dq": (want["dq"][0], want["dq"][1] - extra @ kd.abs()), "dk": (want["dk"][0], want["dk"][1] - extra.transpose(2, 3) @ qd.abs())}
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("S,D,causal", [(3, 64, True), (8, 128, True), (40, 64, False), (64, 32, True), (100, 128, False), (128, 64, True)])
+def test_attention_rounding_of_o_is_not_in_short_rows(ops, S, D, causal, dtype):
+    g = gen(900 + S)
+    q, k, v, dout = normal(g, 2, 3, S, D, to=dtype, scale=1.5), *(normal(g, 2, 3, S, D, to=dtype) for _ in range(3))
+    want, o, lse = R.attention_bwd(dout, q, k, v, causal=causal)
+    dq, dk, _ = ops.attention_bwd(dout, q, k, v, o.to(dtype), lse.float(), causal=causal)
+    tight = of_exact_delta(want, dout, q, k, v, causal)
+    R.close(dq, *tight["dq"], "dq")
+    R.close(dk, *tight["dk"], "dk")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_attention_gradients_of_few_keys_in_the_mean(ops, dtype):
+    """dq and dk pass two roundings, of ds and of themselves: each 0.42 of half a step in the mean square where values spread evenly between powers of two,
+    0.6 together; with the rounding of o in the row sums they would be off by 0.9 (8 causal keys)"""
+    g = gen(980)
+    q, k, v, dout = normal(g, 4, 64, 8, 64, to=dtype, scale=1.5), *(normal(g, 4, 64, 8, 64, to=dtype) for _ in range(3))
+    want, o, lse = R.attention_bwd(dout, q, k, v, causal=True)
+    for name, got in zip(("dq", "dk"), ops.attention_bwd(dout, q, k, v, o.to(dtype), lse.float(), causal=True)):
+        assert (got.double() - want[name][0]).norm() < 0.75 * R.half(dtype) * want[name][0].norm(), name
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("cut", [1, 40, 64, 128, 200])
+def test_attention_backward_of_keys_in_pieces(ops, cut, dtype):
+    """o and lse are those of all keys: each piece gives its own dk and dv, and a part of dq"""
+    g = gen(950 + cut)
+    q, k, v, dout = normal(g, 1, 4, 90, 64, to=dtype), normal(g, 1, 2, 260, 64, to=dtype), normal(g, 1, 2, 260, 64, to=dtype), normal(g, 1, 4, 90, 64, to=dtype)
+    want, o, lse = R.attention_bwd(dout, q, k, v)
+    parts = [ops.attention_bwd(dout, q, k[:, :, a:b], v[:, :, a:b], o.to(dtype), lse.float()) for a, b in ((0, cut), (cut, 260))]
+    dq = parts[0][0].double() + parts[1][0].double()
+    bound = want["dq"][1] + R.half(dtype) * sum(p[0].double().abs() for p in parts) + R.tiny(dtype)
+    R.close(dq, want["dq"][0], bound, "dq")
+    R.close(torch.cat([p[1] for p in parts], 2), *want["dk"], "dk")
+    R.close(torch.cat([p[2] for p in parts], 2), *want["dv"], "dv")
+
+
 # ---- loss over a vocabulary ------------------------------------------------------------
 
 VOC = [(1, 1, 8), (1, 2, 1), (3, 65, 7), (64, 1000, 64), (65, 129, 72), (130, 515, 100), (257, 700, 33), (5, 33000, 40), (300, 3001, 520), (1200, 900, 128), (70, 64, 1001)]
