@@ -490,19 +490,34 @@ __global__ __launch_bounds__(256) void k_vocab_top(const float* dloss, uint32_t 
 
 constexpr uint64_t PIECE_BYTES = 256ull << 20;      // gradient of the logits of a piece: what the last-level cache holds
 
-struct Plan {
-    uint32_t dim;               // a multiple of 8
-    bool copy_x, copy_w, big;
-    uint32_t tile, m_tiles, n_tiles, piece, splits;
-    uint64_t x, w, part, logit, top, g, sum, dw, bytes;
+// How a product of m x n over k is cut: the largest tile of which there are enough, k split where that is allowed into no less than 512 of it and into no more than 16,
+// and none much longer than the shorter side.  256 x 256 tiles are half as fast again as others per product once they run, and take 20 us before and after that:
+// dx of 3328 x 28040 x 1096 with 195 blocks of them 208 us, 128 x 128 321 us; dw with k = 207 114 us, 64 x 64 87 us.  128 x 128 read half as
+// much as 64 x 64: 300 x 8000 x 1024 60 us for all, 64 x 64 66 us.
+struct Tiling {
+    uint32_t tile, ms, ns, splits;
+    uint32_t blocks() const { return ms * ns; }
 };
 
-// A product of fewer tiles than the device has places is split over k, into no less than 512 of it, its sums added up afterwards.
-uint32_t splits_of(uint64_t tiles, uint64_t k, bool big)
+Tiling tiling_of(uint64_t m, uint64_t n, uint64_t k, bool split)
 {
-    if (tiles == 0) return 1;
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>({(big ? 256 : 1024) / tiles, k / 512, 16}));
+    Tiling t = {};
+    for (uint32_t tile : {256u, 128u, 64u}) {
+        const uint64_t tiles = ceil_div(m, tile) * ceil_div(n, tile), places = tile == 256 ? 256 : tile == 128 ? 512 : 1024;
+        const uint64_t splits = split && tiles ? std::max<uint64_t>(1, std::min<uint64_t>({places / tiles, k / 512, 16})) : 1;
+        t = {tile, (uint32_t)ceil_div(m, tile), (uint32_t)ceil_div(n, tile), (uint32_t)splits};
+        if (tile == 64 || (tiles * splits >= (tile == 256 ? 160 : 256) && tile <= round_up(std::min(m, n), 64) && (tile < 256 || k >= 512))) break;
+    }
+    return t;
 }
+
+struct Plan {
+    uint32_t dim;               // a multiple of 8
+    bool copy_x, copy_w;
+    uint32_t piece;
+    Tiling z, dx;               // of the logits, forward or of a piece; of dx
+    uint64_t x, w, part, logit, top, g, sum, dw, bytes;
+};
 
 // 16-byte accesses, and 256 rows within 32 bits
 bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0 && m.stride >= 0 && m.stride < (1 << 22); }
@@ -521,25 +536,21 @@ Plan plan_of(const A* p, bool back)
     };
     q.x = take(q.copy_x ? (uint64_t)p->rows * q.dim * 2 : 0);
     q.w = take(q.copy_w ? (uint64_t)p->vocab * q.dim * 2 : 0);
-    // 256 x 256 tiles where they give every compute unit one; below that 64 x 64, more of them at a time on each
-    q.big = ceil_div(p->vocab, 256) * ceil_div(p->rows, 256) >= 256;
-    q.tile = q.big ? 256 : 64;
-    q.m_tiles = (uint32_t)ceil_div(p->vocab, q.tile), q.n_tiles = (uint32_t)ceil_div(p->rows, q.tile);
     if (!back) {
-        q.part = take((uint64_t)q.m_tiles * p->rows * sizeof(float2));
+        q.z = tiling_of(p->vocab, p->rows, q.dim, false);
+        q.part = take((uint64_t)q.z.ms * p->rows * sizeof(float2));
         q.logit = take((uint64_t)p->rows * sizeof(float));
     } else {
         q.top = take(sizeof(uint32_t));
         const uint64_t fit = PIECE_BYTES / 2 / std::max(1u, p->rows) / 256 * 256;
         q.piece = (uint32_t)std::min<uint64_t>(round_up(p->vocab, 256), std::max<uint64_t>(fit, 256));
         q.g = take((uint64_t)p->rows * q.piece * 2);
-        const uint64_t d_tiles = ceil_div(q.dim, q.tile);
-        q.splits = splits_of(d_tiles * q.n_tiles, std::min(p->vocab, q.piece), q.big);
-        q.sum = take(q.splits > 1 || q.piece < p->vocab ? (uint64_t)q.splits * p->rows * q.dim * sizeof(float) : 0);
+        q.dx = tiling_of(q.dim, p->rows, std::min(p->vocab, q.piece), true);
+        q.sum = take(q.dx.splits > 1 || q.piece < p->vocab ? (uint64_t)q.dx.splits * p->rows * q.dim * sizeof(float) : 0);
         // the last piece may be smaller than the others, and the only one whose dw is split
         uint64_t dw = 0;
         for (const uint64_t words : {(uint64_t)std::min(p->vocab, q.piece), (uint64_t)(p->vocab - 1) % q.piece + 1}) {
-            const uint32_t n = splits_of(d_tiles * ceil_div(words, q.tile), p->rows, q.big);
+            const uint32_t n = tiling_of(q.dim, words, p->rows, true).splits;
             if (n > 1) dw = std::max<uint64_t>(dw, n * words * q.dim * sizeof(float));
         }
         q.dw = take(dw);
@@ -577,7 +588,7 @@ VocabArgs args_of(const A* p, const Plan& q)
 {
     VocabArgs a = {};
     a.rows = p->rows, a.dim = q.dim, a.words = p->vocab, a.ignore = p->ignore_index, a.first_word = p->first_word;
-    a.m_tiles = q.m_tiles, a.n_tiles = q.n_tiles, a.targets = p->targets, a.splits = 1;
+    a.targets = p->targets, a.splits = 1;
     return a;
 }
 
@@ -590,9 +601,10 @@ int fwd(const ff_vocab_loss_fwd_t* p, const Plan& q, hipStream_t st)
     if (const int rc = lay_out<T>(p->w, p->vocab, p->dim, q.dim, q.copy_w, ws + q.w, a.w, st)) return rc;
     a.part = (float2*)(ws + q.part);
     a.target_logit = (float*)(ws + q.logit);
-    const uint32_t tiles = a.m_tiles * a.n_tiles;
-    if (q.big) k_vocab_logits<T, 256, false><<<tiles, 256, 0, st>>>(a);
-    else k_vocab_logits<T, 64, false><<<tiles, 256, 0, st>>>(a);
+    a.m_tiles = q.z.ms, a.n_tiles = q.z.ns;
+    if (q.z.tile == 256) k_vocab_logits<T, 256, false><<<q.z.blocks(), 256, 0, st>>>(a);
+    else if (q.z.tile == 128) k_vocab_logits<T, 128, false><<<q.z.blocks(), 256, 0, st>>>(a);
+    else k_vocab_logits<T, 64, false><<<q.z.blocks(), 256, 0, st>>>(a);
     k_vocab_join<<<(uint32_t)ceil_div(p->rows, 4), 256, 0, st>>>(a, p->loss, p->lse, p->target_logit);
     return launched();
 }
@@ -608,34 +620,37 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
     a.g = ws + q.g, a.g_stride = q.piece, a.sum = (float*)(ws + q.sum);
     k_vocab_clear<<<1, 1, 0, st>>>((uint32_t*)a.top);
     if (p->rows) k_vocab_top<<<(uint32_t)std::min<uint64_t>(ceil_div(p->rows, 256), 256), 256, 0, st>>>(p->dloss, p->rows, (uint32_t*)a.top);
-    const uint32_t d_tiles = (uint32_t)ceil_div(q.dim, q.tile);
-    const bool whole = q.splits == 1 && q.piece >= p->vocab;
+    const bool whole = q.dx.splits == 1 && q.piece >= p->vocab;
     for (uint64_t word0 = 0; word0 < p->vocab; word0 += q.piece) {
         a.word0 = (uint32_t)word0;
         a.words = (uint32_t)std::min<uint64_t>(q.piece, p->vocab - word0);
-        a.m_tiles = (uint32_t)ceil_div(a.words, q.tile), a.n_tiles = q.n_tiles;
-        const uint32_t v_tiles = a.m_tiles;
         if (p->rows) {
-            if (q.big) k_vocab_logits<T, 256, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
-            else k_vocab_logits<T, 64, true><<<a.m_tiles * a.n_tiles, 256, 0, st>>>(a);
+            const Tiling z = tiling_of(a.words, p->rows, q.dim, false);
+            a.m_tiles = z.ms, a.n_tiles = z.ns;
+            if (z.tile == 256) k_vocab_logits<T, 256, true><<<z.blocks(), 256, 0, st>>>(a);
+            else if (z.tile == 128) k_vocab_logits<T, 128, true><<<z.blocks(), 256, 0, st>>>(a);
+            else k_vocab_logits<T, 64, true><<<z.blocks(), 256, 0, st>>>(a);
         }
         if (p->dx.p && p->rows) {
-            a.m_tiles = d_tiles, a.n_tiles = q.n_tiles, a.splits = q.splits, a.first = word0 == 0, a.whole = whole;
+            a.m_tiles = q.dx.ms, a.n_tiles = q.dx.ns, a.splits = q.dx.splits, a.first = word0 == 0, a.whole = whole;
             a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
             a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
             a.dim = whole ? p->dim : q.dim;         // as many as are stored; the tiles of w have zeros beyond
-            const dim3 grid(a.m_tiles * a.n_tiles, q.splits);
-            if (q.big) k_vocab_dx<T, 256><<<grid, 256, 0, st>>>(a);
+            const dim3 grid(q.dx.blocks(), q.dx.splits);
+            if (q.dx.tile == 256) k_vocab_dx<T, 256><<<grid, 256, 0, st>>>(a);
+            else if (q.dx.tile == 128) k_vocab_dx<T, 128><<<grid, 256, 0, st>>>(a);
             else k_vocab_dx<T, 64><<<grid, 256, 0, st>>>(a);
             a.dim = q.dim;
         }
         if (p->dw.p) {
-            a.m_tiles = d_tiles, a.n_tiles = v_tiles;
+            const Tiling t = tiling_of(q.dim, a.words, p->rows, true);
+            a.m_tiles = t.ms, a.n_tiles = t.ns;
             a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
             a.out_vec = aligned(p->dw.p, 8) && p->dw.stride % 4 == 0;
-            a.splits = splits_of((uint64_t)d_tiles * v_tiles, p->rows, q.big), a.sum = (float*)(ws + q.dw);
-            const dim3 grid(a.m_tiles * a.n_tiles, a.splits);
-            if (q.big) k_vocab_dw<T, 256><<<grid, 256, 0, st>>>(a, p->dim);
+            a.splits = t.splits, a.sum = (float*)(ws + q.dw);
+            const dim3 grid(t.blocks(), t.splits);
+            if (t.tile == 256) k_vocab_dw<T, 256><<<grid, 256, 0, st>>>(a, p->dim);
+            else if (t.tile == 128) k_vocab_dw<T, 128><<<grid, 256, 0, st>>>(a, p->dim);
             else k_vocab_dw<T, 64><<<grid, 256, 0, st>>>(a, p->dim);
             if (a.splits > 1) {
                 VocabArgs o = a;
@@ -646,7 +661,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
         }
     }
     if (p->dx.p && p->rows && !whole) {
-        a.splits = q.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
+        a.splits = q.dx.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
         a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
         k_vocab_add<T><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->rows, p->dim);
     }
