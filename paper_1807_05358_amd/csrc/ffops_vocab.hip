@@ -196,7 +196,7 @@ struct VocabArgs {
     uint32_t splits, first, whole;          // dx: the first piece; one piece and no splits, so that dx is written at once
     char* out;
     int64_t out_stride;                     // bytes
-    uint32_t out_vec;                       // rows of the output take 8-byte stores
+    uint32_t out_align;                     // 16, 8, 4 or 2 bytes: where all rows of the output start
 };
 
 // four neighbouring elements of a row of an output, those below `n`
@@ -211,6 +211,42 @@ __device__ __forceinline__ void store_out(char* row, uint32_t x, uint32_t n, boo
         if (x + 2 < n) p[x + 2] = (typename T::elem)c;
         if (x + 3 < n) p[x + 3] = (typename T::elem)d;
     }
+}
+
+// A tile of an output, whose rows are the columns of the products in c, times f: rounded into LDS, which all have read, and from there row by row, so that a wave writes whole lines.  `cols`, `rows`:
+// what of it exists.  From the registers a wave's store is 32 bytes of each of 16 rows, or, where rows start anywhere, 2 bytes of each:
+// dw of 16 x 15216 x 3754, of which storing is nearly all, 107 us then, 49 us this way; dw and dx of 8192 x 32000 x 4096 a tenth less.
+template <class T, class P, int M>
+__device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM][P::TN], float f, char* out, int64_t stride, uint32_t align, int rows, int cols, int wm, int wn)
+{
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+    constexpr int PITCH = M * 2 + 16, THREADS = P::WM * P::WN * 64;
+    static_assert(M * PITCH <= P::LDS, "a tile of the result fits in the place of the factors'");
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int n = 0; n < P::TN; ++n)
+#pragma unroll
+        for (int m = 0; m < P::TM; ++m) *(lds_u32x2*)(lds + (wn + n * 16 + lane % 16) * PITCH + (wm + m * 16 + lane / 16 * 4) * 2) = __builtin_bit_cast(u32x2, pack4<T>(c[m][n] * f));
+    __syncthreads();
+    const auto write = [&](auto kind) {
+        typedef decltype(kind) V;
+        constexpr int E = sizeof(V) / 2, PER = M / E;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < M * PER; i += THREADS) {
+            const int r = i / PER, x = i % PER * E;
+            if (r >= rows || x >= cols) continue;
+            const lds_char* from = lds + r * PITCH + x * 2;
+            char* to = out + r * stride + x * 2;
+            if (x + E <= cols) *(V*)to = *(__attribute__((address_space(3))) const V*)from;
+            else
+                for (int e = 0; e < cols - x; ++e) ((uint16_t*)to)[e] = ((__attribute__((address_space(3))) const uint16_t*)from)[e];
+        }
+    };
+    if (align == 16) write(u32x4());
+    else if (align >= 4) write(uint32_t());
+    else write(uint16_t());
 }
 
 // z^T = w x^T: words down, tokens across, so that a lane holds words of one token.  GRAD false: maximum and sum of exp per
@@ -393,22 +429,26 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
 #pragma unroll
         for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
     P::run((lds_char*)lds_, sw, sg, k0, k1, c, wm, wn);
-#pragma unroll
-    for (int n = 0; n < P::TN; ++n) {
-        const uint32_t token = n0 + wn + n * 16 + lane % 16;
-        if (token >= a.rows) continue;
-#pragma unroll
-        for (int m = 0; m < P::TM; ++m) {
-            const uint32_t x = m0 + wm + m * 16 + 4 * quarter;
-            if (x >= a.dim) continue;
-            const f32x4 q = c[m][n];
-            if (a.whole) store_out<T>(a.out + (int64_t)token * a.out_stride, x, a.dim, a.out_vec, q[0] * f, q[1] * f, q[2] * f, q[3] * f);
-            else {          // dim is a multiple of 8
-                f32x4* p = (f32x4*)(sum + (uint64_t)token * a.dim + x);
-                *p = a.first ? q : *p + q;
-            }
-        }
+    if (a.whole) {
+        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + (int64_t)n0 * a.out_stride + m0 * 2, a.out_stride, a.out_align, (int)min(a.rows - n0, (uint32_t)N), (int)min(a.dim - m0, (uint32_t)M), wm, wn);
+        return;
     }
+    const auto sums = [&](auto first) {
+#pragma unroll
+        for (int n = 0; n < P::TN; ++n) {
+            const uint32_t token = n0 + wn + n * 16 + lane % 16, x = m0 + wm + 4 * quarter;
+            f32x4* p = (f32x4*)(sum + (uint64_t)token * a.dim + x);
+            f32x4 old[P::TM];
+#pragma unroll
+            for (int m = 0; m < P::TM; ++m) old[m] = !first && token < a.rows && x + m * 16 < a.dim ? p[m * 4] : f32x4{};
+#pragma unroll
+            for (int m = 0; m < P::TM; ++m)             // dim is a multiple of 8
+                if (token < a.rows && x + m * 16 < a.dim) p[m * 4] = c[m][n] + old[m];
+            asm volatile("" ::: "memory");              // no more of them in registers than this
+        }
+    };
+    if (a.first) sums(std::true_type());
+    else sums(std::false_type());
 }
 
 // rows of an output from the sums of their splits
@@ -420,7 +460,7 @@ __global__ __launch_bounds__(256) void k_vocab_add(VocabArgs a, uint32_t rows, u
     f32x4 s = {};
     for (uint32_t k = 0; k < a.splits; ++k) s += *(const f32x4*)(a.sum + k * n + at);
     const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
-    store_out<T>(a.out + (int64_t)(at / a.dim) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_vec, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+    store_out<T>(a.out + (int64_t)(at / a.dim) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_align >= 8, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
 }
 
 // dw of a piece = g^T x, made transposed over the tokens: elements down, words across
@@ -447,32 +487,48 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
     P::run((lds_char*)lds_, sx, sg, k0, k1, c, wm, wn);
     const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
     float* sum = a.sum + (uint64_t)blockIdx.y * a.words * a.dim;
+    if (a.splits == 1) {
+        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + (int64_t)(a.word0 + n0) * a.out_stride + m0 * 2, a.out_stride, a.out_align, (int)min(a.words - n0, (uint32_t)N), (int)dim - (int)m0, wm, wn);
+        return;
+    }
 #pragma unroll
     for (int n = 0; n < P::TN; ++n) {
         const uint32_t word = n0 + wn + n * 16 + lane % 16;
         if (word >= a.words) continue;
-        char* row = a.out + (int64_t)(a.word0 + word) * a.out_stride;
 #pragma unroll
         for (int m = 0; m < P::TM; ++m) {
             const uint32_t x = m0 + wm + m * 16 + 4 * quarter;
-            if (x >= a.dim) continue;
-            const f32x4 q = c[m][n];
-            if (a.splits == 1) store_out<T>(row, x, dim, a.out_vec, q[0] * f, q[1] * f, q[2] * f, q[3] * f);
-            else *(f32x4*)(sum + (uint64_t)word * a.dim + x) = q;
+            if (x < a.dim) *(f32x4*)(sum + (uint64_t)word * a.dim + x) = c[m][n];
         }
     }
 }
 
-// rows whose length or place does not suit 16-byte accesses, laid out anew: `dim` elements, zeros up to `to`, a multiple of 8
-template <class E>
+// Rows whose length or place does not suit 16-byte accesses, laid out anew: `dim` elements, zeros up to `to`, a multiple of 8.  A thread makes 16 bytes, from
+// reads of the widest kind that the rows' places allow (N elements: 2 or 1); blockIdx.x: groups of rows, as many of a row's chunks as fit side by side.
+template <class E, int N>
 __global__ __launch_bounds__(256) void k_vocab_lay_out(const E* p, int64_t stride, uint64_t rows, uint32_t dim, uint32_t to, E* out)
 {
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / (to / 2);
-    const uint32_t x = (uint32_t)(at % (to / 2)) * 2;
+    typedef E piece __attribute__((ext_vector_type(N)));
+    typedef E chunk __attribute__((ext_vector_type(8)));
+    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const uint64_t row = (uint64_t)blockIdx.x * 4 + wave;
     if (row >= rows) return;
     const E* s = p + (int64_t)row * stride;
-    out[row * to + x] = x < dim ? s[x] : (E)0;
-    out[row * to + x + 1] = x + 1 < dim ? s[x + 1] : (E)0;
+#pragma unroll 2
+    for (uint32_t x = lane * 8; x < to; x += 512) {
+        chunk v;
+        if (x + 8 <= dim) {
+#pragma unroll
+            for (int e = 0; e < 8; e += N) {
+                const piece u = *(const piece*)(s + x + e);
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[e + i] = N == 1 ? s[x + e] : u[i];
+            }
+        } else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x + e < dim ? s[x + e] : (E)0;
+        *(chunk*)(out + row * to + x) = v;
+    }
 }
 
 __global__ void k_vocab_clear(uint32_t* top) { *top = 0; }
@@ -521,6 +577,13 @@ struct Plan {
 
 // 16-byte accesses, and 256 rows within 32 bits
 bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0 && m.stride >= 0 && m.stride < (1 << 22); }
+
+uint32_t alignment_of(const ff_rows_t& m)
+{
+    for (uint32_t n : {16u, 8u, 4u})
+        if (aligned(m.p, n) && m.stride * 2 % n == 0) return n;
+    return 2;
+}
 
 template <class A>
 Plan plan_of(const A* p, bool back)
@@ -573,13 +636,15 @@ int check_vocab(const A* p)
 template <class T>
 int lay_out(const ff_rows_t& m, uint64_t rows, uint32_t dim, uint32_t to, bool copy, char* ws, Mat& out, hipStream_t st)
 {
-    if (!copy) {
+    if (!copy || rows == 0) {
         out = {(const char*)m.p, m.stride * 2};
         return FF_OK;
     }
     out = {ws, (int64_t)to * 2};
-    if (rows * (to / 2) > (1ull << 38)) return FF_ERANGE;
-    k_vocab_lay_out<typename T::elem><<<(uint32_t)ceil_div(rows * (to / 2), 256), 256, 0, st>>>((const typename T::elem*)m.p, m.stride, rows, dim, to, (typename T::elem*)ws);
+    typedef typename T::elem E;
+    const uint32_t blocks = (uint32_t)ceil_div(rows, 4);
+    if (aligned(m.p, 4) && m.stride % 2 == 0) k_vocab_lay_out<E, 2><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
+    else k_vocab_lay_out<E, 1><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
     return launched();
 }
 
@@ -634,7 +699,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
         if (p->dx.p && p->rows) {
             a.m_tiles = q.dx.ms, a.n_tiles = q.dx.ns, a.splits = q.dx.splits, a.first = word0 == 0, a.whole = whole;
             a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
-            a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
+            a.out_align = alignment_of(p->dx);
             a.dim = whole ? p->dim : q.dim;         // as many as are stored; the tiles of w have zeros beyond
             const dim3 grid(q.dx.blocks(), q.dx.splits);
             if (q.dx.tile == 256) k_vocab_dx<T, 256><<<grid, 256, 0, st>>>(a);
@@ -646,7 +711,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             const Tiling t = tiling_of(q.dim, a.words, p->rows, true);
             a.m_tiles = t.ms, a.n_tiles = t.ns;
             a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
-            a.out_vec = aligned(p->dw.p, 8) && p->dw.stride % 4 == 0;
+            a.out_align = alignment_of(p->dw);
             a.splits = t.splits, a.sum = (float*)(ws + q.dw);
             const dim3 grid(t.blocks(), t.splits);
             if (t.tile == 256) k_vocab_dw<T, 256><<<grid, 256, 0, st>>>(a, p->dim);
@@ -662,7 +727,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
     }
     if (p->dx.p && p->rows && !whole) {
         a.splits = q.dx.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
-        a.out_vec = aligned(p->dx.p, 8) && p->dx.stride % 4 == 0;
+        a.out_align = alignment_of(p->dx);
         k_vocab_add<T><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->rows, p->dim);
     }
     return launched();
