@@ -34,19 +34,25 @@ __device__ __forceinline__ typename T::vec8 operand(const lds_char* tile, int at
 }
 
 // The product of a block: c[m][n] += sum_k a[m][k] b[n][k] over k0 .. k1, M x N of it in WM x WN waves of 16 x 16 tiles, the
-// tiles of both sides loaded straight into LDS one tile of k ahead.  Along sides have k in multiples of 8.
+// tiles of both sides loaded straight into LDS, STAGES - 1 tiles of k ahead.  Along sides have k in multiples of 8.  A tile of k of 64 x 64 is 8 products of a wave, far less than
+// memory takes to answer, so a block alone on its unit needs more than one on the way: 64 x 2472 x 3280 backward (39 blocks) 62 us with two stages, 49 with three, 49 with four.
+// 128 x 128 with three leaves room for one block on a unit instead of two: 982 x 4635 x 1892 forward 59 us, 75 then.
 template <class T, int M, int N, int WAVES_M, int WAVES_N, bool A_ACROSS, bool B_ACROSS>
 struct Product {
     static constexpr int KT = 64;       // k of a tile in LDS
-    static constexpr int WM = WAVES_M, WN = WAVES_N, WAVES = WM * WN, TM = M / WM / 16, TN = N / WN / 16, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2, LDS = 2 * BYTES;
+    static constexpr int WM = WAVES_M, WN = WAVES_N, WAVES = WM * WN, TM = M / WM / 16, TN = N / WN / 16, A_BYTES = M * KT * 2, BYTES = (M + N) * KT * 2;
+    static constexpr int STAGES = M == 64 ? 3 : 2, LDS = STAGES * BYTES, LOADS = BYTES / 1024 / WAVES;
 
-    static __device__ __forceinline__ void step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const Side& a, const Side& b, int64_t k,
-                                                f32x4 (&c)[TM][TN], int wm, int wn)
+    static __device__ __forceinline__ void load(lds_char* __restrict dst, const Side& a, const Side& b, int64_t k)
     {
-        if (more) {
-            stage_side<M, KT, A_ACROSS, WAVES>(next, a, k + KT);
-            stage_side<N, KT, B_ACROSS, WAVES>(next + A_BYTES, b, k + KT);
-        }
+        stage_side<M, KT, A_ACROSS, WAVES>(dst, a, k);
+        stage_side<N, KT, B_ACROSS, WAVES>(dst + A_BYTES, b, k);
+    }
+
+    template <bool LOAD>
+    static __device__ __forceinline__ void step(const lds_char* __restrict cur, lds_char* __restrict into, const Side& a, const Side& b, int64_t k, f32x4 (&c)[TM][TN], int wm, int wn)
+    {
+        if (LOAD) load(into, a, b, k);
 #pragma unroll
         for (int st = 0; st < KT / 32; ++st) {
             typename T::vec8 fa[TM], fb[TN];
@@ -63,17 +69,20 @@ struct Product {
 
     static __device__ __forceinline__ void run(lds_char* lds, const Side& a, const Side& b, int64_t k0, int64_t k1, f32x4 (&c)[TM][TN], int wm, int wn)
     {
-        if (k0 < k1) {
-            stage_side<M, KT, A_ACROSS, WAVES>(lds, a, k0);
-            stage_side<N, KT, B_ACROSS, WAVES>(lds + A_BYTES, b, k0);
-        }
-        __syncthreads();
+        for (int j = 0; j < STAGES - 1 && k0 + j * KT < k1; ++j) load(lds + j * BYTES, a, b, k0 + j * KT);
         int now = 0;
-        for (int64_t k = k0; k < k1; k += KT) {
-            step(lds + now, lds + (BYTES - now), k + KT < k1, a, b, k, c, wm, wn);
-            now = BYTES - now;
-            __syncthreads();
+        int64_t k = k0;
+        for (; k + (STAGES - 1) * KT < k1; k += KT) {
+            meet<(STAGES - 2) * LOADS>();           // the tile is there, and the one before has been read by all
+            step<true>(lds + now, lds + (now == 0 ? (STAGES - 1) * BYTES : now - BYTES), a, b, k + (STAGES - 1) * KT, c, wm, wn);
+            now = now == (STAGES - 1) * BYTES ? 0 : now + BYTES;
         }
+        meet<0>();
+        for (; k < k1; k += KT) {
+            step<false>(lds + now, lds, a, b, k, c, wm, wn);
+            now = now == (STAGES - 1) * BYTES ? 0 : now + BYTES;
+        }
+        meet<0>();
     }
 };
 
@@ -215,7 +224,8 @@ __device__ __forceinline__ void store_out(char* row, uint32_t x, uint32_t n, boo
 
 // A tile of an output, whose rows are the columns of the products in c, times f: rounded into LDS, which all have read, and from there row by row, so that a wave writes whole lines.  `cols`, `rows`:
 // what of it exists.  From the registers a wave's store is 32 bytes of each of 16 rows, or, where rows start anywhere, 2 bytes of each:
-// dw of 16 x 15216 x 3754, of which storing is nearly all, 107 us then, 49 us this way; dw and dx of 8192 x 32000 x 4096 a tenth less.
+// dw of 16 x 15216 x 3754, of which storing is nearly all, 107 us then, 49 us this way.  All of
+// 8192 x 50257 x 2048 4017 us then, 3750 to 3830 this way.
 template <class T, class P, int M>
 __device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM][P::TN], float f, char* out, int64_t stride, uint32_t align, int rows, int cols, int wm, int wn)
 {
