@@ -136,9 +136,10 @@ typedef struct {
 size_t ff_op_vocab_loss_fwd_workspace_bytes(const ff_vocab_loss_fwd_t* a);
 int ff_op_vocab_loss_fwd(const ff_vocab_loss_fwd_t* a, void* stream);
 
-/* Its backward pass:  g_iv = (exp(z_iv - lse_i) - [v = t_i]) * dloss_i,  dx = g w,  dw = g^T x.  dloss is float [rows], finite.
- * z is made again, in pieces of the vocabulary; g is rounded to the tensors' type (relative to the largest |dloss|, so that a small
- * dloss loses nothing), sums are held in 32 bits.  Either of dx and dw may have a null pointer. */
+/* Its backward pass:  g_iv = (exp(z_iv - lse_i) - [v = t_i]) * dloss_i,  dx = g w,  dw = g^T x.  dloss is float [rows], finite
+ * where the row takes part; what x, dloss and lse hold in the others is not used, and they cost no products.  z is made again, in
+ * pieces of the vocabulary; g is rounded to the tensors' type (relative to the largest |dloss|, so that a small dloss loses nothing),
+ * sums are held in 32 bits.  Either of dx and dw may have a null pointer. */
 typedef struct {
     uint32_t dtype, rows, vocab, dim;
     int32_t ignore_index, first_word;

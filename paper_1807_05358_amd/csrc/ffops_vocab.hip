@@ -196,7 +196,10 @@ struct VocabArgs {
     Mat x, w;
     const int32_t* targets;
     const float *dloss, *lse_in;
-    const uint32_t* top;
+    // Backward: the number of rows that take part, and the bits of their largest |dloss|; row_of has them, in their order, and the others behind.
+    // Where there are others, or x does not suit the products, `gathered` has theirs of x: what is in the others reaches no product, and they take no time.
+    const uint32_t *live, *row_of;
+    Mat gathered;
     float2* part;                           // [rows][m_tiles]: maximum and sum of a tile's words
     float* target_logit;
     char* g;                                // [rows][g_stride]: gradient of the logits of a piece
@@ -223,11 +226,11 @@ __device__ __forceinline__ void store_out(char* row, uint32_t x, uint32_t n, boo
 }
 
 // A tile of an output, whose rows are the columns of the products in c, times f: rounded into LDS, which all have read, and from there row by row, so that a wave writes whole lines.  `cols`, `rows`:
-// what of it exists.  From the registers a wave's store is 32 bytes of each of 16 rows, or, where rows start anywhere, 2 bytes of each:
+// what of it exists; of(r): the output's row of the tile's row r.  From the registers a wave's store is 32 bytes of each of 16 rows, or, where rows start anywhere, 2 bytes of each:
 // dw of 16 x 15216 x 3754, of which storing is nearly all, 107 us then, 49 us this way.  All of
 // 8192 x 50257 x 2048 4017 us then, 3750 to 3830 this way.
-template <class T, class P, int M>
-__device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM][P::TN], float f, char* out, int64_t stride, uint32_t align, int rows, int cols, int wm, int wn)
+template <class T, class P, int M, class RowOf>
+__device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM][P::TN], float f, char* out, int64_t stride, uint32_t align, int rows, int cols, int wm, int wn, RowOf of)
 {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -248,7 +251,7 @@ __device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM
             const int r = i / PER, x = i % PER * E;
             if (r >= rows || x >= cols) continue;
             const lds_char* from = lds + r * PITCH + x * 2;
-            char* to = out + r * stride + x * 2;
+            char* to = out + of(r) * stride + x * 2;
             if (x + E <= cols) *(V*)to = *(__attribute__((address_space(3))) const V*)from;
             else
                 for (int e = 0; e < cols - x; ++e) ((uint16_t*)to)[e] = ((__attribute__((address_space(3))) const uint16_t*)from)[e];
@@ -267,9 +270,12 @@ __device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM
 template <class T>
 constexpr float G_SHIFT = std::is_same<T, F16>::value ? 12.0f : 40.0f;
 
-__device__ __forceinline__ float unit_of(const uint32_t* top)
+__device__ __forceinline__ uint32_t live_rows(const VocabArgs& a) { return a.live[0]; }
+__device__ __forceinline__ Mat live_x(const VocabArgs& a, uint32_t rows) { return rows == a.rows && a.x.p ? a.x : a.gathered; }
+
+__device__ __forceinline__ float unit_of(const VocabArgs& a)
 {
-    const float m = __uint_as_float(*top);
+    const float m = __uint_as_float(a.live[1]);
     return m > 0 && m < INFINITY ? m : 1.0f;
 }
 
@@ -299,11 +305,14 @@ __global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
     lds_char* lds = (lds_char*)lds_;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
+    const uint32_t rows = GRAD ? live_rows(a) : a.rows, n_tiles = GRAD ? (rows + N - 1) / N : a.n_tiles;
+    if (GRAD && blockIdx.x >= a.m_tiles * n_tiles) return;
     uint32_t tm, tn;
-    tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
+    tile_of_block(blockIdx.x, a.m_tiles, n_tiles, tm, tn);
     const uint32_t m0 = tm * M, n0 = tn * N;
+    const Mat x = GRAD ? live_x(a, rows) : a.x;
     const Side sw = {{a.w.p + (int64_t)(a.word0 + m0) * a.w.stride, a.w.stride}, (int)min(a.words - m0, (uint32_t)M), a.dim};
-    const Side sx = {{a.x.p + (int64_t)n0 * a.x.stride, a.x.stride}, (int)min(a.rows - n0, (uint32_t)N), a.dim};
+    const Side sx = {{x.p + (int64_t)n0 * x.stride, x.stride}, (int)min(rows - n0, (uint32_t)N), a.dim};
     f32x4 c[P::TM][P::TN];
 #pragma unroll
     for (int m = 0; m < P::TM; ++m)
@@ -314,8 +323,9 @@ __global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
 #pragma unroll
     for (int n = 0; n < P::TN; ++n) {
         const uint32_t token = n0 + wn + n * 16 + lane % 16;
-        const bool in = token < a.rows;
-        const int32_t target = in ? a.targets[token] : a.ignore;
+        const bool in = token < rows;
+        const uint32_t of = GRAD && in ? a.row_of[token] : token;
+        const int32_t target = in ? a.targets[of] : a.ignore;
         const bool live = target != a.ignore;
         // the target's place among the words that the lane holds: register r of tile m has word 16 * m + r after its first
         const uint32_t v0 = m0 + wm + 4 * quarter;
@@ -325,7 +335,7 @@ __global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
         // almost no tile has a lane's target or the last word
         if constexpr (GRAD) {
             // a row that takes no part has exp(-inf)
-            const float ls = live ? a.lse_in[token] * LOG2E - G_SHIFT<T> : INFINITY, f = live ? a.dloss[token] / unit_of(a.top) : 0;
+            const float ls = live ? a.lse_in[of] * LOG2E - G_SHIFT<T> : INFINITY, f = live ? a.dloss[of] / unit_of(a) : 0;
             char* row = a.g + ((uint64_t)token * a.g_stride + v0 + (quarter & 1) * 12) * 2;
 #pragma unroll
             for (int m = 0; m < P::TM; ++m)
@@ -422,17 +432,19 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
     __shared__ __attribute__((aligned(256))) char lds_[P::LDS];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), quarter = lane / 16;
     const int wm = wave / WN * (M / WM), wn = wave % WN * (N / WN);
+    const uint32_t rows = live_rows(a), n_tiles = (rows + N - 1) / N;
+    if (blockIdx.x >= a.m_tiles * n_tiles) return;
     uint32_t tm, tn;
-    tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
+    tile_of_block(blockIdx.x, a.m_tiles, n_tiles, tm, tn);
     const uint32_t m0 = tm * M, n0 = tn * N;
     const Side sw = {{a.w.p + (int64_t)a.word0 * a.w.stride + m0 * 2, a.w.stride}, (int)min(a.dim - m0, (uint32_t)M), a.words};
     // g has zeros beyond the last word, up to a multiple of 8
     const int64_t ks = ((int64_t)a.words + 7) / 8 * 8;
-    const Side sg = {{a.g + (uint64_t)n0 * a.g_stride * 2, (int64_t)a.g_stride * 2}, (int)min(a.rows - n0, (uint32_t)N), ks};
+    const Side sg = {{a.g + (uint64_t)n0 * a.g_stride * 2, (int64_t)a.g_stride * 2}, (int)min(rows - n0, (uint32_t)N), ks};
     const int64_t run = ((ks + a.splits - 1) / a.splits + 63) / 64 * 64;
     const int64_t k0 = min(ks, run * blockIdx.y), k1 = min(ks, k0 + run);
     f32x4 c[P::TM][P::TN];
-    const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
+    const float f = unit_of(a) * exp2f(-G_SHIFT<T>);
     float* sum = a.sum + (uint64_t)blockIdx.y * a.rows * a.dim;
 #pragma unroll
     for (int m = 0; m < P::TM; ++m)
@@ -440,7 +452,7 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
         for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
     P::run((lds_char*)lds_, sw, sg, k0, k1, c, wm, wn);
     if (a.whole) {
-        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + (int64_t)n0 * a.out_stride + m0 * 2, a.out_stride, a.out_align, (int)min(a.rows - n0, (uint32_t)N), (int)min(a.dim - m0, (uint32_t)M), wm, wn);
+        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + m0 * 2, a.out_stride, a.out_align, (int)min(rows - n0, (uint32_t)N), (int)min(a.dim - m0, (uint32_t)M), wm, wn, [&](int r) { return a.row_of[n0 + r]; });
         return;
     }
     const auto sums = [&](auto first) {
@@ -450,10 +462,10 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
             f32x4* p = (f32x4*)(sum + (uint64_t)token * a.dim + x);
             f32x4 old[P::TM];
 #pragma unroll
-            for (int m = 0; m < P::TM; ++m) old[m] = !first && token < a.rows && x + m * 16 < a.dim ? p[m * 4] : f32x4{};
+            for (int m = 0; m < P::TM; ++m) old[m] = !first && token < rows && x + m * 16 < a.dim ? p[m * 4] : f32x4{};
 #pragma unroll
             for (int m = 0; m < P::TM; ++m)             // dim is a multiple of 8
-                if (token < a.rows && x + m * 16 < a.dim) p[m * 4] = c[m][n] + old[m];
+                if (token < rows && x + m * 16 < a.dim) p[m * 4] = c[m][n] + old[m];
             asm volatile("" ::: "memory");              // no more of them in registers than this
         }
     };
@@ -461,16 +473,17 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
     else sums(std::false_type());
 }
 
-// rows of an output from the sums of their splits
-template <class T>
+// rows of an output from the sums of their splits: of dw, and of dx where it has row_of
+template <class T, bool DX>
 __global__ __launch_bounds__(256) void k_vocab_add(VocabArgs a, uint32_t rows, uint32_t dim)
 {
     const uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = (uint64_t)rows * a.dim;
-    if (at >= n) return;
+    const uint32_t row = (uint32_t)(at / a.dim);
+    if (row >= (DX ? live_rows(a) : rows)) return;
     f32x4 s = {};
     for (uint32_t k = 0; k < a.splits; ++k) s += *(const f32x4*)(a.sum + k * n + at);
-    const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
-    store_out<T>(a.out + (int64_t)(at / a.dim) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_align >= 8, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+    const float f = unit_of(a) * exp2f(-G_SHIFT<T>);
+    store_out<T>(a.out + (int64_t)(DX ? a.row_of[row] : row) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_align >= 8, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
 }
 
 // dw of a piece = g^T x, made transposed over the tokens: elements down, words across
@@ -485,20 +498,23 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
     uint32_t tm, tn;
     tile_of_block(blockIdx.x, a.m_tiles, a.n_tiles, tm, tn);
     const uint32_t m0 = tm * M, n0 = tn * N;
-    const Side sx = {{a.x.p + m0 * 2, a.x.stride}, (int)min(a.dim - m0, (uint32_t)M), a.rows};
-    const Side sg = {{a.g + n0 * 2, (int64_t)a.g_stride * 2}, (int)min(a.words - n0, (uint32_t)N), a.rows};
+    const uint32_t rows = live_rows(a);
+    const Mat x = live_x(a, rows);
+    const Side sx = {{x.p + m0 * 2, x.stride}, (int)min(a.dim - m0, (uint32_t)M), rows};
+    const Side sg = {{a.g + n0 * 2, (int64_t)a.g_stride * 2}, (int)min(a.words - n0, (uint32_t)N), rows};
     f32x4 c[P::TM][P::TN];
 #pragma unroll
     for (int m = 0; m < P::TM; ++m)
 #pragma unroll
         for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
-    const int64_t run = (((int64_t)a.rows + a.splits - 1) / a.splits + 63) / 64 * 64;
-    const int64_t k0 = min((int64_t)a.rows, run * blockIdx.y), k1 = min((int64_t)a.rows, k0 + run);
+    const int64_t run = (((int64_t)rows + a.splits - 1) / a.splits + 63) / 64 * 64;
+    const int64_t k0 = min((int64_t)rows, run * blockIdx.y), k1 = min((int64_t)rows, k0 + run);
     P::run((lds_char*)lds_, sx, sg, k0, k1, c, wm, wn);
-    const float f = unit_of(a.top) * exp2f(-G_SHIFT<T>);
+    const float f = unit_of(a) * exp2f(-G_SHIFT<T>);
     float* sum = a.sum + (uint64_t)blockIdx.y * a.words * a.dim;
     if (a.splits == 1) {
-        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + (int64_t)(a.word0 + n0) * a.out_stride + m0 * 2, a.out_stride, a.out_align, (int)min(a.words - n0, (uint32_t)N), (int)dim - (int)m0, wm, wn);
+        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + m0 * 2, a.out_stride, a.out_align, (int)min(a.words - n0, (uint32_t)N), (int)dim - (int)m0, wm, wn,
+                            [&](int r) { return (int64_t)a.word0 + n0 + r; });
         return;
     }
 #pragma unroll
@@ -513,17 +529,14 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
     }
 }
 
-// Rows whose length or place does not suit 16-byte accesses, laid out anew: `dim` elements, zeros up to `to`, a multiple of 8.  A thread makes 16 bytes, from
-// reads of the widest kind that the rows' places allow (N elements: 2 or 1); blockIdx.x: groups of rows, as many of a row's chunks as fit side by side.
+// A row whose length or place does not suit 16-byte accesses, laid out anew by a wave: `dim` elements, zeros up to `to`, a multiple of 8.  A lane makes 16 bytes, from
+// reads of the widest kind that the rows' places allow (N elements: 8, 2 or 1).
 template <class E, int N>
-__global__ __launch_bounds__(256) void k_vocab_lay_out(const E* p, int64_t stride, uint64_t rows, uint32_t dim, uint32_t to, E* out)
+__device__ __forceinline__ void lay_out_row(const E* s, uint32_t dim, uint32_t to, E* out)
 {
     typedef E piece __attribute__((ext_vector_type(N)));
     typedef E chunk __attribute__((ext_vector_type(8)));
-    const uint32_t wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-    const uint64_t row = (uint64_t)blockIdx.x * 4 + wave;
-    if (row >= rows) return;
-    const E* s = p + (int64_t)row * stride;
+    const uint32_t lane = threadIdx.x % 64;
 #pragma unroll 2
     for (uint32_t x = lane * 8; x < to; x += 512) {
         chunk v;
@@ -537,19 +550,89 @@ __global__ __launch_bounds__(256) void k_vocab_lay_out(const E* p, int64_t strid
         } else
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = x + e < dim ? s[x + e] : (E)0;
-        *(chunk*)(out + row * to + x) = v;
+        *(chunk*)(out + x) = v;
     }
 }
 
-__global__ void k_vocab_clear(uint32_t* top) { *top = 0; }
-
-__global__ __launch_bounds__(256) void k_vocab_top(const float* dloss, uint32_t rows, uint32_t* top)
+template <class E, int N>
+__global__ __launch_bounds__(256) void k_vocab_lay_out(const E* p, int64_t stride, uint64_t rows, uint32_t dim, uint32_t to, E* out)
 {
-    float m = 0;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < rows; i += (uint64_t)gridDim.x * 256) m = fmaxf(m, fabsf(dloss[i]));
+    const uint64_t row = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (row < rows) lay_out_row<E, N>(p + (int64_t)row * stride, dim, to, out + row * to);
+}
+
+// The live rows' number and largest |dloss|, and the rows in order: one block, RUN runs of as many rows as it has threads at a time.  More blocks would have to meet in between;
+// 8192 rows take this one 5 us.
+__global__ __launch_bounds__(1024) void k_vocab_live(const int32_t* targets, int32_t ignore, const float* dloss, uint32_t rows, uint32_t* live, uint32_t* row_of)
+{
+    constexpr uint32_t RUN = 8;
+    __shared__ uint32_t sums[RUN * 16], total;
+    __shared__ float tops[16];
+    const uint32_t lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    uint32_t before = 0;            // live rows of the rounds before
+    float top = 0;
+    for (uint64_t r0 = 0; r0 < rows; r0 += blockDim.x * RUN) {
+        const uint64_t first = r0 + threadIdx.x;
+        int32_t target[RUN];
+        float weight[RUN];
+        uint64_t lives[RUN];
 #pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    if (threadIdx.x % 64 == 0) atomicMax(top, __float_as_uint(m));         // the largest of a set does not depend on the order
+        for (uint32_t i = 0; i < RUN; ++i) {            // all at once
+            const uint64_t r = min(first + i * blockDim.x, (uint64_t)rows - 1);
+            target[i] = targets[r], weight[i] = dloss[r];
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < RUN; ++i) {
+            const bool is = first + i * blockDim.x < rows && target[i] != ignore;
+            lives[i] = __ballot(is);
+            top = is ? fmaxf(top, fabsf(weight[i])) : top;
+            if (lane == 0) sums[i * waves + wave] = __popcll(lives[i]);
+        }
+        __syncthreads();
+        if (wave == 0) {            // sums of what stands before each of them
+            const uint32_t n = RUN * waves, u = 2 * lane < n ? sums[2 * lane] : 0, v = 2 * lane < n ? sums[2 * lane + 1] : 0;
+            uint32_t upto = u + v;
+#pragma unroll
+            for (uint32_t d = 1; d < 64; d *= 2) {
+                const uint32_t o = __shfl_up(upto, d);
+                if (lane >= d) upto += o;
+            }
+            if (2 * lane < n) sums[2 * lane] = upto - u - v, sums[2 * lane + 1] = upto - v;
+            if (lane == 63) total = upto;
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < RUN; ++i) {
+            const uint64_t r = first + i * blockDim.x;
+            if (r >= rows) break;
+            const uint32_t at = before + sums[i * waves + wave] + __popcll(lives[i] & ((1ull << lane) - 1));
+            // r - at of the others came before one of them
+            row_of[lives[i] >> lane & 1 ? at : rows - 1 - (r - at)] = (uint32_t)r;
+        }
+        before += total;
+        __syncthreads();
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (uint32_t w = 1; w < waves; ++w) top = fmaxf(top, tops[w]);
+    live[0] = before, live[1] = __float_as_uint(top);
+}
+
+// a wave per place of row_of: the live rows of x side by side, where some are not live or x does not suit the products (`suits`), and zeros in the others' dx
+template <class E, int N>
+__global__ __launch_bounds__(256) void k_vocab_gather(VocabArgs a, const E* x, int64_t stride, uint32_t dim, bool suits, char* dx, int64_t dx_stride)
+{
+    const uint32_t i = blockIdx.x * 4 + threadIdx.x / 64, rows = a.live[0];
+    if (i >= a.rows) return;
+    if (i < rows) {
+        if (rows < a.rows || !suits) lay_out_row<E, N>(x + (int64_t)a.row_of[i] * stride, dim, a.dim, (E*)(a.gathered.p + (int64_t)i * a.gathered.stride));
+    } else if (dx) {
+        E* row = (E*)(dx + (int64_t)a.row_of[i] * dx_stride);
+        for (uint32_t e = threadIdx.x % 64; e < dim; e += 64) row[e] = (E)0;
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------
@@ -582,7 +665,7 @@ struct Plan {
     bool copy_x, copy_w;
     uint32_t piece;
     Tiling z, dx;               // of the logits, forward or of a piece; of dx
-    uint64_t x, w, part, logit, top, g, sum, dw, bytes;
+    uint64_t x, w, part, logit, live, row_of, g, sum, dw, bytes;
 };
 
 // 16-byte accesses, and 256 rows within 32 bits
@@ -607,14 +690,15 @@ Plan plan_of(const A* p, bool back)
         at += round_up(bytes, 256);
         return o;
     };
-    q.x = take(q.copy_x ? (uint64_t)p->rows * q.dim * 2 : 0);
+    q.x = take(q.copy_x || back ? (uint64_t)p->rows * q.dim * 2 : 0);
     q.w = take(q.copy_w ? (uint64_t)p->vocab * q.dim * 2 : 0);
     if (!back) {
         q.z = tiling_of(p->vocab, p->rows, q.dim, false);
         q.part = take((uint64_t)q.z.ms * p->rows * sizeof(float2));
         q.logit = take((uint64_t)p->rows * sizeof(float));
     } else {
-        q.top = take(sizeof(uint32_t));
+        q.live = take(2 * sizeof(uint32_t));
+        q.row_of = take((uint64_t)p->rows * sizeof(uint32_t));
         const uint64_t fit = PIECE_BYTES / 2 / std::max(1u, p->rows) / 256 * 256;
         q.piece = (uint32_t)std::min<uint64_t>(round_up(p->vocab, 256), std::max<uint64_t>(fit, 256));
         q.g = take((uint64_t)p->rows * q.piece * 2);
@@ -653,7 +737,7 @@ int lay_out(const ff_rows_t& m, uint64_t rows, uint32_t dim, uint32_t to, bool c
     out = {ws, (int64_t)to * 2};
     typedef typename T::elem E;
     const uint32_t blocks = (uint32_t)ceil_div(rows, 4);
-    if (aligned(m.p, 4) && m.stride % 2 == 0) k_vocab_lay_out<E, 2><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
+    if (alignment_of(m) >= 4) k_vocab_lay_out<E, 2><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
     else k_vocab_lay_out<E, 1><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
     return launched();
 }
@@ -689,12 +773,20 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
 {
     char* ws = (char*)p->workspace;
     VocabArgs a = args_of(p, q);
-    if (const int rc = lay_out<T>(p->x, p->rows, p->dim, q.dim, q.copy_x, ws + q.x, a.x, st)) return rc;
     if (const int rc = lay_out<T>(p->w, p->vocab, p->dim, q.dim, q.copy_w, ws + q.w, a.w, st)) return rc;
-    a.dloss = p->dloss, a.lse_in = p->lse, a.top = (uint32_t*)(ws + q.top);
+    a.dloss = p->dloss, a.lse_in = p->lse, a.live = (uint32_t*)(ws + q.live);
     a.g = ws + q.g, a.g_stride = q.piece, a.sum = (float*)(ws + q.sum);
-    k_vocab_clear<<<1, 1, 0, st>>>((uint32_t*)a.top);
-    if (p->rows) k_vocab_top<<<(uint32_t)std::min<uint64_t>(ceil_div(p->rows, 256), 256), 256, 0, st>>>(p->dloss, p->rows, (uint32_t*)a.top);
+    a.row_of = (uint32_t*)(ws + q.row_of);
+    a.x = {q.copy_x ? nullptr : (const char*)p->x.p, p->x.stride * 2}, a.gathered = {ws + q.x, (int64_t)q.dim * 2};
+    k_vocab_live<<<1, p->rows > 512 ? 1024 : 64, 0, st>>>(p->targets, p->ignore_index, p->dloss, p->rows, (uint32_t*)(ws + q.live), (uint32_t*)(ws + q.row_of));
+    if (p->rows) {
+        typedef typename T::elem E;
+        const uint32_t blocks = (uint32_t)ceil_div(p->rows, 4);
+        const auto gather = [&](auto kernel) { kernel<<<blocks, 256, 0, st>>>(a, (const E*)p->x.p, p->x.stride, p->dim, !q.copy_x, (char*)p->dx.p, p->dx.stride * 2); };
+        if (!q.copy_x) gather(k_vocab_gather<E, 8>);
+        else if (alignment_of(p->x) >= 4) gather(k_vocab_gather<E, 2>);
+        else gather(k_vocab_gather<E, 1>);
+    }
     const bool whole = q.dx.splits == 1 && q.piece >= p->vocab;
     for (uint64_t word0 = 0; word0 < p->vocab; word0 += q.piece) {
         a.word0 = (uint32_t)word0;
@@ -730,7 +822,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             if (a.splits > 1) {
                 VocabArgs o = a;
                 o.out += (int64_t)word0 * a.out_stride;
-                k_vocab_add<T><<<(uint32_t)ceil_div((uint64_t)a.words * q.dim / 4, 256), 256, 0, st>>>(o, a.words, p->dim);
+                k_vocab_add<T, false><<<(uint32_t)ceil_div((uint64_t)a.words * q.dim / 4, 256), 256, 0, st>>>(o, a.words, p->dim);
             }
             a.sum = (float*)(ws + q.sum);
         }
@@ -738,7 +830,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
     if (p->dx.p && p->rows && !whole) {
         a.splits = q.dx.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
         a.out_align = alignment_of(p->dx);
-        k_vocab_add<T><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->rows, p->dim);
+        k_vocab_add<T, true><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->rows, p->dim);
     }
     return launched();
 }

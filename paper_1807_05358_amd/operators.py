@@ -349,7 +349,8 @@ def vocab_loss_fwd(x, weight, targets, *, ignore_index=-100, first_word=None):
 
 
 def vocab_loss_bwd(dloss, x, weight, targets, lse, *, ignore_index=-100, first_word=None):
-    """(dx, dweight) from the gradient of each row's loss (float32 [rows]) and the forward pass' lse; for a shard of the vocabulary, dx is its share of the sum"""
+    """(dx, dweight) from the gradient of each row's loss (float32 [rows]) and the forward pass' lse; for a shard of the vocabulary, dx is its share of the sum.
+    Rows with ignore_index cost no products: their dx is 0, and what x, dloss and lse hold there is not used."""
     torch = _torch()
     sizes, xs, ws, targets = _vocab_args(x, weight, targets, ignore_index, first_word or 0)
     _check(dloss, "dloss", targets.shape, torch.float32, x.device)

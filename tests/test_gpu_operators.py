@@ -376,6 +376,26 @@ def test_vocab_loss_targets_and_strides(ops):
     assert dx.shape == (0, 64) and dw.shape == w.shape and not dw.any()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,vocab,dim", [(5, 70, 33), (64, 300, 64), (65, 515, 100), (700, 1300, 72), (2100, 600, 64), (9000, 130, 16)])
+@pytest.mark.parametrize("share", [0.03, 0.5, 0.97, 1.0])
+def test_vocab_loss_rows_that_take_no_part(ops, rows, vocab, dim, share, dtype):
+    """their vectors, weights and statistics may hold anything, and the others' gradients are those of a call without them"""
+    g = gen(rows + int(share * 100))
+    x, w, t = vocab_case(g, rows, vocab, dim, dtype, 0.0)
+    dloss = normal(g, rows)
+    out = torch.rand(rows, generator=g, device="cuda") < share
+    t[out] = -100
+    x[out] = math.nan
+    dloss[out] = math.inf
+    _, lse, _ = ops.vocab_loss_fwd(x, w, t)
+    dx, dw = ops.vocab_loss_bwd(dloss, x, w, t, lse)
+    assert not dx[out].any()
+    some = R.vocab_loss_bwd(dloss[~out], x[~out], w, t[~out], lse[~out])
+    R.close(dx[~out], *some["dx"], "dx")
+    R.close(dw, *some["dw"], "dw")
+
+
 def test_vocab_loss_large_logits(ops):
     """logits of hundreds, all of them negative for some rows"""
     g = gen(23)
