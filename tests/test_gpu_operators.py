@@ -131,7 +131,9 @@ ATT = [(1, 1, 1, 1, 1, 64, False, False, "bhsd"),
        (1, 3, 1, 300, 33, 104, False, False, "bhsd"),
        (1, 1, 1, 700, 700, 16, True, False, "bhsd"),
        (1, 4, 1, 513, 640, 64, True, False, "bshd"),
-       (1, 24, 8, 64, 1, 64, True, False, "bhsd")]
+       (1, 24, 8, 64, 1, 64, True, False, "bhsd"),
+       (16, 64, 8, 512, 100, 16, False, False, "bhsd"),    # more than half of the compute units have a block, and long ones: split over queries,
+       (1, 8, 8, 2048, 4096, 16, True, False, "bhsd")]     # and over keys
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
