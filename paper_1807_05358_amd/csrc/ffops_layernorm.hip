@@ -26,38 +26,64 @@ struct BwdArgs {
     float* part;                    // [2][groups][cols]
 };
 
-// V elements at p[i] as floats; V * sizeof(elem) is 16 bytes, or V = 1
-template <class T, int V>
-__device__ __forceinline__ void load(const void* p, int64_t i, float* f)
-{
-    typedef typename T::elem vec __attribute__((ext_vector_type(V)));
-    if constexpr (V == 1) f[0] = (float)((const typename T::elem*)p)[i];
-    else {
-        const vec v = *(const vec*)((const typename T::elem*)p + i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) f[e] = (float)v[e];
-    }
-}
+// The elements of a row that a lane takes at a time: 16 bytes of the type, from element `at`, of which it owns first .. last - 1.  LOOSE: rows start at any element and have any length; the
+// device takes accesses of 16 bytes anywhere, and the last ones of a row are moved back to end with it, where their first elements are the lane's before.  That way no load
+// stands in a branch, where it would be waited for.  One element at a time 16384 x 4095 bfloats take 101 us forward
+// and 250 backward, this way 55 and 111; where rows suit it (4096) 42 and 90.  Rows of 645 elements alone are slower backward, 19 us to 17.
+template <class T, bool LOOSE>
+struct Chunk {
+    typedef typename T::elem elem;
+    static constexpr int V = T::VEC;
+    typedef elem vec __attribute__((ext_vector_type(V), aligned(LOOSE ? sizeof(elem) : 16)));
+    int64_t at;
+    int first, last;
+    bool any;
 
-template <class T, int V>
-__device__ __forceinline__ void store(void* p, int64_t i, const float* f)
-{
-    typedef typename T::elem vec __attribute__((ext_vector_type(V)));
-    if constexpr (V == 1) ((typename T::elem*)p)[i] = (typename T::elem)f[0];
-    else {
-        vec v;
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = (typename T::elem)f[e];
-        *(vec*)((typename T::elem*)p + i) = v;
+    __device__ __forceinline__ Chunk(uint32_t c, uint32_t cols)
+    {
+        any = c < cols;
+        at = LOOSE ? max(min((int)c, (int)cols - V), 0) : c;
+        first = LOOSE ? (int)c - (int)at : 0;
+        last = LOOSE ? min(V, (int)cols) : V;
     }
-}
+    __device__ __forceinline__ bool owns(int e) const { return !LOOSE || (e >= first && e < last); }
+    __device__ __forceinline__ void load(const void* p, int64_t row, float* f) const
+    {
+        const elem* q = (const elem*)p + row + at;
+        if (!LOOSE || last == V) {
+            const vec v = *(const vec*)q;
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = (float)v[e];
+        } else              // a row shorter than that
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = e < last ? (float)q[e] : 0.0f;
+    }
+    __device__ __forceinline__ void store(void* p, int64_t row, const float* f) const
+    {
+        elem* q = (elem*)p + row + at;
+        if (!LOOSE || last - first == V) {
+            vec v;
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = (elem)f[e];
+            *(vec*)q = v;
+        } else
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (owns(e)) q[e] = (elem)f[e];
+    }
+};
 
 // sums of N values over the THREADS lanes that share a row; every lane gets them.  `red` holds N floats per wave.
 template <int THREADS, int N>
 __device__ __forceinline__ void row_sum(float* s, float* red)
 {
 #pragma unroll
-    for (int n = 0; n < N; ++n) s[n] = wave_sum(s[n]);
+    for (int n = 0; n < N; ++n) {
+        if constexpr (THREADS >= 64) s[n] = wave_sum(s[n]);
+        else
+#pragma unroll
+            for (int d = THREADS / 2; d; d /= 2) s[n] += __shfl_xor(s[n], d);
+    }
     if constexpr (THREADS > 64) {
         const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
         __syncthreads();        // the previous sums have been read
@@ -72,48 +98,52 @@ __device__ __forceinline__ void row_sum(float* s, float* red)
     }
 }
 
-// A row is held in registers by THREADS lanes, E elements each, in accesses of V; rows of a wave of their own go four to a
+constexpr int block_of(int threads) { return threads <= 64 ? 256 : threads; }
+constexpr int rows_of(int threads) { return block_of(threads) / threads; }
+
+// A row is held in registers by THREADS lanes, E elements each; rows of a wave, or of less of it, go side by side in a
 // block.  One read of x (and res), one write of h and y: the kernel is bound by memory.
-template <class T, int V, int THREADS, int E>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_fwd(FwdArgs a)
+template <class T, bool LOOSE, int THREADS, int E>
+__global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_fwd(FwdArgs a)
 {
-    constexpr int RPB = THREADS == 64 ? 4 : 1, N = E / V;
-    __shared__ float red[THREADS / 64];
+    constexpr int V = T::VEC, N = E / V;
+    __shared__ float red[THREADS > 64 ? THREADS / 64 : 1];
     const int t = threadIdx.x % THREADS;
-    const uint64_t row = (uint64_t)blockIdx.x * RPB + threadIdx.x / THREADS;
-    if (row >= a.rows) return;      // whole waves, and no barrier where a row is a wave's
+    const uint64_t row = (uint64_t)blockIdx.x * rows_of(THREADS) + threadIdx.x / THREADS;
+    if (row >= a.rows) return;      // all lanes of a row, and no barrier where a block has several
     const int64_t r = (int64_t)row;
     float f[E];
     float s = 0;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        const uint32_t c = (n * THREADS + t) * V;
+        const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
         float* v = f + n * V;
-        if (c < a.cols) {
-            load<T, V>(a.x, r * a.xs + c, v);
+        if (c.any) {
+            c.load(a.x, r * a.xs, v);
             if (a.res) {
                 float u[V];
-                load<T, V>(a.res, r * a.rs + c, u);
+                c.load(a.res, r * a.rs, u);
 #pragma unroll
                 for (int e = 0; e < V; ++e) v[e] = (float)(typename T::elem)(v[e] + u[e]);     // the sum is an output, and what is normed
-                store<T, V>(a.h, r * a.hs + c, v);
+                c.store(a.h, r * a.hs, v);
             }
 #pragma unroll
-            for (int e = 0; e < V; ++e) s += v[e];
-        } else
-            for (int e = 0; e < V; ++e) v[e] = 0;
+            for (int e = 0; e < V; ++e) s += c.owns(e) ? v[e] : 0.0f;
+        }
     }
     row_sum<THREADS, 1>(&s, red);
     const float mean = s / (float)a.cols;
     float q = 0;                    // of the differences, from registers: no cancellation
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-        if ((uint32_t)(n * THREADS + t) * V < a.cols)
+    for (int n = 0; n < N; ++n) {
+        const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
+        if (c.any)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = f[n * V + e] - mean;
+                const float d = c.owns(e) ? f[n * V + e] - mean : 0.0f;
                 q += d * d;
             }
+    }
     row_sum<THREADS, 1>(&q, red);
     const float rstd = 1.0f / sqrtf(q / (float)a.cols + a.eps);
     if (t == 0) {
@@ -122,35 +152,35 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_fwd
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        const uint32_t c = (n * THREADS + t) * V;
-        if (c < a.cols) {
+        const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
+        if (c.any) {
             float w[V], b[V], y[V];
-            load<T, V>(a.w, c, w);
-            if (a.b) load<T, V>(a.b, c, b);
+            c.load(a.w, 0, w);
+            if (a.b) c.load(a.b, 0, b);
 #pragma unroll
             for (int e = 0; e < V; ++e) y[e] = (f[n * V + e] - mean) * rstd * w[e] + (a.b ? b[e] : 0.0f);
-            store<T, V>(a.y, r * a.ys + c, y);
+            c.store(a.y, r * a.ys, y);
         }
     }
 }
 
-// Rows are dealt to the groups in turn (block b takes rows b, b + groups, ...; a wave of its own the rows of its place in
+// Rows are dealt to the groups in turn (block b takes rows b, b + groups, ...; a wave, or less, of its own the rows of its place in
 // the block too), so that a lane keeps its columns and sums the weight's and the bias's gradient in registers.  One read
 // of dy, h (and dh), one write of dx; the partial sums are groups * cols * 8 bytes more, each way.
-template <class T, int V, int THREADS, int E>
-__global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_bwd(BwdArgs a)
+template <class T, bool LOOSE, int THREADS, int E>
+__global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_bwd(BwdArgs a)
 {
-    constexpr int RPB = THREADS == 64 ? 4 : 1, N = E / V;
-    __shared__ float red[2 * THREADS / 64];
-    __shared__ float both[THREADS == 64 ? 2 * 64 * E : 1];
+    constexpr int RPB = rows_of(THREADS), V = T::VEC, N = E / V, SHARED = THREADS < 64 ? THREADS : 64;
+    __shared__ float red[THREADS > 64 ? 2 * THREADS / 64 : 1];
+    __shared__ float both[RPB > 1 ? 2 * SHARED * E : 1];
     const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
     float w[E], dw[E], db[E];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        const uint32_t c = (n * THREADS + t) * V;
+        const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
 #pragma unroll
         for (int e = 0; e < V; ++e) w[n * V + e] = dw[n * V + e] = db[n * V + e] = 0;
-        if (c < a.cols) load<T, V>(a.w, c, w + n * V);
+        if (c.any) c.load(a.w, 0, w + n * V);
     }
     for (uint64_t row = (uint64_t)blockIdx.x * RPB + sub; row < a.rows; row += (uint64_t)a.groups * RPB) {
         const int64_t r = (int64_t)row;
@@ -158,15 +188,15 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_bwd
         float g[E], xh[E], s[2] = {0, 0};
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const uint32_t c = (n * THREADS + t) * V;
+            const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
             float *gn = g + n * V, *xn = xh + n * V;
-            if (c < a.cols) {
-                load<T, V>(a.dy, r * a.dys + c, gn);
-                load<T, V>(a.h, r * a.hs + c, xn);
+            if (c.any) {
+                c.load(a.dy, r * a.dys, gn);
+                c.load(a.h, r * a.hs, xn);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float dy = gn[e];
-                    xn[e] = (xn[e] - mean) * rstd;
+                    const float dy = c.owns(e) ? gn[e] : 0.0f;
+                    xn[e] = c.owns(e) ? (xn[e] - mean) * rstd : 0.0f;
                     gn[e] = dy * w[n * V + e];
                     dw[n * V + e] += dy * xn[e];
                     db[n * V + e] += dy;
@@ -179,41 +209,51 @@ __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_layernorm_bwd
         const float mg = s[0] / (float)a.cols, mx = s[1] / (float)a.cols;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const uint32_t c = (n * THREADS + t) * V;
-            if (c < a.cols) {
+            const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
+            if (c.any) {
                 float d[V], u[V];
-                if (a.dh) load<T, V>(a.dh, r * a.dhs + c, u);
+                if (a.dh) c.load(a.dh, r * a.dhs, u);
 #pragma unroll
                 for (int e = 0; e < V; ++e) d[e] = rstd * (g[n * V + e] - mg - xh[n * V + e] * mx) + (a.dh ? u[e] : 0.0f);
-                store<T, V>(a.dx, r * a.dxs + c, d);
+                c.store(a.dx, r * a.dxs, d);
             }
         }
     }
     if (!a.part) return;
-    if constexpr (THREADS == 64) {          // the four waves of a block into one, in turn
-        for (int k = 0; k < RPB; ++k) {
-            if (sub == k)
+    if constexpr (RPB > 1) {                // the rows of a wave into one, and then the four waves of a block, in turn
+#pragma unroll
+        for (int d = THREADS; d < 64; d *= 2)
+#pragma unroll
+            for (int e = 0; e < E; ++e) dw[e] += __shfl_xor(dw[e], d), db[e] += __shfl_xor(db[e], d);
+        const int wave = threadIdx.x / 64;
+        for (int k = 0; k < 4; ++k) {
+            if (wave == k && threadIdx.x % 64 < SHARED)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    if (k) dw[e] += both[e * 64 + t], db[e] += both[(E + e) * 64 + t];
-                    both[e * 64 + t] = dw[e], both[(E + e) * 64 + t] = db[e];
+                    if (k) dw[e] += both[e * SHARED + t], db[e] += both[(E + e) * SHARED + t];
+                    both[e * SHARED + t] = dw[e], both[(E + e) * SHARED + t] = db[e];
                 }
             __syncthreads();
         }
-        if (sub != RPB - 1) return;
+        if (wave != 3 || threadIdx.x % 64 >= SHARED) return;
     }
     float *pw = a.part + (uint64_t)blockIdx.x * a.cols, *pb = pw + (uint64_t)a.groups * a.cols;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-        const uint32_t c = (n * THREADS + t) * V;
-        if (c < a.cols) {
-            store<F32, V == 1 ? 1 : 4>(pw, c, dw + n * V);
-            store<F32, V == 1 ? 1 : 4>(pb, c, db + n * V);
-            if constexpr (V == 8) {
-                store<F32, 4>(pw, c + 4, dw + n * V + 4);
-                store<F32, 4>(pb, c + 4, db + n * V + 4);
+        const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
+        typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+        if (c.any)
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+                const float *u = dw + n * V + e, *v = db + n * V + e;
+                if (c.owns(e) && c.owns(e + 3)) {
+                    *(f32x4*)(pw + c.at + e) = f32x4{u[0], u[1], u[2], u[3]};
+                    *(f32x4*)(pb + c.at + e) = f32x4{v[0], v[1], v[2], v[3]};
+                } else
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (c.owns(e + i)) pw[c.at + e + i] = u[i], pb[c.at + e + i] = v[i];
             }
-        }
     }
 }
 
@@ -249,6 +289,7 @@ struct Row {        // lanes that share a row, and elements of a lane
 template <class F>
 int by_size_fwd(uint32_t cols, F f)
 {
+    if (cols <= 128) return f(Row<16, 8>());
     if (cols <= 512) return f(Row<64, 8>());
     if (cols <= 1024) return f(Row<64, 16>());
     if (cols <= 2048) return f(Row<64, 32>());
@@ -264,6 +305,7 @@ int by_size_fwd(uint32_t cols, F f)
 template <class F>
 int by_size_bwd(uint32_t cols, F f)
 {
+    if (cols <= 128) return f(Row<16, 8>());
     if (cols <= 512) return f(Row<64, 8>());
     if (cols <= 1024) return f(Row<64, 16>());
     if (cols <= 2048) return f(Row<256, 8>());
@@ -279,9 +321,9 @@ int fwd(const FwdArgs& a, bool vec, hipStream_t st)
 {
     return by_size_fwd(a.cols, [&](auto row) {
         constexpr int TH = decltype(row)::threads, E = decltype(row)::elems;
-        const dim3 grid((uint32_t)ceil_div(a.rows, TH == 64 ? 4 : 1)), block(TH == 64 ? 256 : TH);
-        if (vec) k_layernorm_fwd<T, T::VEC, TH, E><<<grid, block, 0, st>>>(a);
-        else k_layernorm_fwd<T, 1, TH, E><<<grid, block, 0, st>>>(a);
+        const dim3 grid((uint32_t)ceil_div(a.rows, rows_of(TH))), block(block_of(TH));
+        if (vec) k_layernorm_fwd<T, false, TH, E><<<grid, block, 0, st>>>(a);
+        else k_layernorm_fwd<T, true, TH, E><<<grid, block, 0, st>>>(a);
         return launched();
     });
 }
@@ -292,9 +334,9 @@ int bwd(const BwdArgs& a, bool vec, void* dw, void* db, hipStream_t st)
     if (a.groups) {
         const int rc = by_size_bwd(a.cols, [&](auto row) {
             constexpr int TH = decltype(row)::threads, E = decltype(row)::elems;
-            const dim3 grid(a.groups), block(TH == 64 ? 256 : TH);
-            if (vec) k_layernorm_bwd<T, T::VEC, TH, E><<<grid, block, 0, st>>>(a);
-            else k_layernorm_bwd<T, 1, TH, E><<<grid, block, 0, st>>>(a);
+            const dim3 grid(a.groups), block(block_of(TH));
+            if (vec) k_layernorm_bwd<T, false, TH, E><<<grid, block, 0, st>>>(a);
+            else k_layernorm_bwd<T, true, TH, E><<<grid, block, 0, st>>>(a);
             return launched();
         });
         if (rc != FF_OK) return rc;
@@ -319,7 +361,7 @@ uint32_t groups_of(uint64_t rows, uint32_t cols)
 {
     return (uint32_t)by_size_bwd(cols, [&](auto row) {
         constexpr uint64_t TH = decltype(row)::threads, most = TH >= 512 ? 512 : 1024;
-        return (int)std::min<uint64_t>(ceil_div(rows, TH == 64 ? 4 : 1), most);
+        return (int)std::min<uint64_t>(ceil_div(rows, rows_of(TH)), most);
     });
 }
 

@@ -79,6 +79,23 @@ def test_layernorm_strides(ops):
         compare(ops.layernorm_bwd(dy, h, w, mean, rstd, dh=res), R.layernorm_bwd(dy, h, w, mean, rstd, res))
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("cols", [2, 3, 5, 9, 12, 15, 77, 127, 128, 129, 255, 645, 1025, 2433, 4097, 5811, 14233])
+def test_layernorm_rows_of_any_length_and_place(ops, cols, dtype):
+    """rows that start at any element: the last lanes' accesses overlap those before, and nothing beyond a row is read or written"""
+    g = gen(cols)
+    rows = 37
+    big = [torch.full((rows, cols + 7), math.nan, device="cuda", dtype=dtype) for _ in range(4)]
+    x, res, dy, dh = (m[:, 3:3 + cols] for m in big)
+    for m in (x, res, dy, dh):
+        m.copy_(normal(g, rows, cols))
+    w, b = normal(g, cols + 1, to=dtype)[1:], normal(g, cols + 1, to=dtype)[1:]
+    got = ops.layernorm_fwd(x, w, b, residual=res)
+    compare(got, R.layernorm_fwd(x, w, b, res, 1e-5))
+    _, h, mean, rstd = got
+    compare(ops.layernorm_bwd(dy, h, w, mean, rstd, dh=dh), R.layernorm_bwd(dy, h, w, mean, rstd, dh))
+
+
 def test_layernorm_special_values(ops):
     g = gen(6)
     w = torch.ones(256, device="cuda")
