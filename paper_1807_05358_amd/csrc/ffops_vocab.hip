@@ -208,7 +208,7 @@ struct VocabArgs {
     uint32_t splits, first, whole;          // dx: the first piece; one piece and no splits, so that dx is written at once
     char* out;
     int64_t out_stride;                     // bytes
-    uint32_t out_align;                     // 16, 8, 4 or 2 bytes: where all rows of the output start
+    uint32_t out_vec;                       // rows of the output take 8-byte stores
 };
 
 // four neighbouring elements of a row of an output, those below `n`
@@ -230,7 +230,7 @@ __device__ __forceinline__ void store_out(char* row, uint32_t x, uint32_t n, boo
 // dw of 16 x 15216 x 3754, of which storing is nearly all, 107 us then, 49 us this way.  All of
 // 8192 x 50257 x 2048 4017 us then, 3750 to 3830 this way.
 template <class T, class P, int M, class RowOf>
-__device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM][P::TN], float f, char* out, int64_t stride, uint32_t align, int rows, int cols, int wm, int wn, RowOf of)
+__device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM][P::TN], float f, char* out, int64_t stride, int rows, int cols, int wm, int wn, RowOf of)
 {
     typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
     typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -243,23 +243,17 @@ __device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM
 #pragma unroll
         for (int m = 0; m < P::TM; ++m) *(lds_u32x2*)(lds + (wn + n * 16 + lane % 16) * PITCH + (wm + m * 16 + lane / 16 * 4) * 2) = __builtin_bit_cast(u32x2, pack4<T>(c[m][n] * f));
     __syncthreads();
-    const auto write = [&](auto kind) {
-        typedef decltype(kind) V;
-        constexpr int E = sizeof(V) / 2, PER = M / E;
+    typedef u32x4 out16 __attribute__((aligned(2)));        // the device takes them anywhere
 #pragma unroll 4
-        for (int i = threadIdx.x; i < M * PER; i += THREADS) {
-            const int r = i / PER, x = i % PER * E;
-            if (r >= rows || x >= cols) continue;
-            const lds_char* from = lds + r * PITCH + x * 2;
-            char* to = out + of(r) * stride + x * 2;
-            if (x + E <= cols) *(V*)to = *(__attribute__((address_space(3))) const V*)from;
-            else
-                for (int e = 0; e < cols - x; ++e) ((uint16_t*)to)[e] = ((__attribute__((address_space(3))) const uint16_t*)from)[e];
-        }
-    };
-    if (align == 16) write(u32x4());
-    else if (align >= 4) write(uint32_t());
-    else write(uint16_t());
+    for (int i = threadIdx.x; i < M * M / 8; i += THREADS) {
+        const int r = i / (M / 8), x = i % (M / 8) * 8;
+        if (r >= rows || x >= cols) continue;
+        const lds_char* from = lds + r * PITCH + x * 2;
+        char* to = out + of(r) * stride + x * 2;
+        if (x + 8 <= cols) *(out16*)to = *(__attribute__((address_space(3))) const u32x4*)from;
+        else
+            for (int e = 0; e < cols - x; ++e) ((uint16_t*)to)[e] = ((__attribute__((address_space(3))) const uint16_t*)from)[e];
+    }
 }
 
 // z^T = w x^T: words down, tokens across, so that a lane holds words of one token.  GRAD false: maximum and sum of exp per
@@ -452,7 +446,7 @@ __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
         for (int n = 0; n < P::TN; ++n) c[m][n] = f32x4{};
     P::run((lds_char*)lds_, sw, sg, k0, k1, c, wm, wn);
     if (a.whole) {
-        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + m0 * 2, a.out_stride, a.out_align, (int)min(rows - n0, (uint32_t)N), (int)min(a.dim - m0, (uint32_t)M), wm, wn, [&](int r) { return a.row_of[n0 + r]; });
+        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + m0 * 2, a.out_stride, (int)min(rows - n0, (uint32_t)N), (int)min(a.dim - m0, (uint32_t)M), wm, wn, [&](int r) { return a.row_of[n0 + r]; });
         return;
     }
     const auto sums = [&](auto first) {
@@ -483,7 +477,7 @@ __global__ __launch_bounds__(256) void k_vocab_add(VocabArgs a, uint32_t rows, u
     f32x4 s = {};
     for (uint32_t k = 0; k < a.splits; ++k) s += *(const f32x4*)(a.sum + k * n + at);
     const float f = unit_of(a) * exp2f(-G_SHIFT<T>);
-    store_out<T>(a.out + (int64_t)(DX ? a.row_of[row] : row) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_align >= 8, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
+    store_out<T>(a.out + (int64_t)(DX ? a.row_of[row] : row) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_vec, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
 }
 
 // dw of a piece = g^T x, made transposed over the tokens: elements down, words across
@@ -513,7 +507,7 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
     const float f = unit_of(a) * exp2f(-G_SHIFT<T>);
     float* sum = a.sum + (uint64_t)blockIdx.y * a.words * a.dim;
     if (a.splits == 1) {
-        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + m0 * 2, a.out_stride, a.out_align, (int)min(a.words - n0, (uint32_t)N), (int)dim - (int)m0, wm, wn,
+        store_tile<T, P, M>((lds_char*)lds_, c, f, a.out + m0 * 2, a.out_stride, (int)min(a.words - n0, (uint32_t)N), (int)dim - (int)m0, wm, wn,
                             [&](int r) { return (int64_t)a.word0 + n0 + r; });
         return;
     }
@@ -529,36 +523,29 @@ __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
     }
 }
 
-// A row whose length or place does not suit 16-byte accesses, laid out anew by a wave: `dim` elements, zeros up to `to`, a multiple of 8.  A lane makes 16 bytes, from
-// reads of the widest kind that the rows' places allow (N elements: 8, 2 or 1).
-template <class E, int N>
+// A row whose length or place does not suit the products' loads, laid out anew by a wave: `dim` elements, zeros up to `to`, a multiple of 8.
+template <class E>
 __device__ __forceinline__ void lay_out_row(const E* s, uint32_t dim, uint32_t to, E* out)
 {
-    typedef E piece __attribute__((ext_vector_type(N)));
     typedef E chunk __attribute__((ext_vector_type(8)));
+    typedef E piece __attribute__((ext_vector_type(8), aligned(sizeof(E))));        // the device takes them anywhere
     const uint32_t lane = threadIdx.x % 64;
 #pragma unroll 2
     for (uint32_t x = lane * 8; x < to; x += 512) {
         chunk v;
-        if (x + 8 <= dim) {
-#pragma unroll
-            for (int e = 0; e < 8; e += N) {
-                const piece u = *(const piece*)(s + x + e);
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[e + i] = N == 1 ? s[x + e] : u[i];
-            }
-        } else
+        if (x + 8 <= dim) v = *(const piece*)(s + x);
+        else
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = x + e < dim ? s[x + e] : (E)0;
         *(chunk*)(out + x) = v;
     }
 }
 
-template <class E, int N>
+template <class E>
 __global__ __launch_bounds__(256) void k_vocab_lay_out(const E* p, int64_t stride, uint64_t rows, uint32_t dim, uint32_t to, E* out)
 {
     const uint64_t row = (uint64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (row < rows) lay_out_row<E, N>(p + (int64_t)row * stride, dim, to, out + row * to);
+    if (row < rows) lay_out_row(p + (int64_t)row * stride, dim, to, out + row * to);
 }
 
 // The live rows' number and largest |dloss|, and the rows in order: one block, RUN runs of as many rows as it has threads at a time.  More blocks would have to meet in between;
@@ -622,13 +609,13 @@ __global__ __launch_bounds__(1024) void k_vocab_live(const int32_t* targets, int
 }
 
 // a wave per place of row_of: the live rows of x side by side, where some are not live or x does not suit the products (`suits`), and zeros in the others' dx
-template <class E, int N>
+template <class E>
 __global__ __launch_bounds__(256) void k_vocab_gather(VocabArgs a, const E* x, int64_t stride, uint32_t dim, bool suits, char* dx, int64_t dx_stride)
 {
     const uint32_t i = blockIdx.x * 4 + threadIdx.x / 64, rows = a.live[0];
     if (i >= a.rows) return;
     if (i < rows) {
-        if (rows < a.rows || !suits) lay_out_row<E, N>(x + (int64_t)a.row_of[i] * stride, dim, a.dim, (E*)(a.gathered.p + (int64_t)i * a.gathered.stride));
+        if (rows < a.rows || !suits) lay_out_row(x + (int64_t)a.row_of[i] * stride, dim, a.dim, (E*)(a.gathered.p + (int64_t)i * a.gathered.stride));
     } else if (dx) {
         E* row = (E*)(dx + (int64_t)a.row_of[i] * dx_stride);
         for (uint32_t e = threadIdx.x % 64; e < dim; e += 64) row[e] = (E)0;
@@ -671,12 +658,7 @@ struct Plan {
 // 16-byte accesses, and 256 rows within 32 bits
 bool suits(const ff_rows_t& m, uint32_t dim) { return aligned(m.p, 16) && m.stride % 8 == 0 && dim % 8 == 0 && m.stride >= 0 && m.stride < (1 << 22); }
 
-uint32_t alignment_of(const ff_rows_t& m)
-{
-    for (uint32_t n : {16u, 8u, 4u})
-        if (aligned(m.p, n) && m.stride * 2 % n == 0) return n;
-    return 2;
-}
+bool eight_bytes(const ff_rows_t& m) { return aligned(m.p, 8) && m.stride % 4 == 0; }
 
 template <class A>
 Plan plan_of(const A* p, bool back)
@@ -736,9 +718,7 @@ int lay_out(const ff_rows_t& m, uint64_t rows, uint32_t dim, uint32_t to, bool c
     }
     out = {ws, (int64_t)to * 2};
     typedef typename T::elem E;
-    const uint32_t blocks = (uint32_t)ceil_div(rows, 4);
-    if (alignment_of(m) >= 4) k_vocab_lay_out<E, 2><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
-    else k_vocab_lay_out<E, 1><<<blocks, 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
+    k_vocab_lay_out<<<(uint32_t)ceil_div(rows, 4), 256, 0, st>>>((const E*)m.p, m.stride, rows, dim, to, (E*)ws);
     return launched();
 }
 
@@ -781,11 +761,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
     k_vocab_live<<<1, p->rows > 512 ? 1024 : 64, 0, st>>>(p->targets, p->ignore_index, p->dloss, p->rows, (uint32_t*)(ws + q.live), (uint32_t*)(ws + q.row_of));
     if (p->rows) {
         typedef typename T::elem E;
-        const uint32_t blocks = (uint32_t)ceil_div(p->rows, 4);
-        const auto gather = [&](auto kernel) { kernel<<<blocks, 256, 0, st>>>(a, (const E*)p->x.p, p->x.stride, p->dim, !q.copy_x, (char*)p->dx.p, p->dx.stride * 2); };
-        if (!q.copy_x) gather(k_vocab_gather<E, 8>);
-        else if (alignment_of(p->x) >= 4) gather(k_vocab_gather<E, 2>);
-        else gather(k_vocab_gather<E, 1>);
+        k_vocab_gather<<<(uint32_t)ceil_div(p->rows, 4), 256, 0, st>>>(a, (const E*)p->x.p, p->x.stride, p->dim, !q.copy_x, (char*)p->dx.p, p->dx.stride * 2);
     }
     const bool whole = q.dx.splits == 1 && q.piece >= p->vocab;
     for (uint64_t word0 = 0; word0 < p->vocab; word0 += q.piece) {
@@ -801,7 +777,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
         if (p->dx.p && p->rows) {
             a.m_tiles = q.dx.ms, a.n_tiles = q.dx.ns, a.splits = q.dx.splits, a.first = word0 == 0, a.whole = whole;
             a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
-            a.out_align = alignment_of(p->dx);
+            a.out_vec = eight_bytes(p->dx);
             a.dim = whole ? p->dim : q.dim;         // as many as are stored; the tiles of w have zeros beyond
             const dim3 grid(q.dx.blocks(), q.dx.splits);
             if (q.dx.tile == 256) k_vocab_dx<T, 256><<<grid, 256, 0, st>>>(a);
@@ -813,7 +789,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
             const Tiling t = tiling_of(q.dim, a.words, p->rows, true);
             a.m_tiles = t.ms, a.n_tiles = t.ns;
             a.out = (char*)p->dw.p, a.out_stride = p->dw.stride * 2;
-            a.out_align = alignment_of(p->dw);
+            a.out_vec = eight_bytes(p->dw);
             a.splits = t.splits, a.sum = (float*)(ws + q.dw);
             const dim3 grid(t.blocks(), t.splits);
             if (t.tile == 256) k_vocab_dw<T, 256><<<grid, 256, 0, st>>>(a, p->dim);
@@ -829,7 +805,7 @@ int bwd(const ff_vocab_loss_bwd_t* p, const Plan& q, hipStream_t st)
     }
     if (p->dx.p && p->rows && !whole) {
         a.splits = q.dx.splits, a.out = (char*)p->dx.p, a.out_stride = p->dx.stride * 2;
-        a.out_align = alignment_of(p->dx);
+        a.out_vec = eight_bytes(p->dx);
         k_vocab_add<T, true><<<(uint32_t)ceil_div((uint64_t)p->rows * q.dim / 4, 256), 256, 0, st>>>(a, p->rows, p->dim);
     }
     return launched();
