@@ -8,7 +8,10 @@ namespace {
 // and values in LDS, loaded one tile ahead.  Scores are made transposed, s^T = k q^T: a lane then holds 16 of 32 keys
 // of one row, the softmax of a row needs one exchange with lane ^ 32, its statistics are one register each, and the
 // probabilities are the second operand of o^T += v^T p^T as they lie.  The running maximum moves only when it grows by more than
-// 2^8: sums then stay within 2^8 of their scale, which costs 32-bit sums nothing and saves most rescalings.
+// 2^8: sums then stay within 2^8 of their scale, which costs 32-bit sums nothing and saves most rescalings.  The probabilities are rounded to the type because the products take nothing wider.
+// Two waves on a SIMD, so that one's products run beside the other's exponentials, maxima and conversions, which are what bounds it: 2 sequences of 4096, 32 heads on 8 of
+// 128, causal, 293 us, 939 TFLOP/s, matrix units busy 45 % of the time, LDS 24 %.  One wave with 64 rows, which reads half as much from LDS, takes 352 us.
+// A single token (8 sequences of up to 16384 keys, 32 heads on 8) is bound by memory: 60 us, 4.5 TB/s; the heads of a group share a wave's rows, so that keys are read once.
 constexpr int KEYS = 64;
 
 template <class T, int D, int WAVES>
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_fwd(AttnArgs a)
         }
 }
 
-// joins the parts of a row: o = sum_s 2^(lse_s - lse) o_s.  A wave per row: 16 lanes cover its elements, 8 each, and four of them the splits in turn.
+// joins the parts of a row (5 us for 256 rows of 8 splits, most of it the launch): o = sum_s 2^(lse_s - lse) o_s.  A wave per row: 16 lanes cover its elements, 8 each, and four of them the splits in turn.
 template <class T>
 __global__ __launch_bounds__(256) void k_attention_join(AttnArgs a)
 {
