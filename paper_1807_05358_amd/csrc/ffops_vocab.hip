@@ -641,7 +641,7 @@ Tiling tiling_of(uint64_t m, uint64_t n, uint64_t k, bool split)
 {
     Tiling t = {};
     for (uint32_t tile : {256u, 128u, 64u}) {
-        const uint64_t tiles = ceil_div(m, tile) * ceil_div(n, tile), places = tile == 256 ? 256 : tile == 128 ? 512 : 1024;
+        const uint64_t tiles = ceil_div(m, tile) * ceil_div(n, tile), places = tile == 256 ? 256 : tile == 128 ? 512 : 768;      // one, two and three on a unit, by their LDS
         const uint64_t splits = split && tiles ? std::max<uint64_t>(1, std::min<uint64_t>({places / tiles, k / 512, 16})) : 1;
         t = {tile, (uint32_t)ceil_div(m, tile), (uint32_t)ceil_div(n, tile), (uint32_t)splits};
         if (tile == 64 || (tiles * splits >= (tile == 256 ? 160 : 256) && tile <= round_up(std::min(m, n), 64) && (tile < 256 || k >= 512))) break;
