@@ -168,7 +168,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
     __shared__ __attribute__((aligned(256))) char lds_[Q::STAGES * Q::STAGE];
     lds_char* lds = (lds_char*)lds_;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    const uint32_t bk = blockIdx.x, b = bk / a.kv_heads, kh = bk % a.kv_heads;
+    const uint32_t bk = heads_of_block(a), b = bk / a.kv_heads, kh = bk % a.kv_heads;
     const int nq = seq_len(a.q_lengths, a.q_len, b), nk = seq_len(a.kv_lengths, a.kv_len, b), shift = nk - nq;
     const int block0 = blockIdx.y * (WAVES * 32), key0 = block0 + wave * 32, key = key0 + lane % 32;       // causal: the keys that most queries see first
     const bool own = key < nk;
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     __shared__ __attribute__((aligned(256))) char lds_[4 * TILE];
     lds_char* lds = (lds_char*)lds_;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    const uint32_t bk = blockIdx.x, b = bk / a.kv_heads, kh = bk % a.kv_heads;
+    const uint32_t bk = heads_of_block(a), b = bk / a.kv_heads, kh = bk % a.kv_heads;
     const Rows w = rows_of_wave<WAVES>(a, b, kh, wave, lane);
     const int nk = w.nk, chunks = a.dim / 8;
     int t0 = 0, t1 = (w.keys + STEP - 1) / STEP;

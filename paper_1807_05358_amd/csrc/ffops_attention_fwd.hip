@@ -89,7 +89,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_fwd(AttnArgs a)
     __shared__ __attribute__((aligned(256))) char lds_[4 * TILE];
     lds_char* lds = (lds_char*)lds_;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), half = lane / 32;
-    const uint32_t bk = blockIdx.x, b = bk / a.kv_heads, kh = bk % a.kv_heads;
+    const uint32_t bk = heads_of_block(a), b = bk / a.kv_heads, kh = bk % a.kv_heads;
     const Rows w = rows_of_wave<WAVES>(a, b, kh, wave, lane);
     const uint32_t i = w.i, h = w.h;
     const int nk = w.nk;
