@@ -29,7 +29,7 @@ struct BwdArgs {
 // The elements of a row that a lane takes at a time: 16 bytes of the type, from element `at`, of which it owns first .. last - 1.  LOOSE: rows start at any element and have any length; the
 // device takes accesses of 16 bytes anywhere, and the last ones of a row are moved back to end with it, where their first elements are the lane's before.  That way no load
 // stands in a branch, where it would be waited for.  One element at a time 16384 x 4095 bfloats take 101 us forward
-// and 250 backward, this way 55 and 111; where rows suit it (4096) 42 and 90.  Rows of 645 elements alone are slower backward, 19 us to 17.
+// and 250 backward, this way 55 and 98; where rows suit it (4096) 42 and 80.
 template <class T, bool LOOSE>
 struct Chunk {
     typedef typename T::elem elem;
@@ -47,16 +47,20 @@ struct Chunk {
         last = LOOSE ? min(V, (int)cols) : V;
     }
     __device__ __forceinline__ bool owns(int e) const { return !LOOSE || (e >= first && e < last); }
-    __device__ __forceinline__ void load(const void* p, int64_t row, float* f) const
+    __device__ __forceinline__ vec fetch(const void* p, int64_t row) const
     {
         const elem* q = (const elem*)p + row + at;
-        if (!LOOSE || last == V) {
-            const vec v = *(const vec*)q;
+        if (!LOOSE || last == V) return *(const vec*)q;
+        vec v;              // a row shorter than that
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] = (float)v[e];
-        } else              // a row shorter than that
+        for (int e = 0; e < V; ++e) v[e] = e < last ? q[e] : (elem)0;
+        return v;
+    }
+    __device__ __forceinline__ void load(const void* p, int64_t row, float* f) const
+    {
+        const vec v = fetch(p, row);
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] = e < last ? (float)q[e] : 0.0f;
+        for (int e = 0; e < V; ++e) f[e] = (float)v[e];
     }
     __device__ __forceinline__ void store(void* p, int64_t row, const float* f) const
     {
@@ -166,7 +170,8 @@ __global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_fwd(FwdArgs a)
 
 // Rows are dealt to the groups in turn (block b takes rows b, b + groups, ...; a wave, or less, of its own the rows of its place in
 // the block too), so that a lane keeps its columns and sums the weight's and the bias's gradient in registers.  One read
-// of dy, h (and dh), one write of dx; the partial sums are groups * cols * 8 bytes more, each way.  Bound by memory: 16384 x 4096 bfloats with a residual 109 us, 4.9 TB/s.
+// of dy, h (and dh), one write of dx; the partial sums are groups * cols * 8 bytes more, each way.  Bound by memory: 16384 x 4096 bfloats with a residual 109 us, 4.9 TB/s.  Kept as they are in memory, dy and h take
+// half the registers of what is made of them: 16384 x 4096 without a residual 80 us, 90 the other way; 3000 x 14233 95 and 130.
 template <class T, bool LOOSE, int THREADS, int E>
 __global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_bwd(BwdArgs a)
 {
@@ -174,34 +179,36 @@ __global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_bwd(BwdArgs a)
     __shared__ float red[THREADS > 64 ? 2 * THREADS / 64 : 1];
     __shared__ float both[RPB > 1 ? 2 * SHARED * E : 1];
     const int t = threadIdx.x % THREADS, sub = threadIdx.x / THREADS;
-    float w[E], dw[E], db[E];
+    typedef typename Chunk<T, LOOSE>::vec vec;
+    constexpr bool KEEP = E < 32;       // the weights, where there is room for them
+    vec w[KEEP ? N : 1];
+    float dw[E], db[E];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
         const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
 #pragma unroll
-        for (int e = 0; e < V; ++e) w[n * V + e] = dw[n * V + e] = db[n * V + e] = 0;
-        if (c.any) c.load(a.w, 0, w + n * V);
+        for (int e = 0; e < V; ++e) dw[n * V + e] = db[n * V + e] = 0;
+        if (KEEP && c.any) w[n] = c.fetch(a.w, 0);
     }
     for (uint64_t row = (uint64_t)blockIdx.x * RPB + sub; row < a.rows; row += (uint64_t)a.groups * RPB) {
         const int64_t r = (int64_t)row;
         const float mean = a.mean[r], rstd = a.rstd[r];
-        float g[E], xh[E], s[2] = {0, 0};
+        vec y[N], h[N];             // as they are in memory: what is made of them takes twice the registers, and is made twice
+        float s[2] = {0, 0};
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const Chunk<T, LOOSE> c((n * THREADS + t) * V, a.cols);
-            float *gn = g + n * V, *xn = xh + n * V;
             if (c.any) {
-                c.load(a.dy, r * a.dys, gn);
-                c.load(a.h, r * a.hs, xn);
+                y[n] = c.fetch(a.dy, r * a.dys);
+                h[n] = c.fetch(a.h, r * a.hs);
+                const vec wn = KEEP ? w[KEEP ? n : 0] : c.fetch(a.w, 0);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float dy = c.owns(e) ? gn[e] : 0.0f;
-                    xn[e] = c.owns(e) ? (xn[e] - mean) * rstd : 0.0f;
-                    gn[e] = dy * w[n * V + e];
-                    dw[n * V + e] += dy * xn[e];
+                    const float dy = c.owns(e) ? (float)y[n][e] : 0.0f, xh = c.owns(e) ? ((float)h[n][e] - mean) * rstd : 0.0f, g = dy * (float)wn[e];
+                    dw[n * V + e] += dy * xh;
                     db[n * V + e] += dy;
-                    s[0] += gn[e];
-                    s[1] += gn[e] * xn[e];
+                    s[0] += g;
+                    s[1] += g * xh;
                 }
             }
         }
@@ -213,8 +220,9 @@ __global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_bwd(BwdArgs a)
             if (c.any) {
                 float d[V], u[V];
                 if (a.dh) c.load(a.dh, r * a.dhs, u);
+                const vec wn = KEEP ? w[KEEP ? n : 0] : c.fetch(a.w, 0);
 #pragma unroll
-                for (int e = 0; e < V; ++e) d[e] = rstd * (g[n * V + e] - mg - xh[n * V + e] * mx) + (a.dh ? u[e] : 0.0f);
+                for (int e = 0; e < V; ++e) d[e] = rstd * ((float)y[n][e] * (float)wn[e] - mg - ((float)h[n][e] - mean) * rstd * mx) + (a.dh ? u[e] : 0.0f);
                 c.store(a.dx, r * a.dxs, d);
             }
         }
@@ -300,8 +308,9 @@ int by_size_fwd(uint32_t cols, F f)
     return f(Row<1024, 64>());
 }
 
-// Backward: five values an element, so few elements a lane (8192 x 8192 elements: 1024 x 8 takes 101 us, 512 x 16 117; 16384 x 2048: 256 x 8 41 us, 64 x 32
-// 49), but for rows of a wave's own, whose sums need no barrier.  Beyond 16384 elements a lane's values no longer fit its registers.
+// Backward: five values an element, three of them of the type, so few elements a lane (8192 x 8192 elements: 1024 x 8 takes 101 us, 512 x 16 117; 16384 x 2048: 256 x 8 41 us,
+// 64 x 32 49), but for rows of a wave's own, whose sums need no barrier.  Beyond 16384 elements the weights are read again for every row (1000 x 30000 bfloats 101 us, kept 211), and a lane's
+// values fit its registers barely (bfloat) or not.
 template <class F>
 int by_size_bwd(uint32_t cols, F f)
 {
