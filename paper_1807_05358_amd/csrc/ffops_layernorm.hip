@@ -170,7 +170,7 @@ __global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_fwd(FwdArgs a)
 
 // Rows are dealt to the groups in turn (block b takes rows b, b + groups, ...; a wave, or less, of its own the rows of its place in
 // the block too), so that a lane keeps its columns and sums the weight's and the bias's gradient in registers.  One read
-// of dy, h (and dh), one write of dx; the partial sums are groups * cols * 8 bytes more, each way.  Bound by memory: 16384 x 4096 bfloats with a residual 109 us, 4.9 TB/s.  Kept as they are in memory, dy and h take
+// of dy, h (and dh), one write of dx; the partial sums are groups * cols * 8 bytes more, each way.  Bound by memory: 16384 x 4096 bfloats with a residual 102 us, 5.3 TB/s.  Kept as they are in memory, dy and h take
 // half the registers of what is made of them: 16384 x 4096 without a residual 80 us, 90 the other way; 3000 x 14233 95 and 130.
 template <class T, bool LOOSE, int THREADS, int E>
 __global__ __launch_bounds__(block_of(THREADS)) void k_layernorm_bwd(BwdArgs a)
