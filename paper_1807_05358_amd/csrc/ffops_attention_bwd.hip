@@ -18,6 +18,12 @@ constexpr int STEP = 64;            // rows (keys) of a tile in LDS
 template <class T>
 constexpr float P_SHIFT = std::is_same<T, F16>::value ? 10.0f : 0.0f;
 
+// half a step of the type, relative to the value, and near zero
+template <class T>
+constexpr float HALF_STEP = std::is_same<T, F16>::value ? 0x1p-11f : 0x1p-8f;
+template <class T>
+constexpr float HALF_LEAST = std::is_same<T, F16>::value ? 0x1p-25f : 0x1p-134f;
+
 __device__ __forceinline__ float unit_below(float m)
 {
     return m > 0 && m < INFINITY ? ldexpf(1.0f, ilogbf(m)) : 1.0f;
@@ -287,12 +293,12 @@ __device__ __forceinline__ void dq_scores(const lds_char* kt, int r, const typen
     interleave<D / 8, 1, 4, 0>();
 }
 
-// What a row's probabilities sum to over the tiles (of which 0 is at lds, 1 behind it), and their products with dp.
+// What a row's probabilities sum to over the tiles (of which 0 is at lds, 1 behind it), and their products with dp and with its size.
 template <class T, int D>
-__device__ __forceinline__ void dq_row_sums(const lds_char* lds, const typename T::vec8* qf, const typename T::vec8* df, float c, float ls, int seen, int seen_most, float& sum_p, float& sum_pdp)
+__device__ __forceinline__ void dq_row_sums(const lds_char* lds, const typename T::vec8* qf, const typename T::vec8* df, float c, float ls, int seen, int seen_most, float& sum_p, float& sum_pdp, float& sum_abs)
 {
     const int half = (threadIdx.x % 64) / 32;
-    sum_p = sum_pdp = 0;
+    sum_p = sum_pdp = sum_abs = 0;
 #pragma unroll 1
     for (int kb = 0; kb < seen_most; kb += 32) {
         f32x16 s, dp;
@@ -305,10 +311,12 @@ __device__ __forceinline__ void dq_row_sums(const lds_char* lds, const typename 
             const float p = exp2_(fmaf(s[r], c, -ls));
             sum_p += sees ? p : 0.0f;
             sum_pdp += sees ? p * dp[r] : 0.0f;
+            sum_abs += sees ? p * fabsf(dp[r]) : 0.0f;
         }
     }
     sum_p += other_half(sum_p);
     sum_pdp += other_half(sum_pdp);
+    sum_abs += other_half(sum_abs);
 }
 
 template <class T, int D, int WAVES>
@@ -372,6 +380,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     row_operand<T, D>(df, query ? a.dout.p + b * a.dout.batch + w.h * a.dout.head + w.i * a.dout.pos : nullptr, a.dim, half);
     const uint64_t at = ((uint64_t)b * a.heads + w.h) * a.q_len + w.i;
     float ls = INFINITY, de = 0, unit = 1.0f, top = 0;
+    float slack = 0;                // how far the rounding of o can take <do, o>
     {
         typename T::vec8 of[D / 16];
         row_operand<T, D>(of, query ? a.o.p + b * a.o.batch + w.h * a.o.head + w.i * a.o.pos : nullptr, a.dim, half);
@@ -380,9 +389,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 de += (float)df[st][e] * (float)of[st][e];
+                slack += fabsf((float)df[st][e]) * fmaf(fabsf((float)of[st][e]), HALF_STEP<T>, HALF_LEAST<T>);
                 top = fmaxf(top, fabsf((float)df[st][e]));
             }
         de += other_half(de);
+        slack += other_half(slack);
     }
     if constexpr (std::is_same<T, F16>::value) {
         top = fmaxf(top, other_half(top));
@@ -412,11 +423,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     // The rounding of o to the type is in <do, o> for all keys of the row alike, and where few keys share the probability it is the largest error of
     // dq and dk (2^-8 and 8 causal keys: 3.5e-3 of dq, without it 2.3e-3; 128 keys: 2.7e-3).  The sum of p dp has no such part.  It takes the scores twice,
     // so it is taken where that costs no load; and only if these keys hold all of the probability, which they do not where o and lse are
-    // of more keys than the call's.
+    // of more keys than the call's.  That the probabilities sum to 1, as far as the rounding of lse lets them, does not say so by itself: values of the other keys may be large
+    // enough for the rest to count.  But then <do, o> differs from the sum by more than the roundings of o, and of the probabilities that made it, explain.
     if (few && t0 < t1) {
-        float sum_p, sum_pdp;
-        dq_row_sums<T, D>(lds, qf, df, a.scale_log2, ls, w.seen, w.seen_most, sum_p, sum_pdp);
-        if (fabsf(sum_p - 1.0f) < 0x1p-10f) de = sum_pdp;
+        float sum_p, sum_pdp, sum_abs;
+        dq_row_sums<T, D>(lds, qf, df, a.scale_log2, ls, w.seen, w.seen_most, sum_p, sum_pdp, sum_abs);
+        if (fabsf(sum_p - 1.0f) < 0x1p-14f * (1.0f + fabsf(ls) * 0x1p-5f) && fabsf(sum_pdp - de) <= fmaf(sum_abs, HALF_STEP<T>, slack)) de = sum_pdp;
     }
     if (w.in && half == 0 && blockIdx.z == 0) a.delta[at] = de, a.lse2[at] = ls - P_SHIFT<T>;
     de /= unit;
