@@ -102,8 +102,8 @@ int ff_op_attention_fwd(const ff_attention_fwd_t* a, void* stream);
  * ds_ij = p_ij (<do_i, v_j> - <do_i, o_i>),  dq_i = scale * sum_j ds_ij k_j,  dk_j = scale * sum_i ds_ij q_i; dk and dv sum
  * over the query heads of a key head.  Gradients beyond the lengths, and of queries that see no key, are 0.
  * o and lse may be of more keys than the call's (a sequence's keys in pieces, the pieces' o and lse joined): dq is then this piece's
- * part of the sum.  p and ds are rounded to the tensors' type before they are multiplied, ds in float16 relative to a power of two near the
- * largest |do| of its row (for dq) or of its key head's rows (for dk). */
+ * part of the sum.  p and ds are rounded to the tensors' type before they are multiplied, in float16 2^10 times p, and ds times a power of two, of
+ * the row for dq and of the key for dk, that keeps all of them in its range. */
 typedef struct {
     uint32_t dtype, batch, heads, kv_heads, q_len, kv_len, head_dim, causal;
     float scale;

@@ -16,7 +16,7 @@ struct AttnArgs {
     float* lse;                     // [batch][heads][q_len]
     float* delta;                   // the same shape: <do_i, o_i>
     float* lse2;                    // the same shape: lse in powers of two, infinite where a query sees nothing
-    float* top;                     // [batch][kv_heads][tops]: the largest |do| of 32 rows, 16-bit floats only
+    float2* top;                    // [batch][kv_heads][tops]: the largest |do| and |do| |o| (as vectors) of 32 rows, 16-bit floats only
     uint32_t tops;
     uint32_t deal;                  // 1: a sequence's blocks go to all dies, see heads_of_block
     const int32_t *q_lengths, *kv_lengths;

@@ -13,8 +13,11 @@ namespace {
 // both are bound by what comes between products, exponentials and conversions, and LDS is busy for a quarter of the time.
 constexpr int STEP = 64;            // rows (keys) of a tile in LDS
 
-// A 16-bit float has too few exponents for probabilities and gradients of small losses: p is kept times 2^10 (it is at most 1),
-// ds relative to the power of two below the largest |do| of its row (dq) or of its heads (dkv).  bfloat has a float's exponents and needs neither.
+// A 16-bit float has too few exponents for probabilities and gradients of small losses: p is kept times 2^10 (it is at most 1), ds relative to a power of two.
+// On the keys' side that is 2^-14 of the one below what bounds the key's |dp - delta|: the largest |do| of its heads (as vectors) times |v|, and the largest |do| |o|.  (Relative to |do|
+// alone, values of 2000 along do gave infinities.)  On the queries' side it is 2^-14 of the one below the row's sum of p |dp|, and |delta|, where the block sees few keys.  Where they are many that sum is not at hand: there it is the one below the largest
+// |do_d| of the row, and if ds has left the type's range with it, which takes values of hundreds that point along do, the block starts again with 2^10 times that for those rows: |dp - delta| is
+// below 2 * 128 * 65504 times twice that power, so ds stays below 2^15 then.  bfloat has a float's exponents and needs none of this.
 template <class T>
 constexpr float P_SHIFT = std::is_same<T, F16>::value ? 10.0f : 0.0f;
 
@@ -24,10 +27,13 @@ constexpr float HALF_STEP = std::is_same<T, F16>::value ? 0x1p-11f : 0x1p-8f;
 template <class T>
 constexpr float HALF_LEAST = std::is_same<T, F16>::value ? 0x1p-25f : 0x1p-134f;
 
-__device__ __forceinline__ float unit_below(float m)
+// the exponent of the power of two below m, which is above the least float; 0 where there is none
+__device__ __forceinline__ int exponent(float m)
 {
-    return m > 0 && m < INFINITY ? ldexpf(1.0f, ilogbf(m)) : 1.0f;
+    return m > 0 && m < INFINITY ? __builtin_amdgcn_frexp_expf(m) - 1 : 0;
 }
+
+constexpr int MORE_EXPONENT = 10;
 
 __device__ __forceinline__ void store_part(float* p, const f32x16& c, int x, int dim, int half, float f)
 {
@@ -180,19 +186,10 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
     const bool own = key < nk;
     const int chunks = a.dim / 8;
     const bool causal = a.causal;
-    float unit = 1.0f;
-    if constexpr (std::is_same<T, F16>::value) {
-        float top = 0;
-        for (uint32_t i = lane; i < a.tops; i += 64) top = fmaxf(top, a.top[(uint64_t)bk * a.tops + i]);
-#pragma unroll
-        for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-        unit = unit_below(top);
-    }
-    // p is 2^P_SHIFT too large in ds, too
-    const float per = exp2_(-P_SHIFT<T>) / unit;
     Keys32<T, D, WAVES> x;
     row_operand<T, D>(x.k, own ? a.k.p + b * a.k.batch + kh * a.k.head + key * a.k.pos : nullptr, a.dim, half);
     row_operand<T, D>(x.v, own ? a.v.p + b * a.v.batch + kh * a.v.head + key * a.v.pos : nullptr, a.dim, half);
+    int unit = 0;                   // exponent, of the lane's key
 #pragma unroll
     for (int d = 0; d < DB; ++d) x.dk[d] = x.dv[d] = f32x16{};
     // tiles of queries that see a key of the block, for each head of the group; a split takes a run of them
@@ -232,6 +229,24 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
             advance();
         }
         queries.load(lds + (Q::STAGES - 1) * Q::STAGE, qp, dp, lp, ep, 0);      // zeros, for the queries before the first
+        if constexpr (std::is_same<T, F16>::value) {
+            float2 top = make_float2(0, 0);
+            for (uint32_t i = lane; i < a.tops; i += 64) {
+                const float2 more = a.top[(uint64_t)bk * a.tops + i];
+                top = make_float2(fmaxf(top.x, more.x), fmaxf(top.y, more.y));
+            }
+#pragma unroll
+            for (int d = 32; d; d >>= 1) top = make_float2(fmaxf(top.x, __shfl_xor(top.x, d)), fmaxf(top.y, __shfl_xor(top.y, d)));
+            float vv = 0;
+#pragma unroll
+            for (int st = 0; st < D / 16; ++st)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) vv += (float)x.v[st][e] * (float)x.v[st][e];
+            vv += other_half(vv);
+            unit = exponent(fmaf(top.x, __builtin_amdgcn_sqrtf(vv), top.y)) - 14;
+        }
+        // p is 2^P_SHIFT too large in ds, too
+        const float per = ldexpf(1.0f, -(int)P_SHIFT<T> - unit);
         meet<0>();
         typedef typename T::vec8 vec8;
         const float c = a.scale_log2;
@@ -255,7 +270,7 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
         x.sums(lds + (now == 0 ? (Q::STAGES - 1) * Q::STAGE : now - Q::STAGE), 32, p1, e1);
     }
     if (key >= (int)a.kv_len) return;
-    const float fk = a.scale * unit, fv = exp2_(-P_SHIFT<T>);
+    const float fk = ldexpf(a.scale, unit), fv = exp2_(-P_SHIFT<T>);
     if (a.splits > 1) {
         const uint64_t n = (uint64_t)a.batch * a.kv_heads * a.kv_len, at = ((uint64_t)bk * a.kv_len + key);
         float *pk = a.part + (2 * (uint64_t)blockIdx.z * n + at) * a.dim, *pv = pk + n * a.dim;
@@ -272,6 +287,21 @@ __global__ __launch_bounds__(WAVES * 64, 1) void k_attention_dkv(AttnArgs a)
         store_row<T>(pk, x.dk[d], d * 32, a.dim, half, fk);
         store_row<T>(pv, x.dv[d], d * 32, a.dim, half, fv);
     }
+}
+
+// whether `x` is true for any lane of the block; uses 4 bytes at lds, which nobody needs
+template <int WAVES>
+__device__ __forceinline__ bool any_of_block(bool x, lds_char* lds)
+{
+    if (WAVES == 1) return __any(x);
+    volatile __attribute__((address_space(3))) int* flag = (volatile __attribute__((address_space(3))) int*)lds;
+    if (threadIdx.x == 0) *flag = 0;
+    __syncthreads();
+    if (x) *flag = 1;
+    __syncthreads();
+    const bool any = *flag;
+    __syncthreads();
+    return any;
 }
 
 struct Next {           // what is loaded while a tile is worked on
@@ -375,39 +405,12 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
     const char* kp = a.k.p + b * a.k.batch + kh * a.k.head;
     const char* vp = a.v.p + b * a.v.batch + kh * a.v.head;
     const bool query = w.in && (int)w.i < w.nq;
-    typename T::vec8 qf[D / 16], df[D / 16];
+    typename T::vec8 qf[D / 16], df[D / 16], of[D / 16];
     row_operand<T, D>(qf, query ? a.q.p + b * a.q.batch + w.h * a.q.head + w.i * a.q.pos : nullptr, a.dim, half);
     row_operand<T, D>(df, query ? a.dout.p + b * a.dout.batch + w.h * a.dout.head + w.i * a.dout.pos : nullptr, a.dim, half);
     const uint64_t at = ((uint64_t)b * a.heads + w.h) * a.q_len + w.i;
-    float ls = INFINITY, de = 0, unit = 1.0f, top = 0;
-    float slack = 0;                // how far the rounding of o can take <do, o>
-    {
-        typename T::vec8 of[D / 16];
-        row_operand<T, D>(of, query ? a.o.p + b * a.o.batch + w.h * a.o.head + w.i * a.o.pos : nullptr, a.dim, half);
-#pragma unroll
-        for (int st = 0; st < D / 16; ++st)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                de += (float)df[st][e] * (float)of[st][e];
-                slack += fabsf((float)df[st][e]) * fmaf(fabsf((float)of[st][e]), HALF_STEP<T>, HALF_LEAST<T>);
-                top = fmaxf(top, fabsf((float)df[st][e]));
-            }
-        de += other_half(de);
-        slack += other_half(slack);
-    }
-    if constexpr (std::is_same<T, F16>::value) {
-        top = fmaxf(top, other_half(top));
-        unit = unit_below(top);
-        // and of the wave's rows, for the keys' side
-        float most = top;
-#pragma unroll
-        for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-        if (lane == 0 && blockIdx.z == 0) a.top[(uint64_t)bk * a.tops + (gridDim.y - 1 - blockIdx.y) * WAVES + wave] = most;
-    }
-    if (query) {
-        const float x = a.lse[at];
-        if (x != -INFINITY) ls = x * LOG2E;
-    }
+    row_operand<T, D>(of, query ? a.o.p + b * a.o.batch + w.h * a.o.head + w.i * a.o.pos : nullptr, a.dim, half);
+    float ls = query ? a.lse[at] : -INFINITY;
     TileLoads<STEP, D, WAVES> kl, vl;
     kl.init(a.k.pos, chunks);
     vl.init(a.v.pos, chunks);
@@ -419,6 +422,33 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
         kl.load(lds + 2 * TILE, kp + (int64_t)STEP * a.k.pos, nk - STEP);
         vl.load(lds + 3 * TILE, vp + (int64_t)STEP * a.v.pos, nk - STEP);
     }
+    ls = ls != -INFINITY ? ls * LOG2E : INFINITY;
+    float de = 0, top = 0, oo = 0;
+    float slack = 0;                // how far the rounding of o can take <do, o>
+    int unit = 0;                   // exponent
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            de += (float)df[st][e] * (float)of[st][e];
+            slack += fabsf((float)df[st][e]) * fabsf((float)of[st][e]);
+            top = fmaxf(top, fabsf((float)df[st][e]));
+            oo += (float)of[st][e] * (float)of[st][e];
+        }
+    de += other_half(de);
+    slack += other_half(slack);
+    top = fmaxf(top, other_half(top));
+    slack = fmaf(slack, HALF_STEP<T>, top * (D * HALF_LEAST<T>));
+    if constexpr (std::is_same<T, F16>::value) {
+        unit = exponent(top);
+        // what bounds the keys' side: the largest of the wave's rows; do as a vector is no longer than sqrt(D) times its largest element
+        oo += other_half(oo);
+        float2 most = make_float2(top * (D == 64 ? 8.0f : 11.32f), 0);
+        most.y = most.x * __builtin_amdgcn_sqrtf(oo);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) most = make_float2(fmaxf(most.x, __shfl_xor(most.x, d)), fmaxf(most.y, __shfl_xor(most.y, d)));
+        if (lane == 0 && blockIdx.z == 0) a.top[(uint64_t)bk * a.tops + (gridDim.y - 1 - blockIdx.y) * WAVES + wave] = most;
+    }
     __syncthreads();
     // The rounding of o to the type is in <do, o> for all keys of the row alike, and where few keys share the probability it is the largest error of
     // dq and dk (2^-8 and 8 causal keys: 3.5e-3 of dq, without it 2.3e-3; 128 keys: 2.7e-3).  The sum of p dp has no such part.  It takes the scores twice,
@@ -429,20 +459,40 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_attention_dq(AttnArgs a)
         float sum_p, sum_pdp, sum_abs;
         dq_row_sums<T, D>(lds, qf, df, a.scale_log2, ls, w.seen, w.seen_most, sum_p, sum_pdp, sum_abs);
         if (fabsf(sum_p - 1.0f) < 0x1p-14f * (1.0f + fabsf(ls) * 0x1p-5f) && fabsf(sum_pdp - de) <= fmaf(sum_abs, HALF_STEP<T>, slack)) de = sum_pdp;
+        if (std::is_same<T, F16>::value) unit = exponent(sum_abs + fabsf(de)) - 14;
     }
     if (w.in && half == 0 && blockIdx.z == 0) a.delta[at] = de, a.lse2[at] = ls - P_SHIFT<T>;
-    de /= unit;
     f32x16 dq[DB];
+#pragma unroll 1
+    for (bool again = false;; again = true) {
 #pragma unroll
-    for (int d = 0; d < DB; ++d) dq[d] = f32x16{};
-    for (int t = t0; t < t1; ++t) {
-        const int now = ((t - t0) & 1) * 2 * TILE, k1 = (t + 1) * STEP;
-        const Next n = {kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, nk - k1, !few && t + 1 < t1};
-        dq_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), n, kl, vl, qf, df, dq, a.scale_log2, ls, de, 1.0f / unit, t * STEP, w.seen, w.seen_least, w.seen_most);
+        for (int d = 0; d < DB; ++d) dq[d] = f32x16{};
+        const float du = ldexpf(de, -unit), per = ldexpf(1.0f, -unit);
+        for (int t = t0; t < t1; ++t) {
+            const int now = ((t - t0) & 1) * 2 * TILE, k1 = (t + 1) * STEP;
+            const Next n = {kp + (int64_t)k1 * a.k.pos, vp + (int64_t)k1 * a.v.pos, nk - k1, !few && t + 1 < t1};
+            dq_step<T, D, WAVES>(lds + now, lds + (2 * TILE - now), n, kl, vl, qf, df, dq, a.scale_log2, ls, du, per, t * STEP, w.seen, w.seen_least, w.seen_most);
+            __syncthreads();
+        }
+        if (!std::is_same<T, F16>::value || few || again) break;
+        float z = 0;                // a NaN where a sum is infinite, or one
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z = fmaf(dq[d][r], 0.0f, z);
+        z += other_half(z);
+        // all waves of a block start again, since they load together
+        const bool left = !(z == 0);
+        if (!any_of_block<WAVES>(left, lds)) break;
+        if (left) unit += MORE_EXPONENT;
+        if (t0 < t1) {
+            kl.load(lds, kp + (int64_t)t0 * STEP * a.k.pos, nk - t0 * STEP);
+            vl.load(lds + TILE, vp + (int64_t)t0 * STEP * a.v.pos, nk - t0 * STEP);
+        }
         __syncthreads();
     }
     if (!w.in) return;
-    const float f = a.scale * unit;
+    const float f = ldexpf(a.scale, unit);
     if (a.splits > 1) {
         float* p = a.part + ((uint64_t)blockIdx.z * a.batch * a.heads * a.q_len + at) * a.dim;
 #pragma unroll
@@ -499,7 +549,7 @@ Plan plan_of(const AttnArgs& a)
     p.lse2 = round_up((uint64_t)a.batch * a.heads * a.q_len * sizeof(float), 256);
     p.top = 2 * p.lse2;
     p.tops = (uint32_t)ceil_div(rows, p.q_waves * 32) * p.q_waves;
-    p.part = p.top + round_up(bk * p.tops * sizeof(float), 256);
+    p.part = p.top + round_up(bk * p.tops * sizeof(float2), 256);
     // one area for the partial sums of both: the kernels run one after another
     const uint64_t kv = p.kv_splits > 1 ? 2ull * p.kv_splits * bk * a.kv_len * a.dim : 0, q = p.q_splits > 1 ? (uint64_t)p.q_splits * bk * rows * a.dim : 0;
     p.bytes = p.part + std::max(kv, q) * sizeof(float);
@@ -570,7 +620,7 @@ extern "C" int ff_op_attention_bwd(const ff_attention_bwd_t* p, void* stream)
     char* ws = (char*)p->workspace;
     a.delta = (float*)ws;
     a.lse2 = (float*)(ws + plan.lse2);
-    a.top = (float*)(ws + plan.top), a.tops = plan.tops;
+    a.top = (float2*)(ws + plan.top), a.tops = plan.tops;
     a.part = (float*)(ws + plan.part);
     return p->dtype == FF_F16 ? run<F16>(a, plan, (hipStream_t)stream) : run<BF16>(a, plan, (hipStream_t)stream);
 }
