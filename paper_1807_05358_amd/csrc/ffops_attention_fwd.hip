@@ -14,6 +14,14 @@ namespace {
 // A single token (8 sequences of up to 16384 keys, 32 heads on 8) is bound by memory: 60 us, 4.5 TB/s; the heads of a group share a wave's rows, so that keys are read once.
 constexpr int KEYS = 64;
 
+// A 16-bit float ends at 2^-24: probabilities of 3e-8 of the largest would be none, and of 1e-5 have few bits, which counts where thousands of such keys make up the output beside one whose
+// value is small (4096 keys 17.5 below a key without a value: o off by 35 %).  They are kept times 2^8, and the maximum moves when it grows by more than 2^7: they then stay below 2^15.
+// Keys of 1e-10 of the largest still count.
+template <class T>
+constexpr float P_SHIFT = std::is_same<T, F16>::value ? 8.0f : 0.0f;
+template <class T>
+constexpr float MAX_BEHIND = std::is_same<T, F16>::value ? 7.0f : 8.0f;
+
 template <class T, int D, int WAVES>
 __device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_char* __restrict next, bool more, const char* kn, const char* vn, int rows_next,
                                           const TileLoads<KEYS, D, WAVES>& kl, const TileLoads<KEYS, D, WAVES>& vl, const typename T::vec8* qf, f32x16* o, float& m, float& l,
@@ -49,8 +57,8 @@ __device__ __forceinline__ void tile_step(const lds_char* __restrict cur, lds_ch
 #pragma unroll
         for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
     top = fmaxf(top, other_half(top)) * c;
-    if (__any(top > m + 8.0f)) {        // m starts at -inf; a row that sees nothing keeps it
-        const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.0f : exp2_(m - mn);
+    if (__any(top > m + (MAX_BEHIND<T> + P_SHIFT<T>))) {        // m, the maximum less the shift, starts at -inf; a row that sees nothing keeps it
+        const float mn = fmaxf(m, top - P_SHIFT<T>), f = mn == -INFINITY ? 1.0f : exp2_(m - mn);
         l *= f;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
