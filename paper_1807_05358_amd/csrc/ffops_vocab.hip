@@ -1,5 +1,6 @@
 // Softmax cross entropy over a vocabulary, forward and backward, from the vectors and the vocabulary's matrix.
 #include "ffops_tiles.h"
+#include "ffops_vocab_tiling.h"
 
 namespace ffops {
 namespace {
@@ -626,29 +627,6 @@ __global__ __launch_bounds__(256) void k_vocab_gather(VocabArgs a, const E* x, i
 
 // ---- host ------------------------------------------------------------------------------
 
-constexpr uint64_t PIECE_BYTES = 256ull << 20;      // gradient of the logits of a piece: what the last-level cache holds
-
-// How a product of m x n over k is cut: the largest tile of which there are enough, k split where that is allowed into no less than 512 of it and into no more than 16,
-// and none much longer than the shorter side.  256 x 256 tiles are half as fast again as others per product once they run, and take 20 us before and after that:
-// dx of 3328 x 28040 x 1096 with 195 blocks of them 208 us, 128 x 128 321 us; dw with k = 207 114 us, 64 x 64 87 us.  128 x 128 read half as
-// much as 64 x 64: 300 x 8000 x 1024 60 us for all, 64 x 64 66 us.
-struct Tiling {
-    uint32_t tile, ms, ns, splits;
-    uint32_t blocks() const { return ms * ns; }
-};
-
-Tiling tiling_of(uint64_t m, uint64_t n, uint64_t k, bool split)
-{
-    Tiling t = {};
-    for (uint32_t tile : {256u, 128u, 64u}) {
-        const uint64_t tiles = ceil_div(m, tile) * ceil_div(n, tile), places = tile == 256 ? 256 : tile == 128 ? 512 : 768;      // one, two and three on a unit, by their LDS
-        const uint64_t splits = split && tiles ? std::max<uint64_t>(1, std::min<uint64_t>({places / tiles, k / 512, 16})) : 1;
-        t = {tile, (uint32_t)ceil_div(m, tile), (uint32_t)ceil_div(n, tile), (uint32_t)splits};
-        if (tile == 64 || (tiles * splits >= (tile == 256 ? 160 : 256) && tile <= round_up(std::min(m, n), 64) && (tile < 256 || k >= 512))) break;
-    }
-    return t;
-}
-
 struct Plan {
     uint32_t dim;               // a multiple of 8
     bool copy_x, copy_w;
@@ -683,8 +661,7 @@ Plan plan_of(const A* p, bool back)
     } else {
         q.live = take(2 * sizeof(uint32_t));
         q.row_of = take((uint64_t)p->rows * sizeof(uint32_t));
-        const uint64_t fit = PIECE_BYTES / 2 / std::max(1u, p->rows) / 256 * 256;
-        q.piece = (uint32_t)std::min<uint64_t>(round_up(p->vocab, 256), std::max<uint64_t>(fit, 256));
+        q.piece = piece_of(p->rows, p->vocab);
         q.g = take((uint64_t)p->rows * q.piece * 2);
         q.dx = tiling_of(q.dim, p->rows, std::min(p->vocab, q.piece), true);
         q.sum = take(q.dx.splits > 1 || q.piece < p->vocab ? (uint64_t)q.dx.splits * p->rows * q.dim * sizeof(float) : 0);
