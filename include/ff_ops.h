@@ -30,8 +30,12 @@ enum { FF_F32 = 0, FF_F16 = 1, FF_BF16 = 2 }; /* types of tensors; layer norm ta
 #define FF_OP_MAX_COLS 65536      /* layer norm: elements of a row */
 #define FF_OP_MAX_HEAD_DIM 128    /* attention: elements of a head, a multiple of 8 */
 #define FF_OP_MAX_LEN (1u << 28)  /* attention: positions of a sequence */
-#define FF_OP_MAX_ROWS (1u << 28) /* layer norm, vocabulary loss: rows; vocabulary loss: words */
+#define FF_OP_MAX_SIDE (65535u * 128) /* attention: queries of a sequence times query heads of a key head; backward: its keys, too */
+#define FF_OP_MAX_ROWS (1u << 28) /* layer norm: rows */
+#define FF_OP_MAX_TOKENS ((1u << 26) - 4) /* vocabulary loss: rows, words */
 #define FF_OP_MAX_DIM 65536       /* vocabulary loss: elements of a token's vector */
+/* and of the vocabulary loss, backward, rows * dim up to 2^34, and products (rows x words, rows x dim, dim x words) of fewer than 2^24 tiles, which are
+ * 256 x 256 in products that large, but 128 x 128 where fewer than 512 is summed over.  attention: heads and batch up to 65535, batch * kv_heads up to 65535 * 32. */
 
 /* rows of a matrix: element (r, c) is p[r * stride + c].  stride counts elements and may be any number that keeps
  * outputs from overlapping themselves (inputs may repeat rows: stride 0). */

@@ -131,9 +131,10 @@ static int check_attention(const P* p)
     if (p->kv_heads == 0 || p->heads == 0 || p->heads % p->kv_heads || p->head_dim == 0 || p->head_dim % 8) return FF_EINVAL;
     if (!(p->scale > 0) || !std::isfinite(p->scale)) return FF_EINVAL;
     if (p->head_dim > FF_OP_MAX_HEAD_DIM || p->q_len > FF_OP_MAX_LEN || p->kv_len > FF_OP_MAX_LEN) return FF_ERANGE;
-    // launch grids: heads of keys of all sequences, and blocks of rows, which 32 bits count
-    if (p->heads > 65535 || p->batch > 65535 || (uint64_t)p->batch * p->kv_heads > 65535u * 32 || (uint64_t)p->q_len * (p->heads / p->kv_heads) > 65535u * 32)
+    // launch grids: heads of keys of all sequences, and blocks of 128 rows
+    if (p->heads > 65535 || p->batch > 65535 || (uint64_t)p->batch * p->kv_heads > 65535u * 32 || (uint64_t)p->q_len * (p->heads / p->kv_heads) > FF_OP_MAX_SIDE)
         return FF_ERANGE;
+    static_assert(FF_OP_MAX_SIDE == MOST_BLOCKS_Y * 128, "as many blocks as a launch takes along y");
     return FF_OK;
 }
 

@@ -523,6 +523,12 @@ __global__ __launch_bounds__(256) void k_attention_add(const float* part, uint32
     *(typename T::vec8*)(o.p + bh / heads * o.batch + bh % heads * o.head + i * o.pos + x * 2) = round8<T>(s);
 }
 
+int check_backward(const ff_attention_bwd_t* p)
+{
+    if (const int rc = check_attention(p)) return rc;
+    return p->kv_len > FF_OP_MAX_SIDE ? FF_ERANGE : FF_OK;         // blocks of 128 keys
+}
+
 uint32_t waves_of(uint64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
 // Work is split over the other axis where the owners alone leave some of the device's 256 compute units without a block: more than half of them by no more than leaves a split four
@@ -601,14 +607,14 @@ using namespace ffops;
 
 extern "C" size_t ff_op_attention_bwd_workspace_bytes(const ff_attention_bwd_t* p)
 {
-    if (!p || check_attention(p) != FF_OK) return 0;
+    if (!p || check_backward(p) != FF_OK) return 0;
     return plan_of(args_of(p)).bytes;
 }
 
 extern "C" int ff_op_attention_bwd(const ff_attention_bwd_t* p, void* stream)
 {
     if (!p) return FF_EINVAL;
-    if (const int rc = check_attention(p)) return rc;
+    if (const int rc = check_backward(p)) return rc;
     if (p->batch == 0 || (p->q_len == 0 && p->kv_len == 0)) return FF_OK;
     if (p->q_len && (!heads_ok(p->q) || !heads_ok(p->o) || !heads_ok(p->dout) || !heads_ok(p->dq) || !p->lse)) return FF_EINVAL;
     if (p->kv_len && (!heads_ok(p->k) || !heads_ok(p->v) || !heads_ok(p->dk) || !heads_ok(p->dv))) return FF_EINVAL;

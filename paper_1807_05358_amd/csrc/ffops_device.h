@@ -136,6 +136,9 @@ static __device__ __forceinline__ float wave_sum(float x)
     return x;
 }
 
+constexpr uint64_t MOST_THREADS = 0xffffffffull;       // of a launch, along x
+constexpr uint32_t MOST_BLOCKS_Y = 65535;              // of a launch, along y
+
 static inline int launched() { return hipGetLastError() == hipSuccess ? FF_OK : FF_EHIP; }
 static inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 static inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }

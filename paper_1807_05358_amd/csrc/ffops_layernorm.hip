@@ -326,14 +326,25 @@ int by_size_bwd(uint32_t cols, F f)
 }
 
 template <class T>
-int fwd(const FwdArgs& a, bool vec, hipStream_t st)
+int fwd(FwdArgs a, bool vec, hipStream_t st)
 {
     return by_size_fwd(a.cols, [&](auto row) {
         constexpr int TH = decltype(row)::threads, E = decltype(row)::elems;
-        const dim3 grid((uint32_t)ceil_div(a.rows, rows_of(TH))), block(block_of(TH));
-        if (vec) k_layernorm_fwd<T, false, TH, E><<<grid, block, 0, st>>>(a);
-        else k_layernorm_fwd<T, true, TH, E><<<grid, block, 0, st>>>(a);
-        return launched();
+        // a launch has fewer than 2^32 threads
+        constexpr uint64_t MOST = MOST_THREADS / block_of(TH) * rows_of(TH);
+        const dim3 block(block_of(TH));
+        for (uint64_t left = a.rows; left; left -= a.rows) {
+            a.rows = std::min(left, MOST);
+            const dim3 grid((uint32_t)ceil_div(a.rows, rows_of(TH)));
+            if (vec) k_layernorm_fwd<T, false, TH, E><<<grid, block, 0, st>>>(a);
+            else k_layernorm_fwd<T, true, TH, E><<<grid, block, 0, st>>>(a);
+            if (const int rc = launched()) return rc;
+            const auto on = [&](auto* p, int64_t stride) { return p ? (decltype(p))((char*)p + (int64_t)a.rows * stride * (int64_t)sizeof(typename T::elem)) : p; };
+            a.x = on(a.x, a.xs), a.res = on(a.res, a.rs), a.h = on(a.h, a.hs), a.y = on(a.y, a.ys);
+            if (a.mean) a.mean += a.rows;
+            if (a.rstd) a.rstd += a.rows;
+        }
+        return (int)FF_OK;
     });
 }
 

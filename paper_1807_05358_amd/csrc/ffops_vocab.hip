@@ -677,14 +677,23 @@ Plan plan_of(const A* p, bool back)
     return q;
 }
 
+// whether the blocks of a product are as many as a launch takes
+bool fits(const Tiling& t) { return (uint64_t)t.ms * t.ns <= MOST_THREADS / 256; }
+
+// the sizes, and the plan for them
 template <class A>
-int check_vocab(const A* p)
+int check_vocab(const A* p, bool back, Plan& q)
 {
     if (p->dtype != FF_F16 && p->dtype != FF_BF16) return FF_EINVAL;
     if (p->vocab == 0 || p->dim == 0) return FF_EINVAL;
-    if (p->rows > FF_OP_MAX_ROWS || p->vocab > FF_OP_MAX_ROWS || p->dim > FF_OP_MAX_DIM) return FF_ERANGE;
-    // tiles of a launch, which 32 bits count
-    if (ceil_div(p->vocab, 64) * ceil_div(p->rows, 64) >= (1ull << 31) || ceil_div(p->vocab, 64) * ceil_div(p->dim, 64) >= (1ull << 31)) return FF_ERANGE;
+    static_assert(FF_OP_MAX_TOKENS == MOST_THREADS / 256 * 4, "a wave per row, four in a block");
+    if (p->rows > FF_OP_MAX_TOKENS || p->vocab > FF_OP_MAX_TOKENS || p->dim > FF_OP_MAX_DIM) return FF_ERANGE;
+    q = plan_of(p, back);
+    if (!back) return fits(q.z) ? FF_OK : FF_ERANGE;
+    // the last piece is no larger than the others, but may be cut into smaller tiles
+    for (const uint32_t words : {std::min(p->vocab, q.piece), (p->vocab - 1) % q.piece + 1})
+        if (!fits(tiling_of(words, p->rows, q.dim, false)) || !fits(tiling_of(q.dim, words, p->rows, true))) return FF_ERANGE;
+    if (!fits(q.dx) || ((q.dx.splits > 1 || q.piece < p->vocab) && (uint64_t)p->rows * q.dim / 4 > MOST_THREADS / 256 * 256)) return FF_ERANGE;
     return FF_OK;
 }
 
@@ -797,34 +806,34 @@ using namespace ffops;
 
 extern "C" size_t ff_op_vocab_loss_fwd_workspace_bytes(const ff_vocab_loss_fwd_t* p)
 {
-    if (!p || check_vocab(p) != FF_OK || p->rows == 0) return 0;
-    return plan_of(p, false).bytes;
+    Plan q;
+    return p && check_vocab(p, false, q) == FF_OK && p->rows ? q.bytes : 0;
 }
 
 extern "C" int ff_op_vocab_loss_fwd(const ff_vocab_loss_fwd_t* p, void* stream)
 {
     if (!p) return FF_EINVAL;
-    if (const int rc = check_vocab(p)) return rc;
+    Plan q;
+    if (const int rc = check_vocab(p, false, q)) return rc;
     if (p->rows == 0) return FF_OK;
     if (!p->x.p || !p->w.p || !p->targets || !p->lse) return FF_EINVAL;
-    const Plan q = plan_of(p, false);
     if (!p->workspace || p->workspace_bytes < q.bytes || !aligned(p->workspace, 256)) return FF_EWORKSPACE;
     return p->dtype == FF_F16 ? fwd<F16>(p, q, (hipStream_t)stream) : fwd<BF16>(p, q, (hipStream_t)stream);
 }
 
 extern "C" size_t ff_op_vocab_loss_bwd_workspace_bytes(const ff_vocab_loss_bwd_t* p)
 {
-    if (!p || check_vocab(p) != FF_OK) return 0;
-    return plan_of(p, true).bytes;
+    Plan q;
+    return p && check_vocab(p, true, q) == FF_OK ? q.bytes : 0;
 }
 
 extern "C" int ff_op_vocab_loss_bwd(const ff_vocab_loss_bwd_t* p, void* stream)
 {
     if (!p) return FF_EINVAL;
-    if (const int rc = check_vocab(p)) return rc;
+    Plan q;
+    if (const int rc = check_vocab(p, true, q)) return rc;
     if (!p->w.p || (p->rows && (!p->x.p || !p->targets || !p->dloss || !p->lse))) return FF_EINVAL;
     if (!p->dx.p && !p->dw.p) return FF_OK;
-    const Plan q = plan_of(p, true);
     if (!p->workspace || p->workspace_bytes < q.bytes || !aligned(p->workspace, 256)) return FF_EWORKSPACE;
     return p->dtype == FF_F16 ? bwd<F16>(p, q, (hipStream_t)stream) : bwd<BF16>(p, q, (hipStream_t)stream);
 }
