@@ -142,8 +142,8 @@ int ff_op_vocab_loss_fwd(const ff_vocab_loss_fwd_t* a, void* stream);
 
 /* Its backward pass:  g_iv = (exp(z_iv - lse_i) - [v = t_i]) * dloss_i,  dx = g w,  dw = g^T x.  dloss is float [rows], finite
  * where the row takes part; what x, dloss and lse hold in the others is not used, and they cost no products.  z is made again, in
- * pieces of the vocabulary; g is rounded to the tensors' type (relative to the largest |dloss|, so that a small dloss loses nothing),
- * sums are held in 32 bits.  Either of dx and dw may have a null pointer. */
+ * pieces of the vocabulary; g is rounded to the tensors' type, in float16 to steps of 2^-39 of the largest |dloss| of all rows and no smaller ones (a loss may be
+ * small, but a row that weighs 2^-k of the largest keeps probabilities from 2^(k-39) on, to 11 bits from 2^(k-29) on); sums are held in 32 bits.  Either of dx and dw may have a null pointer. */
 typedef struct {
     uint32_t dtype, rows, vocab, dim;
     int32_t ignore_index, first_word;

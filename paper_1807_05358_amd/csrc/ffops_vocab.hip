@@ -263,9 +263,9 @@ __device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM
 // token and tile of words, and the target's logit; GRAD true: the gradient of the logits, rounded, into g.
 // g is kept relative to the largest |dloss| and times a power of two.  Where all rows weigh the same, a row's entry for its target is then
 // p - 1, which for a small p rounds to nearly itself; and a 16-bit float's exponents do not hold a probability of 1 / vocabulary times a loss' weight.
-// 2^12 keeps them, and 1 stays below its largest number.  With bfloat 2^40 keeps probabilities that a float's exponents do not hold.
+// 2^15 keeps them, and 1 stays below its largest number: a step of g is 2^-39 of the largest |dloss| at least (rows of smaller weight have no smaller one).  With bfloat 2^40 keeps probabilities that a float's exponents do not hold.
 template <class T>
-constexpr float G_SHIFT = std::is_same<T, F16>::value ? 12.0f : 40.0f;
+constexpr float G_SHIFT = std::is_same<T, F16>::value ? 15.0f : 40.0f;
 
 __device__ __forceinline__ uint32_t live_rows(const VocabArgs& a) { return a.live[0]; }
 __device__ __forceinline__ Mat live_x(const VocabArgs& a, uint32_t rows) { return rows == a.rows && a.x.p ? a.x : a.gathered; }
