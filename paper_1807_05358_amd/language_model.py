@@ -124,12 +124,12 @@ class DeviceMeasure:
 
         b, s, c = shape
         rows, back, op_type = b * s, op_type >= BACKWARD, op_type % BACKWARD
-        if op_type == T_NORM:
+        if op_type == T_NORM:             # the sum before it is an operation of its own in the graph
             x, w, bias = normal(rows, c), normal(c), normal(c)
             if not back:
-                return lambda: O.layernorm_fwd(x, w, bias, residual=x)
-            _, h, mean, rstd = O.layernorm_fwd(x, w, bias, residual=x)
-            return lambda: O.layernorm_bwd(x, h, w, mean, rstd, dh=x)
+                return lambda: O.layernorm_fwd(x, w, bias)
+            _, h, mean, rstd = O.layernorm_fwd(x, w, bias)
+            return lambda: O.layernorm_bwd(x, h, w, mean, rstd)
         if op_type == W.T_ATTN:           # a part smaller than a head takes the time of one
             q, k, v = (normal(b, s, -(-c // self.head_dim), self.head_dim).transpose(1, 2) for _ in range(3))
             if not back:
