@@ -107,13 +107,13 @@ class Decoder:
 
 class DeviceMeasure:
     """measure(op_type, shape) -> ns of one task of a decoder's operation on the current GPU; shape is the task's output, (sample, position,
-    channel), for the loss (sample, position, word).  hidden, head_dim and wide say what the output's size does not.
+    channel), for the loss (sample, position, word).  hidden, head_dim, wide and vocab (words of the embedding's table) say what the output's size does not.
     Tasks follow each other without a pause, so the time of a very small one is that of its launches."""
 
-    def __init__(self, hidden, head_dim, wide=None, dtype=None, repeats=20):
+    def __init__(self, hidden, head_dim, wide=None, dtype=None, repeats=20, vocab=1024):
         import torch
         self.torch = torch
-        self.hidden, self.head_dim, self.wide, self.repeats = hidden, head_dim, 4 * hidden if wide is None else wide, repeats
+        self.hidden, self.head_dim, self.wide, self.repeats, self.vocab = hidden, head_dim, 4 * hidden if wide is None else wide, repeats, vocab
         self.dtype = torch.bfloat16 if dtype is None else dtype
 
     def _task(self, op_type, shape):
@@ -151,12 +151,12 @@ class DeviceMeasure:
                 return lambda: x @ w.t()
             dy = normal(rows, c)
             return lambda: (dy @ w, dy.t() @ x)
-        if op_type == W.T_EMBED:          # from a table of 1024 words
-            table, at = normal(1024, c), torch.randint(0, 1024, (rows,), device="cuda")
+        if op_type == W.T_EMBED:
+            table, at = normal(self.vocab, c), torch.randint(0, self.vocab, (rows,), device="cuda")
             if not back:
                 return lambda: table[at]
-            dx = normal(rows, c)
-            return lambda: torch.zeros_like(table).index_add_(0, at, dx)
+            dx = normal(rows, c)          # as Decoder.step sums it
+            return lambda: torch.zeros_like(table, dtype=torch.float32).index_add_(0, at, dx.float()).to(t)
         if op_type == W.T_ELEM:           # a sum; its backward hands the gradient on, and adds where two meet
             x, y = normal(rows, c), normal(rows, c)
             return lambda: x + y
@@ -238,9 +238,9 @@ def main():
             model.params[name] -= 0.5 * grad
         if i % 10 == 0:
             print(f"step {i}: loss {float(loss):.3f}")
-    machine, hidden, heads, choices = W.Machine(4, 4, elem_bytes=2), 1024, 16, (1, 2, 4, 8, 16)
-    ops, edges, leader, params = graph(batch=16, length=512, hidden=hidden, vocab=32768, layers=4)
-    costs, cache = measured_costs(ops, 16, choices, DeviceMeasure(hidden, hidden // heads))
+    machine, hidden, heads, vocab, choices = W.Machine(4, 4, elem_bytes=2), 1024, 16, 32768, (1, 2, 4, 8, 16)
+    ops, edges, leader, params = graph(batch=16, length=512, hidden=hidden, vocab=vocab, layers=4)
+    costs, cache = measured_costs(ops, 16, choices, DeviceMeasure(hidden, hidden // heads, vocab=vocab))
     print(f"{len(ops)} ops, {cache.misses} task sizes measured on {torch.cuda.get_device_name()}, {cache.hits} taken from them")
     sim = binding.Simulator(ops, edges, machine, costs, params=params, ties=leader)
     found = search.find_strategy(sim, ops, machine, 16, choices, n_chains=64, steps=512)

@@ -29,3 +29,10 @@ def test_a_norms_task_has_no_residual_sum(monkeypatch):
     assert all(residual is None and dh is None for _, residual, dh in asked)
     ops = L.graph(batch=4, length=32, hidden=64, vocab=512, layers=1)[0]
     assert (ops["type"] == W.T_ELEM).sum() == 2
+
+
+def test_the_embeddings_table_has_the_words_of_the_vocabulary():
+    measure = L.DeviceMeasure(64, 32, vocab=5000)
+    grad = measure._task(W.T_EMBED + L.BACKWARD, (2, 8, 16))()
+    assert grad.shape == (5000, 16) and grad.dtype == torch.bfloat16
+    assert measure._task(W.T_EMBED, (2, 8, 16))().shape == (16, 16)
