@@ -6,6 +6,9 @@ no CPU fallback.
 The functions check what they are given (ValueError), allocate their outputs and workspace with torch on the tensors'
 device and put the kernels on its current stream; they do not wait.  Captured into a HIP graph, they use the graph's
 memory.  What a call refuses on the library's side raises binding.FFSimError.
+
+autograd does not see them: gradients are the ..._bwd functions' outputs.  So tensors that require gradients are refused
+where they would be recorded; under torch.no_grad() they are taken.
 """
 from __future__ import annotations
 
@@ -160,6 +163,12 @@ def _check(t, what, shape, dtype, device):
         raise ValueError(f"{what} is on {t.device}, {device} is wanted")
 
 
+def _not_recorded(*ts):
+    for t in ts:
+        if t is not None and t.requires_grad and _torch().is_grad_enabled():
+            raise ValueError("a tensor requires gradients, which autograd would lose here: call this under torch.no_grad(), and the _bwd function for the gradients")
+
+
 def _dense_rows(t):
     """the matrix itself where its rows' elements lie side by side, else a copy"""
     return t if t is None or t.stride(1) == 1 or t.shape[1] <= 1 else t.contiguous()
@@ -203,6 +212,7 @@ def layernorm_fwd(x, weight, bias=None, *, residual=None, eps=1e-5):
     """(y, h, mean, rstd) of rows x [rows, cols] (float32, float16 or bfloat16): h = x + residual (x itself without one),
     y = (h - mean) * rstd * weight + bias.  mean and rstd [rows] are float32."""
     torch = _torch()
+    _not_recorded(x, weight, bias, residual)
     if x.dim() != 2:
         raise ValueError("x is a matrix [rows, cols]")
     dtype, device = _dtype(x, "x", True), x.device
@@ -225,6 +235,7 @@ def layernorm_bwd(dy, h, weight, mean, rstd, *, dh=None):
     """(dx, dweight, dbias) from what layernorm_fwd returned; dh: the gradient that reaches h past the norm.  dx is the
     gradient of x and of residual alike."""
     torch = _torch()
+    _not_recorded(dy, h, weight, mean, rstd, dh)
     if h.dim() != 2:
         raise ValueError("h is a matrix [rows, cols]")
     dtype, device = _dtype(h, "h", True), h.device
@@ -293,6 +304,7 @@ def attention_fwd(q, k, v, *, causal=False, q_lengths=None, kv_lengths=None, sca
     int32 [batch].  With causal the last query sees all keys and those before it one fewer each.  A query that sees no key has
     o = 0 and lse = -inf.  scale: 1 / sqrt(dim) if not given."""
     torch = _torch()
+    _not_recorded(q, k, v)
     sizes, q_lengths, kv_lengths = _attention_args(q, k, v, causal, q_lengths, kv_lengths, scale)
     o = _like_heads(q)
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
@@ -305,6 +317,7 @@ def attention_bwd(dout, q, k, v, o, lse, *, causal=False, q_lengths=None, kv_len
     """(dq, dk, dv) from the gradient of o and what attention_fwd returned for the same arguments.  Where k and v are a piece of the
     keys, o and lse those of all pieces: this piece's dk and dv, and its part of dq."""
     torch = _torch()
+    _not_recorded(dout, q, k, v, o, lse)
     sizes, q_lengths, kv_lengths = _attention_args(q, k, v, causal, q_lengths, kv_lengths, scale)
     _check(dout, "dout", q.shape, q.dtype, q.device)
     _check(o, "o", q.shape, q.dtype, q.device)
@@ -340,6 +353,7 @@ def vocab_loss_fwd(x, weight, targets, *, ignore_index=-100, first_word=None):
     loss is then None; target_logit is 0 where the target is another shard's.  log sum exp of the shards' lse, and the sum of
     their target_logit, make the loss, and vocab_loss_bwd of a shard takes the joined lse."""
     torch = _torch()
+    _not_recorded(x, weight)
     sizes, x, weight, targets = _vocab_args(x, weight, targets, ignore_index, first_word or 0)
     loss, lse, logit = torch.empty((3, x.shape[0]), dtype=torch.float32, device=x.device).unbind()
     if first_word is not None:
@@ -352,6 +366,7 @@ def vocab_loss_bwd(dloss, x, weight, targets, lse, *, ignore_index=-100, first_w
     """(dx, dweight) from the gradient of each row's loss (float32 [rows]) and the forward pass' lse; for a shard of the vocabulary, dx is its share of the sum.
     Rows with ignore_index cost no products: their dx is 0, and what x, dloss and lse hold there is not used."""
     torch = _torch()
+    _not_recorded(dloss, x, weight, lse)
     sizes, xs, ws, targets = _vocab_args(x, weight, targets, ignore_index, first_word or 0)
     _check(dloss, "dloss", targets.shape, torch.float32, x.device)
     _check(lse, "lse", targets.shape, torch.float32, x.device)
