@@ -332,19 +332,29 @@ __global__ __launch_bounds__(256) void k_vocab_logits(VocabArgs a)
         // almost no tile has a lane's target or the last word
         if constexpr (GRAD) {
             // a row that takes no part has exp(-inf)
-            const float ls = live ? a.lse_in[of] * LOG2E - G_SHIFT<T> : INFINITY, f = live ? a.dloss[of] / unit_of(a) : 0;
+            const float lse = live ? a.lse_in[of] : INFINITY, ls = fmaf(lse, LOG2E, -G_SHIFT<T>), f = live ? a.dloss[of] / unit_of(a) : 0;
+            // The target's entry is p - 1, to which the rounding of ls (2^-19 with bfloat) would be what is left of it where p is near 1: it is made from the difference itself.
+            float gt = 0;
+            const bool targets = __any(want >= 0);
+            if (targets) {
+#pragma unroll
+                for (int m = 0; m < P::TM; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) gt = m * 16 + e == want ? c[m][n][e] : gt;
+                gt = (exp2_((gt - lse) * LOG2E) - 1.0f) * (exp2f(G_SHIFT<T>) * f);
+            }
             char* row = a.g + ((uint64_t)token * a.g_stride + v0 + (quarter & 1) * 12) * 2;
 #pragma unroll
             for (int m = 0; m < P::TM; ++m)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) c[m][n][e] = exp2_(fmaf(c[m][n][e], LOG2E, -ls)) * f;
-            if (edge || __any(want >= 0))
+            if (edge || targets)
 #pragma unroll
                 for (int m = 0; m < P::TM; ++m)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int v = m * 16 + e;
-                        if (v == want) c[m][n][e] -= exp2f(G_SHIFT<T>) * f;
+                        if (v == want) c[m][n][e] = gt;
                         if (!live || v0 + v >= a.words) c[m][n][e] = 0;
                     }
             // of two tiles, even quarters take their own and their odd neighbour's words of the first, odd ones of the second: 16 bytes a lane
