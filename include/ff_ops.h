@@ -87,7 +87,8 @@ int ff_op_layernorm_bwd(const ff_layernorm_bwd_t* a, void* stream);
  * kv_lengths[b] keys (int32 [batch] each, values 0 .. q_len / kv_len, others are clamped to that; null: all of them);
  * with `causal`, query i sees the keys j <= i + kv_lengths[b] - q_lengths[b], the last query all of them.  A query that sees no key, and one
  * beyond q_lengths[b], gets o = 0 and lse = -inf.  Keys and values beyond kv_lengths[b] are not read.  A value row that
- * some queries of a block of 64 keys see and others do not has to be finite, as has every query and gradient within the lengths.
+ * some queries of a block of 64 keys see and others do not has to be finite (in the backward pass a key row, too), as has every query and gradient within the
+ * lengths, and every key where head_dim is neither 64 nor 128.  Probabilities below 2^-126 are 0.
  * lse is float [batch][heads][q_len].  scale > 0.  Products are summed in 32 bits; the probabilities are rounded to the
  * tensors' type before they meet the values, in float16 2^8 times what they are of the row's largest. */
 typedef struct {

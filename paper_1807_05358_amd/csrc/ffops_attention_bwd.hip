@@ -9,8 +9,9 @@ namespace {
 //   k_attention_dq   owns 32 rows a wave: s^T = k q^T, dp^T = v do^T, dq^T += k^T ds^T; and delta_i = <do_i, o_i>, which it leaves to
 //   k_attention_dkv  owns 32 keys a wave: s = q k^T, dp = do v^T, dv^T += do^T p, dk^T += q^T ds
 // In both, what the wave owns is the column of every product, so that p and ds are second operands as they lie in the registers; they are rounded to the type because the products
-// take nothing wider.  2 sequences of 4096, 32 heads on 8 of 128, causal: 979 us for both; profiled by themselves dq 424 (matrix units busy 51 % of the time) and dkv 654 (43 %);
-// both are bound by what comes between products, exponentials and conversions, and LDS is busy for a quarter of the time.
+// take nothing wider.  2 sequences of 4096, 32 heads on 8 of 128, causal: 950 to 1000 us for both; profiled by themselves dq 383 (matrix units busy 51 % of the time) and dkv 578 (43 %).
+// Both are bound by the vector instructions between products; LDS is busy for a quarter of the time.  Around 32 products a body of dkv has, masks aside, 80 for p and ds (16 of them exponentials),
+// 32 to 48 copies out of accumulator registers and some 25 for addresses in LDS; dq makes scores, exponentials and sums of 32 keys one after another.
 constexpr int STEP = 64;            // rows (keys) of a tile in LDS
 
 // A 16-bit float has too few exponents for probabilities and gradients of small losses: p is kept times 2^10 (it is at most 1), ds relative to a power of two.

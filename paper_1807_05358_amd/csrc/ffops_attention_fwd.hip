@@ -10,8 +10,9 @@ namespace {
 // probabilities are the second operand of o^T += v^T p^T as they lie.  The running maximum moves only when it grows by more than
 // 2^8: sums then stay within 2^8 of their scale, which costs 32-bit sums nothing and saves most rescalings.  The probabilities are rounded to the type because the products take nothing wider.
 // Two waves on a SIMD, so that one's products run beside the other's exponentials, maxima and conversions, which are what bounds it: 2 sequences of 4096, 32 heads on 8 of
-// 128, causal, 293 us, 939 TFLOP/s, matrix units busy 45 % of the time, LDS 24 %.  One wave with 64 rows, which reads half as much from LDS, takes 352 us.
-// A single token (8 sequences of up to 16384 keys, 32 heads on 8) is bound by memory: 60 us, 4.5 TB/s; the heads of a group share a wave's rows, so that keys are read once.
+// 128, causal, 278 to 292 us, 940 to 990 TFLOP/s, matrix units busy 45 % of the time, LDS 24 %.  One wave with 64 rows, which reads half as much from LDS, takes 352 us.
+// A single token (8 sequences of up to 16384 keys, 51622 together, 32 heads on 8): 58 us for 211 MB of keys and values, 3.65 TB/s; the heads of a group share a wave's rows, so that keys are
+// read once.  Every sequence has as many splits, so that the longest one's blocks run on when the others' have ended.
 constexpr int KEYS = 64;
 
 // A 16-bit float ends at 2^-24: probabilities of 3e-8 of the largest would be none, and of 1e-5 have few bits, which counts where thousands of such keys make up the output beside one whose

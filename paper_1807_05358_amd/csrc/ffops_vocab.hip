@@ -257,8 +257,8 @@ __device__ __forceinline__ void store_tile(lds_char* lds, const f32x4 (&c)[P::TM
     }
 }
 
-// z^T = w x^T: words down, tokens across, so that a lane holds words of one token.  2560 x 32768 x 1024 forward: 149 us with its join, 1154 TFLOP/s, matrix units busy 51 %, the rest
-// the tiles' beginnings and ends around 16 steps of k; 64 x 32768 x 1024: 14 us, w's bytes at 4.8 TB/s.  The gradient of 7782 x 16384 x 2048: 368 us, 1419 TFLOP/s,
+// z^T = w x^T: words down, tokens across, so that a lane holds words of one token.  2560 x 32768 x 1024 forward: 141 to 149 us with its join, 1150 to 1220 TFLOP/s, matrix units busy 51 %, the rest
+// the tiles' beginnings and ends around 16 steps of k; 64 x 32768 x 1024: 14 us, w's bytes at 4.8 TB/s.  The gradient of 7782 x 16384 x 2048: 449 us, 1163 TFLOP/s,
 // with 255 MB of g written.  GRAD false: maximum and sum of exp per
 // token and tile of words, and the target's logit; GRAD true: the gradient of the logits, rounded, into g.
 // g is kept relative to the largest |dloss| and times a power of two.  Where all rows weigh the same, a row's entry for its target is then
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(256) void k_vocab_join(VocabArgs a, float* loss, fl
     if (loss) loss[token] = target == a.ignore ? 0.0f : here ? l - z : NAN;
 }
 
-// dx^T = w^T g^T over the words of a piece: elements down, tokens across.  7782 x 16384 x 2048: 306 us, 1707 TFLOP/s, matrix units busy 67 %.
+// dx^T = w^T g^T over the words of a piece: elements down, tokens across.  7782 x 16384 x 2048: 362 us, 1443 TFLOP/s, matrix units busy 67 %.
 template <class T, int M>
 __global__ __launch_bounds__(256) void k_vocab_dx(VocabArgs a)
 {
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(256) void k_vocab_add(VocabArgs a, uint32_t rows, u
     store_out<T>(a.out + (int64_t)(DX ? a.row_of[row] : row) * a.out_stride, (uint32_t)(at % a.dim), dim, a.out_vec, s[0] * f, s[1] * f, s[2] * f, s[3] * f);
 }
 
-// dw of a piece = g^T x, made transposed over the tokens: elements down, words across.  16384 x 2048 over 7782 rows: 304 us, as dx.
+// dw of a piece = g^T x, made transposed over the tokens: elements down, words across.  16384 x 2048 over 7782 rows: 359 us, as dx.
 template <class T, int M>
 __global__ __launch_bounds__(256) void k_vocab_dw(VocabArgs a, uint32_t dim)
 {
