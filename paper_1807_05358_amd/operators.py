@@ -1,5 +1,5 @@
-"""Training operators of language models on the GPU: layer norm, attention and the loss over a vocabulary, forward and
-backward.  Thin ctypes binding of the C boundary in include/ff_ops.h (same names, argument marshalling only) and, on
+"""Operators of language models on the GPU: for training, layer norm, attention and the loss over a vocabulary, forward and
+backward; for answering, a paged cache of keys and values, attention over it and the choice of the next token.  Thin ctypes binding of the C boundary in include/ff_ops.h (same names, argument marshalling only) and, on
 top of it, functions that take torch tensors: torch is used for device memory and streams, nothing else, and there is
 no CPU fallback.
 
@@ -20,10 +20,12 @@ import struct
 from . import binding
 
 FF_F32, FF_F16, FF_BF16 = 0, 1, 2
+FF_HELD_SAME, FF_HELD_E4M3, FF_HELD_E2M1 = 0, 1, 2
 
 EXPORTS = ["ff_op_layernorm_fwd", "ff_op_layernorm_bwd_workspace_bytes", "ff_op_layernorm_bwd",
            "ff_op_attention_fwd_workspace_bytes", "ff_op_attention_fwd", "ff_op_attention_bwd_workspace_bytes", "ff_op_attention_bwd",
-           "ff_op_vocab_loss_fwd_workspace_bytes", "ff_op_vocab_loss_fwd", "ff_op_vocab_loss_bwd_workspace_bytes", "ff_op_vocab_loss_bwd"]
+           "ff_op_vocab_loss_fwd_workspace_bytes", "ff_op_vocab_loss_fwd", "ff_op_vocab_loss_bwd_workspace_bytes", "ff_op_vocab_loss_bwd",
+           "ff_op_cache_write", "ff_op_cache_read", "ff_op_attention_paged_fwd_workspace_bytes", "ff_op_attention_paged_fwd", "ff_op_sample_workspace_bytes", "ff_op_sample"]
 
 
 class ff_rows_t(C.Structure):
@@ -71,8 +73,32 @@ class ff_vocab_loss_bwd_t(C.Structure):
     _fields_ = _VOCAB + [(n, ff_rows_t) for n in ("x", "w", "dx", "dw")] + [(n, _vp) for n in ("targets", "dloss", "lse")] + _WS
 
 
+class ff_cache_t(C.Structure):
+    _fields_ = [(n, _vp) for n in ("k", "v", "k_scale", "v_scale", "table")] + \
+        [(n, C.c_int64) for n in ("k_stride", "v_stride", "k_scale_stride", "v_scale_stride", "table_stride")] + [(n, _u32) for n in ("pages", "page", "table_pages", "held")]
+
+
+class ff_cache_write_t(C.Structure):
+    _fields_ = [(n, _u32) for n in ("dtype", "batch", "kv_heads", "head_dim", "new_len")] + [("k", ff_heads_t), ("v", ff_heads_t), ("cache", ff_cache_t), ("start", _vp), ("lengths", _vp)]
+
+
+class ff_cache_read_t(C.Structure):
+    _fields_ = [(n, _u32) for n in ("dtype", "batch", "kv_heads", "head_dim", "kv_len")] + [("k", ff_heads_t), ("v", ff_heads_t), ("cache", ff_cache_t), ("lengths", _vp)]
+
+
+class ff_attention_paged_fwd_t(C.Structure):
+    _fields_ = [(n, _u32) for n in ("dtype", "batch", "heads", "kv_heads", "q_len", "head_dim", "causal")] + [("scale", C.c_float), ("q", ff_heads_t), ("o", ff_heads_t), ("cache", ff_cache_t)] + \
+        [(n, _vp) for n in ("lse", "q_lengths", "kv_lengths")] + _WS
+
+
+class ff_sample_t(C.Structure):
+    _fields_ = [(n, _u32) for n in ("dtype", "rows", "vocab")] + [("logits", ff_rows_t)] + [(n, _vp) for n in ("u", "temperatures", "top_ps", "min_ps", "top_ks")] + \
+        [(n, C.c_float) for n in ("temperature", "top_p", "min_p")] + [("top_k", C.c_int32), ("words", _vp), ("logprob", _vp)] + _WS
+
+
 _RECORDS = {"ff_op_layernorm_fwd": ff_layernorm_fwd_t, "ff_op_layernorm_bwd": ff_layernorm_bwd_t, "ff_op_attention_fwd": ff_attention_fwd_t,
-            "ff_op_attention_bwd": ff_attention_bwd_t, "ff_op_vocab_loss_fwd": ff_vocab_loss_fwd_t, "ff_op_vocab_loss_bwd": ff_vocab_loss_bwd_t}
+            "ff_op_attention_bwd": ff_attention_bwd_t, "ff_op_vocab_loss_fwd": ff_vocab_loss_fwd_t, "ff_op_vocab_loss_bwd": ff_vocab_loss_bwd_t,
+            "ff_op_cache_write": ff_cache_write_t, "ff_op_cache_read": ff_cache_read_t, "ff_op_attention_paged_fwd": ff_attention_paged_fwd_t, "ff_op_sample": ff_sample_t}
 _declared = None
 
 
@@ -377,3 +403,171 @@ def vocab_loss_bwd(dloss, x, weight, targets, lse, *, ignore_index=-100, first_w
     _launch("ff_op_vocab_loss_bwd", x.device, *sizes, xs.data_ptr(), xs.stride(0), ws.data_ptr(), ws.stride(0), dx.data_ptr(), D, dw.data_ptr(), D,
             targets.data_ptr(), dloss.data_ptr(), lse.data_ptr())
     return dx, dw
+
+
+def _pages(t, what):
+    """bytes from page to page; the rest of a page lies side by side"""
+    n, h, p, e = t.shape
+    _, sh, sp, se = t.stride()
+    if not (e == 1 or se == 1) or not (p == 1 or sp == e) or not (h == 1 or sh == p * e):
+        raise ValueError(f"{what}: the elements of a page lie side by side; only pages may have room between them")
+    return t.stride(0) * t.element_size() if n > 1 else h * p * e * t.element_size()
+
+
+def _cache_args(k_pages, v_pages, table, k_scales, v_scales, dtype):
+    """(kv_heads, head_dim, values of the cache's record) of a cache for tensors of `dtype`"""
+    torch = _torch()
+    if k_pages.dim() != 4 or table.dim() != 2:
+        raise ValueError("k_pages are [pages, kv_heads, page, elements], the table [batch, entries]")
+    if not k_pages.is_cuda:
+        raise ValueError(f"k_pages is on {k_pages.device}: the operators have no CPU path")
+    device = k_pages.device
+    N, K, P, E = k_pages.shape
+    _check(v_pages, "v_pages", k_pages.shape, k_pages.dtype, device)
+    _check(table, "table", table.shape, torch.int32, device)
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("a row of the table lies side by side")
+    if k_pages.dtype is dtype:
+        held, D, blocks, unit = FF_HELD_SAME, E, 0, 8
+    elif k_pages.dtype is torch.float8_e4m3fn:
+        held, D, blocks, unit = FF_HELD_E4M3, E, 1, 16
+    elif k_pages.dtype is torch.uint8:
+        held, D, blocks, unit = FF_HELD_E2M1, 2 * E, E // 16, 32
+    else:
+        raise ValueError(f"k_pages is {k_pages.dtype}; {dtype}, float8_e4m3fn or uint8 (two 4-bit floats) is wanted")
+    if N == 0 or K == 0:
+        raise ValueError("a cache without pages or heads")
+    if D == 0 or D % unit or D > 128:
+        raise ValueError(f"a head has {D} elements; a multiple of {unit} up to 128 is wanted for {k_pages.dtype}")
+    if P < 16 or P & (P - 1) or P > 32768:
+        raise ValueError(f"a page has {P} positions; a power of two from 16 to 32768 is wanted")
+    scales = [0, 0]
+    if held == FF_HELD_SAME:
+        if k_scales is not None or v_scales is not None:
+            raise ValueError(f"{dtype} is held without scales")
+        k_scales = v_scales = None
+    else:
+        for i, (t, what) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
+            if t is None:
+                raise ValueError(f"{what} are missing: {k_pages.dtype} is held with scales")
+            _check(t, what, (N, K, blocks, P), torch.uint8, device)
+            _, sh, sb, sp = t.stride()
+            if sp != 1 or not (blocks == 1 or sb == P) or not (K == 1 or sh == blocks * P) or (N > 1 and t.stride(0) % 4) or t.data_ptr() % 4:
+                raise ValueError(f"{what}: the scales of a page lie side by side; only pages may have room between them, in steps of 4")
+            scales[i] = t.stride(0) if N > 1 else K * blocks * P
+    strides = [_pages(k_pages, "k_pages"), _pages(v_pages, "v_pages")]
+    for t, n, what in ((k_pages, strides[0], "k_pages"), (v_pages, strides[1], "v_pages")):
+        if n % 16 or t.data_ptr() % 16:
+            raise ValueError(f"{what}: pages begin at multiples of 16 bytes")
+    return K, D, (k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales), _ptr(v_scales), table.data_ptr(), *strides, *scales, table.stride(0), N, P, table.shape[1], held)
+
+
+def cache_write(k, v, k_pages, v_pages, table, start, *, lengths=None, k_scales=None, v_scales=None):
+    """Writes new keys and values k, v [batch, kv_heads, new, dim] (float16 or bfloat16) into a paged cache: position i of sequence b becomes its
+    position start[b] + i, for the first lengths[b] of them (int32 [batch] both; all of them without lengths).
+
+    The cache: k_pages, v_pages [pages, kv_heads, page, dim]; position i of sequence b is in page table[b, i // page] (int32 [batch, entries]) at place
+    i % page.  Pages hold the tensors' type, or float8_e4m3fn with k_scales, v_scales (uint8 [pages, kv_heads, 1, page]: a power of two for
+    each row of dim), or uint8 [pages, kv_heads, page, dim / 2], 4-bit floats, two a byte, with scales [pages, kv_heads, dim / 32, page] for each 32 elements.
+    A scale s stands for 2^(s - 127); 255: the block held a value that was not finite and is read as NaN.  Positions outside the table, and entries that are no page, are not
+    written.  Sequences may share pages, but no two positions of a call the same place."""
+    torch = _torch()
+    _not_recorded(k, v)
+    if k.dim() != 4:
+        raise ValueError("k is [batch, kv_heads, positions, elements]")
+    dtype, device = _dtype(k, "k"), k.device
+    K, D, cache = _cache_args(k_pages, v_pages, table, k_scales, v_scales, k.dtype)
+    _check(k, "k", (table.shape[0], K, k.shape[2], D), k.dtype, k_pages.device)
+    _check(v, "v", k.shape, k.dtype, device)
+    B = k.shape[0]
+    _check(start, "start", (B,), torch.int32, device)
+    if lengths is not None:
+        _check(lengths, "lengths", (B,), torch.int32, device)
+    n, start, lengths = k.shape[2], _vector(start), _vector(lengths)
+    k, v = _dense_heads(k), _dense_heads(v)
+    _launch("ff_op_cache_write", device, dtype, B, K, D, n, *_heads(k, v), *cache, start.data_ptr(), _ptr(lengths))
+
+
+def cache_read(k_pages, v_pages, table, lengths, *, kv_len=None, dtype=None, k_scales=None, v_scales=None):
+    """(k, v) [batch, kv_heads, kv_len, dim] of the first lengths[b] positions (int32 [batch]) of each sequence of a paged cache (see cache_write), zeros behind them.
+    kv_len: the positions of the table if not given; dtype: float16 or bfloat16, the pages' own if they hold one of these.  A position whose entry is no page gives NaN."""
+    torch = _torch()
+    if dtype is None and k_pages.dtype in (torch.float16, torch.bfloat16):
+        dtype = k_pages.dtype
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("dtype is float16 or bfloat16")
+    K, D, cache = _cache_args(k_pages, v_pages, table, k_scales, v_scales, dtype)
+    B, device = table.shape[0], k_pages.device
+    _check(lengths, "lengths", (B,), torch.int32, device)
+    kv_len = table.shape[1] * k_pages.shape[2] if kv_len is None else kv_len
+    if kv_len < 0:
+        raise ValueError("kv_len is a number of positions")
+    lengths = _vector(lengths)
+    k, v = torch.empty((2, B, K, kv_len, D), dtype=dtype, device=device).unbind()
+    _launch("ff_op_cache_read", device, FF_F16 if dtype is torch.float16 else FF_BF16, B, K, D, kv_len, *_heads(k, v), *cache, lengths.data_ptr())
+    return k, v
+
+
+def attention_paged_fwd(q, k_pages, v_pages, table, kv_lengths, *, causal=False, q_lengths=None, scale=None, k_scales=None, v_scales=None):
+    """(o, lse) of new queries q [batch, heads, q_len, dim] (float16 or bfloat16) over the first kv_lengths[b] positions (int32 [batch]) of a paged cache (see cache_write), their own among
+    them; otherwise as attention_fwd: with causal the last query sees all positions and those before it one fewer each, q_lengths are int32 [batch], a query that sees nothing has o = 0 and
+    lse = -inf.  A query that sees a position whose entry is no page gets NaN.  Keys and values are read once for a few queries of each head (16 queries times heads of a key head are worked together, 32 where there are more), so
+    long prompts are better read back with cache_read for attention_fwd."""
+    torch = _torch()
+    _not_recorded(q)
+    if q.dim() != 4:
+        raise ValueError("q is [batch, heads, positions, elements]")
+    dtype, device = _dtype(q, "q"), q.device
+    K, D, cache = _cache_args(k_pages, v_pages, table, k_scales, v_scales, q.dtype)
+    B, H, n, _ = q.shape
+    _check(q, "q", (table.shape[0], H, n, D), q.dtype, k_pages.device)
+    if H == 0 or H % K:
+        raise ValueError(f"{H} query heads do not share {K} key heads evenly")
+    _check(kv_lengths, "kv_lengths", (B,), torch.int32, device)
+    if q_lengths is not None:
+        _check(q_lengths, "q_lengths", (B,), torch.int32, device)
+    scale = 1 / math.sqrt(D) if scale is None else float(scale)
+    if not (scale > 0 and math.isfinite(scale)):
+        raise ValueError("scale is a positive number")
+    o, lse = _like_heads(q), torch.empty((B, H, n), dtype=torch.float32, device=device)
+    q, q_lengths, kv_lengths = _dense_heads(q), _vector(q_lengths), _vector(kv_lengths)
+    _launch("ff_op_attention_paged_fwd", device, dtype, B, H, K, n, D, 1 if causal else 0, scale, *_heads(q, o), *cache, lse.data_ptr(), _ptr(q_lengths), kv_lengths.data_ptr())
+    return o, lse
+
+
+def sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(words, logprob), int32 and float32 [rows]: a word for each row of logits [rows, vocab] (float32, float16 or bfloat16), chosen by the given random number u[row] in [0, 1) (float32 [rows]).
+
+    Words are taken in the order of their logits, equal ones in the order of their numbers, and weigh exp((z - max z) / temperature), in 64 bits.  The first top_k are
+    kept (0: all), of these the shortest beginning that has top_p of their weight, of these the words that weigh at least min_p (the first weighs 1); the word is the first at which the running
+    sum exceeds u times the weight of all that are kept.  logprob: the logarithm of its share of that.  At temperature 0 it is the first word, with
+    logprob 0.  Each parameter is a number, or a tensor with one for each row (float32, top_k int32).  Rows that hold a NaN or only -inf, or
+    whose temperature is below 0 or another parameter no number, give word -1 and logprob NaN."""
+    torch = _torch()
+    _not_recorded(logits)
+    if logits.dim() != 2:
+        raise ValueError("logits are a matrix [rows, vocab]")
+    dtype, device = _dtype(logits, "logits", True), logits.device
+    R, V = logits.shape
+    if V == 0:
+        raise ValueError("an empty vocabulary")
+    _check(u, "u", (R,), torch.float32, device)
+    numbers, vectors = [], []
+    for x, what, to, kind in ((temperature, "temperature", torch.float32, float), (top_p, "top_p", torch.float32, float), (min_p, "min_p", torch.float32, float), (top_k, "top_k", torch.int32, int)):
+        if isinstance(x, torch.Tensor):
+            _not_recorded(x)
+            _check(x, what, (R,), to, device)
+            vectors.append(_vector(x))
+            numbers.append(kind())
+        else:
+            vectors.append(None)
+            numbers.append(kind(x))
+    if not -2 ** 31 <= numbers[3] < 2 ** 31:
+        raise ValueError("top_k does not fit 32 bits")
+    for n, what, least in zip(numbers, ("temperature", "top_p", "min_p"), (0.0, -math.inf, -math.inf)):
+        if not n >= least or not abs(n) <= 3e38:
+            raise ValueError(f"{what} is {n}")
+    logits, u = _dense_rows(logits), _vector(u)
+    words, logprob = torch.empty(R, dtype=torch.int32, device=device), torch.empty(R, dtype=torch.float32, device=device)
+    _launch("ff_op_sample", device, dtype, R, V, logits.data_ptr(), logits.stride(0), u.data_ptr(), *(_ptr(t) for t in vectors), *numbers, words.data_ptr(), logprob.data_ptr())
+    return words, logprob

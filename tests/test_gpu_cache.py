@@ -1,0 +1,219 @@
+"""A paged cache as it is written and read back, against plain definitions, value for value: there is one right code for every value."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import answering_reference as R  # noqa: E402
+from paper_1807_05358_amd import operators as O  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def empty_cache(pages, kv_heads, page, dim, held, t, fill=None):
+    """(k_pages, v_pages, scales by name), filled with bytes that were there before"""
+    def some(*shape, dtype):
+        n = torch.empty(0, dtype=dtype).element_size()
+        x = torch.randint(0, 120, (math.prod(shape) * n,), dtype=torch.uint8, device="cuda") if fill is None else torch.full((math.prod(shape) * n,), fill, dtype=torch.uint8, device="cuda")
+        return x.view(dtype).view(*shape)
+    if held == "same":
+        return some(pages, kv_heads, page, dim, dtype=t), some(pages, kv_heads, page, dim, dtype=t), {}
+    rows = (dim, torch.float8_e4m3fn, 1) if held == "e4m3" else (dim // 2, torch.uint8, dim // 32)
+    k, v = (some(pages, kv_heads, page, rows[0], dtype=rows[1]) for _ in range(2))
+    return k, v, {n: some(pages, kv_heads, rows[2], page, dtype=torch.uint8) for n in ("k_scales", "v_scales")}
+
+
+def as_bytes(t):
+    return t.view(torch.uint8).clone() if t.dtype != torch.uint8 else t.clone()
+
+
+def expected(before, x, tab, start, lengths, scales_before, held):
+    """the pages' (and scales') bytes after writing x [batch, kv_heads, new, dim]"""
+    pages, scales = as_bytes(before), None if scales_before is None else scales_before.clone()
+    N, P = before.shape[0], before.shape[2]
+    if held != "same":
+        codes, powers = R.hold(x, held)
+        rows = codes if held == "e4m3" else codes[..., 0::2] + 16 * codes[..., 1::2]
+    else:
+        rows = x.contiguous().view(torch.uint8)
+    for b in range(x.shape[0]):
+        for i in range(x.shape[2] if lengths is None else min(max(int(lengths[b]), 0), x.shape[2])):
+            at = int(start[b]) + i
+            if at < 0 or at // P >= tab.shape[1] or not 0 <= int(tab[b, at // P]) < N:
+                continue
+            pages[int(tab[b, at // P]), :, at % P] = rows[b, :, i].to(torch.uint8)
+            if scales is not None:
+                scales[int(tab[b, at // P]), :, :, at % P] = powers[b, :, i].to(torch.uint8)
+    return pages, scales
+
+
+def tables(batch, entries, pages, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randperm(pages, generator=g)[:batch * entries].view(batch, entries).int().cuda()
+
+
+WRITES = [  # held, type, batch, kv_heads, new, dim, page
+    ("same", "bf16", 3, 2, 1, 128, 16), ("same", "f16", 2, 3, 37, 72, 16), ("same", "bf16", 1, 1, 1, 8, 64), ("e4m3", "bf16", 2, 4, 33, 128, 32), ("e4m3", "f16", 3, 1, 5, 80, 16),
+    ("e4m3", "bf16", 1, 2, 50, 16, 16), ("e2m1", "bf16", 2, 2, 21, 128, 16), ("e2m1", "f16", 3, 3, 40, 96, 64), ("e2m1", "bf16", 2, 5, 1, 32, 16), ("e2m1", "f16", 1, 1, 70, 64, 32)]
+
+
+@pytest.mark.parametrize("held,t,B,K,n,D,P", WRITES)
+@pytest.mark.parametrize("layout", ["bshd", "bhsd"])
+def test_written_bytes(held, t, B, K, n, D, P, layout):
+    torch.manual_seed(n * D)
+    t = TYPES[t]
+    entries = -(-(n + 40) // P)
+    k_pages, v_pages, scales = empty_cache(B * entries + 3, K, P, D, held, t)
+    tab = tables(B, entries, B * entries + 3, n)
+    # values of very different sizes, halves of steps among them
+    shape = (B, n, K, D) if layout == "bshd" else (B, K, n, D)
+    k, v = ((torch.randn(*shape, device="cuda") * 2.0 ** torch.randint(-8, 8, (*shape[:-1], 1), device="cuda")).to(t) for _ in range(2))
+    if layout == "bshd":
+        k, v = k.transpose(1, 2), v.transpose(1, 2)
+    start = torch.randint(0, 40, (B,), device="cuda", dtype=torch.int32)
+    lengths = None if n == 1 else torch.randint(0, n + 1, (B,), device="cuda", dtype=torch.int32)
+    want = [expected(p, x, tab, start, lengths, scales.get(s), held) for p, x, s in ((k_pages, k, "k_scales"), (v_pages, v, "v_scales"))]
+    O.cache_write(k, v, k_pages, v_pages, tab, start, lengths=lengths, **scales)
+    for p, s, (bytes_, powers) in zip((k_pages, v_pages), ("k_scales", "v_scales"), want):
+        assert torch.equal(as_bytes(p), bytes_)
+        if held != "same":
+            assert torch.equal(scales[s], powers)
+
+
+@pytest.mark.parametrize("held", ["e4m3", "e2m1"])
+@pytest.mark.parametrize("t", ["f16", "bf16"])
+def test_every_kind_of_value_is_held(held, t):
+    """all bit patterns of the type that are finite, rows of zeros, the largest and smallest values, ties; and blocks with a NaN or an infinity"""
+    t = TYPES[t]
+    D, P = 64, 16
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(t).cuda()
+    x = x[torch.isfinite(x)]
+    rows = [x[: len(x) // D * D].view(-1, D)]
+    torch.manual_seed(1)
+    rows.append(rows[0].flatten()[torch.randperm(rows[0].numel(), device="cuda")].view(-1, D))
+    rows.append(torch.zeros(3, D, device="cuda", dtype=t))
+    near = (torch.randint(-900, 900, (200, D), device="cuda") / 2.0).to(t)         # ties of e4m3's and e2m1's steps
+    rows += [near, near * 2.0 ** -9, (near / 64).round() / 4]
+    odd = torch.randn(6, D, device="cuda").to(t)
+    odd[0, 3], odd[1, 40], odd[2, 63], odd[3, 0] = math.nan, math.inf, -math.inf, torch.finfo(t).max
+    odd[5, 32:] = -0.0
+    x = torch.cat(rows + [odd]).to(t)
+    n = x.shape[0]
+    entries = -(-n // P)
+    k_pages, v_pages, scales = empty_cache(entries, 1, P, D, held, t)
+    tab, start = tables(1, entries, entries, 3), torch.zeros(1, dtype=torch.int32, device="cuda")
+    O.cache_write(x.view(1, 1, n, D), -x.view(1, 1, n, D), k_pages, v_pages, tab, start, **scales)
+    k, v = O.cache_read(k_pages, v_pages, tab, torch.tensor([n], dtype=torch.int32, device="cuda"), kv_len=n, dtype=t, **scales)
+    for got, src, pages, s in ((k, x, k_pages, "k_scales"), (v, -x, v_pages, "v_scales")):
+        codes, powers = R.hold(src, held)
+        want = R.stands_for(codes, powers, held, t)
+        g = got[0, 0].double()
+        assert torch.equal(torch.isnan(g), torch.isnan(want)) and torch.equal(g.nan_to_num(7), want.nan_to_num(7))
+        assert bool(torch.isfinite(want[:-6]).all())                        # the largest values do not become infinite
+        at = tab[0].long()[torch.arange(n, device="cuda") // P], torch.arange(n, device="cuda") % P
+        assert torch.equal(R.codes_of(pages)[at[0], 0, at[1]], codes) and torch.equal(scales[s][at[0], 0, :, at[1]].long(), powers)
+
+
+@pytest.mark.parametrize("held,t,B,K,n,D,P", WRITES)
+def test_read_back(held, t, B, K, n, D, P):
+    """lengths from none to all and beyond, NaN behind them, entries beyond them that are no pages; bytes of any kind in the pages"""
+    torch.manual_seed(n + D)
+    t = TYPES[t]
+    entries = -(-n // P)
+    k_pages, v_pages, scales = empty_cache(B * entries, K, P, D, held, t)
+    tab = tables(B, entries, B * entries, n)
+    lengths = torch.tensor([n, 0, max(0, n - 1)][:B], dtype=torch.int32, device="cuda")
+    for b in range(B):
+        tab[b, -(-int(lengths[b]) // P):] = -1
+    for kv_len in (n, entries * P, n + 3 * P):
+        k, v = O.cache_read(k_pages, v_pages, tab, lengths, kv_len=kv_len, dtype=t, **scales)
+        for got, p, s in ((k, k_pages, "k_scales"), (v, v_pages, "v_scales")):
+            want = R.dense(p, scales.get(s), tab, lengths, kv_len, t)
+            assert got.dtype == t and torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.double().nan_to_num(7), want.nan_to_num(7))
+    if held == "same":
+        assert torch.equal(O.cache_read(k_pages, v_pages, tab, lengths)[0], O.cache_read(k_pages, v_pages, tab, lengths, kv_len=entries * P, dtype=t)[0])
+
+
+def test_what_is_no_page_is_not_followed():
+    """entries below 0 and beyond the pages, positions below 0 and beyond the table, lengths beyond the call: nothing else is written, reading gives NaN"""
+    D, P, t = 64, 16, torch.bfloat16
+    for held in ("same", "e4m3", "e2m1"):
+        k_pages, v_pages, scales = empty_cache(4, 2, P, D, held, t)
+        tab = torch.tensor([[0, -1, 1], [2, 4, 2 ** 31 - 1], [-2 ** 31, 3, 7]], dtype=torch.int32, device="cuda")
+        start = torch.tensor([-5, 10, 30], dtype=torch.int32, device="cuda")
+        lengths = torch.tensor([60, 2 ** 31 - 1, 33], dtype=torch.int32, device="cuda")
+        k, v = (torch.randn(3, 2, 60, D, device="cuda").to(t) for _ in range(2))
+        want = [expected(p, x, tab, start, lengths, scales.get(s), held) for p, x, s in ((k_pages, k, "k_scales"), (v_pages, v, "v_scales"))]
+        O.cache_write(k, v, k_pages, v_pages, tab, start, lengths=lengths, **scales)
+        for p, (bytes_, _) in zip((k_pages, v_pages), want):
+            assert torch.equal(as_bytes(p), bytes_)
+        got = O.cache_read(k_pages, v_pages, tab, torch.tensor([48, 48, -3], dtype=torch.int32, device="cuda"), dtype=t, **scales)[0]
+        where = torch.isnan(got).all(3).all(1)
+        assert bool(where[0, 16:32].all()) and bool(where[1, 16:].all()) and not bool(where[0, :16].any()) and not bool(where[0, 32:].any()) and not bool(where[2].any())
+        assert int((got[2] != 0).sum()) == 0
+    # lengths below 0: nothing
+    before = as_bytes(k_pages)
+    O.cache_write(k, v, k_pages, v_pages, tab, start, lengths=torch.tensor([-1, 0, -2 ** 31], dtype=torch.int32, device="cuda"), **scales)
+    assert torch.equal(as_bytes(k_pages), before)
+
+
+def test_pages_with_room_between_them_and_strided_inputs():
+    """a layer's pages out of all layers' pool, new keys out of one product's output, a table out of a wider one, starts and lengths out of a wider tensor"""
+    D, P, B, K, n, t = 64, 16, 3, 2, 9, torch.float16
+    for held in ("same", "e4m3", "e2m1"):
+        shape, dt, blocks = {"same": (D, t, 1), "e4m3": (D, torch.float8_e4m3fn, 1), "e2m1": (D // 2, torch.uint8, D // 32)}[held]
+        pool = torch.zeros(7, 3, 2, K, P, shape, device="cuda").to(dt) if held != "same" else torch.zeros(7, 3, 2, K, P, shape, device="cuda", dtype=dt)
+        k_pages, v_pages = pool[:, 1, 0], pool[:, 1, 1]
+        scales = {}
+        if held != "same":
+            all_scales = torch.zeros(7, 3, 2, K, blocks, P, dtype=torch.uint8, device="cuda")
+            scales = {"k_scales": all_scales[:, 1, 0], "v_scales": all_scales[:, 1, 1]}
+        tab = tables(B, 6, 18, 3).remainder(7)[:, ::1]
+        wide = torch.randperm(7)[:6].view(3, 2).int().cuda()
+        tab = torch.cat([wide, tab], 1)[:, :2]
+        qkv = torch.randn(B, n, 3, K, D + 3, device="cuda").to(t)[..., :D]                    # copied: rows are no multiples of 16 bytes apart
+        k, v = qkv[:, :, 1].transpose(1, 2), qkv[:, :, 2].transpose(1, 2)
+        pair = torch.tensor([[3, 0], [7, 0], [20, 0]], dtype=torch.int32, device="cuda")[:, 0]
+        want = [expected(p.contiguous(), x, tab, pair, None, None if not scales else scales[s].contiguous(), held) for p, x, s in ((k_pages, k, "k_scales"), (v_pages, v, "v_scales"))]
+        O.cache_write(k, v, k_pages, v_pages, tab, pair, **scales)
+        assert torch.equal(as_bytes(k_pages.contiguous()), want[0][0]) and torch.equal(as_bytes(v_pages.contiguous()), want[1][0])
+        others = pool.view(torch.uint8) if held != "e2m1" else pool
+        assert int(others[:, 0].count_nonzero()) == 0 and int(others[:, 2].count_nonzero()) == 0
+        got = O.cache_read(k_pages, v_pages, tab, torch.full((B,), 29, dtype=torch.int32, device="cuda"), dtype=t, **scales)
+        for g, p, s in zip(got, (k_pages, v_pages), ("k_scales", "v_scales")):
+            assert torch.equal(g.double(), R.dense(p.contiguous(), None if not scales else scales[s].contiguous(), tab, torch.full((B,), 29), 32, t))
+
+
+def test_offsets_beyond_32_bits():
+    """pages that lie more than 4 GiB behind the first"""
+    D, P, K, t = 128, 256, 16, torch.bfloat16
+    N = 4400                        # 1 MiB each
+    k_pages = torch.empty(N, K, P, D, dtype=t, device="cuda")
+    v_pages = torch.empty_like(k_pages)
+    tab = torch.tensor([[N - 1, 0], [2, N - 2]], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(2, K, 300, D, device="cuda").to(t) for _ in range(2))
+    O.cache_write(k, v, k_pages, v_pages, tab, torch.zeros(2, dtype=torch.int32, device="cuda"))
+    assert torch.equal(k_pages[N - 1], k[0, :, :256]) and torch.equal(v_pages[N - 2][:, :44], v[1, :, 256:])
+    got = O.cache_read(k_pages, v_pages, tab, torch.tensor([300, 299], dtype=torch.int32, device="cuda"), kv_len=300)
+    assert torch.equal(got[0][0], k[0]) and torch.equal(got[1][1, :, :299], v[1, :, :299]) and int(got[1][1, :, 299].count_nonzero()) == 0
+    q = torch.randn(2, K, 1, D, device="cuda").to(t)
+    lengths = torch.tensor([300, 299], dtype=torch.int32, device="cuda")
+    o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, lengths)
+    want = R.attention(q, k.double(), v.double(), lengths)
+    assert bool(((o.double() - want[0]).abs() <= want[1]).all()) and bool(((lse.double() - want[2]).abs() <= want[3]).all())
+
+
+def test_another_stream():
+    D, P, t = 64, 16, torch.bfloat16
+    k_pages, v_pages, _ = empty_cache(8, 2, P, D, "same", t)
+    tab, zero = tables(2, 4, 8, 1), torch.zeros(2, dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(2, 2, 64, D, device="cuda").to(t) for _ in range(2))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        O.cache_write(k, v, k_pages, v_pages, tab, zero)
+        a, b = O.cache_read(k_pages, v_pages, tab, zero + 64)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(a, k) and torch.equal(b, v)
