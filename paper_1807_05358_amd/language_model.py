@@ -1,15 +1,16 @@
 """A small language model on the training operators, and what they are for here: exeTimes measured on the device.
 
-Three things, each in a few lines of its own:
+Four things, each in a few lines of its own:
 
 * Decoder: a pre-norm decoder whose training step is written out, forward and backward, with layer norm, attention and the
   loss over the vocabulary from `operators` (plain matrix products are torch's);
+* Decoder.extend / generate: what it answers, token by token, from a paged Cache of what it has read, with the operators for that;
 * DeviceMeasure: the measurement that costcache.ExeTimeCache asks for (Section 5.1, task properties: a task's exeTime is
   taken from running the operation once at the task's output size), for the operations of such a model;
 * graph / measured_costs: the model's training iteration as an operator graph with costs so measured, for Simulator and
   find_strategy.
 
-  python -m paper_1807_05358_amd.language_model      trains a little, measures, and searches a strategy for 16 devices
+  python -m paper_1807_05358_amd.language_model      trains a little, answers, measures, and searches a strategy for 16 devices
 """
 from __future__ import annotations
 
@@ -103,6 +104,74 @@ class Decoder:
             dh = norm_bwd(name, dy, h, stat, dh)
         grads["embedding"] = torch.zeros_like(p["embedding"], dtype=torch.float32).index_add_(0, flat, dh.float()).to(dh.dtype)
         return (loss * weight).sum(), grads
+
+
+    def extend(self, cache, tokens, lengths=None):
+        """logits [batch, vocab], float32, behind the last of the new tokens [batch, length] of each sequence (the first lengths[b] of them, int32 [batch]; at least one); the
+        cache then holds them, too.  What follows them is padding, any word."""
+        import torch
+        p, H = self.params, self.heads
+        B, S = tokens.shape
+        if S == 0 or cache.filled + S > cache.positions:
+            raise ValueError(f"{S} new tokens behind up to {cache.filled} do not fit a cache of {cache.positions} positions")
+        D = self.hidden
+        new = torch.full_like(cache.lengths, S) if lengths is None else lengths
+        start, total = cache.lengths, cache.lengths + new
+        cache.filled += S
+        h, add = p["embedding"][tokens.reshape(-1).long()], None
+        for n in range(self.layers):
+            x, res = (h, None) if add is None else (add, h)
+            y, h, *_ = O.layernorm_fwd(x, p[f"{n}.a.w"], p[f"{n}.a.b"], residual=res)
+            q, k, v = (y @ p[f"{n}.qkv"].t()).view(B, S, 3, H, D // H).permute(2, 0, 3, 1, 4).unbind()
+            pages, scales = cache.layer(n)
+            O.cache_write(k, v, *pages, cache.table, start, lengths=new, **scales)
+            if S <= cache.FEW:
+                o, _ = O.attention_paged_fwd(q, *pages, cache.table, total, causal=True, q_lengths=new, **scales)
+            else:                         # many queries share a tile of keys in the contiguous kernel
+                k, v = O.cache_read(*pages, cache.table, total, kv_len=cache.filled, dtype=q.dtype, **scales)
+                o, _ = O.attention_fwd(q, k, v, causal=True, q_lengths=new, kv_lengths=total)
+            add = o.transpose(1, 2).reshape(B * S, D) @ p[f"{n}.out"].t()
+            y, h, *_ = O.layernorm_fwd(add, p[f"{n}.b.w"], p[f"{n}.b.b"], residual=h)
+            add = torch.relu(y @ p[f"{n}.up"].t()) @ p[f"{n}.down"].t()
+        cache.lengths = total
+        last = torch.arange(B, device=h.device) * S + (new.long() - 1).clamp_min(0)
+        y = O.layernorm_fwd(add[last], p["last.w"], p["last.b"], residual=h[last])[0]
+        return (y @ p["words"].t()).float()
+
+    def generate(self, cache, tokens, u, lengths=None, **choice):
+        """(words, logprob) [batch, new] chosen one after the other behind tokens [batch, length] (lengths as in extend): u [batch, new] are the random numbers, `choice` the
+        parameters of operators.sample.  The cache holds all but the last of them."""
+        import torch
+        words, logprob = [], []
+        for i in range(u.shape[1]):
+            word, log = O.sample(self.extend(cache, tokens, lengths), u[:, i], **choice)
+            words.append(word)
+            logprob.append(log)
+            tokens, lengths = word[:, None], None
+        return torch.stack(words, 1), torch.stack(logprob, 1)
+
+
+class Cache:
+    """keys and values of up to `positions` tokens of each sequence, for every layer of a Decoder, in pages; held: None (the model's type), "e4m3" or "e2m1".
+    lengths: int32 [batch], what each sequence has; filled: no sequence has more."""
+    FEW = 8                               # new tokens that are worked straight from the pages
+
+    def __init__(self, model, batch, positions, held=None, page=64, device="cuda"):
+        import torch
+        if held not in (None, "e4m3", "e2m1"):
+            raise ValueError("held is None, 'e4m3' or 'e2m1'")
+        dim, t = model.hidden // model.heads, model.params["words"].dtype
+        entries = -(-positions // page)
+        self.positions, self.filled = positions, 0
+        self.table = torch.arange(batch * entries, dtype=torch.int32, device=device).view(batch, entries)
+        self.lengths = torch.zeros(batch, dtype=torch.int32, device=device)
+        elements, kind, blocks = {None: (dim, t, 0), "e4m3": (dim, torch.float8_e4m3fn, 1), "e2m1": (dim // 2, torch.uint8, dim // 32)}[held]
+        self.pages = torch.empty(model.layers, 2, batch * entries, model.heads, page, elements, dtype=kind, device=device)
+        self.scales = torch.empty(model.layers, 2, batch * entries, model.heads, blocks, page, dtype=torch.uint8, device=device) if held else None
+
+    def layer(self, n):
+        """((k_pages, v_pages), the scales by name) of layer n"""
+        return (self.pages[n, 0], self.pages[n, 1]), {} if self.scales is None else {"k_scales": self.scales[n, 0], "v_scales": self.scales[n, 1]}
 
 
 class DeviceMeasure:
@@ -238,6 +307,8 @@ def main():
             model.params[name] -= 0.5 * grad
         if i % 10 == 0:
             print(f"step {i}: loss {float(loss):.3f}")
+    words, logprob = model.generate(Cache(model, 8, 160), tokens[:, :128], torch.rand(8, 16, generator=gen, device="cuda"), temperature=0.7, top_p=0.95)
+    print(f"16 words behind 128 of the first sequence: {words[0].tolist()}; logarithm of their share {float(logprob.mean()):.3f} on average")
     machine, hidden, heads, vocab, choices = W.Machine(4, 4, elem_bytes=2), 1024, 16, 32768, (1, 2, 4, 8, 16)
     ops, edges, leader, params = graph(batch=16, length=512, hidden=hidden, vocab=vocab, layers=4)
     costs, cache = measured_costs(ops, 16, choices, DeviceMeasure(hidden, hidden // heads, vocab=vocab))
