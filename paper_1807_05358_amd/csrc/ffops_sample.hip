@@ -16,7 +16,16 @@ struct SampleArgs {
     float* logprob;
 };
 
+// A block takes a row.  It reads it twice: once to sum weights in bins of logits, once for the few words of the bins that decide; these are sorted and gone through with exact sums.  What
+// bounds it is the first reading: 24 instructions an element, a third of them in 64 bits, and an addition in LDS.
+//   Bins are 1 / per_nat wide in units of the temperature, from an anchor on, the largest logit of what the block's threads read first.  A word weighs e^r 2^-shift steps, r its place
+// in its bin: whole numbers, whose sums do not depend on an order, to 2^-shift of the weight whatever its size.  Sums of bins are in 64-bit floats.  Where the anchor was too low, or words beyond the lowest bin
+// weigh more than e^-42, the row is read again with other bins; words that weigh less than that beside the largest do not count.
+//   The bins that decide are those in which the border of top_k, that of top_p, that of min_p and the chosen word can lie; they depend on one another, so each is a range
+// until the words are there.  Bins with more than MOST words (equal logits, or nearly so) are left to select(), which reads the row for every eight bits of the key of each border.
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
+constexpr int BINS = 4096, BELOW = 2816;    // bins; those below the anchor
+constexpr int MOST = 2 * THREADS;           // words of the bins that decide
 
 // Logits as whole numbers in the same order, -0 as 0.
 template <class T>
@@ -47,14 +56,31 @@ struct Key<F16> : Key16<F16> {};
 template <>
 struct Key<BF16> : Key16<BF16> {};
 
-struct Shared {
+// what select() counts
+struct Digits {
     uint64_t mass[256];
     uint32_t count[256];
-    uint64_t a[WAVES], b[WAVES];
-    uint32_t c[WAVES];
-    uint32_t found, word;
+    uint32_t found;
     uint64_t above_mass;
     uint32_t above_count;
+};
+
+struct Shared {
+    union {
+        uint64_t steps[BINS];       // a bin's sum, then:
+        double above[BINS];         // the weight of all bins above it
+    };
+    uint32_t count[BINS];           // words, then those of all bins above; top_k alone
+    union {
+        uint64_t list[MOST];        // key and number of each word of the bins that decide
+        Digits digits;
+    };
+    uint64_t a[WAVES], b[WAVES];
+    double d[WAVES];
+    uint32_t c[WAVES];
+    uint32_t n, word, lo, hi, again;
+    double value, weight;
+    uint32_t found;
 };
 
 template <class V>
@@ -96,7 +122,7 @@ struct Weigh {
 // The shortest beginning of the words' order with more than `target` words (BY_COUNT) or steps of weight: its last word's key, the words before it with larger keys and
 // their steps (sh.above_...), bit group after bit group of the keys.
 template <class T, bool BY_COUNT>
-__device__ uint32_t select(const typename T::elem* z, uint32_t vocab, const Weigh& w, uint64_t target, Shared& sh, uint64_t& above_mass, uint32_t& above_count)
+__device__ uint32_t select(const typename T::elem* z, uint32_t vocab, const Weigh& w, uint64_t target, Digits& sh, uint64_t& above_mass, uint32_t& above_count)
 {
     uint32_t prefix = 0;
     above_mass = 0, above_count = 0;
@@ -130,33 +156,10 @@ __device__ uint32_t select(const typename T::elem* z, uint32_t vocab, const Weig
     return prefix;
 }
 
-// A block takes a row and reads it from the cache again for every step.
+// The word by reading the row again for every border; all of its threads.  `first`: the largest key.
 template <class T>
-__global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
+__device__ void choose_by_digits(const typename T::elem* z, uint32_t V, float most, float temperature, int32_t top_k, float top_p, float min_p, float u, Shared& sh, uint32_t& word, float& logprob)
 {
-    __shared__ Shared sh;
-    const uint32_t row = blockIdx.x, V = a.vocab;
-    const typename T::elem* z = (const typename T::elem*)(a.logits + row * a.stride);
-    const float temperature = a.temperatures ? a.temperatures[row] : a.temperature, top_p = a.top_ps ? a.top_ps[row] : a.top_p, min_p = a.min_ps ? a.min_ps[row] : a.min_p, u = a.u[row];
-    const int32_t top_k = a.top_ks ? a.top_ks[row] : a.top_k;
-    // the first word of the order: the largest key, of these the lowest number
-    uint64_t first = 0;
-    uint32_t nan = 0;
-    for (uint32_t i = threadIdx.x; i < V; i += THREADS) {
-        const uint32_t k = Key<T>::of(z[i]);
-        const float f = (float)z[i];
-        nan |= f != f;
-        const uint64_t x = (uint64_t)k << 32 | (0xffffffffu - i);
-        first = x > first ? x : first;
-    }
-    first = block_max(first, sh.a);
-    nan = block_sum(nan, sh.c);
-    const float most = Key<T>::value((uint32_t)(first >> 32));
-    const bool fine = nan == 0 && most > -INFINITY && temperature >= 0 && temperature < INFINITY && top_p == top_p && min_p == min_p && u == u;
-    if (!fine || temperature == 0) {
-        if (threadIdx.x == 0) a.words[row] = fine ? (int32_t)(0xffffffffu - (uint32_t)first) : -1, a.logprob[row] = fine ? 0.0f : NAN;
-        return;
-    }
     Weigh w = {most, (double)temperature, 1.0};
     int shift = 62;
     while ((1ull << (62 - shift)) < V) --shift;
@@ -174,13 +177,13 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
     uint64_t above;
     uint32_t before;
     if (top_k > 0 && (uint32_t)top_k < V) {
-        const uint32_t k = select<T, true>(z, V, w, (uint64_t)top_k - 1, sh, above, before);
+        const uint32_t k = select<T, true>(z, V, w, (uint64_t)top_k - 1, sh.digits, above, before);
         kept = (uint32_t)top_k, mass = above + (kept - before) * w.steps(Key<T>::value(k));
     }
     if (top_p < 1) {
         const double t = ceil((double)top_p * (double)mass);
         const uint64_t target = t < 1 ? 0 : t <= (double)(mass - 1) ? (uint64_t)t - 1 : mass - 1;
-        const uint32_t k = select<T, false>(z, V, w, target, sh, above, before);
+        const uint32_t k = select<T, false>(z, V, w, target, sh.digits, above, before);
         const uint64_t s = w.steps(Key<T>::value(k)), more = (target - above) / s + 1;
         if (before + more < kept) kept = before + (uint32_t)more, mass = above + more * s;
     }
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
     }
     const double t = floor((double)(u < 0 ? 0 : u) * (double)mass);
     const uint64_t target = t < (double)(mass - 1) ? (uint64_t)t : mass - 1;
-    const uint32_t k = select<T, false>(z, V, w, target, sh, above, before);
+    const uint32_t k = select<T, false>(z, V, w, target, sh.digits, above, before);
     const float chosen = Key<T>::value(k);
     uint64_t rank = (target - above) / w.steps(chosen);         // words of that key before it
     if (before + rank >= kept) rank = kept - 1 - before;
@@ -210,7 +213,359 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         if (seen > rank) break;
     }
     __syncthreads();
-    if (threadIdx.x == 0) a.words[row] = (int32_t)sh.word, a.logprob[row] = (float)log(w.of(chosen) / ((double)mass / w.unit));
+    word = sh.word, logprob = (float)log(w.of(chosen) / ((double)mass / w.unit));
+}
+
+// sixteen bytes of a row at any element's place
+template <class T>
+struct Piece {
+    typedef typename T::elem vec __attribute__((ext_vector_type(T::VEC), aligned(sizeof(typename T::elem))));
+    vec v;
+};
+
+constexpr int AHEAD = 4;        // pieces that a thread asks for at once
+
+// calls f(element, its number) for all of a row's elements, a thread's in the order of their numbers
+template <class T, class F>
+__device__ __forceinline__ void for_each(const typename T::elem* z, uint32_t V, F f)
+{
+    constexpr uint32_t STEP = THREADS * T::VEC;
+    uint32_t i = threadIdx.x * T::VEC;
+    for (; i + (AHEAD - 1) * STEP + T::VEC <= V; i += AHEAD * STEP) {
+        Piece<T> p[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) p[k].v = *(const typename Piece<T>::vec*)(z + i + k * STEP);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e) f((float)p[k].v[e], i + k * STEP + e);
+    }
+    for (; i + T::VEC <= V; i += STEP) {
+        const typename Piece<T>::vec p = *(const typename Piece<T>::vec*)(z + i);
+#pragma unroll
+        for (int e = 0; e < T::VEC; ++e) f((float)p[e], i + e);
+    }
+    for (; i < V; ++i) f((float)z[i], i);
+}
+
+// The bins of a row.
+struct Bins {
+    float anchor;
+    double per_logit, per_nat;      // bins in a unit of the logits, and of the exponent
+    double c[7];                    // e^(x / per_nat) as a sum of powers of x
+
+    __device__ void set(float anchor_, double temperature, double per_nat_)
+    {
+        anchor = anchor_, per_nat = per_nat_, per_logit = per_nat / temperature;
+        c[0] = 1;
+#pragma unroll
+        for (int k = 1; k < 7; ++k) c[k] = c[k - 1] / (per_nat * k);
+    }
+    // the place of a logit, in bins above the anchor's lower edge
+    __device__ __forceinline__ double place(float z) const { return z == anchor ? 0.0 : ((double)z - (double)anchor) * per_logit; }
+    // e^(r / per_nat) of 0 <= r < 1 in steps of 2^-shift, cut off
+    __device__ __forceinline__ uint64_t steps(double r, int shift) const
+    {
+        double e = c[6];
+#pragma unroll
+        for (int k = 5; k >= 0; --k) e = fma(e, r, c[k]);
+        return (__builtin_bit_cast(uint64_t, e) & 0xfffffffffffffull | 1ull << 52) >> (52 - shift);
+    }
+    // the weight of a bin's lower edge beside that of logit z
+    __device__ double edge(int bin, float z, double temperature) const
+    {
+        const double shift = z == anchor ? 0.0 : ((double)anchor - (double)z) / temperature;
+        return exp((bin - BELOW) / per_nat + shift);
+    }
+};
+
+__device__ __forceinline__ void add_lds(uint64_t* p, uint64_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+__device__ __forceinline__ void add_lds(uint32_t* p, uint32_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
+
+// sums of x over the threads before this one, and over all of them
+template <class V>
+__device__ __forceinline__ V block_before(V x, V* at, V& all)
+{
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    V s = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const V t = __shfl_up(s, d);
+        if (lane >= d) s += t;
+    }
+    const V own = __shfl_up(s, 1);
+    __syncthreads();
+    if (lane == 63) at[wave] = s;
+    __syncthreads();
+    V before = 0;
+    all = 0;
+    for (int w = 0; w < WAVES; ++w) {
+        if (w == wave) before = all;
+        all += at[w];
+    }
+    return before + (lane ? own : (V)0);
+}
+
+// The bins whose weights a sum from `lo` to `hi` can end in: above[bin] <= sum < above[bin - 1], the lowest one for more than all.  All threads; sh.above is there.
+struct Range {
+    int lo, hi;
+};
+__device__ Range bins_of(double lo, double hi, double all, Shared& sh)
+{
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < BINS / THREADS; ++k) {
+        const int b = threadIdx.x * (BINS / THREADS) + k;
+        const double from = sh.above[b], to = b ? sh.above[b - 1] : INFINITY;
+        if (from <= lo && lo < to) sh.hi = b;
+        if (from <= hi && hi < to) sh.lo = b;
+    }
+    __syncthreads();
+    return {(int)sh.lo, (int)sh.hi};
+}
+
+constexpr double SLACK = 1e-11;     // of sums: what roundings, and words that do not count, can move them
+
+template <class T>
+__global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
+{
+    __shared__ Shared sh;
+    const uint32_t row = blockIdx.x, V = a.vocab, tid = threadIdx.x;
+    const typename T::elem* z = (const typename T::elem*)(a.logits + row * a.stride);
+    const float temperature = a.temperatures ? a.temperatures[row] : a.temperature, top_p = a.top_ps ? a.top_ps[row] : a.top_p, u = a.u[row];
+    const float min_p_ = a.min_ps ? a.min_ps[row] : a.min_p, min_p = min_p_ > 1 ? 1.0f : min_p_;
+    const int32_t top_k_ = a.top_ks ? a.top_ks[row] : a.top_k;
+    const uint32_t top_k = top_k_ > 0 && (uint32_t)top_k_ < V ? (uint32_t)top_k_ : 0;      // 0: all words
+    const bool fine = temperature >= 0 && temperature < INFINITY && top_p == top_p && min_p == min_p && u == u;
+    if (!fine) {
+        if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
+        return;
+    }
+    if (temperature == 0) {         // the largest key, of these the lowest number
+        uint64_t first = 0;
+        uint32_t nan = 0;
+        for_each<T>(z, V, [&](float x, uint32_t i) {
+            nan |= x != x;
+            const uint64_t k = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+            first = k > first ? k : first;
+        });
+        first = block_max(first, sh.a);
+        nan = block_sum(nan, sh.c);
+        const bool any = nan == 0 && Key<F32>::value((uint32_t)(first >> 32)) > -INFINITY;
+        if (tid == 0) a.words[row] = any ? (int32_t)(0xffffffffu - (uint32_t)first) : -1, a.logprob[row] = any ? 0.0f : NAN;
+        return;
+    }
+    // the anchor: the largest of each thread's first elements
+    float most = -INFINITY;
+    for (uint32_t i = tid; i < min(V, (uint32_t)(4 * THREADS)); i += THREADS) most = fmaxf(most, (float)z[i]);
+    most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
+    int shift = 51;
+    while (((1ull << 63) >> (shift + 1)) < V) --shift;
+    Bins bins;
+    double per_nat = 32;
+    while (per_nat < 1024 && per_nat * 2 <= 64 * (double)temperature) per_nat *= 2;
+    bins.set(most, temperature, per_nat);
+    for (;;) {
+        for (int b = tid; b < BINS; b += THREADS) sh.steps[b] = 0, sh.count[b] = 0;
+        if (tid == 0) sh.again = 0;
+        __syncthreads();
+        most = -INFINITY;
+        uint32_t again = 0;         // 1: a NaN, 2: above the bins, 4: below them and not yet without weight
+        const double light = -42 * bins.per_nat;
+        for_each<T>(z, V, [&](float x, uint32_t) {
+            most = fmaxf(most, x);
+            const double at = bins.place(x), whole = floor(at);
+            if (x != x) again |= 1;
+            if (at >= BINS - BELOW) again |= 2;
+            else if (at >= -BELOW) {
+                const int b = (int)whole + BELOW;
+                add_lds(&sh.steps[b], bins.steps(at - whole, shift));
+                if (top_k) add_lds(&sh.count[b], 1u);
+            } else if (at > light) again |= 4;
+        });
+        again = __any(again & 1) * 1 | __any(again & 2) * 2 | __any(again & 4) * 4;
+        if (again && tid % 64 == 0) __hip_atomic_fetch_or(&sh.again, again, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
+        again = sh.again;
+        __syncthreads();
+        if ((again & 1) || most == -INFINITY) {
+            if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
+            return;
+        }
+        if (!(again & 6)) break;
+        bins.set(most, temperature, again & 2 ? bins.per_nat : 64);       // with 64 and the largest logit as the anchor neither comes again
+    }
+    // weights of all bins above each, beside the largest word's, which is 1; a thread has four bins, the first thread the highest
+    constexpr int EACH = BINS / THREADS;
+    double all;
+    uint32_t words_all = 0;
+    {
+        double w[EACH], mine = 0;
+        uint32_t n[EACH], own = 0;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int b = BINS - 1 - (int)(tid * EACH + k);
+            w[k] = sh.steps[b] ? (double)sh.steps[b] * ldexp(bins.edge(b, most, temperature), -shift) : 0;
+            n[k] = sh.count[b];
+            mine += w[k], own += n[k];
+        }
+        double before = block_before(mine, sh.d, all);
+        uint32_t words_before = top_k ? block_before(own, sh.c, words_all) : 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int b = BINS - 1 - (int)(tid * EACH + k);
+            sh.above[b] = before, sh.count[b] = words_before;
+            if (words_before < top_k && top_k <= words_before + n[k]) sh.found = b;
+            before += w[k], words_before += n[k];
+        }
+        __syncthreads();
+    }
+    const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
+    // what each border leaves, from..to, and the bins it can lie in
+    const bool by_k = top_k && words_all >= top_k;      // otherwise words without weight make up the rest
+    double k_lo = all, k_hi = all;
+    const int k_bin = by_k ? (int)sh.found : -1;
+    if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
+    Range p_bins = {1, 0}, m_bins = {1, 0};
+    double p_lo = k_lo, p_hi = k_hi;
+    if (top_p < 1) {
+        const double p = top_p > 0 ? (double)top_p : 0.0;
+        p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
+        p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
+    }
+    double m_lo = all, m_hi = all;
+    if (min_p > 0) {
+        const double at = (log((double)min_p) * bins.per_nat) + bins.place(most);
+        const int lo = (int)floor(fmax(at - 1e-6, -1.0 * BELOW)) + BELOW, hi = (int)floor(fmax(at + 1e-6, -1.0 * BELOW)) + BELOW;
+        m_bins = {min(lo, BINS - 1), min(hi, BINS - 1)};
+        m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
+    }
+    const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
+    // borders that others come before do not count
+    if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
+    const bool no_p = p_lo > hi * (1 + SLACK);
+    if (no_p) p_bins = {1, 0};
+    const bool need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
+    const double share = u < 0 ? 0.0 : u < 1 ? (double)u : 1.0;
+    const Range u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
+    const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
+    // their words
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    {
+        int least = u_bins.lo;
+        if (need_k) least = min(least, k_bin);
+        if (p_bins.lo <= p_bins.hi) least = min(least, p_bins.lo);
+        if (m_bins.lo <= m_bins.hi) least = min(least, m_bins.lo);
+        const double from = least - BELOW;
+        for_each<T>(z, V, [&](float x, uint32_t i) {
+            const double at = bins.place(x);
+            if (at >= from && decides((int)floor(at) + BELOW)) {
+                const uint32_t n = atomicAdd(&sh.n, 1u);
+                if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+            }
+        });
+    }
+    __syncthreads();
+    const uint32_t n = sh.n;
+    uint32_t word = 0xffffffffu;
+    float logprob = NAN;
+    if (n && n <= MOST) {
+        // sorted, the largest first
+        uint32_t size = 128;
+        while (size < n) size *= 2;
+        for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
+        __syncthreads();
+        for (uint32_t k = 2; k <= size; k *= 2)
+            for (uint32_t j = k / 2; j; j /= 2) {
+                if (tid < size / 2) {
+                    const uint32_t i = (tid / j * 2 * j) + tid % j;
+                    const uint64_t x = sh.list[i], y = sh.list[i + j];
+                    if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
+                }
+                if (size > 128) __syncthreads();
+                else asm volatile("" ::: "memory");         // one wave, whose accesses to LDS are done in their order
+            }
+        __syncthreads();
+        // a thread has two neighbours: their weights, the weight before them, their rank
+        const Weigh weigh = {most, (double)temperature, 1.0};
+        double w[2], before[2];
+        int bin[2];
+        uint32_t rank[2];
+        bool in[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t i = 2 * tid + e;
+            in[e] = i < n;
+            const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
+            bin[e] = in[e] ? (int)floor(bins.place(x)) + BELOW : -1;
+            w[e] = in[e] ? weigh.of(x) : 0;
+        }
+        double sum_all;
+        const double sum = block_before(w[0] + w[1], sh.d, sum_all);
+        // where each bin's words begin in the list, and the sum there: steps of other bins are not needed any more, but their sums above are
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t i = 2 * tid + e;
+            before[e] = sum + (e ? w[0] : 0.0);
+            if (!in[e]) continue;
+            const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
+            if (i == 0 || (int)floor(bins.place(prev)) + BELOW != bin[e]) {     // one thread for each bin
+                sh.above[bin[e]] -= before[e];
+                sh.count[bin[e]] -= i;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (in[e]) before[e] += sh.above[bin[e]], rank[e] = sh.count[bin[e]] + 2 * tid + e;
+        // the borders, exactly
+        double left = all;
+        if (need_k) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (in[e] && rank[e] == top_k - 1) sh.value = before[e] + w[e];
+            __syncthreads();
+            left = sh.value;
+        }
+        if (p_bins.lo <= p_bins.hi) {
+            const double target = top_p > 0 ? (double)top_p * left : 0.0;
+            __syncthreads();
+            if (tid == 0) sh.value = -1;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (in[e] && bin[e] >= p_bins.lo && bin[e] <= p_bins.hi && (before[e] < target || before[e] == 0) && !(before[e] + w[e] < target)) sh.value = before[e] + w[e];
+            __syncthreads();
+            left = fmin(left, sh.value);        // below 0: between two bins, by roundings; no word is found then
+        }
+        if (m_bins.lo <= m_bins.hi) {
+            // the words before the bins, and those of them that weigh enough
+            double m = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (in[e] && bin[e] >= m_bins.lo && bin[e] <= m_bins.hi && w[e] >= (double)min_p) m = fmax(m, before[e] + w[e]);
+            m = __builtin_bit_cast(double, block_max(__builtin_bit_cast(uint64_t, m), sh.a));
+            left = fmin(left, fmax(m, m_lo));
+        }
+        const double target = fmin(share, 1 - 1e-14) * left;
+        __syncthreads();
+        if (tid == 0) sh.word = 0xffffffffu;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
+        __syncthreads();
+        word = sh.word;
+        if (word != 0xffffffffu) logprob = (float)log(sh.weight / left);
+    }
+    if (word == 0xffffffffu) {
+        __syncthreads();
+        choose_by_digits<T>(z, V, most, temperature, top_k_, top_p, min_p, u, sh, word, logprob);
+    }
+    if (tid == 0) a.words[row] = (int32_t)word, a.logprob[row] = logprob;
 }
 
 int check(const ff_sample_t* p)
