@@ -42,35 +42,90 @@ __device__ __forceinline__ int positions(const PagedArgs& a, uint32_t b)
     return cached(a.q_lengths, a.q_len, b) ? n : 0;
 }
 
-// The sums of tiles up to a place, by all 256 threads: each takes a stretch of sequences.
+// Where a sequence, or a run, begins in the list of all tiles.  Up to 64 sequences: a lane has the length of each, and a wave finds it by itself; more: the block's threads take a stretch of
+// sequences each.
 struct Finder {
     int64_t sum[WAVES];
     uint32_t b;
     int64_t first;
 };
 
-__device__ __forceinline__ int64_t tiles_of(const PagedArgs& a, uint32_t b) { return (positions(a, b) + TILE - 1) / TILE; }
+struct List {
+    bool few;
+    uint32_t b0, b1;                // the thread's sequences
+    int nk;                         // few: the length of the lane's sequence
+    int64_t before, mine, all;      // places of the list before them, theirs, and all
 
-// the sum of x over the threads before this one; `all`: over all of them
-__device__ __forceinline__ int64_t sum_before(int64_t x, Finder& f, int64_t& all)
-{
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    int64_t s = x;
+    __device__ __forceinline__ void make(const PagedArgs& a, Finder& f)
+    {
+        const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+        few = a.batch <= 64;
+        if (few) {
+            b0 = lane, b1 = lane + 1;
+            nk = lane < (int)a.batch ? positions(a, lane) : 0;
+            int s = (int)places_of(nk);
+            mine = s;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int64_t t = __shfl_up(s, d);
-        if (lane >= d) s += t;
+            for (int d = 1; d < 64; d *= 2) {
+                const int t = __shfl_up(s, d);
+                if (lane >= d) s += t;
+            }
+            before = s - (int)mine, all = __builtin_amdgcn_readlane(s, 63);
+            return;
+        }
+        const uint32_t per = (a.batch + 255) / 256;
+        b0 = min(a.batch, threadIdx.x * per), b1 = min(a.batch, b0 + per), nk = 0, mine = 0;
+        for (uint32_t i = b0; i < b1; ++i) mine += places_of(positions(a, i));
+        int64_t s = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int64_t t = __shfl_up(s, d);
+            if (lane >= d) s += t;
+        }
+        if (lane == 63) f.sum[wave] = s;
+        __syncthreads();
+        before = s - mine, all = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) before += f.sum[w];
+            all += f.sum[w];
+        }
     }
-    if (lane == 63) f.sum[wave] = s;
-    __syncthreads();
-    int64_t before = 0;
-    all = 0;
-    for (int w = 0; w < WAVES; ++w) {
-        if (w < wave) before += f.sum[w];
-        all += f.sum[w];
+    // the sequence that holds a place of the list, and where it begins there
+    __device__ __forceinline__ void sequence_at(const PagedArgs& a, int64_t place, Finder& f, uint32_t& b, int64_t& first) const
+    {
+        const bool here = before <= place && place < before + mine;
+        if (few) {
+            b = (uint32_t)__builtin_ctzll(__ballot(here));
+            first = __builtin_amdgcn_readlane((int)before, b);
+            return;
+        }
+        if (here) {
+            int64_t at = before;
+            for (uint32_t i = b0; i < b1; ++i) {
+                const uint32_t n = places_of(positions(a, i));
+                if (place < at + n) {
+                    f.b = i, f.first = at;
+                    break;
+                }
+                at += n;
+            }
+        }
+        __syncthreads();
+        b = f.b, first = f.first;
     }
-    return before + s - x;
-}
+    __device__ __forceinline__ int64_t begin_of(const PagedArgs& a, uint32_t b, Finder& f) const
+    {
+        if (few) return __builtin_amdgcn_readlane((int)before, b);
+        if (b0 <= b && b < b1) {
+            int64_t at = before;
+            for (uint32_t i = b0; i < b; ++i) at += places_of(positions(a, i));
+            f.first = at;
+        }
+        __syncthreads();
+        return f.first;
+    }
+    __device__ __forceinline__ int length(const PagedArgs& a, uint32_t b) const { return few ? __builtin_amdgcn_readlane(nk, b) : positions(a, b); }
+};
 
 struct Lane {
     int lane, wave, x, g;           // x = lane % 16, g = lane / 16
@@ -80,10 +135,14 @@ struct Lane {
 __device__ __forceinline__ uint32_t low_pair(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100); }
 __device__ __forceinline__ uint32_t high_pair(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302); }
 
+// bytes of a row: FULL: the head has all D elements of the kernel's tiles
+template <int HELD, int D, bool FULL>
+__device__ __forceinline__ uint32_t row_bytes(const PagedArgs& a) { return FULL ? D / 8 * EIGHT<HELD> : a.c.row; }
+
 // ---- a tile's keys ----
 
 // operands of 32 positions: [half][step]; D elements of a row, a.dim of them real
-template <class T, int HELD, int D>
+template <class T, int HELD, int D, bool FULL>
 struct Keys {
     static constexpr int LOADS = HELD == FF_HELD_SAME ? D / 32 : HELD == FF_HELD_E4M3 ? D / 64 : 1;
     static constexpr bool SHORT = HELD == FF_HELD_E2M1 && D == 64;       // 8-byte pieces
@@ -97,14 +156,14 @@ struct Keys {
         if (HELD == FF_HELD_E4M3) return (g + 4 * (st / 2)) * 16 + st % 2 * 8;
         return g * (D / 4) + st * 8;
     }
-    __device__ __forceinline__ void load(const PagedArgs& a, int half, const char* page, const uint8_t* scales, uint32_t place, const Lane& l)
+    // rows: of 16 positions from a place on, the same for all lanes, so that a lane's address is an offset
+    __device__ __forceinline__ void load(const PagedArgs& a, int half, const char* rows, const uint8_t* scales, const Lane& l)
     {
-        const char* p = page + (place + l.x) * a.c.row;
+        const uint32_t at = l.x * row_bytes<HELD, D, FULL>(a);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int first = element(HELD == FF_HELD_E4M3 ? 2 * i : i, l.g);
-            const uint32_t at = HELD == FF_HELD_SAME ? first * 2 : HELD == FF_HELD_E4M3 ? first : first / 2;
-            const char* from = first < (int)a.dim ? p + at : (const char*)&zero16;
+            const int first = element(HELD == FF_HELD_E4M3 ? 2 * i : i, l.g), place = HELD == FF_HELD_SAME ? first * 2 : HELD == FF_HELD_E4M3 ? first : first / 2;
+            const char* from = rows + (at + (FULL || first < (int)a.dim ? (uint32_t)place : 0u));
             if constexpr (SHORT) {
                 const uint2 w = *(const uint2*)from;
                 raw[half][i] = {w.x, w.y, 0, 0};
@@ -112,10 +171,10 @@ struct Keys {
                 raw[half][i] = *(const uint4*)from;
             }
         }
-        if constexpr (HELD == FF_HELD_E4M3) s[half] = scales[place + l.x];
-        if constexpr (HELD == FF_HELD_E2M1) s[half] = scales[min((uint32_t)(l.g * (D / 4) / 32), a.c.blocks - 1) * a.c.page + place + l.x];
+        if constexpr (HELD == FF_HELD_E4M3) s[half] = scales[(uint32_t)l.x];
+        if constexpr (HELD == FF_HELD_E2M1) s[half] = scales[min((uint32_t)(l.g * (D / 4) / 32), a.c.blocks - 1) * a.c.page + l.x];
     }
-    __device__ __forceinline__ typename T::vec8 operand(int half, int st) const
+    __device__ __forceinline__ typename T::vec8 operand(const PagedArgs& a, int half, int st, int g) const
     {
         uint4 v;
         if constexpr (HELD == FF_HELD_SAME) v = raw[half][st];
@@ -126,13 +185,15 @@ struct Keys {
             const uint4 r = raw[half][0];
             v = Eight<T, HELD>::get(st == 0 ? r.x : st == 1 ? r.y : st == 2 ? r.z : r.w, scale_operand(s[half]));
         }
+        if (!FULL && element(st, g) >= (int)a.dim) v = {0, 0, 0, 0};
         return __builtin_bit_cast(typename T::vec8, v);
     }
 };
 
 // ---- a tile's values ----
 
-template <class T, int HELD, int D>
+// Elements beyond a head's are others', and make sums that are not kept.
+template <class T, int HELD, int D, bool FULL>
 struct Values {
     static constexpr int EACH = D / 16, WORDS = EACH / 2;       // elements of a row that a lane holds, and words of them as the type
     static constexpr int BYTES = HELD == FF_HELD_SAME ? EACH * 2 : HELD == FF_HELD_E4M3 ? EACH : EACH / 2;
@@ -140,12 +201,12 @@ struct Values {
     uint32_t raw[8][RAW];
     uint32_t s[2];                  // scales of the four positions of each half
 
-    __device__ __forceinline__ void load(const PagedArgs& a, int half, const char* page, const uint8_t* scales, uint32_t place, const Lane& l)
+    __device__ __forceinline__ void load(const PagedArgs& a, int half, const char* rows, const uint8_t* scales, const Lane& l)
     {
-        const bool in = l.x * EACH < (int)a.dim;
+        const uint32_t row = row_bytes<HELD, D, FULL>(a), at = l.g * 4 * row + (FULL || l.x * EACH < (int)a.dim ? l.x * BYTES : 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const char* p = in ? page + (place + l.g * 4 + r) * a.c.row + l.x * BYTES : (const char*)&zero16;
+            const char* p = rows + (at + r * row);
             uint32_t* to = raw[half * 4 + r];
             if constexpr (BYTES == 16) {
                 const uint4 w = *(const uint4*)p;
@@ -159,22 +220,27 @@ struct Values {
                 to[0] = *(const uint16_t*)p;
             }
         }
-        if constexpr (HELD != FF_HELD_SAME) s[half] = *(const uint32_t*)(scales + (HELD == FF_HELD_E4M3 ? 0 : min((uint32_t)(l.x * EACH / 32), a.c.blocks - 1)) * a.c.page + place + l.g * 4);
+        if constexpr (HELD != FF_HELD_SAME) s[half] = *(const uint32_t*)(scales + ((HELD == FF_HELD_E4M3 ? 0 : min((uint32_t)(l.x * EACH / 32), a.c.blocks - 1)) * a.c.page + l.g * 4));
     }
-    // words of the lane's elements of position e (of its eight)
-    __device__ __forceinline__ void words(int e, uint32_t* w) const
+    // positions from `left` on (of those of lane group 0) are behind the last: what lies there may be anything
+    __device__ __forceinline__ void clear(int left)
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const bool out = 16 * (e / 4) + e % 4 >= left;
+#pragma unroll
+            for (int i = 0; i < RAW; ++i) raw[e][i] = out ? 0 : raw[e][i];
+            if constexpr (HELD != FF_HELD_SAME) s[e / 4] = out ? s[e / 4] & ~(255u << (e % 4 * 8)) : s[e / 4];
+        }
+    }
+    // word i of the lane's elements of position e (of its eight)
+    template <int I>
+    __device__ __forceinline__ uint32_t word(int e) const
     {
         const float f = HELD == FF_HELD_SAME ? 0 : scale_operand(s[e / 4] >> (e % 4 * 8) & 255);
-        if constexpr (HELD == FF_HELD_SAME) {
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) w[i] = raw[e][i];
-        } else if constexpr (HELD == FF_HELD_E4M3) {
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) w[i] = i % 2 ? from_e4m3<T, true>(raw[e][i / 2], f) : from_e4m3<T, false>(raw[e][i / 2], f);
-        } else {
-            w[0] = from_e2m1<T, 0>(raw[e][0], f), w[1] = from_e2m1<T, 1>(raw[e][0], f);
-            if constexpr (WORDS == 4) w[2] = from_e2m1<T, 2>(raw[e][0], f), w[3] = from_e2m1<T, 3>(raw[e][0], f);
-        }
+        if constexpr (HELD == FF_HELD_SAME) return raw[e][I];
+        else if constexpr (HELD == FF_HELD_E4M3) return from_e4m3<T, I % 2 == 1>(raw[e][I / 2], f);
+        else return from_e2m1<T, I>(raw[e][0], f);
     }
 };
 
@@ -208,233 +274,294 @@ __device__ __forceinline__ Columns<NT> columns_of(const PagedArgs& a, uint32_t b
     return c;
 }
 
-// the page of 16 positions from `at`: its number, 0 in the place of one that there is not
-struct Group {
-    uint32_t page, place;
-    bool bad;
+// A tile as it is asked for.  `bad`: which of its halves has no page; what is read in its place does not count.
+template <class T, int HELD, int D, bool FULL>
+struct Tile {
+    Keys<T, HELD, D, FULL> k;
+    Values<T, HELD, D, FULL> v;
+    bool bad[2];
 };
-__device__ __forceinline__ Group group_at(const PagedArgs& a, const int32_t* table, int at, int nk)
+
+// The tiles of a wave of a stretch of a sequence: every WAVES-th one.  A lane keeps the table's entry of one half of 32 of them.
+struct Stretch {
+    const int32_t* table;
+    int nk;
+    int at0;                        // position of the wave's first tile
+    int entries;
+    uint64_t head, scale_head;      // of the key head in a page
+    __device__ __forceinline__ int at(int i) const { return at0 + i * (WAVES * TILE); }
+};
+
+template <class T, int HELD, int D, bool FULL>
+__device__ __forceinline__ void ask(const PagedArgs& a, Tile<T, HELD, D, FULL>& x, Stretch& s, int i, const Lane& l)
 {
-    Group g;
-    const uint32_t page = (uint32_t)__builtin_amdgcn_readfirstlane(table[entry_of(at, nk, a.c.page_log2)]);
-    g.bad = page >= a.c.pages;
-    g.page = g.bad ? 0 : page;
-    g.place = place_of(at, nk, a.c.page);
-    return g;
+    if (i % 32 == 0) s.entries = s.table[entry_of(s.at(i + l.lane / 2) + l.lane % 2 * 16, s.nk, a.c.page_log2)];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t n = (uint32_t)__builtin_amdgcn_readlane(s.entries, i % 32 * 2 + h);
+        x.bad[h] = n >= a.c.pages;
+        n = x.bad[h] ? 0 : n;
+        const uint64_t page = n;
+        const uint32_t place = place_of(s.at(i) + 16 * h, s.nk, a.c.page);
+        const uint32_t rows = place * row_bytes<HELD, D, FULL>(a);
+        x.k.load(a, h, a.c.k + page * a.c.k_stride + s.head + rows, HELD == FF_HELD_SAME ? nullptr : a.c.k_scale + page * a.c.k_scale_stride + s.scale_head + place, l);
+        x.v.load(a, h, a.c.v + page * a.c.v_stride + s.head + rows, HELD == FF_HELD_SAME ? nullptr : a.c.v_scale + page * a.c.v_scale_stride + s.scale_head + place, l);
+    }
 }
 
-template <class T, int HELD, int D, int NT>
-__global__ __launch_bounds__(256) void k_attention_paged(PagedArgs a)
+// sums of a wave's columns
+template <class T, int D, int NT>
+struct Sums {
+    typename T::vec8 q[NT][D / 32];
+    f32x4 o[NT][D / 16];
+    float m[NT], sum[NT];
+    int seen_least;                 // keys that all columns see
+};
+
+// the largest over lanes l, l ^ 16, l ^ 32 and l ^ 48, by exchanges of halves between two registers
+__device__ __forceinline__ float over_groups(float x)
+{
+    uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const uint32_t a0 = a[0], a1 = a[1];        // (a bit cast of a vector's element itself takes the first one)
+    u = __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t b0 = b[0], b1 = b[1];
+    return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+
+// o += v^T p, from the lane's words I on: two columns of v each
+template <int I, class T, int HELD, int D, bool FULL, int NT>
+__device__ __forceinline__ void values_times(const Values<T, HELD, D, FULL>& v, const typename T::vec8* p, const typename T::vec8* rest, Sums<T, D, NT>& y)
+{
+    if constexpr (I < D / 32) {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = v.template word<I>(e);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint4 u;
+            uint32_t* uw = (uint32_t*)&u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) uw[i] = j ? high_pair(w[2 * i], w[2 * i + 1]) : low_pair(w[2 * i], w[2 * i + 1]);
+            const auto vv = __builtin_bit_cast(typename T::vec8, u);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                y.o[t][2 * I + j] = T::mma(vv, p[t], y.o[t][2 * I + j]);
+                if constexpr (std::is_same<T, BF16>::value) y.o[t][2 * I + j] = T::mma(vv, rest[t], y.o[t][2 * I + j]);
+            }
+        }
+        values_times<I + 1, T, HELD, D, FULL, NT>(v, p, rest, y);
+    }
+}
+
+template <class T, int HELD, int D, bool FULL, int NT>
+__device__ __forceinline__ void work(const PagedArgs& a, Tile<T, HELD, D, FULL>& x, Sums<T, D, NT>& y, const Columns<NT>& c, int at, int nk, const Lane& l)
+{
+    constexpr int STEPS = D / 32, DT = D / 16;
+    typedef typename T::vec8 vec8;
+    f32x4 s[NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s[t][h] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+            const vec8 kk = x.k.operand(a, h, st, l.g);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][h] = T::mma(kk, y.q[t][st], s[t][h]);
+        }
+    }
+    const bool bad = x.bad[0] || x.bad[1];
+    if (at + TILE > y.seen_least || bad) {
+        // a position is left out if the column does not see it, and if it has no page; a column that sees one of those becomes a NaN
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            int first = c.seen[t] - at - 4 * l.g;
+            stay_here(first);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (16 * h + r >= first || x.bad[h]) s[t][h][r] = -INFINITY;
+            if ((x.bad[0] && at < c.seen[t]) || (x.bad[1] && at + 16 < c.seen[t])) y.sum[t] = NAN;
+        }
+        if (at + TILE > nk) {
+            int left = nk - at - 4 * l.g;
+            stay_here(left);
+            x.v.clear(left);
+        }
+    }
+    vec8 p[NT], rest[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])), fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+        top = over_groups(top) * a.scale_log2;
+        if (__any(top > y.m[t] + (MAX_BEHIND<T> + P_SHIFT<T>))) {     // m, the maximum less the shift, starts at -inf; a column that sees nothing keeps it
+            const float mn = fmaxf(y.m[t], top - P_SHIFT<T>), f = mn == -INFINITY ? 1.0f : exp2_(y.m[t] - mn);
+            y.sum[t] *= f;
+#pragma unroll
+            for (int j = 0; j < DT; ++j) y.o[t][j] *= f;
+            y.m[t] = mn;
+        }
+        const float base = y.m[t] == -INFINITY ? 0.0f : y.m[t];
+        float e[8], left[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            e[i] = exp2_(fmaf(s[t][i / 4][i % 4], a.scale_log2, -base));
+            y.sum[t] += e[i];
+        }
+        if constexpr (std::is_same<T, BF16>::value) {
+            // cut off, and the rest, which is never 0 beside more than 0: an infinite value then stays one
+            uint4 cut;
+            uint32_t* cw = (uint32_t*)&cut;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) cw[i] = high_pair(__builtin_bit_cast(uint32_t, e[2 * i]), __builtin_bit_cast(uint32_t, e[2 * i + 1]));
+            p[t] = __builtin_bit_cast(vec8, cut);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) left[i] = fmaxf(e[i] - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, e[i]) & 0xffff0000u), e[i] * 0x1p-30f);
+            rest[t] = round8<T>(left);
+        } else {
+            p[t] = round8<T>(e);
+        }
+    }
+    values_times<0, T, HELD, D, FULL, NT>(x.v, p, rest, y);
+}
+
+// a tile asked for while another is worked: where registers hold both
+template <int HELD, int D, int NT>
+constexpr bool TWO = HELD != FF_HELD_SAME || D == 64 || NT == 1;
+// waves of a SIMD, by their registers
+template <int HELD, int D, int NT>
+constexpr int RESIDENT = 2;
+
+template <class T, int HELD, int D, bool FULL, int NT>
+__global__ __launch_bounds__(256, (RESIDENT<HELD, D, NT>)) void k_attention_paged(PagedArgs a)
 {
     constexpr int STEPS = D / 32, DT = D / 16;
     typedef typename T::vec8 vec8;
     __shared__ Finder find;
-    __shared__ float stat[WAVES][2][16];
-    __shared__ float sums[WAVES][16][D + 4];
+    __shared__ float stat[NT][WAVES][2][16];
+    __shared__ float sums[NT][WAVES][16][D + 4];
     Lane l;
     l.lane = threadIdx.x % 64, l.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l.x = l.lane % 16, l.g = l.lane / 16;
     const uint32_t kh = blockIdx.x % a.kv_heads, run = blockIdx.x / a.kv_heads, col0 = blockIdx.y * (16 * NT);
-    int64_t t0, t1, first, all = 0;     // tiles in the list of all, and the first one of sequence b
+    int64_t t0, t1, first;              // places of the run in the list, and where sequence b begins there
     uint32_t b;
+    List list;
     if (a.runs) {
-        const uint32_t per = (a.batch + 255) / 256, b0 = min(a.batch, threadIdx.x * per), b1 = min(a.batch, b0 + per);
-        int64_t mine = 0;
-        for (uint32_t i = b0; i < b1; ++i) mine += tiles_of(a, i);
-        int64_t before = sum_before(mine, find, all);
-        const uint32_t runs = runs_used(a.runs, all);
-        if (run >= runs || all == 0) return;
-        t0 = run_begin(run, runs, all), t1 = run_begin(run + 1, runs, all);
-        if (before <= t0 && t0 < before + mine)
-            for (uint32_t i = b0; i < b1; ++i) {
-                const int64_t n = tiles_of(a, i);
-                if (t0 < before + n) {
-                    find.b = i, find.first = before;
-                    break;
-                }
-                before += n;
-            }
-        __syncthreads();
-        b = find.b, first = find.first;
+        list.make(a, find);
+        const Runs runs = runs_used(a.runs, list.all);
+        if (run >= runs.n || list.all == 0) return;
+        t0 = runs.begin(run), t1 = runs.begin(run + 1);
+        list.sequence_at(a, t0, find, b, first);
     } else {
-        b = run, first = 0, t0 = 0, t1 = tiles_of(a, b);
-        all = t1;
+        b = run, t0 = 0, first = 0, t1 = ENTRY + tiles_of(positions(a, b));
     }
     for (;; ++b) {
-        const int nk = positions(a, b);
-        const int64_t tiles = (nk + TILE - 1) / TILE, last = first + tiles;
-        if (a.runs && tiles == 0) continue;
-        const int64_t e1 = t1 < last ? t1 : last;
+        const int nk = a.runs ? list.length(a, b) : positions(a, b);
+        if (a.runs && nk == 0) continue;
+        // its tiles: all of them, and those of this run, from e0 to e1
+        const int64_t begin = first + ENTRY, end = begin + tiles_of(nk), e0 = t0 > begin ? t0 : begin, e1 = t1 < end ? t1 : end;
+        first = end;
+        if (a.runs && e0 >= e1) break;              // the run ends before the first
         const Columns<NT> c = columns_of<NT>(a, b, kh, col0, nk, l.x);
-        vec8 q[NT][STEPS];
+        uint4 q[NT][STEPS];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                const int d = Keys<T, HELD, D>::element(s, l.g);
-                q[t][s] = *(const vec8*)(c.seen[t] > 0 && d < (int)a.dim ? a.q.p + b * a.q.batch + c.h[t] * a.q.head + c.i[t] * a.q.pos + d * 2 : (const char*)&zero16);
+                const int d = Keys<T, HELD, D, FULL>::element(s, l.g);
+                q[t][s] = *(const uint4*)(a.q.p + b * a.q.batch + c.h[t] * a.q.head + c.i[t] * a.q.pos + (FULL || d < (int)a.dim ? d * 2 : 0));
             }
-        f32x4 o[NT][DT];
-        float m[NT], sum[NT];
+        Stretch at = {a.c.table + b * a.c.table_stride, nk, (int)(e0 + l.wave - begin) * TILE, 0, (uint64_t)kh * a.c.page * a.c.row, (uint64_t)kh * a.c.page * a.c.blocks};
+        const int n = e1 - e0 > l.wave ? (int)((e1 - e0 - l.wave + WAVES - 1) / WAVES) : 0;
+        Tile<T, HELD, D, FULL> x0;
+        if (n > 0) ask(a, x0, at, 0, l);
+        Sums<T, D, NT> y;
+        int least = nk;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            m[t] = -INFINITY, sum[t] = 0;
+            least = min(least, c.in[t] ? c.seen[t] : nk);
+            y.m[t] = -INFINITY, y.sum[t] = 0;
 #pragma unroll
-            for (int j = 0; j < DT; ++j) o[t][j] = f32x4{0, 0, 0, 0};
+            for (int s = 0; s < STEPS; ++s) {
+                const int d = Keys<T, HELD, D, FULL>::element(s, l.g);
+                y.q[t][s] = __builtin_bit_cast(vec8, c.seen[t] > 0 && (FULL || d < (int)a.dim) ? q[t][s] : uint4{0, 0, 0, 0});
+            }
+#pragma unroll
+            for (int j = 0; j < DT; ++j) y.o[t][j] = f32x4{0, 0, 0, 0};
         }
-        const int32_t* table = a.c.table + b * a.c.table_stride;
-        const uint64_t head = (uint64_t)kh * a.c.page * a.c.row, scale_head = (uint64_t)kh * a.c.page * a.c.blocks;
-        for (int64_t tile = t0 + l.wave; tile < e1; tile += WAVES) {
-            const int at = (int)(tile - first) * TILE;
-            Keys<T, HELD, D> k;
-            Values<T, HELD, D> v;
-            Group g[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                g[h] = group_at(a, table, at + 16 * h, nk);
-                const uint64_t page = g[h].page;
-                k.load(a, h, a.c.k + page * a.c.k_stride + head, HELD == FF_HELD_SAME ? nullptr : a.c.k_scale + page * a.c.k_scale_stride + scale_head, g[h].place, l);
-                v.load(a, h, a.c.v + page * a.c.v_stride + head, HELD == FF_HELD_SAME ? nullptr : a.c.v_scale + page * a.c.v_scale_stride + scale_head, g[h].place, l);
+        for (int d = 8; d; d >>= 1) least = min(least, __shfl_xor(least, d));
+        y.seen_least = __builtin_amdgcn_readfirstlane(least);
+        if constexpr (TWO<HELD, D, NT>) {
+            Tile<T, HELD, D, FULL> x1;
+            for (int i = 0; i < n; i += 2) {
+                if (i + 1 < n) ask(a, x1, at, i + 1, l);
+                work(a, x0, y, c, at.at(i), nk, l);
+                if (i + 1 >= n) break;
+                if (i + 2 < n) ask(a, x0, at, i + 2, l);
+                work(a, x1, y, c, at.at(i + 1), nk, l);
             }
-            // scores
-            f32x4 s[NT][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t) s[t][h] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int st = 0; st < STEPS; ++st) {
-                    const vec8 kk = k.operand(h, st);
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) s[t][h] = T::mma(kk, q[t][st], s[t][h]);
-                }
-            }
-            const bool bad = g[0].bad || g[1].bad;
-            vec8 p[NT], rest[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                // a position is left out if the column does not see it, and if it has no page; a column that sees one of those becomes a NaN
-                float top = -INFINITY;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if (at + 16 * h + 4 * l.g + r >= c.seen[t] || g[h].bad) s[t][h][r] = -INFINITY;
-                        top = fmaxf(top, s[t][h][r]);
-                    }
-                if (bad && ((g[0].bad && at < c.seen[t]) || (g[1].bad && at + 16 < c.seen[t]))) sum[t] = NAN;
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
-                if (__any(top > m[t] + (MAX_BEHIND<T> + P_SHIFT<T>))) {     // m, the maximum less the shift, starts at -inf; a column that sees nothing keeps it
-                    const float mn = fmaxf(m[t], top - P_SHIFT<T>), f = mn == -INFINITY ? 1.0f : exp2_(m[t] - mn);
-                    sum[t] *= f;
-#pragma unroll
-                    for (int j = 0; j < DT; ++j) o[t][j] *= f;
-                    m[t] = mn;
-                }
-                const float base = m[t] == -INFINITY ? 0.0f : m[t];
-                float e[8], left[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    e[i] = exp2_(fmaf(s[t][i / 4][i % 4], a.scale_log2, -base));
-                    sum[t] += e[i];
-                }
-                if constexpr (std::is_same<T, BF16>::value) {
-                    // cut off, and the rest, which is never 0 beside more than 0: an infinite value then stays one
-                    uint4 cut;
-                    uint32_t* cw = (uint32_t*)&cut;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) cw[i] = high_pair(__builtin_bit_cast(uint32_t, e[2 * i]), __builtin_bit_cast(uint32_t, e[2 * i + 1]));
-                    p[t] = __builtin_bit_cast(vec8, cut);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) left[i] = fmaxf(e[i] - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, e[i]) & 0xffff0000u), e[i] * 0x1p-30f);
-                    rest[t] = round8<T>(left);
-                } else {
-                    p[t] = round8<T>(e);
-                }
-            }
-            uint32_t w[8][Values<T, HELD, D>::WORDS];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v.words(e, w[e]);
-            if (at + TILE > nk) {           // what lies behind the last position may be anything
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (at + 16 * (e / 4) + 4 * l.g + e % 4 >= nk)
-#pragma unroll
-                        for (int i = 0; i < Values<T, HELD, D>::WORDS; ++i) w[e][i] = 0;
-            }
-#pragma unroll
-            for (int j = 0; j < DT; ++j) {
-                uint4 u;
-                uint32_t* uw = (uint32_t*)&u;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) uw[i] = j % 2 ? high_pair(w[2 * i][j / 2], w[2 * i + 1][j / 2]) : low_pair(w[2 * i][j / 2], w[2 * i + 1][j / 2]);
-                const vec8 vv = __builtin_bit_cast(vec8, u);
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    o[t][j] = T::mma(vv, p[t], o[t][j]);
-                    if constexpr (std::is_same<T, BF16>::value) o[t][j] = T::mma(vv, rest[t], o[t][j]);
-                }
+        } else {
+            for (int i = 0; i < n; ++i) {
+                work(a, x0, y, c, at.at(i), nk, l);
+                if (i + 1 < n) ask(a, x0, at, i + 1, l);
             }
         }
-        // the four waves' sums together, 16 columns at a time
-        const bool whole = t0 == first && e1 == last;
-        const uint32_t slot = slot_of(run, t0 == first);
+        // the four waves' sums together
+        const bool whole = e0 == begin && e1 == end;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float total = sum[t];
+            float total = y.sum[t];
             total += __shfl_xor(total, 16);
             total += __shfl_xor(total, 32);
-            if (l.g == 0) stat[l.wave][0][l.x] = m[t], stat[l.wave][1][l.x] = total;
-            __syncthreads();
-            float most = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, stat[w][0][l.x]);
-            const float f = m[t] == -INFINITY ? 0.0f : exp2_(m[t] - most);
+            if (l.g == 0) stat[t][l.wave][0][l.x] = y.m[t], stat[t][l.wave][1][l.x] = total;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
                 for (int j = 0; j < DT; j += 4)
-                    *(f32x4*)&sums[l.wave][l.x][(l.g * 4 + r) * DT + j] = f32x4{o[t][j][r] * f, o[t][j + 1][r] * f, o[t][j + 2][r] * f, o[t][j + 3][r] * f};
-            __syncthreads();
-            // a thread: column threadIdx.x / 16, D / 16 elements of it
-            const uint32_t cc = threadIdx.x / 16, x0 = threadIdx.x % 16 * DT, col = col0 + t * 16 + cc;
-            float mm = -INFINITY, ll = 0;
+                    *(f32x4*)&sums[t][l.wave][l.x][(l.g * 4 + r) * DT + j] = f32x4{y.o[t][j][r], y.o[t][j + 1][r], y.o[t][j + 2][r], y.o[t][j + 3][r]};
+        }
+        __syncthreads();
+        // a thread: D / 16 elements of column threadIdx.x / 16
+        const uint32_t cc = threadIdx.x / 16, d0 = threadIdx.x % 16 * DT;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) mm = fmaxf(mm, stat[w][0][cc]);
+        for (int t = 0; t < NT; ++t) {
+            const uint32_t col = col0 + t * 16 + cc;
+            if (col >= a.cols) continue;
+            float most = -INFINITY, sum = 0, r[DT] = {};
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, stat[t][w][0][cc]);
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
-                const float mw = stat[w][0][cc], lw = stat[w][1][cc];
-                ll += mw == -INFINITY ? lw : lw * exp2_(mw - mm);      // a sum beside no maximum is 0, or the NaN of a position without a page
+                // a wave that has seen nothing has sums of 0, or the NaN of a position without a page
+                const float m = stat[t][w][0][cc], f = m == -INFINITY ? 1.0f : exp2_(m - most);
+                sum += stat[t][w][1][cc] * f;
+#pragma unroll
+                for (int j = 0; j < DT; ++j) r[j] += sums[t][w][cc][d0 + j] * f;
             }
-            if (col < a.cols) {
-                const float inv = ll > 0 ? 1.0f / ll : ll == ll ? 0.0f : ll;
-                float r[DT];
+            const float inv = sum > 0 ? 1.0f / sum : sum == sum ? 0.0f : sum;
 #pragma unroll
-                for (int j = 0; j < DT; ++j) {
-                    float y = 0;
+            for (int j = 0; j < DT; ++j) r[j] *= inv;
+            const uint32_t i = col / a.group, h = kh * a.group + col % a.group;
+            if (whole) {
+                if (d0 == 0) a.lse[((uint64_t)b * a.heads + h) * a.q_len + i] = (most + log2_(sum)) * LN2;
+                char* to = a.o.p + b * a.o.batch + h * a.o.head + i * a.o.pos;
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) y += sums[w][cc][x0 + j];
-                    r[j] = y * inv;
-                }
-                const uint32_t i = col / a.group, h = kh * a.group + col % a.group;
-                if (whole) {
-                    if (x0 == 0) a.lse[((uint64_t)b * a.heads + h) * a.q_len + i] = (mm + log2_(ll)) * LN2;
-                    char* to = a.o.p + b * a.o.batch + h * a.o.head + i * a.o.pos;
+                for (int j = 0; j < DT; j += 4)
+                    if (d0 + j < a.dim) store4<T>(to + (d0 + j) * 2, r[j], r[j + 1], r[j + 2], r[j + 3]);
+            } else {
+                const uint64_t row = ((uint64_t)slot_of(run, e0 == begin) * a.kv_heads + kh) * a.cols + col;
+                if (d0 == 0) a.part_lse[row] = most + log2_(sum);
 #pragma unroll
-                    for (int j = 0; j < DT; j += 4)
-                        if (x0 + j < a.dim) store4<T>(to + (x0 + j) * 2, r[j], r[j + 1], r[j + 2], r[j + 3]);
-                } else {
-                    const uint64_t row = ((uint64_t)slot * a.kv_heads + kh) * a.cols + col;
-                    if (x0 == 0) a.part_lse[row] = mm + log2_(ll);
-#pragma unroll
-                    for (int j = 0; j < DT; j += 4)
-                        if (x0 + j < a.dim) *(f32x4*)(a.part + row * a.dim + x0 + j) = f32x4{r[j], r[j + 1], r[j + 2], r[j + 3]};
-                }
+                for (int j = 0; j < DT; j += 4)
+                    if (d0 + j < a.dim) *(f32x4*)(a.part + row * a.dim + d0 + j) = f32x4{r[j], r[j + 1], r[j + 2], r[j + 3]};
             }
-            __syncthreads();
         }
-        t0 = e1, first = last;
-        if (t0 >= t1) break;
+        if (t1 <= end) break;
+        __syncthreads();
     }
 }
 
@@ -444,17 +571,9 @@ __global__ __launch_bounds__(256) void k_attention_paged_join(PagedArgs a)
 {
     __shared__ Finder find;
     const uint32_t b = blockIdx.y;
-    const uint32_t per = (a.batch + 255) / 256, b0 = min(a.batch, threadIdx.x * per), b1 = min(a.batch, b0 + per);
-    int64_t mine = 0, all;
-    for (uint32_t i = b0; i < b1; ++i) mine += tiles_of(a, i);
-    const int64_t before = sum_before(mine, find, all);
-    if (b0 <= b && b < b1) {
-        int64_t f = before;
-        for (uint32_t i = b0; i < b; ++i) f += tiles_of(a, i);
-        find.first = f;
-    }
-    __syncthreads();
-    const int64_t first = find.first, n = tiles_of(a, b);
+    List list;
+    list.make(a, find);
+    const int64_t first = list.begin_of(a, b, find) + ENTRY, n = tiles_of(list.length(a, b));
     const uint32_t row = blockIdx.x * WAVES + threadIdx.x / 64, lane = threadIdx.x % 64, x = lane % 16 * 8;      // row: head * q_len + query
     if (row >= a.heads * a.q_len) return;
     const uint32_t h = row / a.q_len, i = row % a.q_len, kh = h / a.group, col = i * a.group + h % a.group;
@@ -465,8 +584,8 @@ __global__ __launch_bounds__(256) void k_attention_paged_join(PagedArgs a)
         if (lane < 16 && x < a.dim) *(uint4*)to = uint4{0, 0, 0, 0};
         return;
     }
-    const uint32_t runs = runs_used(a.runs, all);
-    const uint32_t r0 = run_of(first, runs, all), r1 = run_of(first + n - 1, runs, all);
+    const Runs runs = runs_used(a.runs, list.all);
+    const uint32_t r0 = runs.of(first), r1 = runs.of(first + n - 1);
     if (r0 == r1) return;
     auto slot_row = [&](uint32_t r) { return ((uint64_t)slot_of(r, r == r0) * a.kv_heads + kh) * a.cols + col; };
     float m = -INFINITY;
@@ -480,6 +599,7 @@ __global__ __launch_bounds__(256) void k_attention_paged_join(PagedArgs a)
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     const float base = m == -INFINITY ? 0.0f : m;
     float sum = 0, o[8] = {};
+#pragma unroll 4
     for (uint32_t r = r0 + lane / 16; r <= r1; r += 4) {
         const uint64_t at = slot_row(r);
         const float w = exp2_(a.part_lse[at] - base);
@@ -507,20 +627,22 @@ __global__ __launch_bounds__(256) void k_attention_paged_join(PagedArgs a)
 
 uint32_t column_tiles(const PagedArgs& a) { return a.cols <= 16 ? 1 : 2; }
 
-template <class T, int HELD, int D>
+template <class T, int HELD, int D, bool FULL>
 void launch(const PagedArgs& a, hipStream_t st)
 {
     const uint32_t nt = column_tiles(a);
     const dim3 grid((a.runs ? a.runs : a.batch) * a.kv_heads, (uint32_t)ceil_div(a.cols, 16 * nt));
-    if (nt == 1) k_attention_paged<T, HELD, D, 1><<<grid, 256, 0, st>>>(a);
-    else k_attention_paged<T, HELD, D, 2><<<grid, 256, 0, st>>>(a);
+    if (nt == 1) k_attention_paged<T, HELD, D, FULL, 1><<<grid, 256, 0, st>>>(a);
+    else k_attention_paged<T, HELD, D, FULL, 2><<<grid, 256, 0, st>>>(a);
 }
 
 template <class T, int HELD>
 void launch(const PagedArgs& a, hipStream_t st)
 {
-    if (a.dim <= 64) launch<T, HELD, 64>(a, st);
-    else launch<T, HELD, 128>(a, st);
+    if (a.dim == 64) launch<T, HELD, 64, true>(a, st);
+    else if (a.dim < 64) launch<T, HELD, 64, false>(a, st);
+    else if (a.dim == 128) launch<T, HELD, 128, true>(a, st);
+    else launch<T, HELD, 128, false>(a, st);
 }
 
 template <class T>

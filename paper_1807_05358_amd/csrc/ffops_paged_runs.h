@@ -13,21 +13,37 @@ namespace ffops {
 
 constexpr int TILE = 32;                    // positions of a tile
 constexpr uint32_t TILES_OF_RUN = 8;        // no run is shorter where sequences are cut
+constexpr uint32_t ENTRY = 8;               // what a run takes to begin with a sequence and to end with it, in tiles
 
-// The tiles of all sequences make one list, `all` long, of which run x takes the x-th part.  Runs in use: none is shorter than TILES_OF_RUN tiles.
-FFOPS_BOTH uint32_t runs_used(uint32_t runs, int64_t all)
-{
-    const int64_t n = (all + TILES_OF_RUN - 1) / TILES_OF_RUN;
-    return n < 1 ? 1 : n < (int64_t)runs ? (uint32_t)n : runs;
-}
-FFOPS_BOTH int64_t run_begin(uint32_t run, uint32_t runs, int64_t all) { return (int64_t)run * all / runs; }
+// The tiles of all sequences, each with ENTRY tiles that there are not before its own, make one list, `all` long, which is dealt in runs, one behind the other, the first ones a tile longer where it does not come out even.  Runs in use: none is
+// shorter than TILES_OF_RUN tiles.
+struct Runs {
+    uint32_t n;
+    uint32_t longer;        // runs of each + 1 tiles
+    int64_t each;
+    FFOPS_BOTH int64_t begin(uint32_t run) const { return run * each + (run < longer ? run : longer); }
+    // the run that holds a tile
+    FFOPS_BOTH uint32_t of(int64_t tile) const
+    {
+        const int64_t first = longer * (each + 1);
+        return tile < first ? quotient(tile, each + 1) : longer + quotient(tile - first, each);
+    }
+    static FFOPS_BOTH uint32_t quotient(int64_t a, int64_t b)      // the wide division takes a hundred instructions
+    {
+        return (uint64_t)(a | b) >> 32 ? (uint32_t)((uint64_t)a / (uint64_t)b) : (uint32_t)a / (uint32_t)b;
+    }
+};
+// the places of a sequence of nk positions in the list
+FFOPS_BOTH uint32_t tiles_of(int nk) { return ((uint32_t)nk + TILE - 1) / TILE; }
+FFOPS_BOTH uint32_t places_of(int nk) { return nk ? ENTRY + tiles_of(nk) : 0; }
 
-// the run that holds a tile
-FFOPS_BOTH uint32_t run_of(int64_t tile, uint32_t runs, int64_t all)
+FFOPS_BOTH Runs runs_used(uint32_t runs, int64_t all)
 {
-    uint32_t r = (uint32_t)(tile * runs / all);
-    while (run_begin(r + 1, runs, all) <= tile) ++r;
-    while (run_begin(r, runs, all) > tile) --r;
+    const int64_t most = (all + TILES_OF_RUN - 1) / TILES_OF_RUN;
+    Runs r;
+    r.n = most < 1 ? 1 : most < (int64_t)runs ? (uint32_t)most : runs;
+    r.each = (uint64_t)all >> 32 ? (int64_t)((uint64_t)all / r.n) : (int64_t)((uint32_t)all / r.n);
+    r.longer = (uint32_t)(all - r.each * r.n);
     return r;
 }
 
@@ -43,7 +59,7 @@ inline uint32_t runs_of(uint64_t others, uint64_t batch, uint64_t positions)
 {
     const uint64_t tiles = (positions + TILE - 1) / TILE;
     if (tiles <= 8 || others * batch >= 4096) return 0;
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(1024 / others, (tiles * batch + TILES_OF_RUN - 1) / TILES_OF_RUN));
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / others, (tiles * batch + TILES_OF_RUN - 1) / TILES_OF_RUN));
 }
 
 }  // namespace ffops

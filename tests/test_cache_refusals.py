@@ -131,9 +131,9 @@ int main()
     char what;
     long long a, b, c;
     while (scanf(" %c %lld %lld %lld", &what, &a, &b, &c) == 4) {{
-        if (what == 'u') printf("%u\\n", runs_used((uint32_t)a, b));
-        else if (what == 'b') printf("%lld\\n", (long long)run_begin((uint32_t)a, (uint32_t)b, c));
-        else if (what == 'o') printf("%u\\n", run_of(a, (uint32_t)b, c));
+        if (what == 'u') printf("%u\\n", runs_used((uint32_t)a, b).n);
+        else if (what == 'b') printf("%lld\\n", (long long)runs_used((uint32_t)b, c).begin((uint32_t)a));
+        else if (what == 'o') printf("%u\\n", runs_used((uint32_t)b, c).of(a));
         else if (what == 'e') printf("%u\\n", entry_of((int)a, (int)b, (uint32_t)c));
         else if (what == 'p') printf("%u\\n", place_of((int)a, (int)b, (uint32_t)c));
         else printf("%u\\n", runs_of(a, b, c));
@@ -152,7 +152,7 @@ def test_runs_cover_every_tile_once(ask):
     """every tile is in one run, every run has one, run_of finds it; also where the list is far beyond 32 bits"""
     rng = random.Random(4)
     for _ in range(60):
-        runs, all_ = rng.choice([1, 2, 7, 64, 1024]), rng.choice([1, 7, 8, 9, 100, 8191, rng.randint(1, 5000), 65535 << 23])
+        runs, all_ = rng.choice([1, 2, 7, 64, 1024]), rng.choice([1, 7, 8, 9, 100, 8191, rng.randint(1, 5000), (1 << 32) + 5, 65535 << 23])
         used = ask([("u", runs, all_, 0)])[0]
         assert 1 <= used <= runs and used <= max(1, -(-all_ // 8))
         begins = ask([("b", r, used, all_) for r in range(used + 1)])
@@ -174,6 +174,6 @@ def test_places_are_within_the_table_and_the_page(ask):
 
 
 def test_sequences_are_cut_only_where_blocks_are_few(ask):
-    assert ask([("r", 8, 8, 16384)]) == [128]
+    assert ask([("r", 8, 8, 16384)]) == [64]
     assert ask([("r", 8, 1, 256)]) == [0] and ask([("r", 64, 64, 16384)]) == [0] and ask([("r", 5000, 1, 16384)]) == [0]
     assert ask([("r", 1, 1, 288)]) == [2] and ask([("r", 2000, 1, 16384)]) == [1]
