@@ -26,6 +26,7 @@ struct SampleArgs {
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int BINS = 4096, BELOW = 2816;    // bins; those below the anchor
 constexpr int MOST = 2 * THREADS;           // words of the bins that decide
+constexpr uint32_t NONE = 0xffffffffu;      // no word
 
 // Logits as whole numbers in the same order, -0 as 0.
 template <class T>
@@ -216,66 +217,78 @@ __device__ void choose_by_digits(const typename T::elem* z, uint32_t V, float mo
     word = sh.word, logprob = (float)log(w.of(chosen) / ((double)mass / w.unit));
 }
 
-// sixteen bytes of a row at any element's place
+// sixteen bytes of a row at any element's place; -inf behind its end
 template <class T>
 struct Piece {
     typedef typename T::elem vec __attribute__((ext_vector_type(T::VEC), aligned(sizeof(typename T::elem))));
     vec v;
+    __device__ __forceinline__ void load(const typename T::elem* z, uint32_t i, uint32_t V)
+    {
+        if (i + T::VEC <= V) {
+            v = *(const vec*)(z + i);
+        } else {
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e) v[e] = i + e < V ? z[i + e] : (typename T::elem)(-INFINITY);
+        }
+    }
 };
 
-constexpr int AHEAD = 4;        // pieces that a thread asks for at once
-
-// calls f(element, its number) for all of a row's elements, a thread's in the order of their numbers
-template <class T, class F>
-__device__ __forceinline__ void for_each(const typename T::elem* z, uint32_t V, F f)
-{
-    constexpr uint32_t STEP = THREADS * T::VEC;
-    uint32_t i = threadIdx.x * T::VEC;
-    for (; i + (AHEAD - 1) * STEP + T::VEC <= V; i += AHEAD * STEP) {
-        Piece<T> p[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) p[k].v = *(const typename Piece<T>::vec*)(z + i + k * STEP);
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-#pragma unroll
-            for (int e = 0; e < T::VEC; ++e) f((float)p[k].v[e], i + k * STEP + e);
+// a thread's first pieces, and all of a row's elements: each calls f(element, its number), a thread's in the order of their numbers, two pieces ahead of what is worked
+template <class T>
+struct Row {
+    const typename T::elem* z;
+    uint32_t V;
+    Piece<T> first[2];
+    __device__ __forceinline__ Row(const typename T::elem* z_, uint32_t V_) : z(z_), V(V_)
+    {
+        first[0].load(z, threadIdx.x * T::VEC, V);
+        first[1].load(z, (threadIdx.x + THREADS) * T::VEC, V);
     }
-    for (; i + T::VEC <= V; i += STEP) {
-        const typename Piece<T>::vec p = *(const typename Piece<T>::vec*)(z + i);
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        Piece<T> now = first[0], next = first[1];
+        uint32_t i = threadIdx.x * T::VEC;
+        for (uint32_t base = 0; base < V; base += THREADS * T::VEC) {
+            Piece<T> later;
+            later.load(z, i + 2 * THREADS * T::VEC, V);
 #pragma unroll
-        for (int e = 0; e < T::VEC; ++e) f((float)p[e], i + e);
+            for (int e = 0; e < T::VEC; ++e) f((float)now.v[e], i + e);
+            now = next, next = later;
+            i += THREADS * T::VEC;
+        }
     }
-    for (; i < V; ++i) f((float)z[i], i);
-}
+};
 
-// The bins of a row.
+// The bins of a row; the anchor, a finite logit, is at the lower edge of bin BELOW.
 struct Bins {
-    float anchor;
-    double per_logit, per_nat;      // bins in a unit of the logits, and of the exponent
-    double c[7];                    // e^(x / per_nat) as a sum of powers of x
+    double anchor, per_logit, per_nat;      // bins in a unit of the logits, and of the exponent
+    double c[6];                            // 1.25 e^(r / per_nat) as a sum of powers of r
 
     __device__ void set(float anchor_, double temperature, double per_nat_)
     {
         anchor = anchor_, per_nat = per_nat_, per_logit = per_nat / temperature;
-        c[0] = 1;
+        // five powers of r - 0.5, off by 2^-45 at r = 0 and 1, put in order of those of r
+        const double h = 1 / per_nat, half = 1.25 * exp(0.5 * h);
+        double a[6] = {half};
 #pragma unroll
-        for (int k = 1; k < 7; ++k) c[k] = c[k - 1] / (per_nat * k);
+        for (int k = 1; k < 6; ++k) a[k] = a[k - 1] * h * (1.0 / k);
+#pragma unroll
+        for (int k = 0; k < 6; ++k) c[k] = a[k];
+#pragma unroll
+        for (int n = 0; n < 5; ++n)
+#pragma unroll
+            for (int k = 4; k >= n; --k) c[k] -= 0.5 * c[k + 1];
     }
-    // the place of a logit, in bins above the anchor's lower edge
-    __device__ __forceinline__ double place(float z) const { return z == anchor ? 0.0 : ((double)z - (double)anchor) * per_logit; }
-    // e^(r / per_nat) of 0 <= r < 1 in steps of 2^-shift, cut off
+    // the place of a logit in bins
+    __device__ __forceinline__ double place(float z) const { return fma((double)z - anchor, per_logit, (double)BELOW); }
+    // 1.25 e^(r / per_nat), 0 <= r < 1, in steps of 2^-shift, cut off: between 1 and 2, so its fraction's bits are what is wanted
     __device__ __forceinline__ uint64_t steps(double r, int shift) const
     {
-        double e = c[6];
+        double e = c[5];
 #pragma unroll
-        for (int k = 5; k >= 0; --k) e = fma(e, r, c[k]);
-        return (__builtin_bit_cast(uint64_t, e) & 0xfffffffffffffull | 1ull << 52) >> (52 - shift);
-    }
-    // the weight of a bin's lower edge beside that of logit z
-    __device__ double edge(int bin, float z, double temperature) const
-    {
-        const double shift = z == anchor ? 0.0 : ((double)anchor - (double)z) / temperature;
-        return exp((bin - BELOW) / per_nat + shift);
+        for (int k = 4; k >= 0; --k) e = fma(e, r, c[k]);
+        return ((__builtin_bit_cast(uint64_t, e) & 0xfffffffffffffull) | 1ull << 52) >> (52 - shift);
     }
 };
 
@@ -326,6 +339,11 @@ __device__ Range bins_of(double lo, double hi, double all, Shared& sh)
 
 constexpr double SLACK = 1e-11;     // of sums: what roundings, and words that do not count, can move them
 
+__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+
 template <class T>
 __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
 {
@@ -341,10 +359,11 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
         return;
     }
+    const Row<T> all_of(z, V);
     if (temperature == 0) {         // the largest key, of these the lowest number
         uint64_t first = 0;
         uint32_t nan = 0;
-        for_each<T>(z, V, [&](float x, uint32_t i) {
+        all_of.each([&](float x, uint32_t i) {
             nan |= x != x;
             const uint64_t k = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
             first = k > first ? k : first;
@@ -355,213 +374,289 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         if (tid == 0) a.words[row] = any ? (int32_t)(0xffffffffu - (uint32_t)first) : -1, a.logprob[row] = any ? 0.0f : NAN;
         return;
     }
-    // the anchor: the largest of each thread's first elements
+    // the anchor: the largest of what is read first
     float most = -INFINITY;
-    for (uint32_t i = tid; i < min(V, (uint32_t)(4 * THREADS)); i += THREADS) most = fmaxf(most, (float)z[i]);
+#pragma unroll
+    for (int e = 0; e < T::VEC; ++e) most = fmaxf(most, fmaxf((float)all_of.first[0].v[e], (float)all_of.first[1].v[e]));
     most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
     int shift = 51;
     while (((1ull << 63) >> (shift + 1)) < V) --shift;
     Bins bins;
-    double per_nat = 32;
-    while (per_nat < 1024 && per_nat * 2 <= 64 * (double)temperature) per_nat *= 2;
-    bins.set(most, temperature, per_nat);
+    int per_nat = 32;
+    while (per_nat < 1024 && per_nat * 2 <= 64 * temperature) per_nat *= 2;
+    uint32_t word = NONE;
+    float logprob = NAN;
     for (;;) {
-        for (int b = tid; b < BINS; b += THREADS) sh.steps[b] = 0, sh.count[b] = 0;
+        if (!(most > -INFINITY && most < INFINITY)) {       // no anchor: the largest of all, which may be infinite, or a row without one
+            most = -INFINITY;
+            uint32_t nan = 0;
+            all_of.each([&](float x, uint32_t) { most = fmaxf(most, x), nan |= x != x; });
+            most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
+            nan = block_sum(nan, sh.c);
+            if (nan || most == -INFINITY) {
+                if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
+                return;
+            }
+            if (most == INFINITY) break;
+        }
+        bins.set(most, temperature, per_nat);
+        for (int b = tid; b < BINS; b += THREADS) sh.steps[b] = 0;
+        if (top_k)
+            for (int b = tid; b < BINS; b += THREADS) sh.count[b] = 0;
         if (tid == 0) sh.again = 0;
         __syncthreads();
         most = -INFINITY;
         uint32_t again = 0;         // 1: a NaN, 2: above the bins, 4: below them and not yet without weight
-        const double light = -42 * bins.per_nat;
-        for_each<T>(z, V, [&](float x, uint32_t) {
+        const double light = BELOW - 42.0 * per_nat;
+        const auto add = [&](float x, uint32_t) {
             most = fmaxf(most, x);
-            const double at = bins.place(x), whole = floor(at);
-            if (x != x) again |= 1;
-            if (at >= BINS - BELOW) again |= 2;
-            else if (at >= -BELOW) {
-                const int b = (int)whole + BELOW;
-                add_lds(&sh.steps[b], bins.steps(at - whole, shift));
-                if (top_k) add_lds(&sh.count[b], 1u);
-            } else if (at > light) again |= 4;
-        });
+            const double at = bins.place(x);
+            int b = (int)at;                                // towards 0; 0 of a NaN
+            if ((uint32_t)(b - 1) >= BINS - 1) {            // not one of the bins above the lowest
+                if (x != x) again |= 1;
+                else if (b >= BINS) again |= 2;
+                else if (at < 0 && at > light) again |= 4;
+                if (b || !(at >= 0)) return;
+            }
+            add_lds(&sh.steps[b], bins.steps(__builtin_amdgcn_fract(at), shift));
+            if (top_k) add_lds(&sh.count[b], 1u);
+        };
+        all_of.each(add);
         again = __any(again & 1) * 1 | __any(again & 2) * 2 | __any(again & 4) * 4;
         if (again && tid % 64 == 0) __hip_atomic_fetch_or(&sh.again, again, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
         most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
         again = sh.again;
         __syncthreads();
-        if ((again & 1) || most == -INFINITY) {
+        if (again & 1) {
             if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
             return;
         }
         if (!(again & 6)) break;
-        bins.set(most, temperature, again & 2 ? bins.per_nat : 64);       // with 64 and the largest logit as the anchor neither comes again
+        if (!(again & 2)) per_nat = 64;     // with that, and the largest logit as the anchor, neither comes again
     }
-    // weights of all bins above each, beside the largest word's, which is 1; a thread has four bins, the first thread the highest
-    constexpr int EACH = BINS / THREADS;
-    double all;
-    uint32_t words_all = 0;
-    {
-        double w[EACH], mine = 0;
-        uint32_t n[EACH], own = 0;
+    if (most < INFINITY) {
+        // weights of all bins above each, beside the largest word's, which is 1; a thread has four bins, the first thread the highest
+        constexpr int EACH = BINS / THREADS;
+        double all;
+        uint32_t words_all = 0;
+        {
+            double w[EACH], mine = 0;
+            uint32_t n[EACH], own = 0;
+            const double h = 1.0 / per_nat, less = exp(-h);
+            double edge = ldexp(0.8, -shift) * exp((double)(BINS - 1 - BELOW - (int)(tid * EACH)) * h + (bins.anchor - (double)most) / temperature);
 #pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-            const int b = BINS - 1 - (int)(tid * EACH + k);
-            w[k] = sh.steps[b] ? (double)sh.steps[b] * ldexp(bins.edge(b, most, temperature), -shift) : 0;
-            n[k] = sh.count[b];
-            mine += w[k], own += n[k];
-        }
-        double before = block_before(mine, sh.d, all);
-        uint32_t words_before = top_k ? block_before(own, sh.c, words_all) : 0;
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-            const int b = BINS - 1 - (int)(tid * EACH + k);
-            sh.above[b] = before, sh.count[b] = words_before;
-            if (words_before < top_k && top_k <= words_before + n[k]) sh.found = b;
-            before += w[k], words_before += n[k];
-        }
-        __syncthreads();
-    }
-    const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
-    // what each border leaves, from..to, and the bins it can lie in
-    const bool by_k = top_k && words_all >= top_k;      // otherwise words without weight make up the rest
-    double k_lo = all, k_hi = all;
-    const int k_bin = by_k ? (int)sh.found : -1;
-    if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
-    Range p_bins = {1, 0}, m_bins = {1, 0};
-    double p_lo = k_lo, p_hi = k_hi;
-    if (top_p < 1) {
-        const double p = top_p > 0 ? (double)top_p : 0.0;
-        p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
-        p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
-    }
-    double m_lo = all, m_hi = all;
-    if (min_p > 0) {
-        const double at = (log((double)min_p) * bins.per_nat) + bins.place(most);
-        const int lo = (int)floor(fmax(at - 1e-6, -1.0 * BELOW)) + BELOW, hi = (int)floor(fmax(at + 1e-6, -1.0 * BELOW)) + BELOW;
-        m_bins = {min(lo, BINS - 1), min(hi, BINS - 1)};
-        m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
-    }
-    const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
-    // borders that others come before do not count
-    if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
-    const bool no_p = p_lo > hi * (1 + SLACK);
-    if (no_p) p_bins = {1, 0};
-    const bool need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
-    const double share = u < 0 ? 0.0 : u < 1 ? (double)u : 1.0;
-    const Range u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
-    const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
-    // their words
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    {
-        int least = u_bins.lo;
-        if (need_k) least = min(least, k_bin);
-        if (p_bins.lo <= p_bins.hi) least = min(least, p_bins.lo);
-        if (m_bins.lo <= m_bins.hi) least = min(least, m_bins.lo);
-        const double from = least - BELOW;
-        for_each<T>(z, V, [&](float x, uint32_t i) {
-            const double at = bins.place(x);
-            if (at >= from && decides((int)floor(at) + BELOW)) {
-                const uint32_t n = atomicAdd(&sh.n, 1u);
-                if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+            for (int k = 0; k < EACH; ++k) {
+                const int b = BINS - 1 - (int)(tid * EACH + k);
+                w[k] = (double)sh.steps[b] * edge, n[k] = top_k ? sh.count[b] : 0;
+                mine += w[k], own += n[k];
+                edge *= less;
             }
-        });
-    }
-    __syncthreads();
-    const uint32_t n = sh.n;
-    uint32_t word = 0xffffffffu;
-    float logprob = NAN;
-    if (n && n <= MOST) {
-        // sorted, the largest first
-        uint32_t size = 128;
-        while (size < n) size *= 2;
-        for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
+            double before = block_before(mine, sh.d, all);
+            uint32_t words_before = top_k ? block_before(own, sh.c, words_all) : 0;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int b = BINS - 1 - (int)(tid * EACH + k);
+                sh.above[b] = before;
+                if (top_k) sh.count[b] = words_before;
+                if (words_before < top_k && top_k <= words_before + n[k]) sh.found = b;
+                before += w[k], words_before += n[k];
+            }
+            __syncthreads();
+        }
+        const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
+        // what each border leaves, from..to, and the bins it can lie in
+        const bool by_k = top_k && words_all >= top_k;      // otherwise words without weight make up the rest
+        double k_lo = all, k_hi = all;
+        const int k_bin = by_k ? (int)sh.found : -1;
+        if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
+        Range p_bins = {1, 0}, m_bins = {1, 0};
+        double p_lo = k_lo, p_hi = k_hi;
+        if (top_p < 1) {
+            const double p = top_p > 0 ? (double)top_p : 0.0;
+            p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
+            p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
+        }
+        double m_lo = all, m_hi = all;
+        if (min_p > 0) {
+            const double at = fmax(log((double)min_p) * per_nat + bins.place(most), 0.0);
+            m_bins = {min((int)fmax(at - 1e-6, 0.0), BINS - 1), min((int)(at + 1e-6), BINS - 1)};
+            m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
+        }
+        const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
+        // borders that others come before do not count
+        if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
+        const bool no_p = p_lo > hi * (1 + SLACK);
+        if (no_p) p_bins = {1, 0};
+        const bool need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
+        const double share = u < 0 ? 0.0 : u < 1 ? (double)u : 1.0;
+        const Range u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
+        const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
+        // their words
+        if (tid == 0) sh.n = 0;
         __syncthreads();
-        for (uint32_t k = 2; k <= size; k *= 2)
-            for (uint32_t j = k / 2; j; j /= 2) {
-                if (tid < size / 2) {
-                    const uint32_t i = (tid / j * 2 * j) + tid % j;
-                    const uint64_t x = sh.list[i], y = sh.list[i + j];
-                    if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
+        {
+            int least = u_bins.lo;
+            if (need_k) least = min(least, k_bin);
+            if (p_bins.lo <= p_bins.hi) least = min(least, p_bins.lo);
+            if (m_bins.lo <= m_bins.hi) least = min(least, m_bins.lo);
+            // a logit that no word of these bins is below: most of the words are
+            const double edge = bins.anchor + (least - BELOW) / bins.per_logit;
+            const float from = (float)(edge - fabs(edge) * 1e-6 - 1e-30);
+            const auto take = [&](float x, uint32_t i) {
+                if (!(x >= from)) return;
+                const double at = bins.place(x);
+                if (at >= least && decides((int)at)) {
+                    const uint32_t n = atomicAdd(&sh.n, 1u);
+                    if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
                 }
-                if (size > 128) __syncthreads();
-                else asm volatile("" ::: "memory");         // one wave, whose accesses to LDS are done in their order
-            }
+            };
+            all_of.each(take);
+        }
         __syncthreads();
-        // a thread has two neighbours: their weights, the weight before them, their rank
+        const uint32_t n = sh.n;
         const Weigh weigh = {most, (double)temperature, 1.0};
-        double w[2], before[2];
-        int bin[2];
-        uint32_t rank[2];
-        bool in[2];
+        if (n <= 64) {
+            // one wave, a word a lane
+            if (tid < 64) {
+                const int lane = tid;
+                bool in = lane < (int)n;
+                uint64_t x = in ? sh.list[lane] : 0;
+                uint32_t place = 0;
+                for (uint32_t j = 0; j < n; ++j) place += read_lane(x, j) > x;
+                if (in) sh.list[place] = x;
+                asm volatile("" ::: "memory");      // a wave's accesses to LDS are done in their order
+                x = in ? sh.list[lane] : 0;
+                const float f = Key<F32>::value((uint32_t)(x >> 32));
+                const double w = in ? weigh.of(f) : 0;
+                const int bin = in ? (int)bins.place(f) : -1;
+                double sum = w;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t i = 2 * tid + e;
-            in[e] = i < n;
-            const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
-            bin[e] = in[e] ? (int)floor(bins.place(x)) + BELOW : -1;
-            w[e] = in[e] ? weigh.of(x) : 0;
-        }
-        double sum_all;
-        const double sum = block_before(w[0] + w[1], sh.d, sum_all);
-        // where each bin's words begin in the list, and the sum there: steps of other bins are not needed any more, but their sums above are
-        __syncthreads();
+                for (int d = 1; d < 64; d *= 2) {
+                    const double t = __shfl_up(sum, d);
+                    if (lane >= d) sum += t;
+                }
+                // the first word of the lane's bin in the list
+                const int prev = __shfl_up(bin, 1);
+                const uint64_t heads = __ballot(in && (lane == 0 || prev != bin)) & ~0ull >> (63 - lane);
+                const int head = heads ? 63 - __builtin_clzll(heads) : 0;
+                const double before = (in ? sh.above[bin] : 0) + (sum - w) - __shfl(sum - w, head), to = before + w;
+                double left = all;
+                if (need_k) left = __shfl(to, __builtin_ctzll(__ballot(in && sh.count[in ? bin : 0] + lane - head == top_k - 1) | 1ull << 63));
+                bool found = true;
+                if (p_bins.lo <= p_bins.hi) {
+                    const double target = top_p > 0 ? (double)top_p * left : 0.0;
+                    const uint64_t at = __ballot(in && bin >= p_bins.lo && bin <= p_bins.hi && (before < target || before == 0) && !(to < target));
+                    found = at != 0;
+                    left = fmin(left, __shfl(to, at ? __builtin_ctzll(at) : 0));
+                }
+                if (m_bins.lo <= m_bins.hi) {
+                    double m = in && bin >= m_bins.lo && bin <= m_bins.hi && w >= (double)min_p ? to : 0;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const uint32_t i = 2 * tid + e;
-            before[e] = sum + (e ? w[0] : 0.0);
-            if (!in[e]) continue;
-            const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
-            if (i == 0 || (int)floor(bins.place(prev)) + BELOW != bin[e]) {     // one thread for each bin
-                sh.above[bin[e]] -= before[e];
-                sh.count[bin[e]] -= i;
+                    for (int d = 32; d; d >>= 1) m = fmax(m, __shfl_xor(m, d));
+                    left = fmin(left, fmax(m, m_lo));
+                }
+                const double target = fmin(share, 1 - 1e-14) * left;
+                const uint64_t at = __ballot(in && bin >= u_bins.lo && bin <= u_bins.hi && before <= target && target < to);
+                if (lane == 0) sh.word = NONE;
+                if (found && at && lane == (int)__builtin_ctzll(at)) {
+                    sh.word = 0xffffffffu - (uint32_t)x;
+                    a.words[row] = (int32_t)sh.word, a.logprob[row] = (float)log(w / left);
+                }
             }
-        }
-        __syncthreads();
+            __syncthreads();
+            if (sh.word != NONE) return;
+        } else if (n <= MOST) {
+            // sorted, the largest first
+            uint32_t size = 128;
+            while (size < n) size *= 2;
+            for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
+            __syncthreads();
+            for (uint32_t k = 2; k <= size; k *= 2)
+                for (uint32_t j = k / 2; j; j /= 2) {
+                    if (tid < size / 2) {
+                        const uint32_t i = (tid / j * 2 * j) + tid % j;
+                        const uint64_t x = sh.list[i], y = sh.list[i + j];
+                        if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
+                    }
+                    if (size > 128) __syncthreads();
+                    else asm volatile("" ::: "memory");         // one wave, whose accesses to LDS are done in their order
+                }
+            __syncthreads();
+            // a thread has two neighbours: their weights, the weight before them, their rank
+            double w[2], before[2];
+            int bin[2];
+            uint32_t rank[2];
+            bool in[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (in[e]) before[e] += sh.above[bin[e]], rank[e] = sh.count[bin[e]] + 2 * tid + e;
-        // the borders, exactly
-        double left = all;
-        if (need_k) {
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t i = 2 * tid + e;
+                in[e] = i < n;
+                const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
+                bin[e] = in[e] ? (int)bins.place(x) : -1;
+                w[e] = in[e] ? weigh.of(x) : 0;
+            }
+            double sum_all;
+            const double sum = block_before(w[0] + w[1], sh.d, sum_all);
+            // where each bin's words begin in the list, and the sum there: steps of other bins are not needed any more, but their sums above are
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t i = 2 * tid + e;
+                before[e] = sum + (e ? w[0] : 0.0);
+                if (!in[e]) continue;
+                const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
+                if (i == 0 || (int)bins.place(prev) != bin[e]) {     // one thread for each bin
+                    sh.above[bin[e]] -= before[e];
+                    sh.count[bin[e]] -= i;
+                }
+            }
+            __syncthreads();
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                if (in[e] && rank[e] == top_k - 1) sh.value = before[e] + w[e];
+                if (in[e]) before[e] += sh.above[bin[e]], rank[e] = sh.count[bin[e]] + 2 * tid + e;
+            // the borders, exactly
+            double left = all;
+            if (need_k) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (in[e] && rank[e] == top_k - 1) sh.value = before[e] + w[e];
+                __syncthreads();
+                left = sh.value;
+            }
+            if (p_bins.lo <= p_bins.hi) {
+                const double target = top_p > 0 ? (double)top_p * left : 0.0;
+                __syncthreads();
+                if (tid == 0) sh.value = -1;
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (in[e] && bin[e] >= p_bins.lo && bin[e] <= p_bins.hi && (before[e] < target || before[e] == 0) && !(before[e] + w[e] < target)) sh.value = before[e] + w[e];
+                __syncthreads();
+                left = fmin(left, sh.value);        // below 0: between two bins, by roundings; no word is found then
+            }
+            if (m_bins.lo <= m_bins.hi) {
+                // the words before the bins, and those of them that weigh enough
+                double m = 0;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (in[e] && bin[e] >= m_bins.lo && bin[e] <= m_bins.hi && w[e] >= (double)min_p) m = fmax(m, before[e] + w[e]);
+                m = __builtin_bit_cast(double, block_max(__builtin_bit_cast(uint64_t, m), sh.a));
+                left = fmin(left, fmax(m, m_lo));
+            }
+            const double target = fmin(share, 1 - 1e-14) * left;
             __syncthreads();
-            left = sh.value;
-        }
-        if (p_bins.lo <= p_bins.hi) {
-            const double target = top_p > 0 ? (double)top_p * left : 0.0;
-            __syncthreads();
-            if (tid == 0) sh.value = -1;
+            if (tid == 0) sh.word = NONE;
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                if (in[e] && bin[e] >= p_bins.lo && bin[e] <= p_bins.hi && (before[e] < target || before[e] == 0) && !(before[e] + w[e] < target)) sh.value = before[e] + w[e];
+                if (in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
             __syncthreads();
-            left = fmin(left, sh.value);        // below 0: between two bins, by roundings; no word is found then
+            word = sh.word;
+            if (word != NONE) logprob = (float)log(sh.weight / left);
         }
-        if (m_bins.lo <= m_bins.hi) {
-            // the words before the bins, and those of them that weigh enough
-            double m = 0;
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (in[e] && bin[e] >= m_bins.lo && bin[e] <= m_bins.hi && w[e] >= (double)min_p) m = fmax(m, before[e] + w[e]);
-            m = __builtin_bit_cast(double, block_max(__builtin_bit_cast(uint64_t, m), sh.a));
-            left = fmin(left, fmax(m, m_lo));
-        }
-        const double target = fmin(share, 1 - 1e-14) * left;
-        __syncthreads();
-        if (tid == 0) sh.word = 0xffffffffu;
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
-        __syncthreads();
-        word = sh.word;
-        if (word != 0xffffffffu) logprob = (float)log(sh.weight / left);
     }
-    if (word == 0xffffffffu) {
+    if (word == NONE) {
         __syncthreads();
         choose_by_digits<T>(z, V, most, temperature, top_k_, top_p, min_p, u, sh, word, logprob);
     }
