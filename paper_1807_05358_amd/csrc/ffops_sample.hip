@@ -18,9 +18,9 @@ struct SampleArgs {
 
 // A block takes a row.  It reads it twice: once to sum weights in bins of logits, once for the few words of the bins that decide; these are sorted and gone through with exact sums.  What
 // bounds it is the first reading: 24 instructions an element, a third of them in 64 bits, and an addition in LDS.
-//   Bins are 1 / per_nat wide in units of the temperature, from an anchor on, the largest logit of what the block's threads read first.  A word weighs e^r 2^-shift steps, r its place
-// in its bin: whole numbers, whose sums do not depend on an order, to 2^-shift of the weight whatever its size.  Sums of bins are in 64-bit floats.  Where the anchor was too low, or words beyond the lowest bin
-// weigh more than e^-42, the row is read again with other bins; words that weigh less than that beside the largest do not count.
+//   Bins are 1 / per_nat wide in units of the temperature, from an anchor on, the largest logit of what the block's threads read first.  A word weighs 2^29 e^r steps, r its place
+// in its bin: whole numbers, whose sums do not depend on an order, to 2^-30 of the weight whatever its size, one way or the other.  Sums of bins are in 64-bit floats.  Where the anchor was too low, or words may lie beyond the lowest bin
+// that weigh more than e^-44, the row is read again with other bins; words that weigh less than that beside the largest do not count.
 //   The bins that decide are those in which the border of top_k, that of top_p, that of min_p and the chosen word can lie; they depend on one another, so each is a range
 // until the words are there.  Bins with more than MOST words (equal logits, or nearly so) are left to select(), which reads the row for every eight bits of the key of each border.
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
@@ -68,10 +68,10 @@ struct Digits {
 
 struct Shared {
     union {
-        uint64_t steps[BINS];       // a bin's sum, then:
+        uint64_t steps[BINS + 2];   // a bin's sum, at its number + 1; at the ends what is beyond the bins; then:
         double above[BINS];         // the weight of all bins above it
     };
-    uint32_t count[BINS];           // words, then those of all bins above; top_k alone
+    uint32_t count[BINS + 2];       // words, likewise, then those of all bins above; top_k alone
     union {
         uint64_t list[MOST];        // key and number of each word of the bins that decide
         Digits digits;
@@ -233,63 +233,72 @@ struct Piece {
     }
 };
 
-// a thread's first pieces, and all of a row's elements: each calls f(element, its number), a thread's in the order of their numbers, two pieces ahead of what is worked
+constexpr int GROUP = 2;        // pieces that a thread works between loads; two more groups are on their way (one piece and two: 256 rows of 131071 69 us, so 62)
+
+// a thread's first pieces, and all of a row's elements: each calls f(element, its number), a thread's in the order of their numbers
 template <class T>
 struct Row {
+    static constexpr uint32_t STEP = THREADS * T::VEC;
     const typename T::elem* z;
     uint32_t V;
-    Piece<T> first[2];
+    Piece<T> first[2 * GROUP];
     __device__ __forceinline__ Row(const typename T::elem* z_, uint32_t V_) : z(z_), V(V_)
     {
-        first[0].load(z, threadIdx.x * T::VEC, V);
-        first[1].load(z, (threadIdx.x + THREADS) * T::VEC, V);
+#pragma unroll
+        for (int k = 0; k < 2 * GROUP; ++k) first[k].load(z, threadIdx.x * T::VEC + k * STEP, V);
+    }
+    // f(piece, number of its first element)
+    template <class F>
+    __device__ __forceinline__ void each_piece(F f) const
+    {
+        Piece<T> now[2 * GROUP];
+#pragma unroll
+        for (int k = 0; k < 2 * GROUP; ++k) now[k] = first[k];
+        uint32_t i = threadIdx.x * T::VEC;
+        for (uint32_t base = 0; base < V; base += GROUP * STEP) {
+            Piece<T> later[GROUP];
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) later[k].load(z, i + (2 * GROUP + k) * STEP, V);
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) f(now[k], i + k * STEP);
+#pragma unroll
+            for (int k = 0; k < GROUP; ++k) now[k] = now[GROUP + k], now[GROUP + k] = later[k];
+            i += GROUP * STEP;
+        }
     }
     template <class F>
     __device__ __forceinline__ void each(F f) const
     {
-        Piece<T> now = first[0], next = first[1];
-        uint32_t i = threadIdx.x * T::VEC;
-        for (uint32_t base = 0; base < V; base += THREADS * T::VEC) {
-            Piece<T> later;
-            later.load(z, i + 2 * THREADS * T::VEC, V);
+        each_piece([&](const Piece<T>& p, uint32_t i) {
 #pragma unroll
-            for (int e = 0; e < T::VEC; ++e) f((float)now.v[e], i + e);
-            now = next, next = later;
-            i += THREADS * T::VEC;
-        }
+            for (int e = 0; e < T::VEC; ++e) f((float)p.v[e], i + e);
+        });
     }
 };
 
 // The bins of a row; the anchor, a finite logit, is at the lower edge of bin BELOW.
 struct Bins {
-    double anchor, per_logit, per_nat;      // bins in a unit of the logits, and of the exponent
-    double c[6];                            // 1.25 e^(r / per_nat) as a sum of powers of r
+    double anchor, per_logit, width;        // bins in a unit of the logits, and its inverse
+    float c[4];                             // 2^29 (e^(r / per_nat) - 1) as a sum of powers of r, and 0.5
 
-    __device__ void set(float anchor_, double temperature, double per_nat_)
+    __device__ __forceinline__ void set(float anchor_, float temperature, int per_nat)
     {
-        anchor = anchor_, per_nat = per_nat_, per_logit = per_nat / temperature;
-        // five powers of r - 0.5, off by 2^-45 at r = 0 and 1, put in order of those of r
-        const double h = 1 / per_nat, half = 1.25 * exp(0.5 * h);
-        double a[6] = {half};
-#pragma unroll
-        for (int k = 1; k < 6; ++k) a[k] = a[k - 1] * h * (1.0 / k);
-#pragma unroll
-        for (int k = 0; k < 6; ++k) c[k] = a[k];
-#pragma unroll
-        for (int n = 0; n < 5; ++n)
-#pragma unroll
-            for (int k = 4; k >= n; --k) c[k] -= 0.5 * c[k + 1];
+        anchor = anchor_, per_logit = per_nat / (double)temperature, width = (double)temperature / per_nat;
+        const float h = 1.0f / per_nat;
+        c[0] = 0x1p29f * h, c[1] = 0x1p28f * h * h, c[2] = 0x1p29f / 6 * h * h * h, c[3] = 0x1p29f / 24 * h * h * h * h;
     }
     // the place of a logit in bins
     __device__ __forceinline__ double place(float z) const { return fma((double)z - anchor, per_logit, (double)BELOW); }
-    // 1.25 e^(r / per_nat), 0 <= r < 1, in steps of 2^-shift, cut off: between 1 and 2, so its fraction's bits are what is wanted
-    __device__ __forceinline__ uint64_t steps(double r, int shift) const
+    // a logit on the safe side (-1: below, 1: above) of a bin's lower edge; of the lowest bin, of what counts as of it
+    __device__ __forceinline__ float logit(int bin, int side) const
     {
-        double e = c[5];
-#pragma unroll
-        for (int k = 4; k >= 0; --k) e = fma(e, r, c[k]);
-        return ((__builtin_bit_cast(uint64_t, e) & 0xfffffffffffffull) | 1ull << 52) >> (52 - shift);
+        const double edge = fma((double)(bin - (bin == 0) - BELOW), width, anchor);
+        return (float)(edge + side * (fabs(edge) * 1e-6 + 1e-30));
     }
+    // its number, -1 and BINS beyond them; what is less than a bin below the lowest counts as of that, where it weighs nothing
+    __device__ __forceinline__ int bin(double at) const { return min(max((int)at, -1), BINS); }
+    // e^(r / per_nat), 0 <= r < 1, in steps of 2^-29, to the nearest: what is beyond 1 is below 2^-4.9, so a float has it to half of such a step
+    __device__ __forceinline__ uint32_t steps(float r) const { return (1u << 29) + (uint32_t)fmaf(r, fmaf(r, fmaf(r, fmaf(r, c[3], c[2]), c[1]), c[0]), 0.5f); }
 };
 
 __device__ __forceinline__ void add_lds(uint64_t* p, uint64_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
@@ -337,7 +346,7 @@ __device__ Range bins_of(double lo, double hi, double all, Shared& sh)
     return {(int)sh.lo, (int)sh.hi};
 }
 
-constexpr double SLACK = 1e-11;     // of sums: what roundings, and words that do not count, can move them
+constexpr double SLACK = 1e-8;      // of sums: what roundings, and words that do not count, can move them
 
 __device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane)
 {
@@ -377,10 +386,10 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
     // the anchor: the largest of what is read first
     float most = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < T::VEC; ++e) most = fmaxf(most, fmaxf((float)all_of.first[0].v[e], (float)all_of.first[1].v[e]));
+    for (int k = 0; k < 2 * GROUP; ++k)
+#pragma unroll
+        for (int e = 0; e < T::VEC; ++e) most = fmaxf(most, (float)all_of.first[k].v[e]);
     most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
-    int shift = 51;
-    while (((1ull << 63) >> (shift + 1)) < V) --shift;
     Bins bins;
     int per_nat = 32;
     while (per_nat < 1024 && per_nat * 2 <= 64 * temperature) per_nat *= 2;
@@ -400,39 +409,33 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
             if (most == INFINITY) break;
         }
         bins.set(most, temperature, per_nat);
-        for (int b = tid; b < BINS; b += THREADS) sh.steps[b] = 0;
+        for (int b = tid; b < BINS + 2; b += THREADS) sh.steps[b] = 0;
         if (top_k)
-            for (int b = tid; b < BINS; b += THREADS) sh.count[b] = 0;
+            for (int b = tid; b < BINS + 2; b += THREADS) sh.count[b] = 0;
         if (tid == 0) sh.again = 0;
         __syncthreads();
         most = -INFINITY;
-        uint32_t again = 0;         // 1: a NaN, 2: above the bins, 4: below them and not yet without weight
-        const double light = BELOW - 42.0 * per_nat;
-        const auto add = [&](float x, uint32_t) {
+        bool nan = false;
+        const auto add = [&](float x) {
             most = fmaxf(most, x);
+            nan |= x != x;
             const double at = bins.place(x);
-            int b = (int)at;                                // towards 0; 0 of a NaN
-            if ((uint32_t)(b - 1) >= BINS - 1) {            // not one of the bins above the lowest
-                if (x != x) again |= 1;
-                else if (b >= BINS) again |= 2;
-                else if (at < 0 && at > light) again |= 4;
-                if (b || !(at >= 0)) return;
-            }
-            add_lds(&sh.steps[b], bins.steps(__builtin_amdgcn_fract(at), shift));
-            if (top_k) add_lds(&sh.count[b], 1u);
+            const int b = bins.bin(at);
+            add_lds(&sh.steps[b + 1], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
+            return b;
         };
-        all_of.each(add);
-        again = __any(again & 1) * 1 | __any(again & 2) * 2 | __any(again & 4) * 4;
-        if (again && tid % 64 == 0) __hip_atomic_fetch_or(&sh.again, again, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        if (top_k) all_of.each([&](float x, uint32_t) { add_lds(&sh.count[add(x) + 1], 1u); });
+        else all_of.each([&](float x, uint32_t) { add(x); });
+        if (__any(nan) && tid % 64 == 0) sh.again = 1;
         most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
-        again = sh.again;
+        const bool above = sh.steps[BINS + 1] != 0, below = sh.steps[0] != 0 && per_nat > 64, again = sh.again != 0;
         __syncthreads();
-        if (again & 1) {
+        if (again) {
             if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
             return;
         }
-        if (!(again & 6)) break;
-        if (!(again & 2)) per_nat = 64;     // with that, and the largest logit as the anchor, neither comes again
+        if (!above && !below) break;
+        if (!above) per_nat = 64;           // with that what is beyond the lowest bin weighs less than e^-44, and with the largest logit as the anchor nothing is above the highest
     }
     if (most < INFINITY) {
         // weights of all bins above each, beside the largest word's, which is 1; a thread has four bins, the first thread the highest
@@ -442,12 +445,13 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         {
             double w[EACH], mine = 0;
             uint32_t n[EACH], own = 0;
-            const double h = 1.0 / per_nat, less = exp(-h);
-            double edge = ldexp(0.8, -shift) * exp((double)(BINS - 1 - BELOW - (int)(tid * EACH)) * h + (bins.anchor - (double)most) / temperature);
+            // e^-h, h at most 1/32
+            const double h = 1.0 / per_nat, less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
+            double edge = 0x1p-29 * exp(((double)(BINS - 1 - BELOW - (int)(tid * EACH)) + (bins.anchor - (double)most) * bins.per_logit) * h);
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
                 const int b = BINS - 1 - (int)(tid * EACH + k);
-                w[k] = (double)sh.steps[b] * edge, n[k] = top_k ? sh.count[b] : 0;
+                w[k] = (double)sh.steps[b + 1] * edge, n[k] = top_k ? sh.count[b + 1] : 0;
                 mine += w[k], own += n[k];
                 edge *= less;
             }
@@ -496,22 +500,34 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         if (tid == 0) sh.n = 0;
         __syncthreads();
         {
-            int least = u_bins.lo;
-            if (need_k) least = min(least, k_bin);
-            if (p_bins.lo <= p_bins.hi) least = min(least, p_bins.lo);
-            if (m_bins.lo <= m_bins.hi) least = min(least, m_bins.lo);
-            // a logit that no word of these bins is below: most of the words are
-            const double edge = bins.anchor + (least - BELOW) / bins.per_logit;
-            const float from = (float)(edge - fabs(edge) * 1e-6 - 1e-30);
-            const auto take = [&](float x, uint32_t i) {
-                if (!(x >= from)) return;
-                const double at = bins.place(x);
-                if (at >= least && decides((int)at)) {
-                    const uint32_t n = atomicAdd(&sh.n, 1u);
-                    if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+            // between these logits are all words of the bins: a piece seldom has one
+            int b_lo = BINS, b_hi = -2;
+            if (p_bins.lo <= p_bins.hi) b_lo = p_bins.lo, b_hi = p_bins.hi;
+            if (m_bins.lo <= m_bins.hi) b_lo = min(b_lo, m_bins.lo), b_hi = max(b_hi, m_bins.hi);
+            const int k_at = need_k ? k_bin : u_bins.lo;
+            const float from = b_hi < 0 ? INFINITY : bins.logit(b_lo, -1), to = b_hi < 0 ? -INFINITY : bins.logit(b_hi + 1, 1), u_from = bins.logit(u_bins.lo, -1), u_to = bins.logit(u_bins.hi + 1, 1), k_from = bins.logit(k_at, -1), k_to = bins.logit(k_at + 1, 1);
+            const float lowest = fminf(fminf(from, u_from), k_from);
+            const auto near = [&](float x) { return ((x >= from) & (x <= to)) | ((x >= u_from) & (x <= u_to)) | ((x >= k_from) & (x <= k_to)); };
+            all_of.each_piece([&](const Piece<T>& p, uint32_t i) {
+                float top = (float)p.v[0];
+#pragma unroll
+                for (int e = 1; e < T::VEC; ++e) top = fmaxf(top, (float)p.v[e]);
+                if (!(top >= lowest)) return;
+                bool any = false;
+#pragma unroll
+                for (int e = 0; e < T::VEC; ++e) any |= near((float)p.v[e]);
+                if (!any) return;
+#pragma unroll
+                for (int e = 0; e < T::VEC; ++e) {
+                    const float x = (float)p.v[e];
+                    if (!near(x)) continue;
+                    const int b = bins.bin(bins.place(x));
+                    if (b >= 0 && b < BINS && decides(b)) {
+                        const uint32_t n = atomicAdd(&sh.n, 1u);
+                        if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - (i + e));
+                    }
                 }
-            };
-            all_of.each(take);
+            });
         }
         __syncthreads();
         const uint32_t n = sh.n;
@@ -529,7 +545,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
                 x = in ? sh.list[lane] : 0;
                 const float f = Key<F32>::value((uint32_t)(x >> 32));
                 const double w = in ? weigh.of(f) : 0;
-                const int bin = in ? (int)bins.place(f) : -1;
+                const int bin = in ? bins.bin(bins.place(f)) : -1;
                 double sum = w;
 #pragma unroll
                 for (int d = 1; d < 64; d *= 2) {
@@ -542,12 +558,16 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
                 const int head = heads ? 63 - __builtin_clzll(heads) : 0;
                 const double before = (in ? sh.above[bin] : 0) + (sum - w) - __shfl(sum - w, head), to = before + w;
                 double left = all;
-                if (need_k) left = __shfl(to, __builtin_ctzll(__ballot(in && sh.count[in ? bin : 0] + lane - head == top_k - 1) | 1ull << 63));
                 bool found = true;
+                if (need_k) {
+                    const uint64_t at = __ballot(in && sh.count[in ? bin : 0] + lane - head == top_k - 1);
+                    found = at != 0;
+                    left = __shfl(to, at ? __builtin_ctzll(at) : 0);
+                }
                 if (p_bins.lo <= p_bins.hi) {
                     const double target = top_p > 0 ? (double)top_p * left : 0.0;
                     const uint64_t at = __ballot(in && bin >= p_bins.lo && bin <= p_bins.hi && (before < target || before == 0) && !(to < target));
-                    found = at != 0;
+                    found = found && at != 0;
                     left = fmin(left, __shfl(to, at ? __builtin_ctzll(at) : 0));
                 }
                 if (m_bins.lo <= m_bins.hi) {
@@ -593,7 +613,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
                 const uint32_t i = 2 * tid + e;
                 in[e] = i < n;
                 const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
-                bin[e] = in[e] ? (int)bins.place(x) : -1;
+                bin[e] = in[e] ? bins.bin(bins.place(x)) : -1;
                 w[e] = in[e] ? weigh.of(x) : 0;
             }
             double sum_all;
@@ -606,7 +626,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
                 before[e] = sum + (e ? w[0] : 0.0);
                 if (!in[e]) continue;
                 const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
-                if (i == 0 || (int)bins.place(prev) != bin[e]) {     // one thread for each bin
+                if (i == 0 || bins.bin(bins.place(prev)) != bin[e]) {     // one thread for each bin
                     sh.above[bin[e]] -= before[e];
                     sh.count[bin[e]] -= i;
                 }
@@ -618,6 +638,8 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
             // the borders, exactly
             double left = all;
             if (need_k) {
+                if (tid == 0) sh.value = -1;
+                __syncthreads();
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     if (in[e] && rank[e] == top_k - 1) sh.value = before[e] + w[e];
@@ -650,7 +672,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                if (in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
+                if (left >= 0 && in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
             __syncthreads();
             word = sh.word;
             if (word != NONE) logprob = (float)log(sh.weight / left);
