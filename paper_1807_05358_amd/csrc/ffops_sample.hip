@@ -304,18 +304,43 @@ struct Bins {
 __device__ __forceinline__ void add_lds(uint64_t* p, uint64_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void add_lds(uint32_t* p, uint32_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
+__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// x of the lane that a data-parallel primitive names, 0 where there is none: CTRL as the instruction has it, ROWS the rows of 16 lanes that take part
+template <int CTRL, int ROWS, class V>
+__device__ __forceinline__ V moved(V x)
+{
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+    } else {
+        const uint64_t b = __builtin_bit_cast(uint64_t, x);
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, CTRL, ROWS, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+        return __builtin_bit_cast(V, (uint64_t)hi << 32 | lo);
+    }
+}
+
+// the sum of x over this lane and those before it: in rows of 16 lanes, then their last lanes' sums to the next row, and to the next two (a shuffle through LDS takes as long as three such steps)
+template <class V>
+__device__ __forceinline__ V wave_scan(V x)
+{
+    x += moved<0x111, 0xf>(x);
+    x += moved<0x112, 0xf>(x);
+    x += moved<0x114, 0xf>(x);
+    x += moved<0x118, 0xf>(x);
+    x += moved<0x142, 0xa>(x);
+    x += moved<0x143, 0xc>(x);
+    return x;
+}
+
 // sums of x over the threads before this one, and over all of them
 template <class V>
 __device__ __forceinline__ V block_before(V x, V* at, V& all)
 {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    V s = x;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const V t = __shfl_up(s, d);
-        if (lane >= d) s += t;
-    }
-    const V own = __shfl_up(s, 1);
+    const V s = wave_scan(x), own = moved<0x138, 0xf>(s);       // the lane before
     __syncthreads();
     if (lane == 63) at[wave] = s;
     __syncthreads();
@@ -325,7 +350,7 @@ __device__ __forceinline__ V block_before(V x, V* at, V& all)
         if (w == wave) before = all;
         all += at[w];
     }
-    return before + (lane ? own : (V)0);
+    return before + own;
 }
 
 // The bins whose weights a sum from `lo` to `hi` can end in: above[bin] <= sum < above[bin - 1], the lowest one for more than all.  All threads; sh.above is there.
@@ -337,7 +362,7 @@ __device__ Range bins_of(double lo, double hi, double all, Shared& sh)
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < BINS / THREADS; ++k) {
-        const int b = threadIdx.x * (BINS / THREADS) + k;
+        const int b = threadIdx.x + k * THREADS;
         const double from = sh.above[b], to = b ? sh.above[b - 1] : INFINITY;
         if (from <= lo && lo < to) sh.hi = b;
         if (from <= hi && hi < to) sh.lo = b;
@@ -347,11 +372,6 @@ __device__ Range bins_of(double lo, double hi, double all, Shared& sh)
 }
 
 constexpr double SLACK = 1e-8;      // of sums: what roundings, and words that do not count, can move them
-
-__device__ __forceinline__ uint64_t read_lane(uint64_t x, int lane)
-{
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
-}
 
 template <class T>
 __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
@@ -438,33 +458,55 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         if (!above) per_nat = 64;           // with that what is beyond the lowest bin weighs less than e^-44, and with the largest logit as the anchor nothing is above the highest
     }
     if (most < INFINITY) {
-        // weights of all bins above each, beside the largest word's, which is 1; a thread has four bins, the first thread the highest
+        // weights of all bins above each, beside the largest word's, which is 1: a wave has 256 bins, four times 64 side by side, the first wave the highest
         constexpr int EACH = BINS / THREADS;
-        double all;
+        const int lane = tid % 64, wave = tid / 64, highest = BINS - 1 - wave * (64 * EACH) - lane;
+        double all = 0;
         uint32_t words_all = 0;
         {
-            double w[EACH], mine = 0;
-            uint32_t n[EACH], own = 0;
-            // e^-h, h at most 1/32
-            const double h = 1.0 / per_nat, less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
-            double edge = 0x1p-29 * exp(((double)(BINS - 1 - BELOW - (int)(tid * EACH)) + (bins.anchor - (double)most) * bins.per_logit) * h);
+            uint64_t steps[EACH];
+            uint32_t n[EACH] = {}, c[EACH] = {}, words_before = 0, row_words = 0;
+            double s[EACH] = {}, before = 0, rows = 0;
 #pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                const int b = BINS - 1 - (int)(tid * EACH + k);
-                w[k] = (double)sh.steps[b + 1] * edge, n[k] = top_k ? sh.count[b + 1] : 0;
-                mine += w[k], own += n[k];
-                edge *= less;
+            for (int k = 0; k < EACH; ++k) steps[k] = sh.steps[highest - 64 * k + 1];
+            if (__any((steps[0] | steps[1] | steps[2] | steps[3]) != 0)) {          // most waves have empty bins
+                static_assert(EACH == 4, "as many rows");
+                // e^-h, h at most 1/32, and that for 64 bins
+                const double h = 1.0 / per_nat;
+                double less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
+#pragma unroll
+                for (int k = 0; k < 6; ++k) less *= less;
+                double edge = 0x1p-29 * exp(((double)(highest - BELOW) + (bins.anchor - (double)most) * bins.per_logit) * h);
+                // sums of a row of 64, up to and with the lane, then of the rows before it, then of the waves before
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    s[k] = wave_scan((double)steps[k] * edge);
+                    if (top_k) n[k] = sh.count[highest - 64 * k + 1], c[k] = wave_scan(n[k]);
+                    edge *= less;
+                }
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) {
+                    const double of_row = __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, s[k]), 63));
+                    s[k] = moved<0x138, 0xf>(s[k]) + rows, rows += of_row;
+                    if (top_k) {
+                        const uint32_t words = (uint32_t)__builtin_amdgcn_readlane((int)c[k], 63);
+                        c[k] = moved<0x138, 0xf>(c[k]) + row_words, row_words += words;
+                    }
+                }
             }
-            double before = block_before(mine, sh.d, all);
-            uint32_t words_before = top_k ? block_before(own, sh.c, words_all) : 0;
+            if (lane == 0) sh.d[wave] = rows, sh.c[wave] = row_words;
             __syncthreads();
+            for (int x = 0; x < WAVES; ++x) {
+                if (x == wave) before = all, words_before = words_all;
+                all += sh.d[x], words_all += sh.c[x];
+            }
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
-                const int b = BINS - 1 - (int)(tid * EACH + k);
-                sh.above[b] = before;
-                if (top_k) sh.count[b] = words_before;
-                if (words_before < top_k && top_k <= words_before + n[k]) sh.found = b;
-                before += w[k], words_before += n[k];
+                const int b = highest - 64 * k;
+                sh.above[b] = s[k] + before;
+                const uint32_t words = c[k] + words_before;
+                if (top_k) sh.count[b] = words;
+                if (words < top_k && top_k <= words + n[k]) sh.found = b;
             }
             __syncthreads();
         }
@@ -535,8 +577,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
         if (n <= 64) {
             // one wave, a word a lane
             if (tid < 64) {
-                const int lane = tid;
-                bool in = lane < (int)n;
+                const bool in = lane < (int)n;
                 uint64_t x = in ? sh.list[lane] : 0;
                 uint32_t place = 0;
                 for (uint32_t j = 0; j < n; ++j) place += read_lane(x, j) > x;
@@ -546,12 +587,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
                 const float f = Key<F32>::value((uint32_t)(x >> 32));
                 const double w = in ? weigh.of(f) : 0;
                 const int bin = in ? bins.bin(bins.place(f)) : -1;
-                double sum = w;
-#pragma unroll
-                for (int d = 1; d < 64; d *= 2) {
-                    const double t = __shfl_up(sum, d);
-                    if (lane >= d) sum += t;
-                }
+                const double sum = wave_scan(w);
                 // the first word of the lane's bin in the list
                 const int prev = __shfl_up(bin, 1);
                 const uint64_t heads = __ballot(in && (lane == 0 || prev != bin)) & ~0ull >> (63 - lane);
