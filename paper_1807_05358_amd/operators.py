@@ -405,61 +405,74 @@ def vocab_loss_bwd(dloss, x, weight, targets, lse, *, ignore_index=-100, first_w
     return dx, dw
 
 
-def _pages(t, what):
+def _page_stride(shape, stride, size, what):
     """bytes from page to page; the rest of a page lies side by side"""
-    n, h, p, e = t.shape
-    _, sh, sp, se = t.stride()
+    n, h, p, e = shape
+    _, sh, sp, se = stride
     if not (e == 1 or se == 1) or not (p == 1 or sp == e) or not (h == 1 or sh == p * e):
         raise ValueError(f"{what}: the elements of a page lie side by side; only pages may have room between them")
-    return t.stride(0) * t.element_size() if n > 1 else h * p * e * t.element_size()
+    n = stride[0] * size if n > 1 else h * p * e * size
+    if n % 16:
+        raise ValueError(f"{what}: pages begin at multiples of 16 bytes")
+    return n
+
+
+@functools.lru_cache(maxsize=256)
+def _cache_layout(dtype, k, v, table, k_scales, v_scales):
+    """(kv_heads, head_dim, strides of the cache's record, its other sizes) for tensors of `dtype`, from (shape, stride, type) of each"""
+    torch = _torch()
+    shape, stride, kind = k
+    if len(shape) != 4 or len(table[0]) != 2:
+        raise ValueError("k_pages are [pages, kv_heads, page, elements], the table [batch, entries]")
+    N, K, P, E = shape
+    for t, what, want, to in ((v, "v_pages", shape, kind), (table, "table", table[0], torch.int32)):
+        if t[0] != want or t[2] is not to:
+            raise ValueError(f"{what} has shape {tuple(t[0])} and is {t[2]}, {tuple(want)} and {to} are wanted")
+    if table[0][1] > 1 and table[1][1] != 1:
+        raise ValueError("a row of the table lies side by side")
+    if kind is dtype:
+        held, D, blocks, unit, size = FF_HELD_SAME, E, 0, 8, 2
+    elif kind is torch.float8_e4m3fn:
+        held, D, blocks, unit, size = FF_HELD_E4M3, E, 1, 16, 1
+    elif kind is torch.uint8:
+        held, D, blocks, unit, size = FF_HELD_E2M1, 2 * E, E // 16, 32, 1
+    else:
+        raise ValueError(f"k_pages is {kind}; {dtype}, float8_e4m3fn or uint8 (two 4-bit floats) is wanted")
+    if N == 0 or K == 0:
+        raise ValueError("a cache without pages or heads")
+    if D == 0 or D % unit or D > 128:
+        raise ValueError(f"a head has {D} elements; a multiple of {unit} up to 128 is wanted for {kind}")
+    if P < 16 or P & (P - 1) or P > 32768:
+        raise ValueError(f"a page has {P} positions; a power of two from 16 to 32768 is wanted")
+    scales = [0, 0]
+    for i, (t, what) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
+        if held == FF_HELD_SAME:
+            if t is not None:
+                raise ValueError(f"{dtype} is held without scales")
+            continue
+        if t is None:
+            raise ValueError(f"{what} are missing: {kind} is held with scales")
+        if t[0] != (N, K, blocks, P) or t[2] is not torch.uint8:
+            raise ValueError(f"{what} has shape {tuple(t[0])} and is {t[2]}, {(N, K, blocks, P)} and uint8 are wanted")
+        sn, sh, sb, sp = t[1]
+        if sp != 1 or not (blocks == 1 or sb == P) or not (K == 1 or sh == blocks * P) or (N > 1 and sn % 4):
+            raise ValueError(f"{what}: the scales of a page lie side by side; only pages may have room between them, in steps of 4")
+        scales[i] = sn if N > 1 else K * blocks * P
+    return K, D, (_page_stride(shape, stride, size, "k_pages"), _page_stride(v[0], v[1], size, "v_pages"), *scales, table[1][0]), (N, P, table[0][1], held)
 
 
 def _cache_args(k_pages, v_pages, table, k_scales, v_scales, dtype):
     """(kv_heads, head_dim, values of the cache's record) of a cache for tensors of `dtype`"""
-    torch = _torch()
-    if k_pages.dim() != 4 or table.dim() != 2:
-        raise ValueError("k_pages are [pages, kv_heads, page, elements], the table [batch, entries]")
     if not k_pages.is_cuda:
         raise ValueError(f"k_pages is on {k_pages.device}: the operators have no CPU path")
-    device = k_pages.device
-    N, K, P, E = k_pages.shape
-    _check(v_pages, "v_pages", k_pages.shape, k_pages.dtype, device)
-    _check(table, "table", table.shape, torch.int32, device)
-    if table.shape[1] > 1 and table.stride(1) != 1:
-        raise ValueError("a row of the table lies side by side")
-    if k_pages.dtype is dtype:
-        held, D, blocks, unit = FF_HELD_SAME, E, 0, 8
-    elif k_pages.dtype is torch.float8_e4m3fn:
-        held, D, blocks, unit = FF_HELD_E4M3, E, 1, 16
-    elif k_pages.dtype is torch.uint8:
-        held, D, blocks, unit = FF_HELD_E2M1, 2 * E, E // 16, 32
-    else:
-        raise ValueError(f"k_pages is {k_pages.dtype}; {dtype}, float8_e4m3fn or uint8 (two 4-bit floats) is wanted")
-    if N == 0 or K == 0:
-        raise ValueError("a cache without pages or heads")
-    if D == 0 or D % unit or D > 128:
-        raise ValueError(f"a head has {D} elements; a multiple of {unit} up to 128 is wanted for {k_pages.dtype}")
-    if P < 16 or P & (P - 1) or P > 32768:
-        raise ValueError(f"a page has {P} positions; a power of two from 16 to 32768 is wanted")
-    scales = [0, 0]
-    if held == FF_HELD_SAME:
-        if k_scales is not None or v_scales is not None:
-            raise ValueError(f"{dtype} is held without scales")
-        k_scales = v_scales = None
-    else:
-        for i, (t, what) in enumerate(((k_scales, "k_scales"), (v_scales, "v_scales"))):
-            if t is None:
-                raise ValueError(f"{what} are missing: {k_pages.dtype} is held with scales")
-            _check(t, what, (N, K, blocks, P), torch.uint8, device)
-            _, sh, sb, sp = t.stride()
-            if sp != 1 or not (blocks == 1 or sb == P) or not (K == 1 or sh == blocks * P) or (N > 1 and t.stride(0) % 4) or t.data_ptr() % 4:
-                raise ValueError(f"{what}: the scales of a page lie side by side; only pages may have room between them, in steps of 4")
-            scales[i] = t.stride(0) if N > 1 else K * blocks * P
-    strides = [_pages(k_pages, "k_pages"), _pages(v_pages, "v_pages")]
-    for t, n, what in ((k_pages, strides[0], "k_pages"), (v_pages, strides[1], "v_pages")):
-        if n % 16 or t.data_ptr() % 16:
-            raise ValueError(f"{what}: pages begin at multiples of 16 bytes")
-    return K, D, (k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales), _ptr(v_scales), table.data_ptr(), *strides, *scales, table.stride(0), N, P, table.shape[1], held)
+    few = (k_scales.shape, k_scales.stride(), k_scales.dtype) if k_scales is not None else None, (v_scales.shape, v_scales.stride(), v_scales.dtype) if v_scales is not None else None
+    K, D, strides, sizes = _cache_layout(dtype, (k_pages.shape, k_pages.stride(), k_pages.dtype), (v_pages.shape, v_pages.stride(), v_pages.dtype), (table.shape, table.stride(), table.dtype), *few)
+    device, at = k_pages.device, (k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_scales), _ptr(v_scales), table.data_ptr())
+    if v_pages.device != device or table.device != device or (k_scales is not None and (k_scales.device != device or v_scales.device != device)):
+        raise ValueError(f"the parts of a cache are on one device, {device}")
+    if (at[0] | at[1]) % 16 or (at[2] | at[3]) % 4:
+        raise ValueError("pages begin at multiples of 16 bytes, their scales of 4")
+    return K, D, (*at, *strides, *sizes)
 
 
 def cache_write(k, v, k_pages, v_pages, table, start, *, lengths=None, k_scales=None, v_scales=None):
@@ -503,7 +516,7 @@ def cache_read(k_pages, v_pages, table, lengths, *, kv_len=None, dtype=None, k_s
     if kv_len < 0:
         raise ValueError("kv_len is a number of positions")
     lengths = _vector(lengths)
-    k, v = torch.empty((2, B, K, kv_len, D), dtype=dtype, device=device).unbind()
+    k, v = k_pages.new_empty((2, B, K, kv_len, D), dtype=dtype).unbind()
     _launch("ff_op_cache_read", device, FF_F16 if dtype is torch.float16 else FF_BF16, B, K, D, kv_len, *_heads(k, v), *cache, lengths.data_ptr())
     return k, v
 
@@ -529,7 +542,9 @@ def attention_paged_fwd(q, k_pages, v_pages, table, kv_lengths, *, causal=False,
     scale = 1 / math.sqrt(D) if scale is None else float(scale)
     if not (scale > 0 and math.isfinite(scale)):
         raise ValueError("scale is a positive number")
-    o, lse = _like_heads(q), torch.empty((B, H, n), dtype=torch.float32, device=device)
+    o, lse = torch.empty_like(q), q.new_empty((B, H, n), dtype=torch.float32)
+    if o.stride(3) != 1 or o.stride(0) % 8 or o.stride(1) % 8 or o.stride(2) % 8:
+        o = _like_heads(q)
     q, q_lengths, kv_lengths = _dense_heads(q), _vector(q_lengths), _vector(kv_lengths)
     _launch("ff_op_attention_paged_fwd", device, dtype, B, H, K, n, D, 1 if causal else 0, scale, *_heads(q, o), *cache, lse.data_ptr(), _ptr(q_lengths), kv_lengths.data_ptr())
     return o, lse
@@ -568,6 +583,6 @@ def sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         if not n >= least or not abs(n) <= 3e38:
             raise ValueError(f"{what} is {n}")
     logits, u = _dense_rows(logits), _vector(u)
-    words, logprob = torch.empty(R, dtype=torch.int32, device=device), torch.empty(R, dtype=torch.float32, device=device)
+    words, logprob = u.new_empty(R, dtype=torch.int32), u.new_empty(R)
     _launch("ff_op_sample", device, dtype, R, V, logits.data_ptr(), logits.stride(0), u.data_ptr(), *(_ptr(t) for t in vectors), *numbers, words.data_ptr(), logprob.data_ptr())
     return words, logprob

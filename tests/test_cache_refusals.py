@@ -85,7 +85,7 @@ def test_functions_refuse_what_they_cannot_take():
                 lambda: O.cache_write(new.float(), new.float(), pages, pages, tab, n), lambda: O.sample(z.double(), u), lambda: O.sample(z[:, :0], u)):
         with pytest.raises(ValueError):
             bad()
-    # of a cache, before anything asks where it is
+    # of a cache, as of one on a GPU
     meta = lambda *s, dtype: torch.empty(*s, dtype=dtype, device="meta")
 
     class Elsewhere:
