@@ -10,7 +10,7 @@ struct PagedArgs {
     CacheArgs c;
     uint32_t batch, heads, kv_heads, group, q_len, dim, causal, runs;
     uint32_t cols;                  // queries times heads of a group: what shares the keys of a key head
-    float scale_log2;
+    float scale_log2, per_group;    // per_group: 1 / group
     Heads q, o;
     float* lse;
     const int32_t *q_lengths, *kv_lengths;
@@ -254,6 +254,9 @@ struct Columns {
     int seen[NT];
 };
 
+// the query of a column: col / group.  Columns are below 2^20, so that the quotient of col + 0.5 is off by less than 2^-23 of 2^20 / group, a quarter of what the nearest whole number is away at least
+__device__ __forceinline__ uint32_t query_of(const PagedArgs& a, uint32_t col) { return (uint32_t)(((float)col + 0.5f) * a.per_group); }
+
 template <int NT>
 __device__ __forceinline__ Columns<NT> columns_of(const PagedArgs& a, uint32_t b, uint32_t kh, uint32_t first, int nk, int x)
 {
@@ -263,7 +266,7 @@ __device__ __forceinline__ Columns<NT> columns_of(const PagedArgs& a, uint32_t b
     for (int t = 0; t < NT; ++t) {
         const uint32_t col = first + t * 16 + x;
         c.in[t] = col < a.cols;
-        c.i[t] = c.in[t] ? col / a.group : 0, c.h[t] = kh * a.group + (c.in[t] ? col % a.group : 0);
+        c.i[t] = c.in[t] ? query_of(a, col) : 0, c.h[t] = kh * a.group + (c.in[t] ? col - c.i[t] * a.group : 0);
         int n = 0;
         if (c.in[t] && (int)c.i[t] < nq) {
             n = a.causal ? (int)c.i[t] + 1 + nk - nq : nk;
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(256, (RESIDENT<HELD, D, NT>)) void k_attention_page
     __shared__ float sums[NT][WAVES][16][D + 4];
     Lane l;
     l.lane = threadIdx.x % 64, l.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l.x = l.lane % 16, l.g = l.lane / 16;
-    const uint32_t kh = blockIdx.x % a.kv_heads, run = blockIdx.x / a.kv_heads, col0 = blockIdx.y * (16 * NT);
+    const uint32_t kh = blockIdx.x, run = blockIdx.y, col0 = blockIdx.z * (16 * NT);
     int64_t t0, t1, first;              // places of the run in the list, and where sequence b begins there
     uint32_t b;
     List list;
@@ -545,7 +548,7 @@ __global__ __launch_bounds__(256, (RESIDENT<HELD, D, NT>)) void k_attention_page
             const float inv = sum > 0 ? 1.0f / sum : sum == sum ? 0.0f : sum;
 #pragma unroll
             for (int j = 0; j < DT; ++j) r[j] *= inv;
-            const uint32_t i = col / a.group, h = kh * a.group + col % a.group;
+            const uint32_t i = query_of(a, col), h = kh * a.group + col - i * a.group;
             if (whole) {
                 if (d0 == 0) a.lse[((uint64_t)b * a.heads + h) * a.q_len + i] = (most + log2_(sum)) * LN2;
                 char* to = a.o.p + b * a.o.batch + h * a.o.head + i * a.o.pos;
@@ -588,27 +591,28 @@ __global__ __launch_bounds__(256) void k_attention_paged_join(PagedArgs a)
     const uint32_t r0 = runs.of(first), r1 = runs.of(first + n - 1);
     if (r0 == r1) return;
     auto slot_row = [&](uint32_t r) { return ((uint64_t)slot_of(r, r == r0) * a.kv_heads + kh) * a.cols + col; };
-    float m = -INFINITY;
+    // four of the parts at a time, a quarter of the lanes each, with a maximum of its own
+    float m = -INFINITY, sum = 0, o[8] = {};
     bool none = false;
-    for (uint32_t r = r0 + lane; r <= r1; r += 64) {
-        const float s = a.part_lse[slot_row(r)];
-        none |= s != s;
-        m = fmaxf(m, s);
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    const float base = m == -INFINITY ? 0.0f : m;
-    float sum = 0, o[8] = {};
 #pragma unroll 4
     for (uint32_t r = r0 + lane / 16; r <= r1; r += 4) {
         const uint64_t at = slot_row(r);
-        const float w = exp2_(a.part_lse[at] - base);
-        sum += w;
+        const float s = a.part_lse[at];
         const float* p = a.part + at * a.dim + (x < a.dim ? x : 0);
         const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
+        none |= s != s;
+        const float top = fmaxf(m, s), f = m == -INFINITY ? 0.0f : exp2_(m - top), w = s == -INFINITY ? 0.0f : exp2_(s - top);
+        sum = sum * f + w, m = top;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += w * u[e], o[4 + e] += w * v[e];
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * f + w * u[e], o[4 + e] = o[4 + e] * f + w * v[e];
     }
+    float base = fmaxf(m, __shfl_xor(m, 16));
+    base = fmaxf(base, __shfl_xor(base, 32));
+    const float f = m == -INFINITY ? 0.0f : exp2_(m - base);
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] *= f;
+    if (base == -INFINITY) base = 0;
 #pragma unroll
     for (int d = 16; d < 64; d *= 2) {
         sum += __shfl_xor(sum, d);
@@ -631,7 +635,7 @@ template <class T, int HELD, int D, bool FULL>
 void launch(const PagedArgs& a, hipStream_t st)
 {
     const uint32_t nt = column_tiles(a);
-    const dim3 grid((a.runs ? a.runs : a.batch) * a.kv_heads, (uint32_t)ceil_div(a.cols, 16 * nt));
+    const dim3 grid(a.kv_heads, a.runs ? a.runs : a.batch, (uint32_t)ceil_div(a.cols, 16 * nt));
     if (nt == 1) k_attention_paged<T, HELD, D, FULL, 1><<<grid, 256, 0, st>>>(a);
     else k_attention_paged<T, HELD, D, FULL, 2><<<grid, 256, 0, st>>>(a);
 }
@@ -660,7 +664,7 @@ int check(const ff_attention_paged_fwd_t* p)
     if (p->heads == 0 || p->kv_heads == 0 || p->heads % p->kv_heads) return FF_EINVAL;
     if (!(p->scale > 0) || !std::isfinite(p->scale)) return FF_EINVAL;
     if (const int rc = check_cache_sizes(p->cache, p->dtype, p->batch, p->kv_heads, p->head_dim)) return rc;
-    // launch grids: blocks of 16 columns along y, a wave for every row of the join along x
+    // launch grids: blocks of 16 columns along z, a wave for every row of the join along x
     if (p->heads > 65535 || p->q_len > FF_OP_MAX_LEN || (uint64_t)p->q_len * (p->heads / p->kv_heads) > (uint64_t)MOST_BLOCKS_Y * 16 || ceil_div((uint64_t)p->heads * p->q_len, WAVES) * 256 > MOST_THREADS)
         return FF_ERANGE;
     return FF_OK;
@@ -672,7 +676,7 @@ PagedArgs args_of(const ff_attention_paged_fwd_t* p)
     a.c = cache_args(p->cache, p->head_dim);
     a.batch = p->batch, a.heads = p->heads, a.kv_heads = p->kv_heads, a.group = p->heads / p->kv_heads;
     a.q_len = p->q_len, a.dim = p->head_dim, a.causal = p->causal != 0, a.cols = p->q_len * a.group;
-    a.scale_log2 = p->scale * LOG2E;
+    a.scale_log2 = p->scale * LOG2E, a.per_group = 1.0f / (float)a.group;
     a.q = in_bytes(p->q), a.o = in_bytes(p->o);
     a.q_lengths = p->q_lengths, a.kv_lengths = p->kv_lengths;
     a.runs = p->q_len ? runs_of(a.kv_heads * ceil_div(a.cols, 16 * column_tiles(a)), a.batch, (uint64_t)a.c.table_pages * a.c.page) : 0;
