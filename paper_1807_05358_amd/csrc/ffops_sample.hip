@@ -68,7 +68,7 @@ struct Digits {
 
 struct Shared {
     union {
-        uint64_t steps[BINS + 2];   // a bin's sum, at its number + 1; at the ends what is beyond the bins; then:
+        uint64_t steps[BINS + 2];   // a bin's sum, at its number + 1; at the ends whether something beyond the bins weighs anything; then:
         double above[BINS];         // the weight of all bins above it
     };
     uint32_t count[BINS + 2];       // words, likewise, then those of all bins above; top_k alone
@@ -130,11 +130,25 @@ __device__ uint32_t select(const typename T::elem* z, uint32_t vocab, const Weig
     for (int low = Key<T>::BITS - 8; low >= 0; low -= 8) {
         if (threadIdx.x < 256) sh.mass[threadIdx.x] = 0, sh.count[threadIdx.x] = 0;
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < vocab; i += THREADS) {
-            const uint32_t k = Key<T>::of(z[i]);
-            if (low + 8 < Key<T>::BITS && (k >> (low + 8)) != prefix) continue;
-            atomicAdd((unsigned long long*)&sh.mass[k >> low & 255], (unsigned long long)w.steps(Key<T>::value(k)));
-            atomicAdd(&sh.count[k >> low & 255], 1u);
+        for (uint32_t base = 0; base < vocab; base += THREADS) {
+            const uint32_t i = base + threadIdx.x, k = i < vocab ? Key<T>::of(z[i]) : 0;
+            bool in = i < vocab && !(low + 8 < Key<T>::BITS && (k >> (low + 8)) != prefix);
+            const uint64_t s = in ? w.steps(Key<T>::value(k)) : 0;
+            // it is equal logits that this is for: those of a wave are added at once, up to four different ones
+            for (int t = 0; t < 4 && __any(in); ++t) {
+                const int leader = __builtin_ctzll(__ballot(in));
+                const bool same = in && k == (uint32_t)__builtin_amdgcn_readlane((int)k, leader);
+                const uint32_t n = __popcll(__ballot(same));
+                if ((int)(threadIdx.x % 64) == leader) {
+                    atomicAdd((unsigned long long*)&sh.mass[k >> low & 255], (unsigned long long)(n * s));
+                    atomicAdd(&sh.count[k >> low & 255], n);
+                }
+                in = in && !same;
+            }
+            if (in) {
+                atomicAdd((unsigned long long*)&sh.mass[k >> low & 255], (unsigned long long)s);
+                atomicAdd(&sh.count[k >> low & 255], 1u);
+            }
         }
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -226,9 +240,14 @@ struct Piece {
     {
         if (i + T::VEC <= V) {
             v = *(const vec*)(z + i);
-        } else {
+            return;
+        }
 #pragma unroll
-            for (int e = 0; e < T::VEC; ++e) v[e] = i + e < V ? z[i + e] : (typename T::elem)(-INFINITY);
+        for (int e = 0; e < T::VEC; ++e) v[e] = (typename T::elem)(-INFINITY);
+        if (i < V) {
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e)
+                if (i + e < V) v[e] = z[i + e];
         }
     }
 };
@@ -260,7 +279,8 @@ struct Row {
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) later[k].load(z, i + (2 * GROUP + k) * STEP, V);
 #pragma unroll
-            for (int k = 0; k < GROUP; ++k) f(now[k], i + k * STEP);
+            for (int k = 0; k < GROUP; ++k)
+                if (i + k * STEP < V) f(now[k], i + k * STEP);
 #pragma unroll
             for (int k = 0; k < GROUP; ++k) now[k] = now[GROUP + k], now[GROUP + k] = later[k];
             i += GROUP * STEP;
@@ -273,6 +293,33 @@ struct Row {
 #pragma unroll
             for (int e = 0; e < T::VEC; ++e) f((float)p.v[e], i + e);
         });
+    }
+    // f of all elements for which near() holds, which are `lowest` or more: most pieces have none
+    template <class N, class F>
+    __device__ __forceinline__ void each_near(float lowest, N near, F f) const
+    {
+        each_piece([&](const Piece<T>& p, uint32_t i) {
+            float top = (float)p.v[0];
+#pragma unroll
+            for (int e = 1; e < T::VEC; ++e) top = fmaxf(top, (float)p.v[e]);
+            if (!(top >= lowest)) return;
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e) any |= near((float)p.v[e]);
+            if (!any) return;
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e)
+                if (near((float)p.v[e])) f((float)p.v[e], i + e);
+        });
+    }
+    __device__ __forceinline__ float largest_of_first() const
+    {
+        float most = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < 2 * GROUP; ++k)
+#pragma unroll
+            for (int e = 0; e < T::VEC; ++e) most = fmaxf(most, (float)first[k].v[e]);
+        return most;
     }
 };
 
@@ -373,352 +420,372 @@ __device__ Range bins_of(double lo, double hi, double all, Shared& sh)
 
 constexpr double SLACK = 1e-8;      // of sums: what roundings, and words that do not count, can move them
 
+enum { UNDECIDED, DECIDED, WITHOUT };        // WITHOUT: a row without a word
+
+struct Choice {
+    float temperature, top_p, min_p, u;
+    uint32_t top_k;                 // 0: all words
+    __device__ __forceinline__ Choice(const SampleArgs& a, uint32_t row)
+    {
+        temperature = a.temperatures ? a.temperatures[row] : a.temperature, top_p = a.top_ps ? a.top_ps[row] : a.top_p, u = a.u[row];
+        const float m = a.min_ps ? a.min_ps[row] : a.min_p;
+        min_p = m > 1 ? 1.0f : m;
+        const int32_t k = a.top_ks ? a.top_ks[row] : a.top_k;
+        top_k = k > 0 && (uint32_t)k < a.vocab ? (uint32_t)k : 0;
+    }
+    __device__ __forceinline__ bool fine() const { return temperature >= 0 && temperature < INFINITY && top_p == top_p && min_p == min_p && u == u; }
+    __device__ __forceinline__ int bins_per_nat() const
+    {
+        int n = 32;
+        while (n < 1024 && n * 2 <= 64 * temperature) n *= 2;
+        return n;
+    }
+};
+
+// The word from bins.  most: an anchor, and after that the largest logit.
 template <class T>
-__global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
+__device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c, Shared& sh, float& most, uint32_t& word, float& logprob)
 {
-    __shared__ Shared sh;
-    const uint32_t row = blockIdx.x, V = a.vocab, tid = threadIdx.x;
-    const typename T::elem* z = (const typename T::elem*)(a.logits + row * a.stride);
-    const float temperature = a.temperatures ? a.temperatures[row] : a.temperature, top_p = a.top_ps ? a.top_ps[row] : a.top_p, u = a.u[row];
-    const float min_p_ = a.min_ps ? a.min_ps[row] : a.min_p, min_p = min_p_ > 1 ? 1.0f : min_p_;
-    const int32_t top_k_ = a.top_ks ? a.top_ks[row] : a.top_k;
-    const uint32_t top_k = top_k_ > 0 && (uint32_t)top_k_ < V ? (uint32_t)top_k_ : 0;      // 0: all words
-    const bool fine = temperature >= 0 && temperature < INFINITY && top_p == top_p && min_p == min_p && u == u;
-    if (!fine) {
-        if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
-        return;
-    }
-    const Row<T> all_of(z, V);
-    if (temperature == 0) {         // the largest key, of these the lowest number
-        uint64_t first = 0;
-        uint32_t nan = 0;
-        all_of.each([&](float x, uint32_t i) {
-            nan |= x != x;
-            const uint64_t k = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
-            first = k > first ? k : first;
-        });
-        first = block_max(first, sh.a);
-        nan = block_sum(nan, sh.c);
-        const bool any = nan == 0 && Key<F32>::value((uint32_t)(first >> 32)) > -INFINITY;
-        if (tid == 0) a.words[row] = any ? (int32_t)(0xffffffffu - (uint32_t)first) : -1, a.logprob[row] = any ? 0.0f : NAN;
-        return;
-    }
-    // the anchor: the largest of what is read first
-    float most = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 2 * GROUP; ++k)
-#pragma unroll
-        for (int e = 0; e < T::VEC; ++e) most = fmaxf(most, (float)all_of.first[k].v[e]);
-    most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
+    const uint32_t tid = threadIdx.x;
     Bins bins;
-    int per_nat = 32;
-    while (per_nat < 1024 && per_nat * 2 <= 64 * temperature) per_nat *= 2;
-    uint32_t word = NONE;
-    float logprob = NAN;
+    int per_nat = c.bins_per_nat();
+    word = NONE;
     for (;;) {
         if (!(most > -INFINITY && most < INFINITY)) {       // no anchor: the largest of all, which may be infinite, or a row without one
             most = -INFINITY;
             uint32_t nan = 0;
-            all_of.each([&](float x, uint32_t) { most = fmaxf(most, x), nan |= x != x; });
+            src.each([&](float x, uint32_t) { most = fmaxf(most, x), nan |= x != x; });
             most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
             nan = block_sum(nan, sh.c);
             if (nan || most == -INFINITY) {
-                if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
-                return;
+                return WITHOUT;
             }
-            if (most == INFINITY) break;
+            if (most == INFINITY) return UNDECIDED;
         }
-        bins.set(most, temperature, per_nat);
+        bins.set(most, c.temperature, per_nat);
         for (int b = tid; b < BINS + 2; b += THREADS) sh.steps[b] = 0;
-        if (top_k)
+        if (c.top_k)
             for (int b = tid; b < BINS + 2; b += THREADS) sh.count[b] = 0;
         if (tid == 0) sh.again = 0;
         __syncthreads();
         most = -INFINITY;
         bool nan = false;
+        const double light = BELOW - 42.0 * per_nat;        // places from there on weigh something
+        // (words beyond the lowest bin, many of them -inf at times, are kept off the one place in LDS that they would all add to)
         const auto add = [&](float x) {
             most = fmaxf(most, x);
             nan |= x != x;
             const double at = bins.place(x);
             const int b = bins.bin(at);
-            add_lds(&sh.steps[b + 1], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
+            if (b >= 0) add_lds(&sh.steps[b + 1], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
+            else if (at > light) sh.steps[0] = 1;
             return b;
         };
-        if (top_k) all_of.each([&](float x, uint32_t) { add_lds(&sh.count[add(x) + 1], 1u); });
-        else all_of.each([&](float x, uint32_t) { add(x); });
+        if (c.top_k) src.each([&](float x, uint32_t) {
+            const int b = add(x);
+            if (b >= 0) add_lds(&sh.count[b + 1], 1u);
+        });
+        else src.each([&](float x, uint32_t) { add(x); });
         if (__any(nan) && tid % 64 == 0) sh.again = 1;
         most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
         const bool above = sh.steps[BINS + 1] != 0, below = sh.steps[0] != 0 && per_nat > 64, again = sh.again != 0;
         __syncthreads();
         if (again) {
-            if (tid == 0) a.words[row] = -1, a.logprob[row] = NAN;
-            return;
+            return WITHOUT;
         }
         if (!above && !below) break;
         if (!above) per_nat = 64;           // with that what is beyond the lowest bin weighs less than e^-44, and with the largest logit as the anchor nothing is above the highest
     }
-    if (most < INFINITY) {
-        // weights of all bins above each, beside the largest word's, which is 1: a wave has 256 bins, four times 64 side by side, the first wave the highest
-        constexpr int EACH = BINS / THREADS;
-        const int lane = tid % 64, wave = tid / 64, highest = BINS - 1 - wave * (64 * EACH) - lane;
-        double all = 0;
-        uint32_t words_all = 0;
-        {
-            uint64_t steps[EACH];
-            uint32_t n[EACH] = {}, c[EACH] = {}, words_before = 0, row_words = 0;
-            double s[EACH] = {}, before = 0, rows = 0;
+    // weights of all bins above each, beside the largest word's, which is 1: a wave has 256 bins, four times 64 side by side, the first wave the highest
+    constexpr int EACH = BINS / THREADS;
+    const int lane = tid % 64, wave = tid / 64, highest = BINS - 1 - wave * (64 * EACH) - lane;
+    double all = 0;
+    uint32_t words_all = 0;
+    {
+        uint64_t steps[EACH];
+        uint32_t n[EACH] = {}, t[EACH] = {}, words_before = 0, row_words = 0;
+        double s[EACH] = {}, before = 0, rows = 0;
 #pragma unroll
-            for (int k = 0; k < EACH; ++k) steps[k] = sh.steps[highest - 64 * k + 1];
-            if (__any((steps[0] | steps[1] | steps[2] | steps[3]) != 0)) {          // most waves have empty bins
-                static_assert(EACH == 4, "as many rows");
-                // e^-h, h at most 1/32, and that for 64 bins
-                const double h = 1.0 / per_nat;
-                double less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
+        for (int k = 0; k < EACH; ++k) steps[k] = sh.steps[highest - 64 * k + 1];
+        if (__any((steps[0] | steps[1] | steps[2] | steps[3]) != 0)) {          // most waves have empty bins
+            static_assert(EACH == 4, "as many rows");
+            // e^-h, h at most 1/32, and that for 64 bins
+            const double h = 1.0 / per_nat;
+            double less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
 #pragma unroll
-                for (int k = 0; k < 6; ++k) less *= less;
-                double edge = 0x1p-29 * exp(((double)(highest - BELOW) + (bins.anchor - (double)most) * bins.per_logit) * h);
-                // sums of a row of 64, up to and with the lane, then of the rows before it, then of the waves before
+            for (int k = 0; k < 6; ++k) less *= less;
+            double edge = 0x1p-29 * exp(((double)(highest - BELOW) + (bins.anchor - (double)most) * bins.per_logit) * h);
+            // sums of a row of 64, up to and with the lane, then of the rows before it, then of the waves before
 #pragma unroll
-                for (int k = 0; k < EACH; ++k) {
-                    s[k] = wave_scan((double)steps[k] * edge);
-                    if (top_k) n[k] = sh.count[highest - 64 * k + 1], c[k] = wave_scan(n[k]);
-                    edge *= less;
-                }
-#pragma unroll
-                for (int k = 0; k < EACH; ++k) {
-                    const double of_row = __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, s[k]), 63));
-                    s[k] = moved<0x138, 0xf>(s[k]) + rows, rows += of_row;
-                    if (top_k) {
-                        const uint32_t words = (uint32_t)__builtin_amdgcn_readlane((int)c[k], 63);
-                        c[k] = moved<0x138, 0xf>(c[k]) + row_words, row_words += words;
-                    }
-                }
-            }
-            if (lane == 0) sh.d[wave] = rows, sh.c[wave] = row_words;
-            __syncthreads();
-            for (int x = 0; x < WAVES; ++x) {
-                if (x == wave) before = all, words_before = words_all;
-                all += sh.d[x], words_all += sh.c[x];
+            for (int k = 0; k < EACH; ++k) {
+                s[k] = wave_scan((double)steps[k] * edge);
+                if (c.top_k) n[k] = sh.count[highest - 64 * k + 1], t[k] = wave_scan(n[k]);
+                edge *= less;
             }
 #pragma unroll
             for (int k = 0; k < EACH; ++k) {
-                const int b = highest - 64 * k;
-                sh.above[b] = s[k] + before;
-                const uint32_t words = c[k] + words_before;
-                if (top_k) sh.count[b] = words;
-                if (words < top_k && top_k <= words + n[k]) sh.found = b;
-            }
-            __syncthreads();
-        }
-        const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
-        // what each border leaves, from..to, and the bins it can lie in
-        const bool by_k = top_k && words_all >= top_k;      // otherwise words without weight make up the rest
-        double k_lo = all, k_hi = all;
-        const int k_bin = by_k ? (int)sh.found : -1;
-        if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
-        Range p_bins = {1, 0}, m_bins = {1, 0};
-        double p_lo = k_lo, p_hi = k_hi;
-        if (top_p < 1) {
-            const double p = top_p > 0 ? (double)top_p : 0.0;
-            p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
-            p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
-        }
-        double m_lo = all, m_hi = all;
-        if (min_p > 0) {
-            const double at = fmax(log((double)min_p) * per_nat + bins.place(most), 0.0);
-            m_bins = {min((int)fmax(at - 1e-6, 0.0), BINS - 1), min((int)(at + 1e-6), BINS - 1)};
-            m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
-        }
-        const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
-        // borders that others come before do not count
-        if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
-        const bool no_p = p_lo > hi * (1 + SLACK);
-        if (no_p) p_bins = {1, 0};
-        const bool need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
-        const double share = u < 0 ? 0.0 : u < 1 ? (double)u : 1.0;
-        const Range u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
-        const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
-        // their words
-        if (tid == 0) sh.n = 0;
-        __syncthreads();
-        {
-            // between these logits are all words of the bins: a piece seldom has one
-            int b_lo = BINS, b_hi = -2;
-            if (p_bins.lo <= p_bins.hi) b_lo = p_bins.lo, b_hi = p_bins.hi;
-            if (m_bins.lo <= m_bins.hi) b_lo = min(b_lo, m_bins.lo), b_hi = max(b_hi, m_bins.hi);
-            const int k_at = need_k ? k_bin : u_bins.lo;
-            const float from = b_hi < 0 ? INFINITY : bins.logit(b_lo, -1), to = b_hi < 0 ? -INFINITY : bins.logit(b_hi + 1, 1), u_from = bins.logit(u_bins.lo, -1), u_to = bins.logit(u_bins.hi + 1, 1), k_from = bins.logit(k_at, -1), k_to = bins.logit(k_at + 1, 1);
-            const float lowest = fminf(fminf(from, u_from), k_from);
-            const auto near = [&](float x) { return ((x >= from) & (x <= to)) | ((x >= u_from) & (x <= u_to)) | ((x >= k_from) & (x <= k_to)); };
-            all_of.each_piece([&](const Piece<T>& p, uint32_t i) {
-                float top = (float)p.v[0];
-#pragma unroll
-                for (int e = 1; e < T::VEC; ++e) top = fmaxf(top, (float)p.v[e]);
-                if (!(top >= lowest)) return;
-                bool any = false;
-#pragma unroll
-                for (int e = 0; e < T::VEC; ++e) any |= near((float)p.v[e]);
-                if (!any) return;
-#pragma unroll
-                for (int e = 0; e < T::VEC; ++e) {
-                    const float x = (float)p.v[e];
-                    if (!near(x)) continue;
-                    const int b = bins.bin(bins.place(x));
-                    if (b >= 0 && b < BINS && decides(b)) {
-                        const uint32_t n = atomicAdd(&sh.n, 1u);
-                        if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - (i + e));
-                    }
+                const double of_row = __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, s[k]), 63));
+                s[k] = moved<0x138, 0xf>(s[k]) + rows, rows += of_row;
+                if (c.top_k) {
+                    const uint32_t words = (uint32_t)__builtin_amdgcn_readlane((int)t[k], 63);
+                    t[k] = moved<0x138, 0xf>(t[k]) + row_words, row_words += words;
                 }
-            });
+            }
+        }
+        if (lane == 0) sh.d[wave] = rows, sh.c[wave] = row_words;
+        __syncthreads();
+        for (int x = 0; x < WAVES; ++x) {
+            if (x == wave) before = all, words_before = words_all;
+            all += sh.d[x], words_all += sh.c[x];
+        }
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int b = highest - 64 * k;
+            sh.above[b] = s[k] + before;
+            const uint32_t words = t[k] + words_before;
+            if (c.top_k) sh.count[b] = words;
+            if (words < c.top_k && c.top_k <= words + n[k]) sh.found = b;
         }
         __syncthreads();
-        const uint32_t n = sh.n;
-        const Weigh weigh = {most, (double)temperature, 1.0};
-        if (n <= 64) {
-            // one wave, a word a lane
-            if (tid < 64) {
-                const bool in = lane < (int)n;
-                uint64_t x = in ? sh.list[lane] : 0;
-                uint32_t place = 0;
-                for (uint32_t j = 0; j < n; ++j) place += read_lane(x, j) > x;
-                if (in) sh.list[place] = x;
-                asm volatile("" ::: "memory");      // a wave's accesses to LDS are done in their order
-                x = in ? sh.list[lane] : 0;
-                const float f = Key<F32>::value((uint32_t)(x >> 32));
-                const double w = in ? weigh.of(f) : 0;
-                const int bin = in ? bins.bin(bins.place(f)) : -1;
-                const double sum = wave_scan(w);
-                // the first word of the lane's bin in the list
-                const int prev = __shfl_up(bin, 1);
-                const uint64_t heads = __ballot(in && (lane == 0 || prev != bin)) & ~0ull >> (63 - lane);
-                const int head = heads ? 63 - __builtin_clzll(heads) : 0;
-                const double before = (in ? sh.above[bin] : 0) + (sum - w) - __shfl(sum - w, head), to = before + w;
-                double left = all;
-                bool found = true;
-                if (need_k) {
-                    const uint64_t at = __ballot(in && sh.count[in ? bin : 0] + lane - head == top_k - 1);
-                    found = at != 0;
-                    left = __shfl(to, at ? __builtin_ctzll(at) : 0);
-                }
-                if (p_bins.lo <= p_bins.hi) {
-                    const double target = top_p > 0 ? (double)top_p * left : 0.0;
-                    const uint64_t at = __ballot(in && bin >= p_bins.lo && bin <= p_bins.hi && (before < target || before == 0) && !(to < target));
-                    found = found && at != 0;
-                    left = fmin(left, __shfl(to, at ? __builtin_ctzll(at) : 0));
-                }
-                if (m_bins.lo <= m_bins.hi) {
-                    double m = in && bin >= m_bins.lo && bin <= m_bins.hi && w >= (double)min_p ? to : 0;
-#pragma unroll
-                    for (int d = 32; d; d >>= 1) m = fmax(m, __shfl_xor(m, d));
-                    left = fmin(left, fmax(m, m_lo));
-                }
-                const double target = fmin(share, 1 - 1e-14) * left;
-                const uint64_t at = __ballot(in && bin >= u_bins.lo && bin <= u_bins.hi && before <= target && target < to);
-                if (lane == 0) sh.word = NONE;
-                if (found && at && lane == (int)__builtin_ctzll(at)) {
-                    sh.word = 0xffffffffu - (uint32_t)x;
-                    a.words[row] = (int32_t)sh.word, a.logprob[row] = (float)log(w / left);
-                }
+    }
+    const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
+    // what each border leaves, from..to, and the bins it can lie in
+    const bool by_k = c.top_k && words_all >= c.top_k;      // otherwise words without weight make up the rest
+    double k_lo = all, k_hi = all;
+    const int k_bin = by_k ? (int)sh.found : -1;
+    if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
+    Range p_bins = {1, 0}, m_bins = {1, 0};
+    double p_lo = k_lo, p_hi = k_hi;
+    if (c.top_p < 1) {
+        const double p = c.top_p > 0 ? (double)c.top_p : 0.0;
+        p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
+        p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
+    }
+    double m_lo = all, m_hi = all;
+    if (c.min_p > 0) {
+        const double at = fmax(log((double)c.min_p) * per_nat + bins.place(most), 0.0);
+        m_bins = {min((int)fmax(at - 1e-6, 0.0), BINS - 1), min((int)(at + 1e-6), BINS - 1)};
+        m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
+    }
+    const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
+    // borders that others come before do not count
+    if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
+    const bool no_p = p_lo > hi * (1 + SLACK);
+    if (no_p) p_bins = {1, 0};
+    const bool need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
+    const double share = c.u < 0 ? 0.0 : c.u < 1 ? (double)c.u : 1.0;
+    const Range u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
+    const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
+    // their words
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    {
+        // between these logits are all words of the bins: a piece seldom has one
+        int b_lo = BINS, b_hi = -2;
+        if (p_bins.lo <= p_bins.hi) b_lo = p_bins.lo, b_hi = p_bins.hi;
+        if (m_bins.lo <= m_bins.hi) b_lo = min(b_lo, m_bins.lo), b_hi = max(b_hi, m_bins.hi);
+        const int k_at = need_k ? k_bin : u_bins.lo;
+        const float b_from = b_hi < 0 ? INFINITY : bins.logit(b_lo, -1), to = b_hi < 0 ? -INFINITY : bins.logit(b_hi + 1, 1), u_from = bins.logit(u_bins.lo, -1), u_to = bins.logit(u_bins.hi + 1, 1), k_from = bins.logit(k_at, -1), k_to = bins.logit(k_at + 1, 1);
+        const float lowest = fminf(fminf(b_from, u_from), k_from);
+        const auto near = [&](float x) { return ((x >= b_from) & (x <= to)) | ((x >= u_from) & (x <= u_to)) | ((x >= k_from) & (x <= k_to)); };
+        src.each_near(lowest, near, [&](float x, uint32_t i) {
+            const int b = bins.bin(bins.place(x));
+            if (b >= 0 && b < BINS && decides(b)) {
+                const uint32_t n = atomicAdd(&sh.n, 1u);
+                if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
             }
-            __syncthreads();
-            if (sh.word != NONE) return;
-        } else if (n <= MOST) {
-            // sorted, the largest first
-            uint32_t size = 128;
-            while (size < n) size *= 2;
-            for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
-            __syncthreads();
-            for (uint32_t k = 2; k <= size; k *= 2)
-                for (uint32_t j = k / 2; j; j /= 2) {
-                    if (tid < size / 2) {
-                        const uint32_t i = (tid / j * 2 * j) + tid % j;
-                        const uint64_t x = sh.list[i], y = sh.list[i + j];
-                        if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
-                    }
-                    if (size > 128) __syncthreads();
-                    else asm volatile("" ::: "memory");         // one wave, whose accesses to LDS are done in their order
-                }
-            __syncthreads();
-            // a thread has two neighbours: their weights, the weight before them, their rank
-            double w[2], before[2];
-            int bin[2];
-            uint32_t rank[2];
-            bool in[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t i = 2 * tid + e;
-                in[e] = i < n;
-                const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
-                bin[e] = in[e] ? bins.bin(bins.place(x)) : -1;
-                w[e] = in[e] ? weigh.of(x) : 0;
-            }
-            double sum_all;
-            const double sum = block_before(w[0] + w[1], sh.d, sum_all);
-            // where each bin's words begin in the list, and the sum there: steps of other bins are not needed any more, but their sums above are
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t i = 2 * tid + e;
-                before[e] = sum + (e ? w[0] : 0.0);
-                if (!in[e]) continue;
-                const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
-                if (i == 0 || bins.bin(bins.place(prev)) != bin[e]) {     // one thread for each bin
-                    sh.above[bin[e]] -= before[e];
-                    sh.count[bin[e]] -= i;
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (in[e]) before[e] += sh.above[bin[e]], rank[e] = sh.count[bin[e]] + 2 * tid + e;
-            // the borders, exactly
+        });
+    }
+    __syncthreads();
+    const uint32_t n = sh.n;
+    const Weigh weigh = {most, (double)c.temperature, 1.0};
+    if (n <= 64) {
+        // one wave, a word a lane
+        if (tid < 64) {
+            const bool in = lane < (int)n;
+            uint64_t x = in ? sh.list[lane] : 0;
+            uint32_t place = 0;
+            for (uint32_t j = 0; j < n; ++j) place += read_lane(x, j) > x;
+            if (in) sh.list[place] = x;
+            asm volatile("" ::: "memory");      // a wave's accesses to LDS are done in their order
+            x = in ? sh.list[lane] : 0;
+            const float f = Key<F32>::value((uint32_t)(x >> 32));
+            const double w = in ? weigh.of(f) : 0;
+            const int bin = in ? bins.bin(bins.place(f)) : -1;
+            const double sum = wave_scan(w);
+            // the first word of the lane's bin in the list
+            const int prev = __shfl_up(bin, 1);
+            const uint64_t heads = __ballot(in && (lane == 0 || prev != bin)) & ~0ull >> (63 - lane);
+            const int head = heads ? 63 - __builtin_clzll(heads) : 0;
+            const double before = (in ? sh.above[bin] : 0) + (sum - w) - __shfl(sum - w, head), to = before + w;
             double left = all;
+            bool found = true;
             if (need_k) {
-                if (tid == 0) sh.value = -1;
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (in[e] && rank[e] == top_k - 1) sh.value = before[e] + w[e];
-                __syncthreads();
-                left = sh.value;
+                const uint64_t at = __ballot(in && sh.count[in ? bin : 0] + lane - head == c.top_k - 1);
+                found = at != 0;
+                left = __shfl(to, at ? __builtin_ctzll(at) : 0);
             }
             if (p_bins.lo <= p_bins.hi) {
-                const double target = top_p > 0 ? (double)top_p * left : 0.0;
-                __syncthreads();
-                if (tid == 0) sh.value = -1;
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (in[e] && bin[e] >= p_bins.lo && bin[e] <= p_bins.hi && (before[e] < target || before[e] == 0) && !(before[e] + w[e] < target)) sh.value = before[e] + w[e];
-                __syncthreads();
-                left = fmin(left, sh.value);        // below 0: between two bins, by roundings; no word is found then
+                const double target = c.top_p > 0 ? (double)c.top_p * left : 0.0;
+                const uint64_t at = __ballot(in && bin >= p_bins.lo && bin <= p_bins.hi && (before < target || before == 0) && !(to < target));
+                found = found && at != 0;
+                left = fmin(left, __shfl(to, at ? __builtin_ctzll(at) : 0));
             }
             if (m_bins.lo <= m_bins.hi) {
-                // the words before the bins, and those of them that weigh enough
-                double m = 0;
+                double m = in && bin >= m_bins.lo && bin <= m_bins.hi && w >= (double)c.min_p ? to : 0;
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (in[e] && bin[e] >= m_bins.lo && bin[e] <= m_bins.hi && w[e] >= (double)min_p) m = fmax(m, before[e] + w[e]);
-                m = __builtin_bit_cast(double, block_max(__builtin_bit_cast(uint64_t, m), sh.a));
+                for (int d = 32; d; d >>= 1) m = fmax(m, __shfl_xor(m, d));
                 left = fmin(left, fmax(m, m_lo));
             }
             const double target = fmin(share, 1 - 1e-14) * left;
-            __syncthreads();
-            if (tid == 0) sh.word = NONE;
+            const uint64_t at = __ballot(in && bin >= u_bins.lo && bin <= u_bins.hi && before <= target && target < to);
+            if (lane == 0) sh.word = NONE;
+            if (found && at && lane == (int)__builtin_ctzll(at)) {
+                sh.word = 0xffffffffu - (uint32_t)x;
+                sh.weight = log(w / left);
+            }
+        }
+        __syncthreads();
+        word = sh.word, logprob = (float)sh.weight;
+    } else if (n <= MOST) {
+        // sorted, the largest first
+        uint32_t size = 128;
+        while (size < n) size *= 2;
+        for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
+        __syncthreads();
+        for (uint32_t k = 2; k <= size; k *= 2)
+            for (uint32_t j = k / 2; j; j /= 2) {
+                if (tid < size / 2) {
+                    const uint32_t i = (tid / j * 2 * j) + tid % j;
+                    const uint64_t x = sh.list[i], y = sh.list[i + j];
+                    if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
+                }
+                if (size > 128) __syncthreads();
+                else asm volatile("" ::: "memory");         // one wave, whose accesses to LDS are done in their order
+            }
+        __syncthreads();
+        // a thread has two neighbours: their weights, the weight before them, their rank
+        double w[2], before[2];
+        int bin[2];
+        uint32_t rank[2];
+        bool in[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t i = 2 * tid + e;
+            in[e] = i < n;
+            const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
+            bin[e] = in[e] ? bins.bin(bins.place(x)) : -1;
+            w[e] = in[e] ? weigh.of(x) : 0;
+        }
+        double sum_all;
+        const double sum = block_before(w[0] + w[1], sh.d, sum_all);
+        // where each bin's words begin in the list, and the sum there: steps of other bins are not needed any more, but their sums above are
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t i = 2 * tid + e;
+            before[e] = sum + (e ? w[0] : 0.0);
+            if (!in[e]) continue;
+            const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
+            if (i == 0 || bins.bin(bins.place(prev)) != bin[e]) {     // one thread for each bin
+                sh.above[bin[e]] -= before[e];
+                sh.count[bin[e]] -= i;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (in[e]) before[e] += sh.above[bin[e]], rank[e] = sh.count[bin[e]] + 2 * tid + e;
+        // the borders, exactly
+        double left = all;
+        if (need_k) {
+            if (tid == 0) sh.value = -1;
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                if (left >= 0 && in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
+                if (in[e] && rank[e] == c.top_k - 1) sh.value = before[e] + w[e];
             __syncthreads();
-            word = sh.word;
-            if (word != NONE) logprob = (float)log(sh.weight / left);
+            left = sh.value;
         }
-    }
-    if (word == NONE) {
+        if (p_bins.lo <= p_bins.hi) {
+            const double target = c.top_p > 0 ? (double)c.top_p * left : 0.0;
+            __syncthreads();
+            if (tid == 0) sh.value = -1;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (in[e] && bin[e] >= p_bins.lo && bin[e] <= p_bins.hi && (before[e] < target || before[e] == 0) && !(before[e] + w[e] < target)) sh.value = before[e] + w[e];
+            __syncthreads();
+            left = fmin(left, sh.value);        // below 0: between two bins, by roundings; no word is found then
+        }
+        if (m_bins.lo <= m_bins.hi) {
+            // the words before the bins, and those of them that weigh enough
+            double m = 0;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (in[e] && bin[e] >= m_bins.lo && bin[e] <= m_bins.hi && w[e] >= (double)c.min_p) m = fmax(m, before[e] + w[e]);
+            m = __builtin_bit_cast(double, block_max(__builtin_bit_cast(uint64_t, m), sh.a));
+            left = fmin(left, fmax(m, m_lo));
+        }
+        const double target = fmin(share, 1 - 1e-14) * left;
         __syncthreads();
-        choose_by_digits<T>(z, V, most, temperature, top_k_, top_p, min_p, u, sh, word, logprob);
+        if (tid == 0) sh.word = NONE;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (left >= 0 && in[e] && bin[e] >= u_bins.lo && bin[e] <= u_bins.hi && before[e] <= target && target < before[e] + w[e]) sh.word = 0xffffffffu - (uint32_t)sh.list[2 * tid + e], sh.weight = w[e];
+        __syncthreads();
+        word = sh.word;
+        if (word != NONE) logprob = (float)log(sh.weight / left);
     }
-    if (tid == 0) a.words[row] = (int32_t)word, a.logprob[row] = logprob;
+    return word == NONE ? UNDECIDED : DECIDED;
+}
+
+// the whole row, by one block
+template <class T>
+__device__ __forceinline__ void choose_from_row(const SampleArgs& a, uint32_t row, const Choice& c, Shared& sh)
+{
+    const typename T::elem* z = (const typename T::elem*)(a.logits + row * a.stride);
+    const Row<T> src(z, a.vocab);
+    float most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(src.largest_of_first()), sh.a)), logprob = NAN;
+    uint32_t word;
+    const int state = choose_by_bins(src, c, sh, most, word, logprob);
+    if (state == UNDECIDED) {
+        __syncthreads();
+        choose_by_digits<T>(z, a.vocab, most, c.temperature, (int32_t)c.top_k, c.top_p, c.min_p, c.u, sh, word, logprob);
+    }
+    if (threadIdx.x == 0) a.words[row] = state == WITHOUT ? -1 : (int32_t)word, a.logprob[row] = state == WITHOUT ? NAN : logprob;
+}
+
+// at temperature 0: the largest key, of these the lowest number; 0 where there is a NaN
+template <class T>
+__device__ __forceinline__ uint64_t first_word(const Row<T>& src, Shared& sh)
+{
+    uint64_t first = 0;
+    uint32_t nan = 0;
+    src.each([&](float x, uint32_t i) {
+        nan |= x != x;
+        const uint64_t k = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+        first = k > first ? k : first;
+    });
+    first = block_max(first, sh.a);
+    return block_sum(nan, sh.c) ? 0 : first;
+}
+__device__ __forceinline__ void put_first(const SampleArgs& a, uint32_t row, uint64_t first)
+{
+    const bool any = first && Key<F32>::value((uint32_t)(first >> 32)) > -INFINITY;
+    if (threadIdx.x == 0) a.words[row] = any ? (int32_t)(0xffffffffu - (uint32_t)first) : -1, a.logprob[row] = any ? 0.0f : NAN;
+}
+
+template <class T>
+__global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
+{
+    __shared__ Shared sh;
+    const uint32_t row = blockIdx.x;
+    const Choice c(a, row);
+    if (!c.fine()) put_first(a, row, 0);
+    else if (c.temperature == 0) put_first(a, row, first_word(Row<T>((const typename T::elem*)(a.logits + row * a.stride), a.vocab), sh));
+    else choose_from_row<T>(a, row, c, sh);
 }
 
 int check(const ff_sample_t* p)

@@ -118,6 +118,40 @@ def test_a_large_vocabulary():
         check(z, u, temperature=30.0, top_p=0.5, min_p=0.1)
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_rows_that_are_read_again(t):
+    """the largest logits far behind the first ones, and far above them; logits so far below the others that only a high temperature lets them count; a row whose first part is masked"""
+    z, u = rows(6, 70000, TYPES[t], spread=1.0, seed=9)
+    z[0, 60000:60050] += 60
+    z[1, 69999] = 200.0
+    z[2, 100:] -= 40
+    z[3, ::3] -= 25
+    z[4, :50000] = -math.inf
+    z[5, 17:] = -math.inf
+    for parameters in (dict(), dict(temperature=3.0, top_p=0.99), dict(temperature=9.0), dict(temperature=25.0, min_p=0.1), dict(temperature=0.1, top_k=60), dict(top_p=0.999, min_p=1e-7), dict(temperature=3.0, top_k=30000)):
+        check(z, u, **parameters)
+
+
+@pytest.mark.parametrize("t", ["f32", "f16"])
+@pytest.mark.parametrize("spread", [0.003, 0.02, 0.1, 0.5])
+def test_many_words_in_the_bins_that_decide(t, spread):
+    """logits so near one another that dozens, hundreds or thousands of words have to be put in order"""
+    z, u = rows(5, 9000, TYPES[t], spread=spread, seed=int(1000 * spread))
+    for parameters in (dict(), dict(top_p=0.4), dict(top_k=4000, top_p=0.7), dict(min_p=0.99), dict(temperature=0.01, top_k=100)):
+        check(z, u, **parameters)
+
+
+def test_a_mask_that_leaves_a_few_words():
+    z, u = rows(8, 50000, torch.bfloat16, seed=11)
+    keep = torch.zeros(8, 50000, dtype=torch.bool, device="cuda")
+    for r in range(8):
+        keep[r, torch.randperm(50000, device="cuda")[:2 ** r]] = True
+    z.masked_fill_(~keep, -math.inf)
+    for parameters in (dict(), dict(temperature=4.0, top_p=0.5), dict(top_k=20), dict(temperature=0.0)):
+        words, _ = check(z, u, **parameters)
+        assert bool(keep.gather(1, words.long()[:, None]).all())
+
+
 def test_shares_of_many_choices():
     """with every random number in turn, each word comes as often as its share says"""
     z = torch.randn(1, 40, device="cuda")
