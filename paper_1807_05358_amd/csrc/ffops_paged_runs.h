@@ -54,12 +54,14 @@ FFOPS_BOTH uint32_t slot_of(uint32_t run, bool begins_here) { return 2 * run + (
 FFOPS_BOTH uint32_t entry_of(int at, int nk, uint32_t page_log2) { return (uint32_t)(at < nk ? at : nk - 1) >> page_log2; }
 FFOPS_BOTH uint32_t place_of(int at, int nk, uint32_t page) { return (uint32_t)(at < nk ? at : nk - 1) & (page - 1) & ~15u; }
 
-// Runs of a key head, or none: then a block takes a sequence.  Sequences are cut where they alone do not fill the device.  others: key heads times blocks of columns.
-inline uint32_t runs_of(uint64_t others, uint64_t batch, uint64_t positions)
+// Runs of a key head, or none: then a block takes a sequence.  blocks: key heads times blocks of columns, of one sequence.  Cutting takes a second kernel, 3 to 5 us, and pays where blocks are few and sequences long, or of
+// different lengths: 1 x 8 heads of 4096 positions, bf16, 39 us whole, 20 cut, of 1024 18 and 20; 32 x 16 heads of up to 4000 113 and 91, all of 4000 176 and 179, all of 1000 41 and 44; 64 x 16 heads of 300 29 and 31, of up to 4000
+// 195 and 187.
+inline uint32_t runs_of(uint64_t blocks, uint64_t batch, uint64_t positions)
 {
+    if (positions <= 1024 || blocks * batch >= 1024 || (blocks * batch >= 512 && positions <= 2048)) return 0;
     const uint64_t tiles = (positions + TILE - 1) / TILE;
-    if (tiles <= 8 || others * batch >= 4096) return 0;
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / others, (tiles * batch + TILES_OF_RUN - 1) / TILES_OF_RUN));
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(512 / blocks, (tiles * batch + TILES_OF_RUN - 1) / TILES_OF_RUN));
 }
 
 }  // namespace ffops

@@ -174,6 +174,5 @@ def test_places_are_within_the_table_and_the_page(ask):
 
 
 def test_sequences_are_cut_only_where_blocks_are_few(ask):
-    assert ask([("r", 8, 8, 16384)]) == [64]
-    assert ask([("r", 8, 1, 256)]) == [0] and ask([("r", 64, 64, 16384)]) == [0] and ask([("r", 5000, 1, 16384)]) == [0]
-    assert ask([("r", 1, 1, 288)]) == [2] and ask([("r", 2000, 1, 16384)]) == [1]
+    assert ask([("r", 8, 8, 16384)]) == [64] and ask([("r", 1, 1, 1040)]) == [5] and ask([("r", 600, 1, 16384)]) == [1] and ask([("r", 16, 32, 4096)]) == [32]
+    assert ask([("r", 8, 1, 1024), ("r", 64, 64, 16384), ("r", 5000, 1, 16384), ("r", 16, 32, 2048)]) == [0, 0, 0, 0]

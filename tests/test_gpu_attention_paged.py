@@ -11,6 +11,7 @@ from paper_1807_05358_amd import operators as O  # noqa: E402
 from test_gpu_cache import TYPES, empty_cache, tables  # noqa: E402
 
 pytestmark = pytest.mark.gpu
+CUT = 1040         # positions more in the table: sequences are then cut into runs
 
 
 def filled(lengths, K, P, D, held, t, seed=0, more_entries=0, spread=1.0):
@@ -45,7 +46,7 @@ CASES = [  # held, type, lengths, heads, kv_heads, queries, dim, page, causal
     ("same", "f16", [5, 0, 17], 4, 2, 1, 128, 16, False),
     ("same", "bf16", [33, 16, 15], 8, 1, 1, 72, 32, False),
     ("same", "f16", [100, 64, 31], 12, 4, 2, 8, 16, True),
-    ("same", "bf16", [700, 3, 257, 512], 8, 8, 1, 128, 16, False),            # cut into runs
+    ("same", "bf16", [700, 3, 257, 512], 8, 8, 1, 128, 16, False),
     ("same", "f16", [1, 2000, 0, 0, 900, 13], 6, 2, 3, 64, 64, True),
     ("same", "bf16", [300, 1], 48, 2, 1, 96, 16, False),                      # 24 columns
     ("same", "bf16", [90, 40], 32, 4, 9, 128, 128, True),                     # 72 columns, three blocks of them
@@ -60,10 +61,12 @@ CASES = [  # held, type, lengths, heads, kv_heads, queries, dim, page, causal
 ]
 
 
+@pytest.mark.parametrize("cut", [False, True])
 @pytest.mark.parametrize("held,t,lengths,H,K,n,D,P,causal", CASES)
-def test_against_the_definition(held, t, lengths, H, K, n, D, P, causal):
+def test_against_the_definition(held, t, lengths, H, K, n, D, P, causal, cut):
+    """by a block for each sequence, and, with a table for long ones, by runs of tiles"""
     t = TYPES[t]
-    cache = filled(lengths, K, P, D, held, t, seed=D + n)
+    cache = filled(lengths, K, P, D, held, t, seed=D + n, more_entries=CUT // P if cut else 0)
     q = (1.5 * torch.randn(len(lengths), n, H, D, device="cuda")).to(t).transpose(1, 2)
     o, _ = compare(q, *cache, causal=causal)
     assert o.stride() == q.stride()                                           # an output in the queries' order
@@ -71,10 +74,11 @@ def test_against_the_definition(held, t, lengths, H, K, n, D, P, causal):
     assert torch.equal(o, again)
 
 
+@pytest.mark.parametrize("cut", [False, True])
 @pytest.mark.parametrize("held", ["same", "e4m3", "e2m1"])
-def test_lengths_of_queries_and_masks_that_leave_nothing(held):
+def test_lengths_of_queries_and_masks_that_leave_nothing(held, cut):
     lengths = [3, 40, 0, 600, 7]
-    cache = filled(lengths, 2, 16, 64, held, torch.bfloat16)
+    cache = filled(lengths, 2, 16, 64, held, torch.bfloat16, more_entries=CUT // 16 if cut else 0)
     q = torch.randn(5, 4, 6, 64, device="cuda").bfloat16()
     for q_lengths in ([6, 2, 3, 0, -1], [1, 6, 6, 9, 5]):
         nq = torch.tensor(q_lengths, dtype=torch.int32, device="cuda")
@@ -96,11 +100,11 @@ def test_lengths_outside_the_table_are_clamped():
 
 
 @pytest.mark.parametrize("held", ["same", "e4m3", "e2m1"])
-@pytest.mark.parametrize("lengths", [[40, 100], [900, 600]])
-def test_a_missing_page_is_loud(held, lengths):
+@pytest.mark.parametrize("lengths,cut", [([40, 100], False), ([900, 600], False), ([40, 100], True), ([900, 600], True)])
+def test_a_missing_page_is_loud(held, lengths, cut):
     """queries that see the positions of an entry that is no page get NaN, the others their values"""
     for entry in (-1, 10 ** 6):
-        cache = filled(lengths, 2, 16, 64, held, torch.bfloat16)
+        cache = filled(lengths, 2, 16, 64, held, torch.bfloat16, more_entries=CUT // 16 if cut else 0)
         cache[3][0, 1] = entry                    # positions 16 .. 31 of the first sequence
         q = torch.randn(2, 4, 1, 64, device="cuda").bfloat16()
         o, lse = compare(q, *cache)
@@ -121,7 +125,7 @@ def test_a_missing_page_is_loud(held, lengths):
 def test_large_scores_and_values():
     """scores far apart, where all but a few keys weigh nothing; rows of values at the type's ends"""
     for t in (torch.float16, torch.bfloat16):
-        cache = filled([500, 64], 2, 16, 128, "same", t, spread=6.0)
+        cache = filled([500, 64], 2, 16, 128, "same", t, spread=6.0, more_entries=CUT // 16)
         q = (6 * torch.randn(2, 4, 1, 128, device="cuda")).to(t)
         compare(q, *cache)
         compare(q, *cache, scale=2.0)
@@ -156,7 +160,7 @@ def test_infinities_and_nans_reach_the_queries_that_see_them():
 def test_many_sequences():
     """more sequences than threads of a block, most of them short or empty, one long"""
     lengths = [(i * 7) % 23 if i % 3 else 0 for i in range(700)]
-    lengths[350] = 1800
+    lengths[350] = 2600
     for held in ("same", "e4m3"):
         cache = filled(lengths, 1, 16, 64, held, torch.bfloat16)
         q = torch.randn(700, 2, 1, 64, device="cuda").bfloat16()
@@ -195,7 +199,7 @@ def test_like_the_contiguous_kernel():
 
 def test_captured_and_replayed():
     """a step in a graph, replayed with other lengths and queries, eager work between; a second graph of the same cache beside it"""
-    cache = filled([900, 300], 2, 16, 64, "same", torch.bfloat16)
+    cache = filled([900, 300], 2, 16, 64, "same", torch.bfloat16, more_entries=CUT // 16)
     k_pages, v_pages, scales, tab, nk = cache
     q = torch.randn(2, 4, 1, 64, device="cuda").bfloat16()
     new = torch.randn(2, 2, 1, 64, device="cuda").bfloat16()
