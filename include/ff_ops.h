@@ -212,7 +212,7 @@ typedef struct {
 int ff_op_cache_read(const ff_cache_read_t* a, void* stream);
 
 /* Attention of new queries over a paged cache: as ff_op_attention_fwd with kv_lengths[b] keys of sequence b (clamped to 0 .. the positions of the table; null: all of these).
- * A query that sees a position whose entry is no page gets NaN for o and lse.  Value rows that some queries of a sequence see and others do not have to be finite.
+ * A query that sees a position whose entry is no page gets NaN for o and lse, no other does.  Value rows that some queries of a sequence see, and others that see any do not, have to be finite.
  * Probabilities meet the values in bfloat16 as a sum of two such numbers, in float16 rounded, 2^8 times what they are of the row's largest. */
 typedef struct {
     uint32_t dtype, batch, heads, kv_heads, q_len, head_dim, causal;

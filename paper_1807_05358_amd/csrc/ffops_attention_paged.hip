@@ -222,12 +222,12 @@ struct Values {
         }
         if constexpr (HELD != FF_HELD_SAME) s[half] = *(const uint32_t*)(scales + ((HELD == FF_HELD_E4M3 ? 0 : min((uint32_t)(l.x * EACH / 32), a.c.blocks - 1)) * a.c.page + l.g * 4));
     }
-    // positions from `left` on (of those of lane group 0) are behind the last: what lies there may be anything
-    __device__ __forceinline__ void clear(int left)
+    // positions from left[half] on (of those of lane group 0) are behind the last, or have no page: what lies there, or was read in its place, may be anything
+    __device__ __forceinline__ void clear(const int* left)
     {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const bool out = 16 * (e / 4) + e % 4 >= left;
+            const bool out = e % 4 >= left[e / 4];
 #pragma unroll
             for (int i = 0; i < RAW; ++i) raw[e][i] = out ? 0 : raw[e][i];
             if constexpr (HELD != FF_HELD_SAME) s[e / 4] = out ? s[e / 4] & ~(255u << (e % 4 * 8)) : s[e / 4];
@@ -389,9 +389,13 @@ __device__ __forceinline__ void work(const PagedArgs& a, Tile<T, HELD, D, FULL>&
                     if (16 * h + r >= first || x.bad[h]) s[t][h][r] = -INFINITY;
             if ((x.bad[0] && at < c.seen[t]) || (x.bad[1] && at + 16 < c.seen[t])) y.sum[t] = NAN;
         }
-        if (at + TILE > nk) {
-            int left = nk - at - 4 * l.g;
-            stay_here(left);
+        if (at + TILE > nk || bad) {
+            int left[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                left[h] = x.bad[h] ? 0 : nk - at - 16 * h - 4 * l.g;
+                stay_here(left[h]);
+            }
             x.v.clear(left);
         }
     }
@@ -546,8 +550,9 @@ __global__ __launch_bounds__(256, (RESIDENT<HELD, D, NT>)) void k_attention_page
                 for (int j = 0; j < DT; ++j) r[j] += sums[t][w][cc][d0 + j] * f;
             }
             const float inv = sum > 0 ? 1.0f / sum : sum == sum ? 0.0f : sum;
+            const uint32_t keep = sum == 0 ? 0 : ~0u;           // a query that sees nothing has zeros, whatever values others see
 #pragma unroll
-            for (int j = 0; j < DT; ++j) r[j] *= inv;
+            for (int j = 0; j < DT; ++j) r[j] = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, r[j] * inv) & keep);
             const uint32_t i = query_of(a, col), h = kh * a.group + col - i * a.group;
             if (whole) {
                 if (d0 == 0) a.lse[((uint64_t)b * a.heads + h) * a.q_len + i] = (most + log2_(sum)) * LN2;

@@ -485,7 +485,7 @@ def cache_write(k, v, k_pages, v_pages, table, start, *, lengths=None, k_scales=
     A scale s stands for 2^(s - 127); 255: the block held a value that was not finite and is read as NaN.  Positions outside the table, and entries that are no page, are not
     written.  Sequences may share pages, but no two positions of a call the same place."""
     torch = _torch()
-    _not_recorded(k, v)
+    _not_recorded(k, v, k_pages, v_pages)
     if k.dim() != 4:
         raise ValueError("k is [batch, kv_heads, positions, elements]")
     dtype, device = _dtype(k, "k"), k.device
@@ -505,6 +505,7 @@ def cache_read(k_pages, v_pages, table, lengths, *, kv_len=None, dtype=None, k_s
     """(k, v) [batch, kv_heads, kv_len, dim] of the first lengths[b] positions (int32 [batch]) of each sequence of a paged cache (see cache_write), zeros behind them.
     kv_len: the positions of the table if not given; dtype: float16 or bfloat16, the pages' own if they hold one of these.  A position whose entry is no page gives NaN."""
     torch = _torch()
+    _not_recorded(k_pages, v_pages)
     if dtype is None and k_pages.dtype in (torch.float16, torch.bfloat16):
         dtype = k_pages.dtype
     if dtype not in (torch.float16, torch.bfloat16):
@@ -527,7 +528,7 @@ def attention_paged_fwd(q, k_pages, v_pages, table, kv_lengths, *, causal=False,
     lse = -inf.  A query that sees a position whose entry is no page gets NaN.  Keys and values are read once for a few queries of each head (16 queries times heads of a key head are worked together, 32 where there are more), so
     long prompts are better read back with cache_read for attention_fwd."""
     torch = _torch()
-    _not_recorded(q)
+    _not_recorded(q, k_pages, v_pages)
     if q.dim() != 4:
         raise ValueError("q is [batch, heads, positions, elements]")
     dtype, device = _dtype(q, "q"), q.device

@@ -85,6 +85,11 @@ def test_functions_refuse_what_they_cannot_take():
                 lambda: O.cache_write(new.float(), new.float(), pages, pages, tab, n), lambda: O.sample(z.double(), u), lambda: O.sample(z[:, :0], u)):
         with pytest.raises(ValueError):
             bad()
+    # a cache that autograd would follow: writing and reading are not recorded
+    leaf = pages.clone().requires_grad_()
+    for call in (lambda: O.cache_write(new, new, leaf, pages, tab, n), lambda: O.cache_read(leaf, pages, tab, n), lambda: O.attention_paged_fwd(q, pages, leaf, tab, n)):
+        with pytest.raises(ValueError, match="gradients"):
+            call()
     # of a cache, as of one on a GPU
     meta = lambda *s, dtype: torch.empty(*s, dtype=dtype, device="meta")
 

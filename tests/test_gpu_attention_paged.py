@@ -122,6 +122,42 @@ def test_a_missing_page_is_loud(held, lengths, cut):
     assert bad.tolist() == [False] * 12 + [True] * 8 and bool(torch.isfinite(o[0, :, :12]).all()) and bool(torch.isnan(o[0, :, 12:]).all())
 
 
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("held", ["same", "e4m3", "e2m1"])
+@pytest.mark.parametrize("t", [torch.float16, torch.bfloat16])
+def test_a_missing_page_leaves_the_others_alone(t, held, cut):
+    """whatever lies in the page that is read in its place: queries that do not see the missing positions keep their values"""
+    for n, lengths in ((20, [40]), (3, [1200])):
+        k_pages, v_pages, scales, tab, nk = filled(lengths, 2, 16, 64, held, t, more_entries=CUT // 16 if cut else 0)
+        free = next(i for i in range(len(k_pages)) if i and i not in tab.tolist()[0])
+        for x in (k_pages.view(torch.uint8), v_pages.view(torch.uint8), *scales.values()):
+            x[free] = x[0]
+            x[0] = 0xff                           # NaN, of elements and of scales
+        tab[tab == 0] = free
+        last = -(-lengths[0] // 16) - 1
+        q = torch.randn(1, 2, n, 64, device="cuda").to(t)
+        whole = [x.clone() for x in compare(q, k_pages, v_pages, scales, tab, nk, causal=True)]
+        tab[0, last] = -1
+        o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, nk, causal=True, **scales)
+        sees = [i + lengths[0] - n >= 16 * last for i in range(n)]
+        assert torch.isnan(lse[0, 0]).tolist() == sees and torch.isnan(o[0]).all(2)[1].tolist() == sees
+        for x, y in zip((o, lse), whole):
+            assert torch.equal(x[0][:, :n - sum(sees)], y[0][:, :n - sum(sees)])
+        # queries that are padding see none of it
+        o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, nk, q_lengths=torch.ones_like(nk), **scales)
+        assert bool(torch.isnan(o[0, :, 0]).all()) and int(o[0, :, 1:].count_nonzero()) == 0 and bool((lse[0, :, 1:] == -math.inf).all())
+
+
+@pytest.mark.parametrize("cut", [False, True])
+def test_padding_beside_values_that_are_not_finite(cut):
+    k_pages, v_pages, scales, tab, nk = filled([1100, 30], 1, 16, 64, "same", torch.bfloat16, more_entries=CUT // 16 if cut else 0)
+    v_pages[tab[:, 0].long(), 0, 3, 7] = math.inf
+    q = torch.randn(2, 2, 3, 64, device="cuda").bfloat16()
+    o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, nk, q_lengths=torch.tensor([2, 0], dtype=torch.int32, device="cuda"))
+    assert bool(torch.isinf(o[0, :, :2, 7]).all()) and int((~torch.isfinite(o)).sum()) == 4
+    assert int(o[0, :, 2].count_nonzero()) == int(o[1].count_nonzero()) == 0 and bool((lse[0, :, 2] == -math.inf).all()) and bool((lse[1] == -math.inf).all())
+
+
 def test_large_scores_and_values():
     """scores far apart, where all but a few keys weigh nothing; rows of values at the type's ends"""
     for t in (torch.float16, torch.bfloat16):
