@@ -108,16 +108,17 @@ class Decoder:
 
     def extend(self, cache, tokens, lengths=None):
         """logits [batch, vocab], float32, behind the last of the new tokens [batch, length] of each sequence (the first lengths[b] of them, int32 [batch]; at least one); the
-        cache then holds them, too.  What follows them is padding, any word."""
+        cache then holds them, too.  What follows them is padding, any word.  Captured into a graph, each replay moves the cache's lengths; `filled` is then the caller's to move, and
+        tokens beyond the cache's positions are not kept."""
         import torch
         p, H = self.params, self.heads
         B, S = tokens.shape
         if S == 0 or cache.filled + S > cache.positions:
             raise ValueError(f"{S} new tokens behind up to {cache.filled} do not fit a cache of {cache.positions} positions")
         D = self.hidden
-        new = torch.full_like(cache.lengths, S) if lengths is None else lengths
-        start, total = cache.lengths, cache.lengths + new
-        cache.filled += S
+        new = torch.full_like(cache.lengths, S) if lengths is None else lengths.clamp(0, S)
+        start, total, filled = cache.lengths, cache.lengths + new, cache.filled + S
+        replayed = torch.cuda.is_current_stream_capturing()
         h, add = p["embedding"][tokens.reshape(-1).long()], None
         for n in range(self.layers):
             x, res = (h, None) if add is None else (add, h)
@@ -128,12 +129,14 @@ class Decoder:
             if S <= cache.FEW:
                 o, _ = O.attention_paged_fwd(q, *pages, cache.table, total, causal=True, q_lengths=new, **scales)
             else:                         # many queries share a tile of keys in the contiguous kernel
-                k, v = O.cache_read(*pages, cache.table, total, kv_len=cache.filled, dtype=q.dtype, **scales)
+                k, v = O.cache_read(*pages, cache.table, total, kv_len=cache.positions if replayed else filled, dtype=q.dtype, **scales)
                 o, _ = O.attention_fwd(q, k, v, causal=True, q_lengths=new, kv_lengths=total)
             add = o.transpose(1, 2).reshape(B * S, D) @ p[f"{n}.out"].t()
             y, h, *_ = O.layernorm_fwd(add, p[f"{n}.b.w"], p[f"{n}.b.b"], residual=h)
             add = torch.relu(y @ p[f"{n}.up"].t()) @ p[f"{n}.down"].t()
-        cache.lengths = total
+        cache.lengths.copy_(total)
+        if not replayed:
+            cache.filled = filled
         last = torch.arange(B, device=h.device) * S + (new.long() - 1).clamp_min(0)
         y = O.layernorm_fwd(add[last], p["last.w"], p["last.b"], residual=h[last])[0]
         return (y @ p["words"].t()).float()

@@ -128,3 +128,50 @@ def test_a_step_in_a_graph():
         g.replay()
         got.append(now.clone())
     assert torch.equal(torch.stack(got, 1), want)
+
+
+def test_a_call_that_fails_leaves_the_cache_as_it_was():
+    model = L.Decoder(VOCAB, HIDDEN, HEADS, LAYERS, dtype=torch.bfloat16, seed=8)
+    tokens = prompts(2, 20, seed=9)
+    cache = L.Cache(model, 2, 64)
+    model.extend(cache, tokens)
+    for bad in (lambda: model.extend(cache, prompts(3, 4)), lambda: model.extend(cache, tokens, torch.ones(2, dtype=torch.int64, device="cuda")), lambda: model.extend(cache, tokens[:, :0])):
+        with pytest.raises(ValueError):
+            bad()
+    assert cache.filled == 20 and cache.lengths.tolist() == [20, 20]
+
+
+def test_lengths_beyond_the_new_tokens():
+    """are those of all of them: nothing behind them is looked at"""
+    model = L.Decoder(VOCAB, HIDDEN, HEADS, LAYERS, dtype=torch.bfloat16, seed=8)
+    tokens = prompts(2, 20, seed=9)
+    a, b = L.Cache(model, 2, 64), L.Cache(model, 2, 64)
+    for new in (tokens, tokens[:, :3]):
+        x, y = model.extend(a, new), model.extend(b, new, torch.tensor([10 ** 6, new.shape[1]], dtype=torch.int32, device="cuda"))
+        assert torch.equal(x, y) and a.lengths.tolist() == b.lengths.tolist()
+
+
+@pytest.mark.parametrize("piece", [1, 4, 9])
+def test_a_captured_piece_moves_the_lengths(piece):
+    """replayed as it stands, pieces of a sequence one behind the other: few tokens from the pages, more by way of reading back"""
+    model = L.Decoder(VOCAB, HIDDEN, HEADS, LAYERS, dtype=torch.float16, seed=10)
+    tokens = prompts(2, 11 + 4 * piece, seed=11)
+    eager, cache = L.Cache(model, 2, 64, page=16), L.Cache(model, 2, 64, page=16)
+    model.extend(eager, tokens[:, :11]), model.extend(cache, tokens[:, :11])
+    new = tokens[:, 11:11 + piece].clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        model.extend(L.Cache(model, 2, 64, page=16), new)
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = model.extend(cache, new)
+    assert cache.filled == 11
+    for at in range(11, 11 + 4 * piece, piece):
+        new.copy_(tokens[:, at:at + piece])
+        g.replay()
+        want = model.extend(eager, new)
+        assert cache.lengths.tolist() == eager.lengths.tolist() == [at + piece] * 2
+        # kernels of another number of keys may add in another order: a rounding of each of the layers' outputs
+        assert (got - want).norm() <= (15 * LAYERS + 10) * 2.0 ** -11 * want.norm()
