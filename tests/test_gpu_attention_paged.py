@@ -267,3 +267,46 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         for r in results:
             assert all(torch.equal(x, y) for x, y in zip(r, want))
+
+
+def test_on_two_streams_at_once():
+    """each call has a workspace of its own"""
+    cache = filled([5000, 300], 2, 16, 64, "e4m3", torch.bfloat16)
+    qs = [torch.randn(2, 4, 1, 64, device="cuda").bfloat16() for _ in range(2)]
+
+    def call(q):
+        return O.attention_paged_fwd(q, cache[0], cache[1], cache[3], cache[4], **cache[2])
+
+    want = [call(q) for q in qs]
+    got = []
+    for q in qs:
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            got.append([call(q) for _ in range(10)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for w, several in zip(want, got) for g in several for x, y in zip(g, w))
+
+
+def test_as_many_sequences_and_queries_as_there_may_be():
+    """65535 sequences, cut and not, each as it is by itself; one head's 65535 * 16 queries"""
+    B, D, t = 65535, 8, torch.bfloat16
+    k_pages, v_pages = (torch.randn(64, 1, 16, D, device="cuda").to(t) for _ in range(2))
+    some = torch.tensor([0, 1, 255, 256, 32768, B - 1], device="cuda")
+    for entries in (2, 70):
+        tab = torch.randint(0, 64, (B, entries), dtype=torch.int32, device="cuda")
+        nk = torch.randint(0, 33, (B,), dtype=torch.int32, device="cuda")
+        q = torch.randn(B, 1, 1, D, device="cuda").to(t)
+        o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, nk)
+        a, b = O.attention_paged_fwd(q[some], k_pages, v_pages, tab[some], nk[some])
+        c, d = compare(q[some], k_pages, v_pages, {}, tab[some], nk[some])
+        # parts of a sequence are joined where another call does not cut it: a rounding to float32 each, and one to the type that may fall the other way
+        assert float((lse[some] - d).nan_to_num(0).abs().max()) < 1e-5 and float((o[some].float() - c.float()).abs().max()) <= 2.0 ** -8 * float(v_pages.float().abs().max())
+        assert torch.equal(a, c) and torch.equal(b, d)
+    n = 65535 * 16
+    q = torch.randn(1, 1, n, D, device="cuda").to(t)
+    tab, nk = torch.arange(3, dtype=torch.int32, device="cuda")[None], torch.tensor([41], dtype=torch.int32, device="cuda")
+    o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, nk)
+    for at in (0, n // 2 + 5, n - 3):
+        x, y = compare(q[:, :, at:at + 3].contiguous(), k_pages, v_pages, {}, tab, nk)
+        assert torch.equal(x, o[:, :, at:at + 3]) and torch.equal(y, lse[:, :, at:at + 3])

@@ -205,6 +205,40 @@ def test_offsets_beyond_32_bits():
     assert bool(((o.double() - want[0]).abs() <= want[1]).all()) and bool(((lse.double() - want[2]).abs() <= want[3]).all())
 
 
+@pytest.mark.parametrize("held", ["e4m3", "e2m1"])
+def test_offsets_beyond_32_bits_in_fewer_bits(held):
+    """pages and scales that lie more than 4 GiB behind the first, a view of one buffer"""
+    D, P, K, t, step = 64, 16, 2, torch.bfloat16, 3 << 30
+    room = torch.empty(3 * step, dtype=torch.uint8, device="cuda")
+    elements = D if held == "e4m3" else D // 2
+    blocks = 1 if held == "e4m3" else D // 32
+
+    def view(at, *shape):
+        stride = [step, shape[1] * shape[2], shape[2], 1]
+        return room.as_strided((3, *shape), stride, at)
+
+    k_pages, v_pages = (view(at, K, P, elements) for at in (0, 1 << 20))
+    if held == "e4m3":
+        k_pages, v_pages = k_pages.view(torch.float8_e4m3fn), v_pages.view(torch.float8_e4m3fn)
+    scales = {"k_scales": view(2 << 20, K, blocks, P), "v_scales": view(3 << 20, K, blocks, P)}
+    tab = torch.tensor([[2, 0], [1, -1]], dtype=torch.int32, device="cuda")
+    nk = torch.tensor([30, 16], dtype=torch.int32, device="cuda")
+    k, v = (torch.randn(2, K, 30, D, device="cuda").to(t) for _ in range(2))
+    O.cache_write(k, v, k_pages, v_pages, tab, torch.zeros_like(nk), lengths=nk, **scales)
+    got = O.cache_read(k_pages, v_pages, tab, nk, kv_len=30, dtype=t, **scales)
+    q = torch.randn(2, 4, 1, D, device="cuda").to(t)
+    o, lse = O.attention_paged_fwd(q, k_pages, v_pages, tab, nk, **scales)
+    dense = []
+    for g, x in zip(got, (k, v)):
+        codes, s = R.hold(x.transpose(1, 2).contiguous(), held)
+        want = R.stands_for(codes, s, held, t).transpose(1, 2)
+        want[1, :, 16:] = 0
+        assert torch.equal(g.double(), want)
+        dense.append(want)
+    want = R.attention(q, *dense, nk)
+    assert bool(((o.double() - want[0]).abs() <= want[1]).all()) and bool(((lse.double() - want[2]).abs() <= want[3]).all())
+
+
 def test_another_stream():
     D, P, t = 64, 16, torch.bfloat16
     k_pages, v_pages, _ = empty_cache(8, 2, P, D, "same", t)

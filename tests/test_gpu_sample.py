@@ -187,3 +187,46 @@ def test_requires_grad_is_refused():
         O.sample(z, u)
     with torch.no_grad():
         O.sample(z, u)
+
+
+def test_as_many_rows_and_words_as_there_may_be():
+    torch.manual_seed(11)
+    # every row of two words: the larger one weighs 1 of 1 + e^-d
+    R_, u = (1 << 22) - 1, torch.rand((1 << 22) - 1, device="cuda")
+    z = torch.randn(R_, 2, device="cuda").half()
+    words, logprob = O.sample(z, u)
+    first = (z[:, 1] > z[:, 0]).int()
+    share = 1 / (1 + torch.exp(-(z[:, 0].double() - z[:, 1].double()).abs()))
+    near = (u.double() - share).abs() < 1e-8
+    want = torch.where(u.double() < share, first, 1 - first)
+    assert bool(((words == want) | near).all())
+    p = torch.where(words == first, share, 1 - share)
+    assert float((logprob.double() - p.log()).abs().max()) < 1e-6
+    # 2^24 words, with and without many equal ones
+    for t in (torch.float32, torch.float16):
+        z, u = torch.randn(2, 1 << 24, device="cuda").to(t), torch.tensor([0.3, 0.999], device="cuda")
+        words, logprob = O.sample(z, u, temperature=0.5, top_p=0.7)
+        for row in range(2):
+            w = torch.exp((z[row].double() - z[row].double().max()) / 0.5)
+            order = torch.sort(z[row], descending=True, stable=True)[1]
+            run = torch.cumsum(w[order], 0)
+            n = int(torch.searchsorted(run, 0.7 * run[-1])) + 1
+            at = int((order == words[row]).nonzero()[0])
+            target = float(u[row]) * float(run[n - 1])
+            # the sums: to 2^-29 of themselves, and where top_p cuts by a word, 2e-6 of all, more or less
+            slack = 1e-8 * target + float(w[order[n - 1]])
+            assert float(run[at] - w[words[row]]) - slack <= target <= float(run[at]) + slack
+            assert abs(float(logprob[row]) - math.log(float(w[words[row]] / run[n - 1]))) < 1e-5
+
+
+def test_on_two_streams_at_once():
+    z, u = rows(64, 30000, torch.bfloat16)
+    want = [O.sample(z, u, top_p=p) for p in (0.5, 0.95)]
+    streams = [torch.cuda.Stream() for _ in want]
+    got = []
+    for s, p in zip(streams, (0.5, 0.95)):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            got.append([O.sample(z, u, top_p=p) for _ in range(5)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for w, several in zip(want, got) for g in several for x, y in zip(g, w))
