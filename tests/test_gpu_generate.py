@@ -36,12 +36,14 @@ def prompts(batch, length, seed=0):
     return torch.randint(0, VOCAB, (batch, length), generator=g, device="cuda", dtype=torch.int32)
 
 
+@pytest.mark.parametrize("few", [L.Cache.FEW, 8])
 @pytest.mark.parametrize("t", [torch.float16, torch.bfloat16])
-def test_extend_in_any_pieces(t):
-    """a prompt, then a piece read back, then few tokens, then single ones: behind each, the logits of all that came before"""
+def test_extend_in_any_pieces(t, few):
+    """a prompt, then a piece, from the pages or read back, then few tokens, then single ones: behind each, the logits of all that came before"""
     model = L.Decoder(VOCAB, HIDDEN, HEADS, LAYERS, dtype=t, seed=1)
     tokens = prompts(3, 80)
     cache = L.Cache(model, 3, 80, page=16)
+    cache.FEW = few
     had = [[], [], []]
     # rounding of about 15 tensors in each layer and 10 outside, each at most half a step of its size
     most = (15 * LAYERS + 10) * torch.finfo(t).eps / 2
@@ -157,6 +159,7 @@ def test_a_captured_piece_moves_the_lengths(piece):
     model = L.Decoder(VOCAB, HIDDEN, HEADS, LAYERS, dtype=torch.float16, seed=10)
     tokens = prompts(2, 11 + 4 * piece, seed=11)
     eager, cache = L.Cache(model, 2, 64, page=16), L.Cache(model, 2, 64, page=16)
+    eager.FEW = cache.FEW = 8
     model.extend(eager, tokens[:, :11]), model.extend(cache, tokens[:, :11])
     new = tokens[:, 11:11 + piece].clone()
     s = torch.cuda.Stream()
