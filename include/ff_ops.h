@@ -233,7 +233,8 @@ int ff_op_attention_paged_fwd(const ff_attention_paged_fwd_t* a, void* stream);
  *   of these the shortest beginning whose weights sum to top_p of theirs, at least one word (1 or more: all),
  *   of these the words with w >= min_p, at least the first.
  * The word is the first whose running sum of weights is more than u times the sum of all that are kept (the last of them, if none); logprob is the logarithm of its
- * share of that sum.  At temperature 0 it is the first word, with logprob 0.
+ * share of that sum.  At temperature 0 it is the first word, with logprob 0.  Words that are not next to a border of top_k, top_p, min_p or u are summed to 2^-29 of their
+ * weight, so borders lie that near the exact ones.
  * Every parameter has a value for all rows, or a vector with one for each (which counts if it is not null).  -inf is the logit of a word that is never chosen beside others.  An infinite
  * logit is as good as any other largest one.  A row gives word -1 and logprob NaN where it holds a NaN or nothing but -inf, where its temperature is negative, NaN or
  * infinite, or another parameter or u is NaN; u is taken as 0 below that. */
