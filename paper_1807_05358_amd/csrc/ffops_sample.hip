@@ -27,6 +27,7 @@ struct SampleArgs {
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int BINS = 4096, BELOW = 2816;    // bins; those below the anchor
 constexpr int MOST = 2 * THREADS;           // words of the bins that decide
+constexpr uint32_t FIRST_MOST = 256;        // top_k up to which its words are gathered first
 constexpr uint32_t NONE = 0xffffffffu;      // no word
 
 // Logits as whole numbers in the same order, -0 as 0.
@@ -383,6 +384,18 @@ __device__ __forceinline__ V wave_scan(V x)
     return x;
 }
 
+// the largest of a wave, in its last lane
+__device__ __forceinline__ uint32_t wave_most(uint32_t x)
+{
+    x = max(x, moved<0x111, 0xf>(x));
+    x = max(x, moved<0x112, 0xf>(x));
+    x = max(x, moved<0x114, 0xf>(x));
+    x = max(x, moved<0x118, 0xf>(x));
+    x = max(x, moved<0x142, 0xa>(x));
+    x = max(x, moved<0x143, 0xc>(x));
+    return x;
+}
+
 // sums of x over the threads before this one, and over all of them
 template <class V>
 __device__ __forceinline__ V block_before(V x, V* at, V& all)
@@ -443,177 +456,273 @@ struct Choice {
     }
 };
 
-// The word from bins.  most: an anchor, and after that the largest logit.
+// The words that top_k leaves, and some behind them, in the list, from the first one on: those from a logit on that top_k threads or more have.  Nothing is weighed that is not kept.  UNDECIDED: they are
+// more than the list takes, or too large.
+template <class T>
+__device__ __forceinline__ int gather_top(const Row<T>& src, const Choice& c, Shared& sh, float& most, uint32_t& n)
+{
+    const uint32_t tid = threadIdx.x;
+    for (int b = tid; b < BINS; b += THREADS) sh.count[b] = 0;
+    if (tid == 0) sh.again = 0, sh.found = NONE, sh.n = 0;
+    float mine = -INFINITY;
+    bool nan = false;
+    src.each([&](float x, uint32_t) { mine = fmaxf(mine, x), nan |= x != x; });
+    // the largest and the least of what threads have
+    const bool any = mine > -INFINITY;
+    const uint32_t key = Key<F32>::of(mine), top_of = wave_most(key), least_of = wave_most(any ? ~key : 0);
+    if (tid % 64 == 63) sh.c[tid / 64] = top_of, sh.a[tid / 64] = least_of;
+    __syncthreads();
+    if (__any(nan) && tid % 64 == 0) sh.again = 1;
+    uint32_t top = 0, least = 0;
+    for (int w = 0; w < WAVES; ++w) top = max(top, sh.c[w]), least = max(least, (uint32_t)sh.a[w]);
+    most = Key<F32>::value(top);
+    const float lo = Key<F32>::value(~least), scale = (BINS - 1) / (most - lo);         // of a single value infinite, and places are not numbers: 0
+    const int place = any ? min(max((int)((mine - lo) * scale), 0), BINS - 1) : -1;
+    if (place >= 0) add_lds(&sh.count[place], 1u);
+    __syncthreads();
+    if (sh.again || most == -INFINITY) return WITHOUT;
+    if (most == INFINITY) return UNDECIDED;
+    constexpr int EACH = BINS / THREADS;
+    uint32_t each[EACH], sum = 0, all;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) each[k] = sh.count[BINS - 1 - (tid * EACH + k)], sum += each[k];
+    uint32_t before = block_before(sum, sh.c, all);
+    if (before < c.top_k && c.top_k <= before + sum) {
+        int k = 0;
+        while (before + each[k] < c.top_k) before += each[k++];
+        sh.lo = BINS - 1 - (tid * EACH + k);
+    }
+    __syncthreads();
+    if (tid == 0) sh.above[0] = 0, sh.count[0] = 0;         // the list is one bin, with nothing above it
+    // from here on are top_k words or more, or all that weigh anything
+    if (all >= c.top_k && place == (int)sh.lo) atomicMin(&sh.found, key);
+    __syncthreads();
+    const float from = all >= c.top_k ? Key<F32>::value(sh.found) : Key<F32>::value(1 + Key<F32>::of(-INFINITY));
+    src.each_near(from, [&](float x) { return x >= from; }, [&](float x, uint32_t i) {
+        const uint32_t at = atomicAdd(&sh.n, 1u);
+        if (at < MOST) sh.list[at] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+    });
+    __syncthreads();
+    n = sh.n;
+    return n <= MOST ? DECIDED : UNDECIDED;
+}
+
+// The list in order, the largest first; all threads, which have agreed on it.  Up to 256 words: a word's place is the number of larger ones, counted by 4, 8 or 16 threads together (128 words 1 us); more: by
+// exchanges of pairs (128 words took 4 us so, 512 take 7).
+__device__ __forceinline__ void sort_list(Shared& sh, uint32_t n)
+{
+    const uint32_t tid = threadIdx.x;
+    if (n <= 256) {
+        const uint32_t log = n <= 64 ? 4 : n <= 128 ? 3 : 2, i = tid >> log, each = 1u << log;
+        const uint64_t x = i < n ? sh.list[i] : 0;
+        uint32_t place = 0;
+        if (i < n)
+            for (uint32_t j = tid & (each - 1); j < n; j += each) place += sh.list[j] > x;
+        place += __builtin_amdgcn_update_dpp(0, place, 0xb1, 0xf, 0xf, false);
+        place += __builtin_amdgcn_update_dpp(0, place, 0x4e, 0xf, 0xf, false);
+        if (log >= 3) place += __builtin_amdgcn_update_dpp(0, place, 0x141, 0xf, 0xf, false);
+        if (log >= 4) place += __builtin_amdgcn_update_dpp(0, place, 0x140, 0xf, 0xf, false);
+        __syncthreads();
+        if (i < n && !(tid & (each - 1))) sh.list[place] = x;
+        __syncthreads();
+        return;
+    }
+    uint32_t size = 512;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
+    __syncthreads();
+    for (uint32_t k = 2; k <= size; k *= 2)
+        for (int log = 30 - __builtin_clz(k); log >= 0; --log) {
+            if (tid < size / 2) {
+                const uint32_t j = 1u << log, i = (tid >> log << (log + 1)) | (tid & (j - 1));
+                const uint64_t x = sh.list[i], y = sh.list[i + j];
+                if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
+            }
+            __syncthreads();
+        }
+}
+
+// The word from bins, or of the first top_k.  most: the largest logit.
 template <class T>
 __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c, Shared& sh, float& most, uint32_t& word, float& logprob)
 {
     const uint32_t tid = threadIdx.x;
-    Bins bins;
-    int per_nat = c.bins_per_nat();
+    const int lane = tid % 64, wave = tid / 64;
     word = NONE;
-    for (;;) {
-        if (!(most > -INFINITY && most < INFINITY)) {       // no anchor: the largest of all, which may be infinite, or a row without one
+    uint32_t n = 0;
+    const int top = c.top_k && c.top_k <= FIRST_MOST ? gather_top(src, c, sh, most, n) : UNDECIDED;
+    if (top == WITHOUT) return WITHOUT;
+    const bool whole = top == DECIDED;          // the list has everything from the first word on
+    Bins bins;
+    double all = 0, m_lo = 0;
+    bool need_k = n >= c.top_k;
+    Range p_bins = {c.top_p < 1 ? 0 : BINS, BINS - 1}, m_bins = {c.min_p > 0 ? 0 : BINS, BINS - 1}, u_bins = {0, BINS - 1};
+    const double share = c.u < 0 ? 0.0 : c.u < 1 ? (double)c.u : 1.0;
+    if (!whole) {
+        int per_nat = c.bins_per_nat();
+        __syncthreads();
+        most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(src.largest_of_first()), sh.a));
+        for (;;) {
+            if (!(most > -INFINITY && most < INFINITY)) {       // no anchor: the largest of all, which may be infinite, or a row without one
+                most = -INFINITY;
+                uint32_t nan = 0;
+                src.each([&](float x, uint32_t) { most = fmaxf(most, x), nan |= x != x; });
+                most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
+                nan = block_sum(nan, sh.c);
+                if (nan || most == -INFINITY) {
+                    return WITHOUT;
+                }
+                if (most == INFINITY) return UNDECIDED;
+            }
+            bins.set(most, c.temperature, per_nat);
+            for (int b = tid; b < BINS + 2; b += THREADS) sh.steps[b] = 0;
+            if (c.top_k)
+                for (int b = tid; b < BINS + 2; b += THREADS) sh.count[b] = 0;
+            if (tid == 0) sh.again = 0;
+            __syncthreads();
             most = -INFINITY;
-            uint32_t nan = 0;
-            src.each([&](float x, uint32_t) { most = fmaxf(most, x), nan |= x != x; });
+            bool nan = false;
+            const double light = BELOW - 42.0 * per_nat;        // places from there on weigh something
+            // (words beyond the lowest bin, many of them -inf at times, are kept off the one place in LDS that they would all add to)
+            const auto add = [&](float x) {
+                most = fmaxf(most, x);
+                nan |= x != x;
+                const double at = bins.place(x);
+                const int b = bins.bin(at);
+                if (b >= 0) add_lds(&sh.steps[b + 1], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
+                else if (at > light) sh.steps[0] = 1;
+                return b;
+            };
+            if (c.top_k) src.each([&](float x, uint32_t) {
+                const int b = add(x);
+                if (b >= 0) add_lds(&sh.count[b + 1], 1u);
+            });
+            else src.each([&](float x, uint32_t) { add(x); });
+            if (__any(nan) && tid % 64 == 0) sh.again = 1;
             most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
-            nan = block_sum(nan, sh.c);
-            if (nan || most == -INFINITY) {
+            const bool above = sh.steps[BINS + 1] != 0, below = sh.steps[0] != 0 && per_nat > 64, again = sh.again != 0;
+            __syncthreads();
+            if (again) {
                 return WITHOUT;
             }
-            if (most == INFINITY) return UNDECIDED;
+            if (!above && !below) break;
+            if (!above) per_nat = 64;           // with that what is beyond the lowest bin weighs less than e^-44, and with the largest logit as the anchor nothing is above the highest
         }
-        bins.set(most, c.temperature, per_nat);
-        for (int b = tid; b < BINS + 2; b += THREADS) sh.steps[b] = 0;
-        if (c.top_k)
-            for (int b = tid; b < BINS + 2; b += THREADS) sh.count[b] = 0;
-        if (tid == 0) sh.again = 0;
-        __syncthreads();
-        most = -INFINITY;
-        bool nan = false;
-        const double light = BELOW - 42.0 * per_nat;        // places from there on weigh something
-        // (words beyond the lowest bin, many of them -inf at times, are kept off the one place in LDS that they would all add to)
-        const auto add = [&](float x) {
-            most = fmaxf(most, x);
-            nan |= x != x;
-            const double at = bins.place(x);
-            const int b = bins.bin(at);
-            if (b >= 0) add_lds(&sh.steps[b + 1], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
-            else if (at > light) sh.steps[0] = 1;
-            return b;
-        };
-        if (c.top_k) src.each([&](float x, uint32_t) {
-            const int b = add(x);
-            if (b >= 0) add_lds(&sh.count[b + 1], 1u);
-        });
-        else src.each([&](float x, uint32_t) { add(x); });
-        if (__any(nan) && tid % 64 == 0) sh.again = 1;
-        most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(most), sh.a));
-        const bool above = sh.steps[BINS + 1] != 0, below = sh.steps[0] != 0 && per_nat > 64, again = sh.again != 0;
-        __syncthreads();
-        if (again) {
-            return WITHOUT;
-        }
-        if (!above && !below) break;
-        if (!above) per_nat = 64;           // with that what is beyond the lowest bin weighs less than e^-44, and with the largest logit as the anchor nothing is above the highest
-    }
-    // weights of all bins above each, beside the largest word's, which is 1: a wave has 256 bins, four times 64 side by side, the first wave the highest
-    constexpr int EACH = BINS / THREADS;
-    const int lane = tid % 64, wave = tid / 64, highest = BINS - 1 - wave * (64 * EACH) - lane;
-    double all = 0;
-    uint32_t words_all = 0;
-    {
-        uint64_t steps[EACH];
-        uint32_t n[EACH] = {}, t[EACH] = {}, words_before = 0, row_words = 0;
-        double s[EACH] = {}, before = 0, rows = 0;
+        // weights of all bins above each, beside the largest word's, which is 1: a wave has 256 bins, four times 64 side by side, the first wave the highest
+        constexpr int EACH = BINS / THREADS;
+        const int highest = BINS - 1 - wave * (64 * EACH) - lane;
+        uint32_t words_all = 0;
+        {
+            uint64_t steps[EACH];
+            uint32_t n[EACH] = {}, t[EACH] = {}, words_before = 0, row_words = 0;
+            double s[EACH] = {}, before = 0, rows = 0;
 #pragma unroll
-        for (int k = 0; k < EACH; ++k) steps[k] = sh.steps[highest - 64 * k + 1];
-        if (__any((steps[0] | steps[1] | steps[2] | steps[3]) != 0)) {          // most waves have empty bins
-            static_assert(EACH == 4, "as many rows");
-            // e^-h, h at most 1/32, and that for 64 bins
-            const double h = 1.0 / per_nat;
-            double less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
+            for (int k = 0; k < EACH; ++k) steps[k] = sh.steps[highest - 64 * k + 1];
+            if (__any((steps[0] | steps[1] | steps[2] | steps[3]) != 0)) {          // most waves have empty bins
+                static_assert(EACH == 4, "as many rows");
+                // e^-h, h at most 1/32, and that for 64 bins
+                const double h = 1.0 / per_nat;
+                double less = 1 - h * (1 - h / 2 * (1 - h / 3 * (1 - h / 4 * (1 - h / 5 * (1 - h / 6 * (1 - h / 7))))));
 #pragma unroll
-            for (int k = 0; k < 6; ++k) less *= less;
-            double edge = 0x1p-29 * exp(((double)(highest - BELOW) + (bins.anchor - (double)most) * bins.per_logit) * h);
-            // sums of a row of 64, up to and with the lane, then of the rows before it, then of the waves before
+                for (int k = 0; k < 6; ++k) less *= less;
+                double edge = 0x1p-29 * exp(((double)(highest - BELOW) + (bins.anchor - (double)most) * bins.per_logit) * h);
+                // sums of a row of 64, up to and with the lane, then of the rows before it, then of the waves before
 #pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                s[k] = wave_scan((double)steps[k] * edge);
-                if (c.top_k) n[k] = sh.count[highest - 64 * k + 1], t[k] = wave_scan(n[k]);
-                edge *= less;
-            }
+                for (int k = 0; k < EACH; ++k) {
+                    s[k] = wave_scan((double)steps[k] * edge);
+                    if (c.top_k) n[k] = sh.count[highest - 64 * k + 1], t[k] = wave_scan(n[k]);
+                    edge *= less;
+                }
 #pragma unroll
-            for (int k = 0; k < EACH; ++k) {
-                const double of_row = __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, s[k]), 63));
-                s[k] = moved<0x138, 0xf>(s[k]) + rows, rows += of_row;
-                if (c.top_k) {
-                    const uint32_t words = (uint32_t)__builtin_amdgcn_readlane((int)t[k], 63);
-                    t[k] = moved<0x138, 0xf>(t[k]) + row_words, row_words += words;
+                for (int k = 0; k < EACH; ++k) {
+                    const double of_row = __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, s[k]), 63));
+                    s[k] = moved<0x138, 0xf>(s[k]) + rows, rows += of_row;
+                    if (c.top_k) {
+                        const uint32_t words = (uint32_t)__builtin_amdgcn_readlane((int)t[k], 63);
+                        t[k] = moved<0x138, 0xf>(t[k]) + row_words, row_words += words;
+                    }
                 }
             }
-        }
-        if (lane == 0) sh.d[wave] = rows, sh.c[wave] = row_words;
-        __syncthreads();
-        for (int x = 0; x < WAVES; ++x) {
-            if (x == wave) before = all, words_before = words_all;
-            all += sh.d[x], words_all += sh.c[x];
-        }
-#pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-            const int b = highest - 64 * k;
-            sh.above[b] = s[k] + before;
-            const uint32_t words = t[k] + words_before;
-            if (c.top_k) sh.count[b] = words;
-            if (words < c.top_k && c.top_k <= words + n[k]) sh.found = b;
-        }
-        __syncthreads();
-    }
-    const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
-    // what each border leaves, from..to, and the bins it can lie in
-    const bool by_k = c.top_k && words_all >= c.top_k;      // otherwise words without weight make up the rest
-    double k_lo = all, k_hi = all;
-    const int k_bin = by_k ? (int)sh.found : -1;
-    if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
-    Range p_bins = {1, 0}, m_bins = {1, 0};
-    double p_lo = k_lo, p_hi = k_hi;
-    if (c.top_p < 1) {
-        const double p = c.top_p > 0 ? (double)c.top_p : 0.0;
-        p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
-        p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
-    }
-    double m_lo = all, m_hi = all;
-    if (c.min_p > 0) {
-        const double at = fmax(log((double)c.min_p) * per_nat + bins.place(most), 0.0);
-        m_bins = {min((int)fmax(at - 1e-6, 0.0), BINS - 1), min((int)(at + 1e-6), BINS - 1)};
-        m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
-    }
-    const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
-    // borders that others come before do not count
-    if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
-    const bool no_p = p_lo > hi * (1 + SLACK);
-    if (no_p) p_bins = {1, 0};
-    const bool need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
-    const double share = c.u < 0 ? 0.0 : c.u < 1 ? (double)c.u : 1.0;
-    const Range u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
-    const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
-    // their words
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    {
-        // between these logits are all words of the bins: a piece seldom has one
-        int b_lo = BINS, b_hi = -2;
-        if (p_bins.lo <= p_bins.hi) b_lo = p_bins.lo, b_hi = p_bins.hi;
-        if (m_bins.lo <= m_bins.hi) b_lo = min(b_lo, m_bins.lo), b_hi = max(b_hi, m_bins.hi);
-        const int k_at = need_k ? k_bin : u_bins.lo;
-        const float b_from = b_hi < 0 ? INFINITY : bins.logit(b_lo, -1), to = b_hi < 0 ? -INFINITY : bins.logit(b_hi + 1, 1), u_from = bins.logit(u_bins.lo, -1), u_to = bins.logit(u_bins.hi + 1, 1), k_from = bins.logit(k_at, -1), k_to = bins.logit(k_at + 1, 1);
-        const float lowest = fminf(fminf(b_from, u_from), k_from);
-        const auto near = [&](float x) { return ((x >= b_from) & (x <= to)) | ((x >= u_from) & (x <= u_to)) | ((x >= k_from) & (x <= k_to)); };
-        src.each_near(lowest, near, [&](float x, uint32_t i) {
-            const int b = bins.bin(bins.place(x));
-            if (b >= 0 && b < BINS && decides(b)) {
-                const uint32_t n = atomicAdd(&sh.n, 1u);
-                if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+            if (lane == 0) sh.d[wave] = rows, sh.c[wave] = row_words;
+            __syncthreads();
+            for (int x = 0; x < WAVES; ++x) {
+                if (x == wave) before = all, words_before = words_all;
+                all += sh.d[x], words_all += sh.c[x];
             }
-        });
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int b = highest - 64 * k;
+                sh.above[b] = s[k] + before;
+                const uint32_t words = t[k] + words_before;
+                if (c.top_k) sh.count[b] = words;
+                if (words < c.top_k && c.top_k <= words + n[k]) sh.found = b;
+            }
+            __syncthreads();
+        }
+        const auto below = [&](int b) { return b ? sh.above[b - 1] : all; };        // the weight down to the end of bin b
+        // what each border leaves, from..to, and the bins it can lie in
+        const bool by_k = c.top_k && words_all >= c.top_k;      // otherwise words without weight make up the rest
+        double k_lo = all, k_hi = all;
+        const int k_bin = by_k ? (int)sh.found : -1;
+        if (by_k) k_lo = sh.above[k_bin], k_hi = below(k_bin);
+        p_bins = {1, 0}, m_bins = {1, 0};
+        double p_lo = k_lo, p_hi = k_hi;
+        if (c.top_p < 1) {
+            const double p = c.top_p > 0 ? (double)c.top_p : 0.0;
+            p_bins = bins_of(p * k_lo * (1 - SLACK), p * k_hi * (1 + SLACK), all, sh);
+            p_lo = sh.above[p_bins.hi], p_hi = below(p_bins.lo);
+        }
+        m_lo = all;
+        double m_hi = all;
+        if (c.min_p > 0) {
+            const double at = fmax(log((double)c.min_p) * per_nat + bins.place(most), 0.0);
+            m_bins = {min((int)fmax(at - 1e-6, 0.0), BINS - 1), min((int)(at + 1e-6), BINS - 1)};
+            m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
+        }
+        const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);
+        // borders that others come before do not count
+        if (m_lo > hi * (1 + SLACK)) m_bins = {1, 0};
+        const bool no_p = p_lo > hi * (1 + SLACK);
+        if (no_p) p_bins = {1, 0};
+        need_k = by_k && !(no_p && k_lo > hi * (1 + SLACK));
+        u_bins = bins_of(share * lo * (1 - SLACK), fmin(share, 1 - 1e-14) * hi * (1 + SLACK), all, sh);
+        const auto decides = [&](int b) { return (need_k && b == k_bin) || (b >= p_bins.lo && b <= p_bins.hi) || (b >= m_bins.lo && b <= m_bins.hi) || (b >= u_bins.lo && b <= u_bins.hi); };
+        // their words
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        {
+            // between these logits are all words of the bins: a piece seldom has one
+            int b_lo = BINS, b_hi = -2;
+            if (p_bins.lo <= p_bins.hi) b_lo = p_bins.lo, b_hi = p_bins.hi;
+            if (m_bins.lo <= m_bins.hi) b_lo = min(b_lo, m_bins.lo), b_hi = max(b_hi, m_bins.hi);
+            const int k_at = need_k ? k_bin : u_bins.lo;
+            const float b_from = b_hi < 0 ? INFINITY : bins.logit(b_lo, -1), to = b_hi < 0 ? -INFINITY : bins.logit(b_hi + 1, 1), u_from = bins.logit(u_bins.lo, -1), u_to = bins.logit(u_bins.hi + 1, 1), k_from = bins.logit(k_at, -1), k_to = bins.logit(k_at + 1, 1);
+            const float lowest = fminf(fminf(b_from, u_from), k_from);
+            const auto near = [&](float x) { return ((x >= b_from) & (x <= to)) | ((x >= u_from) & (x <= u_to)) | ((x >= k_from) & (x <= k_to)); };
+            src.each_near(lowest, near, [&](float x, uint32_t i) {
+                const int b = bins.bin(bins.place(x));
+                if (b >= 0 && b < BINS && decides(b)) {
+                    const uint32_t n = atomicAdd(&sh.n, 1u);
+                    if (n < MOST) sh.list[n] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+                }
+            });
+        }
+        __syncthreads();
+        n = sh.n;
     }
-    __syncthreads();
-    const uint32_t n = sh.n;
     const Weigh weigh = {most, (double)c.temperature, 1.0};
+    const auto bin_of = [&](float x) { return whole ? 0 : bins.bin(bins.place(x)); };
+    if (n <= MOST) sort_list(sh, n);
     if (n <= 64) {
         // one wave, a word a lane
         if (tid < 64) {
             const bool in = lane < (int)n;
-            uint64_t x = in ? sh.list[lane] : 0;
-            uint32_t place = 0;
-            for (uint32_t j = 0; j < n; ++j) place += read_lane(x, j) > x;
-            if (in) sh.list[place] = x;
-            asm volatile("" ::: "memory");      // a wave's accesses to LDS are done in their order
-            x = in ? sh.list[lane] : 0;
+            const uint64_t x = in ? sh.list[lane] : 0;
             const float f = Key<F32>::value((uint32_t)(x >> 32));
             const double w = in ? weigh.of(f) : 0;
-            const int bin = in ? bins.bin(bins.place(f)) : -1;
+            const int bin = in ? bin_of(f) : -1;
             const double sum = wave_scan(w);
+            if (whole) all = __builtin_bit_cast(double, read_lane(__builtin_bit_cast(uint64_t, sum), 63));
             // the first word of the lane's bin in the list
             const int prev = __shfl_up(bin, 1);
             const uint64_t heads = __ballot(in && (lane == 0 || prev != bin)) & ~0ull >> (63 - lane);
@@ -649,22 +758,6 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
         __syncthreads();
         word = sh.word, logprob = (float)sh.weight;
     } else if (n <= MOST) {
-        // sorted, the largest first
-        uint32_t size = 128;
-        while (size < n) size *= 2;
-        for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
-        __syncthreads();
-        for (uint32_t k = 2; k <= size; k *= 2)
-            for (uint32_t j = k / 2; j; j /= 2) {
-                if (tid < size / 2) {
-                    const uint32_t i = (tid / j * 2 * j) + tid % j;
-                    const uint64_t x = sh.list[i], y = sh.list[i + j];
-                    if ((x < y) == ((i & k) == 0)) sh.list[i] = y, sh.list[i + j] = x;
-                }
-                if (size > 128) __syncthreads();
-                else asm volatile("" ::: "memory");         // one wave, whose accesses to LDS are done in their order
-            }
-        __syncthreads();
         // a thread has two neighbours: their weights, the weight before them, their rank
         double w[2], before[2];
         int bin[2];
@@ -675,11 +768,12 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
             const uint32_t i = 2 * tid + e;
             in[e] = i < n;
             const float x = in[e] ? Key<F32>::value((uint32_t)(sh.list[i] >> 32)) : 0;
-            bin[e] = in[e] ? bins.bin(bins.place(x)) : -1;
+            bin[e] = in[e] ? bin_of(x) : -1;
             w[e] = in[e] ? weigh.of(x) : 0;
         }
         double sum_all;
         const double sum = block_before(w[0] + w[1], sh.d, sum_all);
+        if (whole) all = sum_all;
         // where each bin's words begin in the list, and the sum there: steps of other bins are not needed any more, but their sums above are
         __syncthreads();
 #pragma unroll
@@ -688,7 +782,7 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
             before[e] = sum + (e ? w[0] : 0.0);
             if (!in[e]) continue;
             const float prev = i ? Key<F32>::value((uint32_t)(sh.list[i - 1] >> 32)) : 0;
-            if (i == 0 || bins.bin(bins.place(prev)) != bin[e]) {     // one thread for each bin
+            if (i == 0 || bin_of(prev) != bin[e]) {     // one thread for each bin
                 sh.above[bin[e]] -= before[e];
                 sh.count[bin[e]] -= i;
             }
@@ -748,7 +842,7 @@ __device__ __forceinline__ void choose_from_row(const SampleArgs& a, uint32_t ro
 {
     const typename T::elem* z = (const typename T::elem*)(a.logits + row * a.stride);
     const Row<T> src(z, a.vocab);
-    float most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(src.largest_of_first()), sh.a)), logprob = NAN;
+    float most = -INFINITY, logprob = NAN;
     uint32_t word;
     const int state = choose_by_bins(src, c, sh, most, word, logprob);
     if (state == UNDECIDED) {
