@@ -16,18 +16,22 @@ struct SampleArgs {
     float* logprob;
 };
 
-// A block takes a row.  It reads it twice: once to sum weights in bins of logits, once for the few words of the bins that decide; these are sorted and gone through with exact sums.  What
-// bounds it is the first reading: 24 instructions an element, a third of them in 64 bits, and an addition in LDS. 256 rows of 131071 float32 take 61 us (134 MB, 2.2 TB/s; the first reading 34 of
-// them, the second, out of the last-level cache, 15), one row of 32768 16 us, 64 rows 22: fewer rows than compute units leave the rest idle, and two kernels that share a row between blocks take 21 us at least.
+// A block takes a row.  It reads it twice: once for what decides which words matter, once for these few words, which are put in order and gone through with exact sums.
+//   With top_k up to FIRST_MOST, or min_p from FIRST_LEAST on and no top_p, the first reading looks for maxima alone: at least top_k words are as large as the largest of that many threads' shares, and everything from there on is listed,
+// a few words more than are kept.  64 rows of 32768 bfloat16, top_k 50: 11 us for 24 by weighing all words; 8 of 200003 float32 24 for 56, 256 of 131071 41 for 54; with top_k 256 21 for 28, 38 for 61 and 50 for 55, one row of 4096
+// 17 for 16.  min_p 0.1, 256 rows of 131071 normal logits, deviation 4: 39 us for 49; 2.5: 44 for 49; 1, where the list does not take all of them and the row is read as follows: 95 for 73.
+//   Otherwise the first reading sums weights in bins of logits: 24 instructions an element, a third of them in 64 bits, and an addition in LDS.  256 rows of 131071 float32, top_p and min_p, take 61 us (134 MB, 2.2 TB/s; the first reading
+// 34 of them, the second, out of the last-level cache, 15), one row of 32768 17 us: fewer rows than compute units leave the rest idle, and two kernels that share a row between blocks take 21 us at least.
 //   Bins are 1 / per_nat wide in units of the temperature, from an anchor on, the largest logit of what the block's threads read first.  A word weighs 2^29 e^r steps, r its place
 // in its bin: whole numbers, whose sums do not depend on an order, to 2^-30 of the weight whatever its size, one way or the other.  Sums of bins are in 64-bit floats.  Where the anchor was too low, or words may lie beyond the lowest bin
-// that weigh more than e^-44, the row is read again with other bins; words that weigh less than that beside the largest do not count.
+// that weigh more than e^-42, the row is read again with other bins; words that weigh less than that beside the largest do not count.
 //   The bins that decide are those in which the border of top_k, that of top_p, that of min_p and the chosen word can lie; they depend on one another, so each is a range
 // until the words are there.  Bins with more than MOST words (equal logits, or nearly so) are left to select(), which reads the row for every eight bits of the key of each border.
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int BINS = 4096, BELOW = 2816;    // bins; those below the anchor
 constexpr int MOST = 2 * THREADS;           // words of the bins that decide
 constexpr uint32_t FIRST_MOST = 256;        // top_k up to which its words are gathered first
+constexpr float FIRST_LEAST = 0x1p-6f;      // min_p from which, without top_p, its words are: they are few in most rows (see below)
 constexpr uint32_t NONE = 0xffffffffu;      // no word
 
 // Logits as whole numbers in the same order, -0 as 0.
@@ -336,16 +340,17 @@ struct Bins {
         const float h = 1.0f / per_nat;
         c[0] = 0x1p29f * h, c[1] = 0x1p28f * h * h, c[2] = 0x1p29f / 6 * h * h * h, c[3] = 0x1p29f / 24 * h * h * h * h;
     }
-    // the place of a logit in bins
-    __device__ __forceinline__ double place(float z) const { return fma((double)z - anchor, per_logit, (double)BELOW); }
-    // a logit on the safe side (-1: below, 1: above) of a bin's lower edge; of the lowest bin, of what counts as of it
+    // the place of a logit in bins, the lowest of which begins at 1: what is below is then cut off to 0
+    __device__ __forceinline__ double place(float z) const { return fma((double)z - anchor, per_logit, (double)(BELOW + 1)); }
+    // a logit on the safe side (-1: below, 1: above) of a bin's lower edge
     __device__ __forceinline__ float logit(int bin, int side) const
     {
-        const double edge = fma((double)(bin - (bin == 0) - BELOW), width, anchor);
+        const double edge = fma((double)(bin - BELOW), width, anchor);
         return (float)(edge + side * (fabs(edge) * 1e-6 + 1e-30));
     }
-    // its number, -1 and BINS beyond them; what is less than a bin below the lowest counts as of that, where it weighs nothing
-    __device__ __forceinline__ int bin(double at) const { return min(max((int)at, -1), BINS); }
+    // a bin's number, -1 and BINS beyond them, and that + 1
+    __device__ __forceinline__ int slot(double at) const { return min(max((int)at, 0), BINS + 1); }
+    __device__ __forceinline__ int bin(double at) const { return slot(at) - 1; }
     // e^(r / per_nat), 0 <= r < 1, in steps of 2^-29, to the nearest: what is beyond 1 is below 2^-4.9, so a float has it to half of such a step
     __device__ __forceinline__ uint32_t steps(float r) const { return (1u << 29) + (uint32_t)fmaf(r, fmaf(r, fmaf(r, fmaf(r, c[3], c[2]), c[1]), c[0]), 0.5f); }
 };
@@ -394,6 +399,21 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t x)
     x = max(x, moved<0x142, 0xa>(x));
     x = max(x, moved<0x143, 0xc>(x));
     return x;
+}
+
+// the largest of what threads have and the least of it, of finite ones and infinity
+struct Ends {
+    float top, least;
+};
+__device__ __forceinline__ Ends block_ends(float mine, Shared& sh)
+{
+    const uint32_t key = Key<F32>::of(mine), top_of = wave_most(key), least_of = wave_most(mine > -INFINITY ? ~key : 0);
+    __syncthreads();
+    if (threadIdx.x % 64 == 63) sh.c[threadIdx.x / 64] = top_of, sh.a[threadIdx.x / 64] = least_of;
+    __syncthreads();
+    uint32_t top = 0, least = 0;
+    for (int w = 0; w < WAVES; ++w) top = max(top, sh.c[w]), least = max(least, (uint32_t)sh.a[w]);
+    return {Key<F32>::value(top), Key<F32>::value(~least)};
 }
 
 // sums of x over the threads before this one, and over all of them
@@ -448,18 +468,12 @@ struct Choice {
         top_k = k > 0 && (uint32_t)k < a.vocab ? (uint32_t)k : 0;
     }
     __device__ __forceinline__ bool fine() const { return temperature >= 0 && temperature < INFINITY && top_p == top_p && min_p == min_p && u == u; }
-    __device__ __forceinline__ int bins_per_nat() const
-    {
-        int n = 32;
-        while (n < 1024 && n * 2 <= 64 * temperature) n *= 2;
-        return n;
-    }
 };
 
 // The words that top_k leaves, and some behind them, in the list, from the first one on: those from a logit on that top_k threads or more have.  Nothing is weighed that is not kept.  UNDECIDED: they are
 // more than the list takes, or too large.
 template <class T>
-__device__ __forceinline__ int gather_top(const Row<T>& src, const Choice& c, Shared& sh, float& most, uint32_t& n)
+__device__ __forceinline__ int gather_top(const Row<T>& src, const Choice& c, Shared& sh, Ends& ends, uint32_t& n)
 {
     const uint32_t tid = threadIdx.x;
     for (int b = tid; b < BINS; b += THREADS) sh.count[b] = 0;
@@ -467,40 +481,45 @@ __device__ __forceinline__ int gather_top(const Row<T>& src, const Choice& c, Sh
     float mine = -INFINITY;
     bool nan = false;
     src.each([&](float x, uint32_t) { mine = fmaxf(mine, x), nan |= x != x; });
-    // the largest and the least of what threads have
     const bool any = mine > -INFINITY;
-    const uint32_t key = Key<F32>::of(mine), top_of = wave_most(key), least_of = wave_most(any ? ~key : 0);
-    if (tid % 64 == 63) sh.c[tid / 64] = top_of, sh.a[tid / 64] = least_of;
-    __syncthreads();
+    const uint32_t key = Key<F32>::of(mine);
+    ends = block_ends(mine, sh);
     if (__any(nan) && tid % 64 == 0) sh.again = 1;
-    uint32_t top = 0, least = 0;
-    for (int w = 0; w < WAVES; ++w) top = max(top, sh.c[w]), least = max(least, (uint32_t)sh.a[w]);
-    most = Key<F32>::value(top);
-    const float lo = Key<F32>::value(~least), scale = (BINS - 1) / (most - lo);         // of a single value infinite, and places are not numbers: 0
+    const float most = ends.top, lo = ends.least, scale = (BINS - 1) / (most - lo);     // of a single value infinite, and places are not numbers: 0
+    const bool by_k = c.top_k && c.top_k <= FIRST_MOST;
     const int place = any ? min(max((int)((mine - lo) * scale), 0), BINS - 1) : -1;
-    if (place >= 0) add_lds(&sh.count[place], 1u);
+    if (by_k && place >= 0) add_lds(&sh.count[place], 1u);
     __syncthreads();
     if (sh.again || most == -INFINITY) return WITHOUT;
     if (most == INFINITY) return UNDECIDED;
-    constexpr int EACH = BINS / THREADS;
-    uint32_t each[EACH], sum = 0, all;
+    float from = Key<F32>::value(1 + Key<F32>::of(-INFINITY));
+    if (by_k) {
+        constexpr int EACH = BINS / THREADS;
+        uint32_t each[EACH], sum = 0, all;
 #pragma unroll
-    for (int k = 0; k < EACH; ++k) each[k] = sh.count[BINS - 1 - (tid * EACH + k)], sum += each[k];
-    uint32_t before = block_before(sum, sh.c, all);
-    if (before < c.top_k && c.top_k <= before + sum) {
-        int k = 0;
-        while (before + each[k] < c.top_k) before += each[k++];
-        sh.lo = BINS - 1 - (tid * EACH + k);
+        for (int k = 0; k < EACH; ++k) each[k] = sh.count[BINS - 1 - (tid * EACH + k)], sum += each[k];
+        uint32_t before = block_before(sum, sh.c, all);
+        if (before < c.top_k && c.top_k <= before + sum) {
+            int k = 0;
+            while (before + each[k] < c.top_k) before += each[k++];
+            sh.lo = BINS - 1 - (tid * EACH + k);
+        }
+        __syncthreads();
+        // from here on are top_k words or more, or all that weigh anything
+        if (all >= c.top_k && place == (int)sh.lo) atomicMin(&sh.found, key);
+        __syncthreads();
+        if (all >= c.top_k) from = Key<F32>::value(sh.found);
     }
-    __syncthreads();
+    if (c.top_p >= 1 && c.min_p > 0) {
+        const double edge = (double)most + (double)c.temperature * log((double)c.min_p);
+        from = fmaxf(from, (float)(edge - (fabs(edge) * 1e-6 + 1e-30)));
+    }
     if (tid == 0) sh.above[0] = 0, sh.count[0] = 0;         // the list is one bin, with nothing above it
-    // from here on are top_k words or more, or all that weigh anything
-    if (all >= c.top_k && place == (int)sh.lo) atomicMin(&sh.found, key);
-    __syncthreads();
-    const float from = all >= c.top_k ? Key<F32>::value(sh.found) : Key<F32>::value(1 + Key<F32>::of(-INFINITY));
-    src.each_near(from, [&](float x) { return x >= from; }, [&](float x, uint32_t i) {
+    bool full = false;
+    src.each_near(from, [&](float x) { return x >= from && !full; }, [&](float x, uint32_t i) {
         const uint32_t at = atomicAdd(&sh.n, 1u);
         if (at < MOST) sh.list[at] = (uint64_t)Key<F32>::of(x) << 32 | (0xffffffffu - i);
+        else full = true;
     });
     __syncthreads();
     n = sh.n;
@@ -542,6 +561,11 @@ __device__ __forceinline__ void sort_list(Shared& sh, uint32_t n)
         }
 }
 
+// Bins in a unit of the temperature, where the largest logits of the threads' shares lie so many units apart: in most rows the others are no more than three times that, and a little, below the largest, so bins are as narrow as
+// reaches that far and the words of a few of them are few.  Where it does not, the row is read again (below).  256 rows of 131071 normal logits, top_p 0.9, with 64 bins a unit and so: deviation 1 unit 1100 us and 80, 2.5 units
+// 71 and 66, 4 units 51 and 50.
+__device__ __forceinline__ int bins_per_nat(float apart) { return max(32, min(1 << 16, (int)(BELOW / (3 * apart + fminf(apart, 2.0f))))); }
+
 // The word from bins, or of the first top_k.  most: the largest logit.
 template <class T>
 __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c, Shared& sh, float& most, uint32_t& word, float& logprob)
@@ -550,18 +574,20 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
     const int lane = tid % 64, wave = tid / 64;
     word = NONE;
     uint32_t n = 0;
-    const int top = c.top_k && c.top_k <= FIRST_MOST ? gather_top(src, c, sh, most, n) : UNDECIDED;
+    Ends ends = {-INFINITY, -INFINITY};         // of all of the row, if top_k or min_p had it looked over
+    const int top = (c.top_k && c.top_k <= FIRST_MOST) || (c.top_p >= 1 && c.min_p >= FIRST_LEAST) ? gather_top(src, c, sh, ends, n) : UNDECIDED;
     if (top == WITHOUT) return WITHOUT;
+    most = ends.top;
     const bool whole = top == DECIDED;          // the list has everything from the first word on
     Bins bins;
     double all = 0, m_lo = 0;
-    bool need_k = n >= c.top_k;
+    bool need_k = c.top_k && n >= c.top_k;
     Range p_bins = {c.top_p < 1 ? 0 : BINS, BINS - 1}, m_bins = {c.min_p > 0 ? 0 : BINS, BINS - 1}, u_bins = {0, BINS - 1};
     const double share = c.u < 0 ? 0.0 : c.u < 1 ? (double)c.u : 1.0;
     if (!whole) {
-        int per_nat = c.bins_per_nat();
+        if (!(most > -INFINITY)) ends = block_ends(src.largest_of_first(), sh), most = ends.top;
+        int per_nat = bins_per_nat((ends.top - ends.least) / c.temperature);
         __syncthreads();
-        most = Key<F32>::value((uint32_t)block_max(Key<F32>::of(src.largest_of_first()), sh.a));
         for (;;) {
             if (!(most > -INFINITY && most < INFINITY)) {       // no anchor: the largest of all, which may be infinite, or a row without one
                 most = -INFINITY;
@@ -582,20 +608,20 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
             __syncthreads();
             most = -INFINITY;
             bool nan = false;
-            const double light = BELOW - 42.0 * per_nat;        // places from there on weigh something
+            const double light = BELOW + 1 - 42.0 * per_nat;        // places from there on weigh something
             // (words beyond the lowest bin, many of them -inf at times, are kept off the one place in LDS that they would all add to)
             const auto add = [&](float x) {
                 most = fmaxf(most, x);
                 nan |= x != x;
                 const double at = bins.place(x);
-                const int b = bins.bin(at);
-                if (b >= 0) add_lds(&sh.steps[b + 1], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
+                const int slot = bins.slot(at);
+                if (slot > 0) add_lds(&sh.steps[slot], (uint64_t)bins.steps((float)__builtin_amdgcn_fract(at)));
                 else if (at > light) sh.steps[0] = 1;
-                return b;
+                return slot;
             };
             if (c.top_k) src.each([&](float x, uint32_t) {
-                const int b = add(x);
-                if (b >= 0) add_lds(&sh.count[b + 1], 1u);
+                const int slot = add(x);
+                if (slot > 0) add_lds(&sh.count[slot], 1u);
             });
             else src.each([&](float x, uint32_t) { add(x); });
             if (__any(nan) && tid % 64 == 0) sh.again = 1;
@@ -675,8 +701,8 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
         m_lo = all;
         double m_hi = all;
         if (c.min_p > 0) {
-            const double at = fmax(log((double)c.min_p) * per_nat + bins.place(most), 0.0);
-            m_bins = {min((int)fmax(at - 1e-6, 0.0), BINS - 1), min((int)(at + 1e-6), BINS - 1)};
+            const double at = fmax(log((double)c.min_p) * per_nat + bins.place(most), 1.0);
+            m_bins = {min((int)fmax(at - 1e-6, 1.0), BINS) - 1, min((int)(at + 1e-6), BINS) - 1};
             m_lo = sh.above[m_bins.hi], m_hi = below(m_bins.lo);
         }
         const double lo = fmin(fmin(k_lo, p_lo), m_lo), hi = fmin(fmin(k_hi, p_hi), m_hi);

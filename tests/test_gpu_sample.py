@@ -230,3 +230,47 @@ def test_on_two_streams_at_once():
             got.append([O.sample(z, u, top_p=p) for _ in range(5)])
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for w, several in zip(want, got) for g in several for x, y in zip(g, w))
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("top_k", [1, 2, 63, 64, 65, 128, 129, 255, 256, 257])
+def test_the_first_words(t, top_k):
+    """rows in whose order the words of top_k lie badly: in turn, all in one thread's share, more alike than are put in order, fewer than top_k, an infinite one"""
+    V = 70001
+    z, u = rows(10, V, TYPES[t], seed=top_k)
+    z[1], z[2] = z[1].sort()[0], z[2].sort(descending=True)[0]
+    for base in range(40, V - 8, 8192):                     # of one thread, whatever it takes at once
+        z[3, base:base + 8] = 20 + torch.randn(8, device="cuda").to(z.dtype)
+    z[4, 100:5000] = 15.0
+    z[5], z[6] = 0.25, -math.inf
+    z[6, ::600] = torch.randn(len(z[6, ::600]), device="cuda").to(z.dtype)
+    z[7, 69000] = math.inf
+    z[8, 69999] = math.nan
+    z[9, :] = -3e38
+    z[9, 5:70] = 3e38
+    for parameters in (dict(), dict(top_p=0.8), dict(min_p=0.3), dict(temperature=40.0, top_p=0.5, min_p=0.01), dict(temperature=0.01)):
+        check(z, u, top_k=top_k, **parameters)
+
+
+@pytest.mark.parametrize("spread", [0.1, 1.0, 6.0])
+def test_the_words_of_min_p(spread):
+    """few and many of them, those next to the border among them"""
+    z, u = rows(6, 30000, torch.float32, spread=spread, seed=5)
+    z[1, 7] = z[1].max() + 3
+    z[2, :3000] = z[2].max()
+    top = z[3].max()
+    for i, f in enumerate((0.05, 0.0499, 0.0501, 0.02)):
+        z[3, 100 * i] = top + math.log(f)
+    for min_p in (0.0157, 0.02, 0.05, 0.3, 1.0):
+        check(z, u, min_p=min_p)
+        check(z, u, min_p=min_p, top_k=100, temperature=2.0)
+
+
+def test_flat_rows():
+    """logits a thousandth apart, and rows of two parts far from one another"""
+    for V, spread in ((40000, 1e-3), (150000, 0.05)):
+        z, u = rows(3, V, torch.float32, spread=spread, seed=7)
+        z[1, V // 2:] -= 30
+        z[2, 17:] -= 5
+        for parameters in (dict(), dict(top_p=0.9), dict(top_k=5000, top_p=0.9), dict(temperature=3.0, min_p=0.9)):
+            check(z, u, **parameters)
