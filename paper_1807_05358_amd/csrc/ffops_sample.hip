@@ -31,7 +31,7 @@ constexpr int THREADS = 1024, WAVES = THREADS / 64;
 constexpr int BINS = 4096, BELOW = 2816;    // bins; those below the anchor
 constexpr int MOST = 2 * THREADS;           // words of the bins that decide
 constexpr uint32_t FIRST_MOST = 256;        // top_k up to which its words are gathered first
-constexpr float FIRST_LEAST = 0x1p-6f;      // min_p from which, without top_p, its words are: they are few in most rows (see below)
+constexpr float FIRST_LEAST = 0x1p-6f;      // min_p from which, without top_p, its words are: they are few in most rows (see above)
 constexpr uint32_t NONE = 0xffffffffu;      // no word
 
 // Logits as whole numbers in the same order, -0 as 0.
