@@ -247,10 +247,7 @@ typedef struct {
     int32_t top_k;
     int32_t* words;
     float* logprob;
-    void* workspace;
-    size_t workspace_bytes;
 } ff_sample_t;
-size_t ff_op_sample_workspace_bytes(const ff_sample_t* a);
 int ff_op_sample(const ff_sample_t* a, void* stream);
 
 #ifdef __cplusplus

@@ -921,8 +921,6 @@ int check(const ff_sample_t* p)
 
 using namespace ffops;
 
-extern "C" size_t ff_op_sample_workspace_bytes(const ff_sample_t*) { return 0; }
-
 extern "C" int ff_op_sample(const ff_sample_t* p, void* stream)
 {
     if (!p) return FF_EINVAL;

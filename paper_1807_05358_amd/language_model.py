@@ -145,8 +145,11 @@ class Decoder:
         """(words, logprob) [batch, new] chosen one after the other behind tokens [batch, length] (lengths as in extend): u [batch, new] are the random numbers, `choice` the
         parameters of operators.sample.  The cache holds all but the last of them."""
         import torch
+        new = u.shape[1]
+        if new == 0 or cache.filled + tokens.shape[1] + new - 1 > cache.positions:
+            raise ValueError(f"{new} words behind {tokens.shape[1]} tokens and up to {cache.filled} before them do not fit a cache of {cache.positions} positions, or are none")
         words, logprob = [], []
-        for i in range(u.shape[1]):
+        for i in range(new):
             word, log = O.sample(self.extend(cache, tokens, lengths), u[:, i], **choice)
             words.append(word)
             logprob.append(log)

@@ -25,7 +25,7 @@ FF_HELD_SAME, FF_HELD_E4M3, FF_HELD_E2M1 = 0, 1, 2
 EXPORTS = ["ff_op_layernorm_fwd", "ff_op_layernorm_bwd_workspace_bytes", "ff_op_layernorm_bwd",
            "ff_op_attention_fwd_workspace_bytes", "ff_op_attention_fwd", "ff_op_attention_bwd_workspace_bytes", "ff_op_attention_bwd",
            "ff_op_vocab_loss_fwd_workspace_bytes", "ff_op_vocab_loss_fwd", "ff_op_vocab_loss_bwd_workspace_bytes", "ff_op_vocab_loss_bwd",
-           "ff_op_cache_write", "ff_op_cache_read", "ff_op_attention_paged_fwd_workspace_bytes", "ff_op_attention_paged_fwd", "ff_op_sample_workspace_bytes", "ff_op_sample"]
+           "ff_op_cache_write", "ff_op_cache_read", "ff_op_attention_paged_fwd_workspace_bytes", "ff_op_attention_paged_fwd", "ff_op_sample"]
 
 
 class ff_rows_t(C.Structure):
@@ -93,7 +93,7 @@ class ff_attention_paged_fwd_t(C.Structure):
 
 class ff_sample_t(C.Structure):
     _fields_ = [(n, _u32) for n in ("dtype", "rows", "vocab")] + [("logits", ff_rows_t)] + [(n, _vp) for n in ("u", "temperatures", "top_ps", "min_ps", "top_ks")] + \
-        [(n, C.c_float) for n in ("temperature", "top_p", "min_p")] + [("top_k", C.c_int32), ("words", _vp), ("logprob", _vp)] + _WS
+        [(n, C.c_float) for n in ("temperature", "top_p", "min_p")] + [("top_k", C.c_int32), ("words", _vp), ("logprob", _vp)]
 
 
 _RECORDS = {"ff_op_layernorm_fwd": ff_layernorm_fwd_t, "ff_op_layernorm_bwd": ff_layernorm_bwd_t, "ff_op_attention_fwd": ff_attention_fwd_t,

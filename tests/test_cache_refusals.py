@@ -26,7 +26,7 @@ def good(name):
         return O.ff_cache_read_t(O.FF_BF16, 2, 2, 64, 3, h, h, cache, P)
     if name == "ff_op_attention_paged_fwd":
         return O.ff_attention_paged_fwd_t(O.FF_BF16, 2, 8, 2, 1, 64, 0, 0.125, h, h, cache, P, P, P, P, 1 << 30)
-    return O.ff_sample_t(O.FF_F32, 2, 100, O.ff_rows_t(P, 100), P, None, None, None, None, 1.0, 1.0, 0.0, 0, P, P, None, 0)
+    return O.ff_sample_t(O.FF_F32, 2, 100, O.ff_rows_t(P, 100), P, None, None, None, None, 1.0, 1.0, 0.0, 0, P, P)
 
 
 CACHE = [(INVALID, dict(dtype=O.FF_F32)), (INVALID, dict(dtype=9)), (INVALID, dict(kv_heads=0)), (INVALID, dict(head_dim=0)), (INVALID, dict(head_dim=60)), (RANGE, dict(head_dim=136)),

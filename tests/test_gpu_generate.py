@@ -137,7 +137,8 @@ def test_a_call_that_fails_leaves_the_cache_as_it_was():
     tokens = prompts(2, 20, seed=9)
     cache = L.Cache(model, 2, 64)
     model.extend(cache, tokens)
-    for bad in (lambda: model.extend(cache, prompts(3, 4)), lambda: model.extend(cache, tokens, torch.ones(2, dtype=torch.int64, device="cuda")), lambda: model.extend(cache, tokens[:, :0])):
+    for bad in (lambda: model.extend(cache, prompts(3, 4)), lambda: model.extend(cache, tokens, torch.ones(2, dtype=torch.int64, device="cuda")), lambda: model.extend(cache, tokens[:, :0]),
+                lambda: model.generate(cache, tokens, torch.rand(2, 26, device="cuda")), lambda: model.generate(cache, tokens, torch.rand(2, 0, device="cuda"))):
         with pytest.raises(ValueError):
             bad()
     assert cache.filled == 20 and cache.lengths.tolist() == [20, 20]
