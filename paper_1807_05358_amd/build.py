@@ -14,7 +14,7 @@ KERNEL_UNITS = ["ffsim_k_loop.hip", "ffsim_k_batch.hip", "ffsim_k_chain.hip", "f
 VARIANTS = [(0, 4), (0, 0), (1, 4), (1, 0), (2, 4), (2, 0)]
 # the operators: kernels and host side of each in one file, compiled once
 OPERATOR_UNITS = ["ffops_layernorm.hip", "ffops_attention_fwd.hip", "ffops_attention_bwd.hip", "ffops_vocab.hip", "ffops_cache.hip", "ffops_attention_paged.hip", "ffops_sample.hip"]
-OPERATOR_HEADERS = ["ffops_cache.h", "ffops_paged_runs.h", "ffops_device.h", "ffops_tiles.h", "ffops_attention.h", "ffops_vocab_tiling.h"]
+OPERATOR_HEADERS = ["ffops_cache.h", "ffops_paged_runs.h", "ffops_sample_bins.h", "ffops_device.h", "ffops_tiles.h", "ffops_attention.h", "ffops_vocab_tiling.h"]
 UNITS = [HOST_UNIT] + KERNEL_UNITS
 HEADERS = ["ffsim_select.h", "ffsim_loop_chain.h", "ffsim_loop_kernels.h", "ffsim_loop.h", "ffsim_kept.h", "ffsim_sweep.h", "ffsim_ahead.h", "ffsim_kernels.h", "ffsim_chain.h", "ffsim_events.h", "ffsim_strategy.h",
            "ffsim_device.h"]

@@ -1,5 +1,6 @@
 // The choice of a word from its logits.
 #include "ffops_device.h"
+#include "ffops_sample_bins.h"
 
 namespace ffops {
 namespace {
@@ -28,7 +29,6 @@ struct SampleArgs {
 //   The bins that decide are those in which the border of top_k, that of top_p, that of min_p and the chosen word can lie; they depend on one another, so each is a range
 // until the words are there.  Bins with more than MOST words (equal logits, or nearly so) are left to select(), which reads the row for every eight bits of the key of each border.
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
-constexpr int BINS = 4096, BELOW = 2816;    // bins; those below the anchor
 constexpr int MOST = 2 * THREADS;           // words of the bins that decide
 constexpr uint32_t FIRST_MOST = 256;        // top_k up to which its words are gathered first
 constexpr float FIRST_LEAST = 0x1p-6f;      // min_p from which, without top_p, its words are: they are few in most rows (see above)
@@ -329,32 +329,6 @@ struct Row {
     }
 };
 
-// The bins of a row; the anchor, a finite logit, is at the lower edge of bin BELOW.
-struct Bins {
-    double anchor, per_logit, width;        // bins in a unit of the logits, and its inverse
-    float c[4];                             // 2^29 (e^(r / per_nat) - 1) as a sum of powers of r, and 0.5
-
-    __device__ __forceinline__ void set(float anchor_, float temperature, int per_nat)
-    {
-        anchor = anchor_, per_logit = per_nat / (double)temperature, width = (double)temperature / per_nat;
-        const float h = 1.0f / per_nat;
-        c[0] = 0x1p29f * h, c[1] = 0x1p28f * h * h, c[2] = 0x1p29f / 6 * h * h * h, c[3] = 0x1p29f / 24 * h * h * h * h;
-    }
-    // the place of a logit in bins, the lowest of which begins at 1: what is below is then cut off to 0
-    __device__ __forceinline__ double place(float z) const { return fma((double)z - anchor, per_logit, (double)(BELOW + 1)); }
-    // a logit on the safe side (-1: below, 1: above) of a bin's lower edge
-    __device__ __forceinline__ float logit(int bin, int side) const
-    {
-        const double edge = fma((double)(bin - BELOW), width, anchor);
-        return (float)(edge + side * (fabs(edge) * 1e-6 + 1e-30));
-    }
-    // a bin's number, -1 and BINS beyond them, and that + 1
-    __device__ __forceinline__ int slot(double at) const { return min(max((int)at, 0), BINS + 1); }
-    __device__ __forceinline__ int bin(double at) const { return slot(at) - 1; }
-    // e^(r / per_nat), 0 <= r < 1, in steps of 2^-29, to the nearest: what is beyond 1 is below 2^-4.9, so a float has it to half of such a step
-    __device__ __forceinline__ uint32_t steps(float r) const { return (1u << 29) + (uint32_t)fmaf(r, fmaf(r, fmaf(r, fmaf(r, c[3], c[2]), c[1]), c[0]), 0.5f); }
-};
-
 __device__ __forceinline__ void add_lds(uint64_t* p, uint64_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 __device__ __forceinline__ void add_lds(uint32_t* p, uint32_t x) { __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP); }
 
@@ -560,11 +534,6 @@ __device__ __forceinline__ void sort_list(Shared& sh, uint32_t n)
             __syncthreads();
         }
 }
-
-// Bins in a unit of the temperature, where the largest logits of the threads' shares lie so many units apart: in most rows the others are no more than three times that, and a little, below the largest, so bins are as narrow as
-// reaches that far and the words of a few of them are few.  Where it does not, the row is read again (below).  256 rows of 131071 normal logits, top_p 0.9, with 64 bins a unit and so: deviation 1 unit 1100 us and 80, 2.5 units
-// 71 and 66, 4 units 51 and 50.
-__device__ __forceinline__ int bins_per_nat(float apart) { return max(32, min(1 << 16, (int)(BELOW / (3 * apart + fminf(apart, 2.0f))))); }
 
 // The word from bins, or of the first top_k.  most: the largest logit.
 template <class T>

@@ -1,0 +1,41 @@
+"""The choice of a word where its borders lie badly: at the edges of the bins that words are counted in, beyond what any word weighs, among millions of words that together weigh little beside one."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import answering_reference as R  # noqa: E402
+from paper_1807_05358_amd import operators as O  # noqa: E402
+from test_gpu_sample import TYPES, check  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+# temperature, largest logit and bins a unit, where the place of logit 0 is a rounding below a whole number: its bin ends at an edge that is 0, or a rounding below
+EDGES = [(0.75, 0.5625, 2392), (0.75, 1.125, 1388), (0.75, 1.875, 776), (0.75, 2.625, 574), (0.75, 3.5625, 592), (0.75, 5.0625, 412), (0.75, 6.9375, 272), (1.5, 1.125, 2704), (1.5, 1.5, 2014), (1.5, 2.25, 1558),
+         (1.5, 3.0, 1163), (1.5, 4.5, 773), (1.5, 6.0, 589), (3.0, 3.0, 2116), (3.0, 4.5, 1304), (3.0, 7.5, 1106)]
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("each", [12, 300])
+def test_logits_of_0_at_the_edge_of_a_bin(t, each):
+    """words of logit 0, as many just above and as many just below decide, beside larger ones"""
+    g = torch.Generator().manual_seed(each)
+    cases = [(*e, part, what) for e in EDGES + [(0.5, 2.0, 333), (1.0, 3.0, 500)] for part in range(3) for what in ("u", "top_p")]
+    step = 16 // torch.empty(0, dtype=TYPES[t]).element_size()                  # each thread of a row's block looks at so many words side by side
+    z = torch.full((len(cases), 1024 * step), -math.inf, dtype=torch.float64)
+    u, top_p = torch.full((len(cases),), 1 - 2.0 ** -24), torch.ones(len(cases))
+    temperature = torch.tensor([c[0] for c in cases])
+    for r, (T, top, per, part, what) in enumerate(cases):
+        # the least of the threads' largest words, from which the bins' width is made
+        apart = 704 / (per + 0.5) if per > 352 else (2816 / (per + 0.5) - 2) / 3
+        z[r, ::step] = top - T * apart * torch.rand(1024, generator=g).double() / 2
+        z[r, 0], z[r, step] = top, top - T * apart
+        at = torch.randperm(1024, generator=g)[:3 * each] * step + 1
+        beside = 1e-7 * (1 + torch.rand(each, generator=g).double())
+        z[r, at[:each]], z[r, at[each:2 * each]], z[r, at[2 * each:]] = 0.0, -beside, beside
+        z[r] = z[r].to(TYPES[t]).double()
+        run = torch.exp((z[r] - top) / T).sort(descending=True)[0].cumsum(0)
+        # in the middle of a word among those
+        k = 1024 + part * each + each // 2
+        (u if what == "u" else top_p)[r] = float((run[k] + run[k - 1]) / 2 / run[-1])
+    check(z.to(TYPES[t]).cuda(), u.cuda(), temperature=temperature.cuda(), top_p=top_p.cuda())
