@@ -436,11 +436,12 @@ struct Choice {
     __device__ __forceinline__ Choice(const SampleArgs& a, uint32_t row)
     {
         temperature = a.temperatures ? a.temperatures[row] : a.temperature, top_p = a.top_ps ? a.top_ps[row] : a.top_p, u = a.u[row];
-        const float m = a.min_ps ? a.min_ps[row] : a.min_p;
-        min_p = m > 1 ? 1.0f : m;
+        min_p = a.min_ps ? a.min_ps[row] : a.min_p;
         const int32_t k = a.top_ks ? a.top_ks[row] : a.top_k;
         top_k = k > 0 && (uint32_t)k < a.vocab ? (uint32_t)k : 0;
     }
+    // temperature 0, or a min_p that no word weighs: the first weighs 1, as do others that are as large, which are not kept then
+    __device__ __forceinline__ bool first_alone() const { return temperature == 0 || min_p > 1; }
     __device__ __forceinline__ bool fine() const { return temperature >= 0 && temperature < INFINITY && top_p == top_p && min_p == min_p && u == u; }
 };
 
@@ -847,7 +848,7 @@ __device__ __forceinline__ void choose_from_row(const SampleArgs& a, uint32_t ro
     if (threadIdx.x == 0) a.words[row] = state == WITHOUT ? -1 : (int32_t)word, a.logprob[row] = state == WITHOUT ? NAN : logprob;
 }
 
-// at temperature 0: the largest key, of these the lowest number; 0 where there is a NaN
+// the largest key, of these the lowest number; 0 where there is a NaN
 template <class T>
 __device__ __forceinline__ uint64_t first_word(const Row<T>& src, Shared& sh)
 {
@@ -874,7 +875,7 @@ __global__ __launch_bounds__(THREADS) void k_sample(SampleArgs a)
     const uint32_t row = blockIdx.x;
     const Choice c(a, row);
     if (!c.fine()) put_first(a, row, 0);
-    else if (c.temperature == 0) put_first(a, row, first_word(Row<T>((const typename T::elem*)(a.logits + row * a.stride), a.vocab), sh));
+    else if (c.first_alone()) put_first(a, row, first_word(Row<T>((const typename T::elem*)(a.logits + row * a.stride), a.vocab), sh));
     else choose_from_row<T>(a, row, c, sh);
 }
 

@@ -1,4 +1,6 @@
 """The choice of a word where its borders lie badly: at the edges of the bins that words are counted in, beyond what any word weighs, among millions of words that together weigh little beside one."""
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -8,6 +10,30 @@ from paper_1807_05358_amd import operators as O  # noqa: E402
 from test_gpu_sample import TYPES, check  # noqa: E402
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("t", ["f32", "f16", "bf16"])
+def test_min_p_that_no_word_reaches(t):
+    """leaves the first word alone, of equal ones that of the lowest number: a few of them, hundreds, and more than are put in order"""
+    z = torch.randn(8, 5003, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    z[0, 4:], z[0, :4] = -math.inf, torch.tensor([3.0, 5.0, 5.0, 1.0], device="cuda")
+    z[1, 100:140] = 9.0
+    z[2, ::10] = 9.0
+    z[3, 7:] = 9.0
+    z[4] = 0.0
+    z[5, ::2], z[5, 1::2] = -0.0, 0.0
+    z[6, 40:50] = math.inf
+    z[7, 4000:4002] = 9.0
+    z, u = z.to(TYPES[t]), torch.linspace(0.1, 0.99, 8, device="cuda")
+    for min_p in (1.0 + 2.0 ** -23, 2.0, 1e30, torch.tensor([0.5, 1.0, 1.5, 7.0, 2.0, 1.0, 3.0, math.inf], device="cuda")):
+        for parameters in (dict(), dict(top_p=0.9), dict(top_k=3), dict(top_k=4000, top_p=0.5), dict(temperature=0.2), dict(temperature=40.0, top_k=300)):
+            words, logprob = check(z, u, min_p=min_p, **parameters)
+            if not torch.is_tensor(min_p):
+                assert int(words[0]) == 1 and float(logprob[0]) == 0.0
+    z[3, 20] = math.nan
+    z[4] = -math.inf
+    words, logprob = check(z, u, min_p=2.0)
+    assert words[3:5].tolist() == [-1, -1] and bool(torch.isnan(logprob[3:5]).all())
 
 
 # temperature, largest logit and bins a unit, where the place of logit 0 is a rounding below a whole number: its bin ends at an edge that is 0, or a rounding below
