@@ -486,8 +486,9 @@ __device__ __forceinline__ int gather_top(const Row<T>& src, const Choice& c, Sh
         if (all >= c.top_k) from = Key<F32>::value(sh.found);
     }
     if (c.top_p >= 1 && c.min_p > 0) {
+        // on the safe side of it, by a float's rounding, and by those of weights, which are up to 1e-14 of a temperature away
         const double edge = (double)most + (double)c.temperature * log((double)c.min_p);
-        from = fmaxf(from, (float)(edge - (fabs(edge) * 1e-6 + 1e-30)));
+        from = fmaxf(from, (float)(edge - (fabs(edge) * 1e-6 + c.temperature * 1e-9 + 1e-30)));
     }
     if (tid == 0) sh.above[0] = 0, sh.count[0] = 0;         // the list is one bin, with nothing above it
     bool full = false;

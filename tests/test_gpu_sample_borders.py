@@ -65,3 +65,21 @@ def test_logits_of_0_at_the_edge_of_a_bin(t, each):
         k = 1024 + part * each + each // 2
         (u if what == "u" else top_p)[r] = float((run[k] + run[k - 1]) / 2 / run[-1])
     check(z.to(TYPES[t]).cuda(), u.cuda(), temperature=temperature.cuda(), top_p=top_p.cuda())
+
+
+def test_weights_that_are_1_in_64_bits():
+    """at a high temperature words far below the largest weigh 1, too, and min_p of 1 or just below it leaves them: a few, and more than are put in order"""
+    for V in (50, 1500, 9000):
+        z = torch.randn(4, V, generator=torch.Generator(device="cuda").manual_seed(V), device="cuda")
+        z[1] *= 1000
+        z[2, ::3] = -math.inf
+        u = torch.tensor([0.0, 0.3, 0.6, 0.97], device="cuda")
+        for temperature in (1e20, 1e30, 3e38):
+            for min_p in (1.0, 1 - 2.0 ** -24, 0.5):
+                for parameters in (dict(), dict(top_k=40)):
+                    check(z, u, temperature=temperature, min_p=min_p, **parameters)
+                # half of equal words ends just where one of them does: both sums are to 2^-29 of themselves, so the border is to 2^-28, and the word behind it may be kept or not
+                words, logprob = O.sample(z, u, temperature=temperature, min_p=min_p, top_p=0.5)
+                for r, row in enumerate(z.cpu()):
+                    may = [R.choose(row, float(u[r]), temperature, 0, 0.5 * (1 + side * 2.0 ** -28), min_p) for side in (-1, 0, 1)]
+                    assert any(int(words[r]) == word and abs(float(logprob[r]) - log) <= 2.0 ** -24 * abs(log) + 1e-9 for word, log in may), (V, r, temperature, min_p, may, words[r], logprob[r])
