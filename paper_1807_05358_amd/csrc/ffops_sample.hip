@@ -63,13 +63,45 @@ struct Key<F16> : Key16<F16> {};
 template <>
 struct Key<BF16> : Key16<BF16> {};
 
+// Weights in steps of 2^-78, so that their sums do not depend on an order; of single ones the upper half, in steps of 2^-39, and the rest, whose sums over 2^24 words fit 64 bits each.  (In 64 bits together a step is 2^-38 of the
+// largest weight for as many words, and equal words that weigh less than half of that would count for nothing, all of them 2^-15.)
+typedef unsigned __int128 Steps;
+struct Halves {
+    uint64_t hi, lo;                // lo with its sign, -2^38 .. 2^38
+    __device__ __forceinline__ Steps sum() const { return ((Steps)hi << 39) + (Steps)(__int128)(int64_t)lo; }
+};
+__device__ __forceinline__ double to_double(Steps x) { return (double)(uint64_t)(x >> 64) * 0x1p64 + (double)(uint64_t)x; }
+// t: at least 0, below 2^127
+__device__ __forceinline__ Steps to_steps(double t)
+{
+    const uint64_t hi = (uint64_t)(t * 0x1p-64);
+    return (Steps)hi << 64 | (uint64_t)(t - (double)hi * 0x1p64);
+}
+// how many times s, which is more than 0, is in x; at most 2^24 times, so that the quotient in 64 bits is off by one at most
+__device__ __forceinline__ uint32_t times(Steps s, Steps x)
+{
+    uint32_t n = (uint32_t)(to_double(x) / to_double(s));
+    if (n * s > x) --n;
+    if ((n + 1) * s <= x) ++n;
+    return n;
+}
+
 // what select() counts
 struct Digits {
-    uint64_t mass[256];
+    uint64_t hi[256], lo[256];      // the halves of sums
     uint32_t count[256];
     uint32_t found;
-    uint64_t above_mass;
+    Steps target, above_mass;       // (one thread works with these; the others keep no registers for them)
     uint32_t above_count;
+    Steps mass, mass_m;             // of the words that are kept, and of those that min_p leaves
+    uint32_t kept, rank;
+    __device__ __forceinline__ void add(uint32_t digit, uint32_t n, Halves s)
+    {
+        atomicAdd((unsigned long long*)&hi[digit], (unsigned long long)s.hi);
+        atomicAdd((unsigned long long*)&lo[digit], (unsigned long long)s.lo);
+        atomicAdd(&count[digit], n);
+    }
+    __device__ __forceinline__ Steps sum(uint32_t digit) const { return Halves{hi[digit], lo[digit]}.sum(); }
 };
 
 struct Shared {
@@ -117,107 +149,121 @@ __device__ __forceinline__ uint64_t block_max(uint64_t x, uint64_t* at)
     return x;
 }
 
-// Weights as whole numbers of steps of 2^-shift, so that their sums do not depend on an order.
 struct Weigh {
     float most;
-    double per;                     // 1 / temperature
-    double unit;                    // 2^shift
+    double per;                     // temperature
     __device__ __forceinline__ double of(float z) const { return z == most ? 1.0 : exp(((double)z - (double)most) / per); }
-    __device__ __forceinline__ uint64_t steps(float z) const { return (uint64_t)rint(of(z) * unit); }
+    __device__ __forceinline__ Halves halves(float z) const
+    {
+        // whole numbers as the lower bits of floats of 2^52 and more, where a step is 1
+        constexpr double ONE = 0x1p52, HALF = 0x1.8p52;
+        const double w = of(z) * 0x1p39, hi = w + ONE, lo = (w - (hi - ONE)) * 0x1p39 + HALF;
+        return {__builtin_bit_cast(uint64_t, hi) - __builtin_bit_cast(uint64_t, ONE), __builtin_bit_cast(uint64_t, lo) - __builtin_bit_cast(uint64_t, HALF)};
+    }
+    __device__ __forceinline__ Steps steps(float z) const { return halves(z).sum(); }
 };
 
-// The shortest beginning of the words' order with more than `target` words (BY_COUNT) or steps of weight: its last word's key, the words before it with larger keys and
+// The shortest beginning of the words' order with more than sh.target words (BY_COUNT) or steps of weight: its last word's key, the words before it with larger keys and
 // their steps (sh.above_...), bit group after bit group of the keys.
 template <class T, bool BY_COUNT>
-__device__ uint32_t select(const typename T::elem* z, uint32_t vocab, const Weigh& w, uint64_t target, Digits& sh, uint64_t& above_mass, uint32_t& above_count)
+__device__ __forceinline__ uint32_t select(const typename T::elem* z, uint32_t vocab, const Weigh& w, Digits& sh)
 {
     uint32_t prefix = 0;
-    above_mass = 0, above_count = 0;
+    if (threadIdx.x == 0) sh.above_mass = 0, sh.above_count = 0;
     for (int low = Key<T>::BITS - 8; low >= 0; low -= 8) {
-        if (threadIdx.x < 256) sh.mass[threadIdx.x] = 0, sh.count[threadIdx.x] = 0;
+        if (threadIdx.x < 256) sh.hi[threadIdx.x] = 0, sh.lo[threadIdx.x] = 0, sh.count[threadIdx.x] = 0;
         __syncthreads();
         for (uint32_t base = 0; base < vocab; base += THREADS) {
             const uint32_t i = base + threadIdx.x, k = i < vocab ? Key<T>::of(z[i]) : 0;
             bool in = i < vocab && !(low + 8 < Key<T>::BITS && (k >> (low + 8)) != prefix);
-            const uint64_t s = in ? w.steps(Key<T>::value(k)) : 0;
+            const Halves s = in ? w.halves(Key<T>::value(k)) : Halves{0, 0};
             // it is equal logits that this is for: those of a wave are added at once, up to four different ones
             for (int t = 0; t < 4 && __any(in); ++t) {
                 const int leader = __builtin_ctzll(__ballot(in));
                 const bool same = in && k == (uint32_t)__builtin_amdgcn_readlane((int)k, leader);
                 const uint32_t n = __popcll(__ballot(same));
-                if ((int)(threadIdx.x % 64) == leader) {
-                    atomicAdd((unsigned long long*)&sh.mass[k >> low & 255], (unsigned long long)(n * s));
-                    atomicAdd(&sh.count[k >> low & 255], n);
-                }
+                if ((int)(threadIdx.x % 64) == leader) sh.add(k >> low & 255, n, {n * s.hi, n * s.lo});
                 in = in && !same;
             }
-            if (in) {
-                atomicAdd((unsigned long long*)&sh.mass[k >> low & 255], (unsigned long long)s);
-                atomicAdd(&sh.count[k >> low & 255], 1u);
-            }
+            if (in) sh.add(k >> low & 255, 1, s);
         }
         __syncthreads();
         if (threadIdx.x == 0) {
-            uint64_t m = above_mass;
-            uint32_t c = above_count, best = 256;
+            Steps m = sh.above_mass;
+            const Steps target = sh.target;
+            uint32_t c = sh.above_count, best = 256;
             for (int d = 255; d >= 0; --d) {
-                if (sh.count[d] && (BY_COUNT ? c + (uint64_t)sh.count[d] > target : m + sh.mass[d] > target)) {
+                const Steps more = sh.sum(d);
+                if (sh.count[d] && (BY_COUNT ? (Steps)c + sh.count[d] > target : m + more > target)) {
                     best = d;
                     break;
                 }
-                m += sh.mass[d], c += sh.count[d];
+                m += more, c += sh.count[d];
             }
             sh.found = best, sh.above_mass = m, sh.above_count = c;
         }
         __syncthreads();
-        above_mass = sh.above_mass, above_count = sh.above_count;
         prefix = prefix << 8 | (sh.found & 255);
         __syncthreads();
     }
     return prefix;
 }
 
-// The word by reading the row again for every border; all of its threads.  `first`: the largest key.
+// The word by reading the row again for every border; all of its threads.
 template <class T>
-__device__ void choose_by_digits(const typename T::elem* z, uint32_t V, float most, float temperature, int32_t top_k, float top_p, float min_p, float u, Shared& sh, uint32_t& word, float& logprob)
+__device__ __forceinline__ void choose_by_digits(const typename T::elem* z, uint32_t V, float most, float temperature, int32_t top_k, float top_p, float min_p, float u, Shared& sh, uint32_t& word, float& logprob)
 {
-    Weigh w = {most, (double)temperature, 1.0};
-    int shift = 62;
-    while ((1ull << (62 - shift)) < V) --shift;
-    w.unit = (double)(1ull << shift);
-    uint64_t mass = 0, mass_m = 0;
+    const Weigh w = {most, (double)temperature};
+    Halves all = {0, 0}, all_m = {0, 0};
     uint32_t count_m = 0;
     for (uint32_t i = threadIdx.x; i < V; i += THREADS) {
         const float f = (float)z[i];
-        const uint64_t s = w.steps(f);
-        mass += s;
-        if (w.of(f) >= (double)min_p) mass_m += s, ++count_m;
+        const Halves s = w.halves(f);
+        all.hi += s.hi, all.lo += s.lo;
+        if (w.of(f) >= (double)min_p) all_m.hi += s.hi, all_m.lo += s.lo, ++count_m;
     }
-    mass = block_sum(mass, sh.a), mass_m = block_sum(mass_m, sh.b), count_m = block_sum(count_m, sh.c);
-    uint32_t kept = V;
-    uint64_t above;
-    uint32_t before;
+    Digits& at = sh.digits;
+    const bool one = threadIdx.x == 0;          // of the threads; the others meet it in select() and behind it
+    if (threadIdx.x < 2) at.hi[threadIdx.x] = 0, at.lo[threadIdx.x] = 0, at.count[threadIdx.x] = 0;
+    __syncthreads();
+    at.add(0, 1, all), at.add(1, count_m, all_m);
+    __syncthreads();
+    if (one) at.mass = at.sum(0), at.mass_m = at.sum(1), at.kept = V, count_m = at.count[1];
+    __syncthreads();
     if (top_k > 0 && (uint32_t)top_k < V) {
-        const uint32_t k = select<T, true>(z, V, w, (uint64_t)top_k - 1, sh.digits, above, before);
-        kept = (uint32_t)top_k, mass = above + (kept - before) * w.steps(Key<T>::value(k));
+        if (one) at.target = (Steps)(top_k - 1);
+        const uint32_t k = select<T, true>(z, V, w, at);
+        if (one) at.kept = (uint32_t)top_k, at.mass = at.above_mass + (at.kept - at.above_count) * w.steps(Key<T>::value(k));
     }
     if (top_p < 1) {
-        const double t = ceil((double)top_p * (double)mass);
-        const uint64_t target = t < 1 ? 0 : t <= (double)(mass - 1) ? (uint64_t)t - 1 : mass - 1;
-        const uint32_t k = select<T, false>(z, V, w, target, sh.digits, above, before);
-        const uint64_t s = w.steps(Key<T>::value(k)), more = (target - above) / s + 1;
-        if (before + more < kept) kept = before + (uint32_t)more, mass = above + more * s;
+        if (one) {
+            const double t = ceil((double)top_p * to_double(at.mass));
+            const Steps target = t < 1 ? 0 : to_steps(t) - 1;
+            at.target = target < at.mass ? target : at.mass - 1;
+        }
+        const uint32_t k = select<T, false>(z, V, w, at);
+        if (one) {
+            const Steps s = w.steps(Key<T>::value(k));
+            const uint32_t more = times(s, at.target - at.above_mass) + 1;
+            if (at.above_count + more < at.kept) at.kept = at.above_count + more, at.mass = at.above_mass + more * s;
+        }
     }
-    if (count_m < kept) {
-        kept = count_m, mass = mass_m;
-        if (!kept) kept = 1, mass = w.steps(most);
+    if (one) {
+        if (count_m < at.kept) {
+            at.kept = count_m, at.mass = at.mass_m;
+            if (!at.kept) at.kept = 1, at.mass = w.steps(most);
+        }
+        const Steps target = to_steps(floor((u < 0 ? 0.0 : u < 1 ? (double)u : 1.0) * to_double(at.mass)));
+        at.target = target < at.mass ? target : at.mass - 1;
     }
-    const double t = floor((double)(u < 0 ? 0 : u) * (double)mass);
-    const uint64_t target = t < (double)(mass - 1) ? (uint64_t)t : mass - 1;
-    const uint32_t k = select<T, false>(z, V, w, target, sh.digits, above, before);
+    const uint32_t k = select<T, false>(z, V, w, at);
     const float chosen = Key<T>::value(k);
-    uint64_t rank = (target - above) / w.steps(chosen);         // words of that key before it
-    if (before + rank >= kept) rank = kept - 1 - before;
+    if (one) {
+        const uint32_t n = times(w.steps(chosen), at.target - at.above_mass), before = at.above_count;       // words of that key before it, and of larger ones
+        at.rank = before + n < at.kept ? n : at.kept - 1 - before;
+    }
+    __syncthreads();
+    const uint32_t rank = at.rank;
     uint32_t seen = 0;
     for (uint32_t base = 0; base < V; base += THREADS) {
         const uint32_t i = base + threadIdx.x;
@@ -234,7 +280,7 @@ __device__ void choose_by_digits(const typename T::elem* z, uint32_t V, float mo
         if (seen > rank) break;
     }
     __syncthreads();
-    word = sh.word, logprob = (float)log(w.of(chosen) / ((double)mass / w.unit));
+    word = sh.word, logprob = (float)log(w.of(chosen) / (to_double(at.mass) * 0x1p-78));
 }
 
 // sixteen bytes of a row at any element's place; -inf behind its end
@@ -707,7 +753,7 @@ __device__ __forceinline__ int choose_by_bins(const Row<T>& src, const Choice& c
         __syncthreads();
         n = sh.n;
     }
-    const Weigh weigh = {most, (double)c.temperature, 1.0};
+    const Weigh weigh = {most, (double)c.temperature};
     const auto bin_of = [&](float x) { return whole ? 0 : bins.bin(bins.place(x)); };
     if (n <= MOST) sort_list(sh, n);
     if (n <= 64) {

@@ -83,3 +83,45 @@ def test_weights_that_are_1_in_64_bits():
                 for r, row in enumerate(z.cpu()):
                     may = [R.choose(row, float(u[r]), temperature, 0, 0.5 * (1 + side * 2.0 ** -28), min_p) for side in (-1, 0, 1)]
                     assert any(int(words[r]) == word and abs(float(logprob[r]) - log) <= 2.0 ** -24 * abs(log) + 1e-9 for word, log in may), (V, r, temperature, min_p, may, words[r], logprob[r])
+
+
+@pytest.mark.parametrize("V", [1 << 14, 1 << 20, 1 << 24])
+def test_many_words_that_weigh_little_each(V):
+    """one word and V - 1 equal ones beside it, each of which may weigh less than 2^-38 of it and all of them 3e-5"""
+    for t in (torch.float32, torch.bfloat16):
+        z = torch.full((1, V), -math.log(V / 3e-5), device="cuda").to(t)
+        at = V // 3
+        z[0, at] = 0.0
+        w = math.exp(float(z[0, 0]))
+        total = 1 + (V - 1) * w
+        for u in (0.5, 1 - 2.0 ** -15, 0.99999, 1 - 2.0 ** -18, 1 - 2.0 ** -24):
+            u = float(torch.tensor(u, dtype=torch.float32))
+            for top_p in (1.0, 0.99999):
+                p = float(torch.tensor(top_p, dtype=torch.float32))
+                n = V - 1 if top_p == 1.0 else math.ceil((p * total - 1) / w)       # of the equal words those that are kept
+                left = 1 + n * w
+                words, logprob = O.sample(z, torch.tensor([u], device="cuda"), top_p=top_p)
+                k = math.floor((u * left - 1) / w)                                   # of them, those before the chosen one; below 0: the first word
+                got = int(words[0])
+                rank = -1 if got == at else got - (got > at)
+                # sums to 2^-53 of themselves and of the largest word's weight a few times, and words rounded to 2^-79 of that, in words; and a word, of top_p and u each, where a border is next to one
+                assert (rank == -1) == (k < 0) and abs(rank - max(k, -1)) <= 2 + (16 * 2.0 ** -53 + V * 2.0 ** -79) / w, (t, u, top_p, rank, k)
+                want = math.log((1.0 if k < 0 else w) / left)
+                assert abs(float(logprob[0]) - want) <= 2.0 ** -24 * abs(want) + 1e-9 + 2 * w
+
+
+def test_sums_of_many_equal_words_beside_others():
+    """a border of top_k, top_p or min_p among more equal words than are put in order, and words that weigh 2^-30 and less of the largest"""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    z = torch.randn(4, 20011, generator=g, device="cuda")
+    z[0, 1::4] = -19.0
+    z[0, 0] = 9.0
+    z[1, ::3] = -30.0
+    z[1, 1::3] = -29.5
+    z[1, 2::3] = -60.0
+    z[1, 100] = 0.0
+    z[2, ::2] = 1.0
+    z[3, 5000:] = -3.0
+    u = torch.tensor([1 - 2.0 ** -24, 1 - 2.0 ** -24, 0.7, 0.95], device="cuda")
+    for parameters in (dict(), dict(top_k=9000), dict(top_k=15000, top_p=0.9), dict(min_p=1e-7), dict(top_p=0.99999994), dict(temperature=2.0), dict(temperature=0.7, top_p=0.99)):
+        check(z, u, **parameters)
