@@ -143,11 +143,14 @@ class Decoder:
 
     def generate(self, cache, tokens, u, lengths=None, **choice):
         """(words, logprob) [batch, new] chosen one after the other behind tokens [batch, length] (lengths as in extend): u [batch, new] are the random numbers, `choice` the
-        parameters of operators.sample.  The cache holds all but the last of them."""
+        parameters of operators.sample.  The cache holds all but the last of them; a call that is refused leaves it as it was."""
         import torch
+        if u.dim() != 2 or tokens.dim() != 2:
+            raise ValueError("tokens and u are matrices, a row for each sequence")
         new = u.shape[1]
         if new == 0 or cache.filled + tokens.shape[1] + new - 1 > cache.positions:
             raise ValueError(f"{new} words behind {tokens.shape[1]} tokens and up to {cache.filled} before them do not fit a cache of {cache.positions} positions, or are none")
+        O.checked_choice(u[:, 0], cache.lengths.shape[0], cache.lengths.device, **choice)       # before the cache holds any of the tokens
         words, logprob = [], []
         for i in range(new):
             word, log = O.sample(self.extend(cache, tokens, lengths), u[:, i], **choice)

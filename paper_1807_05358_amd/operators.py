@@ -551,6 +551,28 @@ def attention_paged_fwd(q, k_pages, v_pages, table, kv_lengths, *, causal=False,
     return o, lse
 
 
+def checked_choice(u, rows, device, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(vectors, numbers) of temperature, top_p, min_p and top_k: what sample would be given beside logits of so many rows, refused as there.  For those who have work to do before there are logits."""
+    torch = _torch()
+    _check(u, "u", (rows,), torch.float32, device)
+    numbers, vectors = [], []
+    for x, what, to, kind in ((temperature, "temperature", torch.float32, float), (top_p, "top_p", torch.float32, float), (min_p, "min_p", torch.float32, float), (top_k, "top_k", torch.int32, int)):
+        if isinstance(x, torch.Tensor):
+            _not_recorded(x)
+            _check(x, what, (rows,), to, device)
+            vectors.append(_vector(x))
+            numbers.append(kind())
+        else:
+            vectors.append(None)
+            numbers.append(kind(x))
+    if not -2 ** 31 <= numbers[3] < 2 ** 31:
+        raise ValueError("top_k does not fit 32 bits")
+    for n, what, least in zip(numbers, ("temperature", "top_p", "min_p"), (0.0, -math.inf, -math.inf)):
+        if not n >= least or not abs(n) <= 3e38:
+            raise ValueError(f"{what} is {n}")
+    return vectors, numbers
+
+
 def sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     """(words, logprob), int32 and float32 [rows]: a word for each row of logits [rows, vocab] (float32, float16 or bfloat16), chosen by the given random number u[row] in [0, 1) (float32 [rows]).
 
@@ -567,22 +589,7 @@ def sample(logits, u, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     R, V = logits.shape
     if V == 0:
         raise ValueError("an empty vocabulary")
-    _check(u, "u", (R,), torch.float32, device)
-    numbers, vectors = [], []
-    for x, what, to, kind in ((temperature, "temperature", torch.float32, float), (top_p, "top_p", torch.float32, float), (min_p, "min_p", torch.float32, float), (top_k, "top_k", torch.int32, int)):
-        if isinstance(x, torch.Tensor):
-            _not_recorded(x)
-            _check(x, what, (R,), to, device)
-            vectors.append(_vector(x))
-            numbers.append(kind())
-        else:
-            vectors.append(None)
-            numbers.append(kind(x))
-    if not -2 ** 31 <= numbers[3] < 2 ** 31:
-        raise ValueError("top_k does not fit 32 bits")
-    for n, what, least in zip(numbers, ("temperature", "top_p", "min_p"), (0.0, -math.inf, -math.inf)):
-        if not n >= least or not abs(n) <= 3e38:
-            raise ValueError(f"{what} is {n}")
+    vectors, numbers = checked_choice(u, R, device, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
     logits, u = _dense_rows(logits), _vector(u)
     words, logprob = u.new_empty(R, dtype=torch.int32), u.new_empty(R)
     _launch("ff_op_sample", device, dtype, R, V, logits.data_ptr(), logits.stride(0), u.data_ptr(), *(_ptr(t) for t in vectors), *numbers, words.data_ptr(), logprob.data_ptr())
