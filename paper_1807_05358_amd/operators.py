@@ -8,7 +8,7 @@ device and put the kernels on its current stream; they do not wait.  Captured in
 memory.  What a call refuses on the library's side raises binding.FFSimError.
 
 autograd does not see them: gradients are the ..._bwd functions' outputs.  So tensors that require gradients are refused
-where they would be recorded; under torch.no_grad() they are taken.
+where they would be recorded; under torch.no_grad() they are taken.  Dual tensors of forward mode are refused.
 """
 from __future__ import annotations
 
@@ -190,9 +190,15 @@ def _check(t, what, shape, dtype, device):
 
 
 def _not_recorded(*ts):
+    torch = _torch()
     for t in ts:
-        if t is not None and t.requires_grad and _torch().is_grad_enabled():
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
             raise ValueError("a tensor requires gradients, which autograd would lose here: call this under torch.no_grad(), and the _bwd function for the gradients")
+    forward = torch.autograd.forward_ad
+    if getattr(forward, "_current_level", 0) >= 0:      # (outside of all levels no tensor has a tangent)
+        for t in ts:
+            if t is not None and forward.unpack_dual(t).tangent is not None:
+                raise ValueError("a tensor has a tangent, which would be lost here: the operators have no forward mode")
 
 
 def _dense_rows(t):
