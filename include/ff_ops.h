@@ -202,7 +202,7 @@ typedef struct {
 int ff_op_cache_write(const ff_cache_write_t* a, void* stream);
 
 /* Reads a cache back: k and v [batch][kv_heads][kv_len][head_dim] are written whole, zeros from lengths[b] on (clamped to 0 .. kv_len and the positions of
- * the table; null: kv_len).  Positions whose entry is no page give NaN. */
+ * the table; null: kv_len).  Positions whose entry is no page give NaN.  batch * kv_heads is at most 65535. */
 typedef struct {
     uint32_t dtype, batch, kv_heads, head_dim, kv_len;
     ff_heads_t k, v;

@@ -524,7 +524,14 @@ def cache_read(k_pages, v_pages, table, lengths, *, kv_len=None, dtype=None, k_s
         raise ValueError("kv_len is a number of positions")
     lengths = _vector(lengths)
     k, v = k_pages.new_empty((2, B, K, kv_len, D), dtype=dtype).unbind()
-    _launch("ff_op_cache_read", device, FF_F16 if dtype is torch.float16 else FF_BF16, B, K, D, kv_len, *_heads(k, v), *cache, lengths.data_ptr())
+    code, most = FF_F16 if dtype is torch.float16 else FF_BF16, max(1, 65535 // K)             # most: sequences of a launch
+    if B <= most:
+        _launch("ff_op_cache_read", device, code, B, K, D, kv_len, *_heads(k, v), *cache, lengths.data_ptr())
+    else:
+        for i in range(0, B, most):
+            some = slice(i, min(B, i + most))
+            cache = _cache_args(k_pages, v_pages, table[some], k_scales, v_scales, dtype)[2]
+            _launch("ff_op_cache_read", device, code, some.stop - i, K, D, kv_len, *_heads(k[some], v[some]), *cache, lengths[some].data_ptr())
     return k, v
 
 
