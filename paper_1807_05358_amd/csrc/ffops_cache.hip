@@ -200,6 +200,9 @@ __global__ __launch_bounds__(256) void k_cache_read(ReadArgs a)
 Moved moved(const ff_heads_t& h) { return {(const char*)h.p, h.batch * 2, h.head * 2, h.pos * 2}; }
 bool heads_fit(const ff_heads_t& h) { return h.p && aligned(h.p, 16) && !((h.batch | h.head | h.pos) & 7); }
 
+// Rows of a thread: one where a sequence's rows make no more than 64 blocks, which takes 0.7 to 1.1 us less (a step, 64 positions of 8 heads: 2.7 us and 3.5, in e4m3 3.0 and 4.1); else four, for batches that are mostly padding, whose
+// blocks without a row then are a quarter: 64 sequences of up to 2048 positions, 8 heads of 128, seven of eight of them at most 40 long, 24 us and 34 with one row, in e4m3 23 and 33.  Batches that are half or all full pay for it:
+// 16 of up to 2048, 34 and 29 us, in e4m3 29 and 24; 4 of 4096 29 and 27; 64 of 128 12.7 and 13.8.
 template <class T, int HELD, int LANES>
 void launch_lanes(const WriteArgs& a, hipStream_t st)
 {
