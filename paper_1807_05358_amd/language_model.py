@@ -143,7 +143,8 @@ class Decoder:
 
     def generate(self, cache, tokens, u, lengths=None, **choice):
         """(words, logprob) [batch, new] chosen one after the other behind tokens [batch, length] (lengths as in extend): u [batch, new] are the random numbers, `choice` the
-        parameters of operators.sample.  The cache holds all but the last of them; a call that is refused leaves it as it was."""
+        parameters of operators.sample.  The cache holds all but the last of them; a call that is refused leaves it as it was.
+        A sequence whose logits hold a NaN has word -1 from there on, or words that mean nothing."""
         import torch
         if u.dim() != 2 or tokens.dim() != 2:
             raise ValueError("tokens and u are matrices, a row for each sequence")

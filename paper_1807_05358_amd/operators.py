@@ -538,7 +538,8 @@ def cache_read(k_pages, v_pages, table, lengths, *, kv_len=None, dtype=None, k_s
 def attention_paged_fwd(q, k_pages, v_pages, table, kv_lengths, *, causal=False, q_lengths=None, scale=None, k_scales=None, v_scales=None):
     """(o, lse) of new queries q [batch, heads, q_len, dim] (float16 or bfloat16) over the first kv_lengths[b] positions (int32 [batch]) of a paged cache (see cache_write), their own among
     them; otherwise as attention_fwd: with causal the last query sees all positions and those before it one fewer each, q_lengths are int32 [batch], a query that sees nothing has o = 0 and
-    lse = -inf.  A query that sees a position whose entry is no page gets NaN.  Keys and values are read once for a few queries of each head (16 queries times heads of a key head are worked together, 32 where there are more), so
+    lse = -inf.  A query that sees a position whose entry is no page gets NaN.  Value rows that some queries of a sequence see and others do not have to be finite (a block
+    held in fewer bits that was not reads back as NaN).  Keys and values are read once for a few queries of each head (16 queries times heads of a key head are worked together, 32 where there are more), so
     long prompts, of more than about 128 queries times heads of a key head, are better read back with cache_read for attention_fwd."""
     torch = _torch()
     _not_recorded(q, k_pages, v_pages)
